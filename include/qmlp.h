@@ -372,6 +372,44 @@ qmlp_status qmlp_linear_batch(const qmlp_qweight *w, int L, const void *x, int M
                               qmlp_dtype dtype, void *y, qmlp_stream stream);
 
 /*
+ * A quantized linear with low-rank adapters of many requests beside it
+ * (Sec. 3.1 Eq. (1) with an adapter per row; Sec. 4.2: the adapters stay
+ * separate from the quantized base, so requests share it):
+ *     y[m] = W x[m] + s_a B_a (A_a x[m]),   a = ids[m].
+ * A [count][rank][k] and B [count][n][rank] in the activation type (adapters
+ * of a lower rank are padded with zeros), scale fp32 [count] (NULL: 1.0), ids
+ * int32 [M], all on the device.  A row whose id lies outside [0, count) has no
+ * adapter and gets W x.  rank 8, 16, 32 or 64.  `adapters` may be NULL or have
+ * count 0: W x alone (ids may then be NULL).
+ */
+typedef struct {
+    const void *A;          /* [count][rank][k] activation type, 16-byte aligned */
+    const void *B;          /* [count][n][rank] */
+    const float *scale;     /* [count], or NULL */
+    int32_t count, rank;
+} qmlp_adapters;
+
+/*
+ * w: 2 or 4 bits, any group, k % 64 == 0, any n.  x [M][k] and y [M][n] are
+ * binary16 or bfloat16, 0 <= M <= 2^20, with rows ldx >= k (a multiple of 8)
+ * and ldy >= n elements apart; elements between the rows are neither read into
+ * a result nor written.  t = A x is formed in one launch (with bfloat16 rows
+ * rewritten as binary16 times a power of two per row, which keeps every element
+ * down to 2^-28 of its row's largest exactly; a row that holds an infinity or
+ * NaN gives infinities or NaNs), the linear in a second: up to 16 rows on the
+ * weight stream (oneshot.h), more as a dense product.
+ * ws/ws_bytes: at least qmlp_linear_lora_workspace_bytes(...), any contents,
+ * nothing is kept between calls; one call at a time per workspace.
+ * M == 0 enqueues nothing.  Nothing is written outside y's M rows and ws.
+ */
+size_t qmlp_linear_lora_workspace_bytes(const qmlp_qweight *w, const qmlp_adapters *adapters, int M,
+                                        qmlp_dtype dtype);
+
+qmlp_status qmlp_linear_lora(const qmlp_qweight *w, const qmlp_adapters *adapters, const int32_t *ids,
+                             const void *x, int64_t ldx, int M, qmlp_dtype dtype, void *y, int64_t ldy,
+                             void *ws, size_t ws_bytes, qmlp_stream stream);
+
+/*
  * The MLP of a mixture-of-experts decoder layer at decode (Sec. 5: the
  * routed experts of the GPT-OSS-20B-class model; only the routed experts'
  * weights are read per token): each of E experts is one block of
@@ -424,6 +462,60 @@ qmlp_status qmlp_forward_moe(const qmlp_mlp *experts, int E, const void *x, int 
  * M, k >= 1, M k <= 40, cus >= 1, non-null outputs.  Host-only. */
 int qmlp_moe_lanes(int d, int f, int gu_bits, int dn_bits, int M, int k, int cus,
                    int *gu_lanes, int *dn_lanes);
+
+/*
+ * The router of a mixture-of-experts layer (Sec. 5: the routed experts of the
+ * MoE decoder): l = x Wr^T + bias for x [M][d] and Wr [E][d] of one activation
+ * type and bias fp32 [E] (or NULL), the k largest of each token in descending
+ * order -- ties to the lower expert -- and their weights:
+ *   TOPK_SOFTMAX  softmax of the k chosen logits;
+ *   SOFTMAX       softmax over all E logits, taken at the chosen (not
+ *                 normalised again);
+ *   SIGMOID       sigmoid(l) over the sum of the k chosen sigmoids.
+ * Logits are summed in fp64 (products of two 16-bit floats are exact there), so
+ * the choice does not depend on how the work was split.  An expert whose logit
+ * is NaN or -inf (a bias of -inf masks it) is never chosen; +inf counts as the
+ * largest fp32.  Where fewer than k experts are left, the remaining slots hold
+ * expert -1 and weight 0.  topk_idx int32 [M][k] and topk_w fp32 [M][k] are what
+ * qmlp_forward_moe takes (it clamps a -1, whose weight is 0).
+ * 1 <= k <= 16, k <= E <= 512, d % 8 == 0, 0 <= M <= 2^20 (0: nothing to do).
+ * ws: qmlp_moe_route_workspace_bytes(E, M) bytes, any contents, nothing kept
+ * between calls; one call at a time per workspace.
+ */
+typedef enum { QMLP_SCORE_TOPK_SOFTMAX = 0, QMLP_SCORE_SOFTMAX = 1, QMLP_SCORE_SIGMOID = 2 } qmlp_score;
+
+size_t qmlp_moe_route_workspace_bytes(int E, int M);
+
+qmlp_status qmlp_moe_route(const void *router, const float *bias, const void *x, int M, int d, int E, int k,
+                           qmlp_score score, qmlp_dtype dtype, int32_t *topk_idx, float *topk_w, void *ws,
+                           size_t ws_bytes, qmlp_stream stream);
+
+/*
+ * A whole mixture-of-experts layer for a few tokens (Sec. 5, Sec. 3.3, Sec.
+ * 4.2): the router above, then y[m] = sum_j w[m][j] expert_{idx[m][j]}(x[m]) with
+ * each expert a gated MLP of qmlp_forward with its own adapters.
+ * `mlp` holds the experts one after another: gate and up [E f][d], down
+ * [E d][f], A_gate/A_up [E][rank][d], B_gate/B_up [E][f][rank] (n_out E f, E f
+ * and E d; a packed matrix of stacked rows is the stack of packed matrices).
+ * Gate/up 2 or 4 bits and down 4 or 2 bits, groups of 32, 64 or 128, d and f
+ * multiples of 64, rank 0, 8, 16 or 32, E <= 512, topk <= 16.  Binary16, 0 <= M
+ * <= 64 (0: nothing to do).  A token none of whose experts can be chosen gets
+ * zeros.  h is rounded to binary16; the experts' outputs stay fp32 until the
+ * weighted sum, slots in order, is rounded once.
+ * ws: qmlp_moe_layer_workspace_bytes(...) bytes, any contents, nothing kept
+ * between calls; one call at a time per workspace.
+ */
+typedef struct {
+    const void *router;      /* [E][d] binary16, 16-byte aligned */
+    const float *bias;       /* [E] or NULL */
+    int32_t experts, topk, score;
+    qmlp_mlp mlp;
+} qmlp_moe;
+
+size_t qmlp_moe_layer_workspace_bytes(const qmlp_moe *layer, int M, qmlp_dtype dtype);
+
+qmlp_status qmlp_moe_layer(const qmlp_moe *layer, const void *x, int M, qmlp_dtype dtype, void *y, void *ws,
+                           size_t ws_bytes, qmlp_stream stream);
 
 /* ---------------------------------------------- inspection (not timed) */
 

@@ -13,6 +13,8 @@ Functions keep the names of the C entry points:
 * ``forward``                     -- the whole block x -> y
 * ``forward_layers``              -- L independent blocks, y_l = block_l(x_l)
 * ``forward_stack``               -- L blocks on a residual stream, x_{l+1} = x_l + block_l(RMSNorm(x_l))
+* ``linear_lora``                 -- a linear with adapters of many requests, y[m] = W x[m] + s_a B_a (A_a x[m])
+* ``moe_route`` / ``moe_layer``   -- a router's top-k choice and weights; a whole MoE layer for a few tokens
 * ``unpack`` / ``dequant``        -- inspection of a packed matrix (not timed)
 """
 from __future__ import annotations
@@ -51,6 +53,16 @@ class MlpC(ctypes.Structure):
                 ("rank", ctypes.c_int32), ("lora_scale", ctypes.c_float)]
 
 
+class AdaptersC(ctypes.Structure):
+    _fields_ = [("A", ctypes.c_void_p), ("B", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("count", ctypes.c_int32), ("rank", ctypes.c_int32)]
+
+
+class MoeC(ctypes.Structure):
+    _fields_ = [("router", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("experts", ctypes.c_int32),
+                ("topk", ctypes.c_int32), ("score", ctypes.c_int32), ("mlp", MlpC)]
+
+
 _LIB = None
 
 
@@ -64,6 +76,8 @@ def _lib():
         P, I, Z = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
         pq = ctypes.POINTER(QWeightC)
         pm = ctypes.POINTER(MlpC)
+        po = ctypes.POINTER(MoeC)
+        pa, L = ctypes.POINTER(AdaptersC), ctypes.c_int64
         sig = {
             "qmlp_codes_bytes": (Z, [I, I, I]),
             "qmlp_meta_bytes": (Z, [I, I, I]),
@@ -95,6 +109,12 @@ def _lib():
             "qmlp_forward_noalloc": (I, [pm, P, I, I, P, P]),
             "qmlp_layers_path": (I, [pm, I, I, I]),
             "qmlp_noalloc_scratch_bytes": (Z, []),
+            "qmlp_linear_lora_workspace_bytes": (Z, [pq, pa, I, I]),
+            "qmlp_moe_route_workspace_bytes": (Z, [I, I]),
+            "qmlp_moe_route": (I, [P, P, P, I, I, I, I, I, I, P, P, P, Z, P]),
+            "qmlp_moe_layer_workspace_bytes": (Z, [po, I, I]),
+            "qmlp_moe_layer": (I, [po, P, I, I, P, P, Z, P]),
+            "qmlp_linear_lora": (I, [pq, pa, P, P, L, I, I, P, L, P, Z, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(lib, name)
@@ -418,6 +438,78 @@ def linear_batch(ws, x: torch.Tensor, y: torch.Tensor | None = None) -> torch.Te
     return y
 
 
+class Adapters:
+    """Low-rank adapters of many requests over one linear: A [count][rank][k] and
+    B [count][n][rank] in the activation type, scale float32 [count] or None (1.0),
+    contiguous on one device.  Lower ranks are padded with zeros."""
+
+    def __init__(self, A: torch.Tensor, B: torch.Tensor, scale: torch.Tensor | None = None):
+        if A.dim() != 3 or B.dim() != 3 or A.shape[0] != B.shape[0] or A.shape[1] != B.shape[2]:
+            raise ValueError("A must be [count][rank][k] and B [count][n][rank]")
+        if A.dtype != B.dtype or not A.is_contiguous() or not B.is_contiguous():
+            raise ValueError("A and B must be contiguous and of one type")
+        if scale is not None and (scale.dtype != torch.float32 or scale.shape != A.shape[:1] or not scale.is_contiguous()):
+            raise ValueError("scale must be float32 [count]")
+        _dtype_code(A)
+        _one_device(A, B, scale)
+        self.A, self.B, self.scale = A, B, scale
+        self.count, self.rank = int(A.shape[0]), int(A.shape[1])
+        self._c = AdaptersC(A.data_ptr(), B.data_ptr(), None if scale is None else scale.data_ptr(), self.count, self.rank)
+
+    def c(self) -> AdaptersC:
+        return self._c
+
+
+def _one_device(*tensors):
+    """The kernels run on the current stream of one device; a tensor elsewhere would fault there."""
+    for t in tensors:
+        if t is not None and (not t.is_cuda or t.device.index != torch.cuda.current_device()):
+            raise ValueError("every tensor must be on the current CUDA device")
+
+
+def linear_lora_workspace_bytes(w: QWeight, adapters: Adapters | None, M: int, dtype=torch.float16) -> int:
+    qc = w.c()
+    return int(_lib().qmlp_linear_lora_workspace_bytes(ctypes.byref(qc), ctypes.byref(adapters.c()) if adapters else None,
+                                                       M, F16 if dtype == torch.float16 else BF16))
+
+
+def linear_lora_workspace(w: QWeight, adapters: Adapters | None, M: int, dtype=torch.float16,
+                          device="cuda") -> torch.Tensor:
+    """A workspace for linear_lora of up to this many rows (any contents)."""
+    return torch.empty(max(linear_lora_workspace_bytes(w, adapters, M, dtype), 256), dtype=torch.uint8, device=device)
+
+
+def linear_lora(w: QWeight, adapters: Adapters | None, ids: torch.Tensor | None, x: torch.Tensor,
+                y: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """y[m] = W x[m] + s_a B_a (A_a x[m]) with a = ids[m] (int32 [M] on the device; outside
+    [0, count): no adapter).  x [M][k] and y [M][n] binary16 or bfloat16, any number of
+    rows, each row contiguous (the rows may be part of a wider buffer)."""
+    M, k = x.shape
+    code = _dtype_code(x)
+    if k != w.k_in or (M > 1 and x.stride(0) < k) or (k > 1 and x.stride(1) != 1):
+        raise ValueError("x must be [M][k] with contiguous rows")
+    if y is None:
+        y = torch.empty((M, w.n_out), dtype=x.dtype, device=x.device)
+    elif y.dtype != x.dtype or y.shape != (M, w.n_out) or (w.n_out > 1 and y.stride(1) != 1) or \
+            (M > 1 and y.stride(0) < w.n_out):
+        raise ValueError("y must be [M][n] of x's type with contiguous rows")
+    ad = None
+    if adapters is not None:
+        if adapters.A.dtype != x.dtype or adapters.A.shape[2] != k or adapters.B.shape[1] != w.n_out:
+            raise ValueError("the adapters are of another type or shape than the linear")
+        if ids is None or ids.dtype != torch.int32 or ids.shape != (M,) or not ids.is_contiguous():
+            raise ValueError("ids must be int32 [M]")
+        ad = ctypes.byref(adapters._c)
+    if ws is None:
+        ws = linear_lora_workspace(w, adapters, M, x.dtype, x.device)
+    _one_device(x, y, ids, ws, w.codes, adapters.A if adapters else None)
+    qc = w.c()
+    _check(_lib().qmlp_linear_lora(ctypes.byref(qc), ad, _ptr(ids) if ad else None, _ptr(x), x.stride(0) if M > 1 else k, M,
+                                   code, _ptr(y), y.stride(0) if M > 1 else w.n_out, _ptr(ws), ws.numel(), _stream()),
+           "linear_lora")
+    return y
+
+
 def moe_workspace_bytes(experts: Layers, M: int, k: int, dtype=torch.float16) -> int:
     code = F16 if dtype == torch.float16 else BF16
     return int(_lib().qmlp_moe_workspace_bytes(experts.c(), len(experts), M, k, code))
@@ -451,6 +543,113 @@ def forward_moe(experts: Layers, x: torch.Tensor, topk_idx: torch.Tensor, topk_w
     _check(_lib().qmlp_forward_moe(experts.c(), len(experts), _ptr(x), M, _dtype_code(x),
                                    _ptr(topk_idx), _ptr(topk_w), k, _ptr(y), _ptr(ws), ws.numel(),
                                    _stream()), "forward_moe")
+    return y
+
+
+SCORES = {"topk_softmax": 0, "softmax": 1, "sigmoid": 2}
+
+
+def moe_route_workspace(router: torch.Tensor, M: int) -> torch.Tensor:
+    """A workspace for moe_route of up to this many tokens (any contents)."""
+    n = int(_lib().qmlp_moe_route_workspace_bytes(router.shape[0], M))
+    return torch.empty(max(n, 256), dtype=torch.uint8, device=router.device)
+
+
+def _router_args(router, bias, d, dtype):
+    if router.dim() != 2 or router.shape[1] != d or router.dtype != dtype or not router.is_contiguous():
+        raise ValueError("router must be [E][d] of x's type, contiguous")
+    if bias is not None and (bias.dtype != torch.float32 or bias.shape != router.shape[:1] or not bias.is_contiguous()):
+        raise ValueError("bias must be float32 [E]")
+
+
+def moe_route(x: torch.Tensor, router: torch.Tensor, k: int, bias: torch.Tensor | None = None,
+              score: str = "topk_softmax", topk_idx: torch.Tensor | None = None, topk_w: torch.Tensor | None = None,
+              ws: torch.Tensor | None = None):
+    """(topk_idx int32 [M][k], topk_w float32 [M][k]) of x [M][d]: the k largest of x Wr^T + bias
+    per token, ties to the lower expert, and their weights (score: "topk_softmax",
+    "softmax" or "sigmoid"; see qmlp_moe_route).  Unused slots: expert -1, weight 0."""
+    M, d = x.shape
+    code = _dtype_code(x)
+    _router_args(router, bias, d, x.dtype)
+    if not x.is_contiguous():
+        raise ValueError("x must be contiguous")
+    if topk_idx is None:
+        topk_idx = torch.empty((M, k), dtype=torch.int32, device=x.device)
+    if topk_w is None:
+        topk_w = torch.empty((M, k), dtype=torch.float32, device=x.device)
+    if topk_idx.dtype != torch.int32 or topk_w.dtype != torch.float32 or topk_idx.shape != (M, k) or \
+            topk_w.shape != (M, k) or not topk_idx.is_contiguous() or not topk_w.is_contiguous():
+        raise ValueError("topk_idx int32 and topk_w float32, both [M][k]")
+    if ws is None:
+        ws = moe_route_workspace(router, M)
+    _one_device(x, router, bias, topk_idx, topk_w, ws)
+    _check(_lib().qmlp_moe_route(_ptr(router), _ptr(bias), _ptr(x), M, d, router.shape[0], k, SCORES[score], code,
+                                 _ptr(topk_idx), _ptr(topk_w), _ptr(ws), ws.numel(), _stream()), "moe_route")
+    return topk_idx, topk_w
+
+
+class MoE:
+    """A whole mixture-of-experts layer: router [E][d], the experts' matrices stacked along their
+    rows (gate and up [E f][d], down [E d][f]; stack_qweights joins packed ones), adapters
+    A [E][rank][d] and B [E][f][rank]."""
+
+    def __init__(self, router: torch.Tensor, gate: QWeight, up: QWeight, down: QWeight, topk: int, A_gate=None,
+                 B_gate=None, A_up=None, B_up=None, lora_scale: float = 1.0, bias: torch.Tensor | None = None,
+                 score: str = "topk_softmax"):
+        E, d = router.shape
+        f = down.k_in
+        _router_args(router, bias, gate.k_in, torch.float16)
+        rank = 0
+        if A_gate is not None:
+            rank = int(A_gate.shape[1])
+            for t, s in ((A_gate, (E, rank, d)), (A_up, (E, rank, d)), (B_gate, (E, f, rank)), (B_up, (E, f, rank))):
+                if t is None or t.dtype != torch.float16 or tuple(t.shape) != s or not t.is_contiguous():
+                    raise ValueError("adapters must be float16, A [E][rank][d] and B [E][f][rank]")
+        _one_device(router, bias, gate.codes, up.codes, down.codes, A_gate, B_gate, A_up, B_up)
+        self.router, self.gate, self.up, self.down, self.bias = router, gate, up, down, bias
+        self.adapters = (A_gate, B_gate, A_up, B_up)
+        self.experts, self.topk, self.d, self.f, self.rank = int(E), int(topk), int(d), int(f), rank
+        p = [None if t is None else t.data_ptr() for t in self.adapters]
+        self._c = MoeC(router.data_ptr(), None if bias is None else bias.data_ptr(), self.experts, self.topk, SCORES[score],
+                       MlpC(gate.c(), up.c(), down.c(), *p, rank, float(lora_scale)))
+
+    def c(self) -> MoeC:
+        return self._c
+
+
+def stack_qweights(ws) -> QWeight:
+    """One packed matrix whose rows are those of packed matrices of one width, group and row length."""
+    w = list(ws)
+    if any((v.bits, v.k_in, v.group) != (w[0].bits, w[0].k_in, w[0].group) for v in w):
+        raise ValueError("stacked matrices must agree in bits, columns and group")
+    return QWeight(w[0].bits, sum(v.n_out for v in w), w[0].k_in, w[0].group, torch.cat([v.codes for v in w]),
+                   torch.cat([v.meta for v in w]))
+
+
+def moe_layer_workspace_bytes(moe: MoE, M: int) -> int:
+    return int(_lib().qmlp_moe_layer_workspace_bytes(ctypes.byref(moe._c), M, F16))
+
+
+def moe_layer_workspace(moe: MoE, M: int, device="cuda") -> torch.Tensor:
+    """A workspace for moe_layer of up to this many tokens (any contents)."""
+    return torch.empty(max(moe_layer_workspace_bytes(moe, M), 256), dtype=torch.uint8, device=device)
+
+
+def moe_layer(moe: MoE, x: torch.Tensor, y: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """y [M][d] = sum_j w[m][j] expert_{idx[m][j]}(x[m]), routed by the layer's own router (qmlp_moe_layer); binary16,
+    up to 64 tokens."""
+    M, d = x.shape
+    if x.dtype != torch.float16 or d != moe.d or not x.is_contiguous():
+        raise ValueError("x must be float16 [M][d], contiguous")
+    if y is None:
+        y = torch.empty_like(x)
+    elif y.dtype != x.dtype or y.shape != x.shape or not y.is_contiguous():
+        raise ValueError("y must be float16 [M][d], contiguous")
+    if ws is None:
+        ws = moe_layer_workspace(moe, M, x.device)
+    _one_device(x, y, ws, moe.router)
+    _check(_lib().qmlp_moe_layer(ctypes.byref(moe._c), _ptr(x), M, F16, _ptr(y), _ptr(ws), ws.numel(), _stream()),
+           "moe_layer")
     return y
 
 

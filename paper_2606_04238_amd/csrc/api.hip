@@ -626,6 +626,8 @@ int device_cus() {
     return n;
 }
 
+qmlp_status weight_check(const qmlp_qweight* w, int bits) { return check_qweight(w, bits); }
+
 // Everything qmlp_forward checks before it looks at the workspace.
 qmlp_status forward_check(const qmlp_mlp* mlp, const void* x, int M, qmlp_dtype dtype, const void* y) {
     qmlp_status s = check_mlp(mlp, M, dtype);

@@ -15,6 +15,9 @@ qmlp_status forward_check(const qmlp_mlp* mlp, const void* x, int M, qmlp_dtype 
 // The smallest workspace qmlp_forward takes (qmlp_workspace_bytes may ask for more).
 size_t forward_least_bytes(const qmlp_mlp* mlp, int M, qmlp_dtype dtype);
 
+// The structural checks of one packed-weight view (bits 0: any width).
+qmlp_status weight_check(const qmlp_qweight* w, int bits);
+
 // Compute units of the current device (asked once per device), 0 without one.
 int device_cus();
 

@@ -1,0 +1,150 @@
+"""linear_lora on the GPU against 64 bits: y[m] = W x[m] + s_a B_a (A_a x[m])."""
+import pytest
+import torch
+
+from tokens_testutil import check, lora_ref
+
+pytestmark = pytest.mark.gpu
+F16, BF16 = torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def q():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    import paper_2606_04238_amd as qm
+    qm.library()
+    return qm
+
+
+def make(q, bits, g, n, k, M, R, T, dtype, seed=0, std=0.02):
+    gen = torch.Generator().manual_seed(1000 * seed + n + 7 * k + 31 * M)
+    rnd = lambda *s: torch.randn(*s, generator=gen)
+    pack = {2: q.pack_w2, 4: q.pack_w4}[bits]
+    w = pack((rnd(n, k) * std).cuda(), g)
+    x = rnd(M, k).to(dtype).cuda()
+    A, B = (rnd(T, R, k) * 0.02).to(dtype).cuda(), (rnd(T, n, R) * 0.02).to(dtype).cuda()
+    scale = (torch.rand(T, generator=gen) + 0.5).cuda()
+    ids = torch.randint(-2, T + 1, (M,), generator=gen, dtype=torch.int32).cuda()
+    return w, x, A, B, scale, ids
+
+
+SHAPES = [
+    # bits, group, n, k, M, R, T
+    (4, 128, 256, 512, 1, 16, 3), (4, 64, 100, 64, 1, 8, 1), (4, 32, 257, 2624, 16, 64, 20),
+    (2, 128, 320, 2688, 7, 32, 4), (2, 64, 15, 832, 5, 16, 2), (2, 32, 1001, 1600, 16, 8, 9),
+    (4, 128, 272, 17408, 3, 16, 3), (2, 64, 48, 8320, 16, 32, 8),
+    (4, 128, 256, 512, 17, 16, 3), (4, 32, 130, 64, 31, 8, 40), (4, 64, 255, 320, 129, 64, 5),
+    (2, 32, 1000, 1600, 130, 32, 3), (2, 128, 1, 256, 257, 16, 2), (4, 128, 511, 1152, 64, 32, 70),
+    (2, 64, 640, 4160, 300, 64, 2),
+]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("shape", SHAPES, ids=lambda s: "x".join(map(str, s)))
+def test_against_64_bits(q, shape, dtype):
+    print("\n[case]", shape, dtype, flush=True)
+    w, x, A, B, scale, ids = make(q, *shape, dtype)
+    y = q.linear_lora(w, q.Adapters(A, B, scale), ids, x)
+    torch.cuda.synchronize()
+    rel = check(y, *lora_ref(w, x, A, B, scale, ids), dtype)
+    print("rel %.2e" % rel)
+
+
+@pytest.mark.parametrize("M", [1, 16, 40])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_no_adapters(q, M, dtype):
+    """No table, and a table no row uses, give W x to the bit of each other; scale None is 1."""
+    w, x, A, B, scale, ids = make(q, 4, 64, 200, 640, M, 16, 2, dtype)
+    plain = q.linear_lora(w, None, None, x)
+    none = q.linear_lora(w, q.Adapters(A, B, scale), torch.full((M,), -1, dtype=torch.int32, device="cuda"), x)
+    assert torch.equal(plain, none)
+    check(plain, *lora_ref(w, x, None, None, None, None), dtype)
+    ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+    check(q.linear_lora(w, q.Adapters(A, B), ids, x), *lora_ref(w, x, A, B, None, ids), dtype)
+
+
+@pytest.mark.parametrize("M", [1, 9, 16, 50, 200])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_rows_of_wider_buffers(q, M, dtype):
+    """Rows of x and y inside wider buffers; what lies between and behind them stays, a NaN there does not matter."""
+    w, x, A, B, scale, ids = make(q, 4, 32, 100, 704, M, 8, 3, dtype)
+    xb = torch.full((M + 2, 704 + 24), float("nan"), dtype=dtype, device="cuda")
+    yb = torch.full((M + 2, 100 + 13), 7.0, dtype=dtype, device="cuda")
+    xb[1:M + 1, 8:712] = x
+    y = q.linear_lora(w, q.Adapters(A, B, scale), ids, xb[1:M + 1, 8:712], yb[1:M + 1, 5:105])
+    assert y.data_ptr() == yb[1, 5:].data_ptr()
+    check(y, *lora_ref(w, x, A, B, scale, ids), dtype)
+    yb[1:M + 1, 5:105] = 7.0
+    assert bool((yb == 7.0).all())
+
+
+@pytest.mark.parametrize("M", [16, 45])
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_bad_rows_and_adapters_stay_alone(q, M, dtype):
+    """A row with NaN, an adapter with infinities: the other rows are those of a clean call."""
+    w, x, A, B, scale, ids = make(q, 2, 64, 144, 576, M, 16, 4, dtype)
+    ids = torch.arange(M, dtype=torch.int32, device="cuda") % 5 - 1
+    good = q.linear_lora(w, q.Adapters(A, B, scale), ids, x)
+    x2, A2, B2 = x.clone(), A.clone(), B.clone()
+    x2[3, 17] = float("nan")
+    x2[6, 0] = float("inf")
+    A2[2, 5, 100] = float("inf")
+    B2[1] = float("inf")
+    bad = q.linear_lora(w, q.Adapters(A2, B2, scale), ids, x2)
+    rows = torch.tensor([m for m in range(M) if m not in (3, 6) and m % 5 - 1 not in (1, 2)])
+    assert torch.equal(good[rows], bad[rows])
+    assert not bool(torch.isfinite(bad[3]).any()) and not bool(torch.isfinite(bad[6]).any())
+
+
+@pytest.mark.parametrize("M", [4, 33])
+@pytest.mark.parametrize("mag", [1e-30, 1e-6, 1e30])
+def test_bfloat16_rows_of_any_magnitude(q, M, mag):
+    w, x, A, B, scale, ids = make(q, 4, 128, 192, 1024, M, 16, 3, BF16)
+    x = x * mag
+    x[M - 1] = 0
+    ref, bound = lora_ref(w, x, A, B, scale, ids)
+    y = q.linear_lora(w, q.Adapters(A, B, scale), ids, x)
+    check(y, ref, bound, BF16)
+    assert bool((y[M - 1] == 0).all())
+
+
+@pytest.mark.parametrize("M", [1, 16, 100])
+def test_small_adapters_count(q, M):
+    """bfloat16 adapters far below binary16's range (B of 1e-9, scale 1e9) keep their share."""
+    w, x, A, B, scale, ids = make(q, 4, 64, 128, 512, M, 8, 2, BF16)
+    B = (B.float() * 1e-9).to(BF16)
+    scale = torch.full((2,), 1e9, device="cuda")
+    ids = torch.zeros(M, dtype=torch.int32, device="cuda")
+    check(q.linear_lora(w, q.Adapters(A, B, scale), ids, x), *lora_ref(w, x, A, B, scale, ids), BF16)
+
+
+@pytest.mark.parametrize("M", [0, 3, 70])
+def test_workspace_contents_and_streams(q, M):
+    """Any workspace contents, another stream, a captured and replayed call: the same bits."""
+    w, x, A, B, scale, ids = make(q, 4, 128, 320, 896, M, 32, 5, BF16)
+    ad = q.Adapters(A, B, scale)
+    ws = q.linear_lora_workspace(w, ad, M, BF16)
+    want = q.linear_lora(w, ad, ids, x, ws=ws).clone()
+    if M == 0:
+        assert want.shape == (0, 320)
+        return
+    ws.fill_(255)
+    assert torch.equal(q.linear_lora(w, ad, ids, x, ws=ws), want)
+    y = torch.empty_like(want)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        q.linear_lora(w, ad, ids, x, y, ws)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(y, want)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        q.linear_lora(w, ad, ids, x, y, ws)
+    for i in range(3):
+        x.copy_(torch.randn_like(x.float()).to(BF16))
+        y.zero_()
+        g.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        assert torch.equal(got, q.linear_lora(w, ad, ids, x, ws=ws)), i
