@@ -20,7 +20,7 @@ qmlp_status from_hip(hipError_t e) { return e == hipSuccess ? QMLP_OK : QMLP_ERR
 
 // ---------------------------------------------------------------- linear with adapters
 
-constexpr int kMaxRows = 1 << 20;
+constexpr int kMaxRows = 1 << 20, kMaxStride = 1 << 21;    // 256 rows, or a column of 1024, within 32-bit offsets
 
 qmlp_status check_lora(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
     const qmlp_status s = weight_check(w, 0);
@@ -30,7 +30,7 @@ qmlp_status check_lora(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qm
         return QMLP_ERR_UNSUPPORTED;
     if (w->k_in % 64 != 0 || M < 0)
         return QMLP_ERR_SHAPE;
-    if (M > kMaxRows)
+    if (M > kMaxRows || w->k_in > kMaxStride)
         return QMLP_ERR_UNSUPPORTED;
     if (!ad)
         return QMLP_OK;
@@ -47,15 +47,17 @@ qmlp_status check_lora(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qm
     return QMLP_OK;
 }
 
-// Workspace: [t: M x R fp32][2^-e: M fp32][x 2^e: M x k binary16], the last
-// two for bfloat16 only.
+// Workspace: [t: M x R fp32, or as two bfloat16 terms], past 16 rows [sets of
+// rows with several adapters][their terms, fp32], and for bfloat16 [2^-e: M
+// fp32][x 2^e: M x k binary16].
 struct LoraSizes {
-    size_t t, xf, x16;
-    size_t all() const { return t + xf + x16; }
+    size_t t, slots, mixed, xf, x16;
+    size_t all() const { return t + slots + mixed + xf + x16; }
 };
 LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
-    const bool bf = dtype == QMLP_BF16;
-    return {ad && ad->count > 0 ? round256((size_t)M * ad->rank * 4) : 0, bf ? round256((size_t)M * 4) : 0,
+    const bool bf = dtype == QMLP_BF16, some = ad && ad->count > 0, many = some && !lora_few_rows(M, w);
+    return {some ? round256((size_t)M * ad->rank * 4) : 0, many ? round256(((size_t)(M + 31) / 32 + kMixedSets) * 4) : 0,
+            many ? round256((size_t)lora_mixed_most(M) * 32 * w->n_out * 4) : 0, bf ? round256((size_t)M * 4) : 0,
             bf ? round256((size_t)M * w->k_in * 2) : 0};
 }
 
@@ -143,6 +145,8 @@ qmlp_status qmlp_linear_lora(const qmlp_qweight* w, const qmlp_adapters* ad, con
         return QMLP_ERR_NULL;
     if (ldx < w->k_in || ldx % 8 != 0 || ldy < w->n_out)
         return QMLP_ERR_SHAPE;
+    if (ldx > kMaxStride)
+        return QMLP_ERR_UNSUPPORTED;
     if (!aligned16(x) || ((uintptr_t)y & 1u) != 0 || (adapters && !aligned4(ids)))
         return QMLP_ERR_ALIGN;
     const LoraSizes z = lora_sizes(w, ad, M, dtype);
@@ -172,14 +176,22 @@ qmlp_status qmlp_linear_lora(const qmlp_qweight* w, const qmlp_adapters* ad, con
     a.bits = w->bits;
     a.g = w->group;
     a.bf = dtype == QMLP_BF16;
-    a.t = reinterpret_cast<float*>(base);
-    a.xf = a.bf ? reinterpret_cast<float*>(base + z.t) : nullptr;
-    a.x16 = a.bf ? reinterpret_cast<uint16_t*>(base + z.t + z.xf) : nullptr;
+    const bool few = lora_few_rows(M, w);
+    a.t = few ? reinterpret_cast<float*>(base) : nullptr;
+    a.tb = few ? nullptr : reinterpret_cast<uint16_t*>(base);
+    base += z.t;
+    a.slots = reinterpret_cast<int*>(base);
+    a.mixed = reinterpret_cast<float*>(base + z.slots);
+    base += z.slots + z.mixed;
+    a.xf = a.bf ? reinterpret_cast<float*>(base) : nullptr;
+    a.x16 = a.bf ? reinterpret_cast<uint16_t*>(base + z.xf) : nullptr;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const hipError_t e = launch_lora_prep(a, st);
+    hipError_t e = launch_lora_prep(a, st);
+    if (e == hipSuccess && !few && adapters)
+        e = launch_lora_mixed(a, st);
     if (e != hipSuccess)
         return QMLP_ERR_HIP;
-    return from_hip(lora_few_fits(a) ? launch_lora_few(a, st) : launch_lora_gemm(a, st));
+    return from_hip(few ? launch_lora_few(a, st) : launch_lora_gemm(a, st));
 }
 
 size_t qmlp_moe_route_workspace_bytes(int E, int M) {

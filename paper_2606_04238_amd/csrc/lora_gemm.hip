@@ -6,19 +6,20 @@
 // v_mfma_f32_32x32x16_f16.  bfloat16 rows come as binary16 times a power of two
 // (lora_linear.hip), so both types run the same products.
 //
-// Adapters first: the accumulators start as s_a B_a t of each row.  The
-// distinct adapters of a workgroup's rows are found in LDS, and for each of
-// them t and B_a are multiplied for all rows, of which only its own take the
-// sums (a select, not a product with zero: an adapter that holds infinities
-// stays with its own rows).  Binary16: t is rounded to it after a power of two
-// per row that brings its largest into [2^14, 2^15), 2^-12 of the adapter's
-// term.  bfloat16: t enters as two bfloat16 terms (2^-17) beside B_a as it is,
-// whose range is that of fp32.  The sums take the row's powers of two before the
-// weights' products are added.
+// Adapters first: the accumulators start as B_a t of each row.  Where a wave's rows
+// all have one adapter (a prompt), its products go there directly.  Sets of 32 rows
+// with many (decoding sequences) find their terms ready in memory
+// (lora_mixed_kernel; kMixedSets of them, the first in the call); for the others,
+// for each adapter of the 32 rows, t and B_a are multiplied for all of them, and its own rows
+// take the sums (a select, not a product with zero: an adapter that holds
+// infinities stays with its own rows).  t enters as two bfloat16 terms (2^-17 of
+// it), whose range is that of fp32, beside B_a as it is, or as the two bfloat16
+// terms that a binary16 value is exactly.
 //
 // Tile engine: BM rows x BN outputs per workgroup, K in steps of 64 staged in
-// LDS, chunk c of row r at c ^ ((r >> 1) & 7), two buffers, the next step's
-// loads in registers while a step runs (prefill.hip's scheme).
+// LDS, chunk c of row r at c ^ ((r >> 1) & 7).  x is copied to LDS by the memory
+// system (ST slots, ST - 1 steps ahead); codes are in registers two steps ahead
+// and unpacked into two buffers, one step ahead; one barrier per step.
 #include "lora_linear.h"
 #include "decode_launch.h"
 #include "oneshot.h"
@@ -42,6 +43,12 @@ __device__ __forceinline__ uint4 ld16(const void* p) {
     return make_uint4(v.x, v.y, v.z, v.w);
 }
 __device__ __forceinline__ void st16(uint4* p, const uint4& v) { *reinterpret_cast<u32x4*>(p) = u32x4{v.x, v.y, v.z, v.w}; }
+// 16 bytes per lane from memory to LDS, lane l to lds + l.  (The host's pass knows no such builtin.)
+__device__ __forceinline__ void load_to_lds(Rsrc r, uint4* lds, uint32_t voff, uint32_t soff) {
+#ifdef __HIP_DEVICE_COMPILE__
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, voff, soff, 0, 0);
+#endif
+}
 __device__ __forceinline__ int swz(int r, int c) { return r * 8 + (c ^ ((r >> 1) & 7)); }
 // Row of accumulator element v of a 32 x 32 tile (the column is lane & 31).
 __device__ __forceinline__ int acc_row(int v, int lane) { return 8 * (v >> 2) + 4 * (lane >> 5) + (v & 3); }
@@ -76,157 +83,233 @@ __device__ __forceinline__ void dequant_store(uint4* lds, const uint32_t (&w)[BI
     }
 }
 
-// Eight values of t as matrix operands: binary16 t f in t0, or the bfloat16
-// t and what that leaves in t0 and t1.
-__device__ __forceinline__ void adapter_operand(const float (&t)[8], float f, bool bf, uint4& t0, uint4& t1) {
-    uint32_t a[4], b[4];
+// The two bfloat16 terms of eight binary16 values (exact: eight bits and the other three).
+__device__ __forceinline__ void split_f16(const uint4& v, uint4& hi, uint4& lo) {
+    float f[8];
+    act8(v, false, f);
+    uint32_t h[4], l[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        if (bf) {
-            const uint32_t l = act_bits(t[2 * i], true), h = act_bits(t[2 * i + 1], true);
-            a[i] = l | h << 16;
-            b[i] = act_bits(t[2 * i] - __uint_as_float(l << 16), true) |
-                   (uint32_t)act_bits(t[2 * i + 1] - __uint_as_float(h << 16), true) << 16;
-        } else {
-            a[i] = f2h(t[2 * i] * f) | f2h(t[2 * i + 1] * f) << 16;
-            b[i] = 0;
-        }
+        const uint32_t a = act_bits(f[2 * i], true), b = act_bits(f[2 * i + 1], true);
+        h[i] = a | b << 16;
+        l[i] = act_bits(f[2 * i] - __uint_as_float(a << 16), true) |
+               (uint32_t)act_bits(f[2 * i + 1] - __uint_as_float(b << 16), true) << 16;
     }
-    t0 = make_uint4(a[0], a[1], a[2], a[3]);
-    t1 = make_uint4(b[0], b[1], b[2], b[3]);
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-template <int BITS, int BM, int BN, int WM, int WN>
-__global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_gemm_kernel(LoraArgs a) {
-    constexpr int WMW = BM / (32 * WM), NT = WMW * (BN / (32 * WN)) * 64;
-    constexpr int CA = BM * 8 / NT, P = NT / BN, CPT = 64 / P, NW = BITS * CPT / 32;
-    static_assert(CA * NT == BM * 8 && P * BN == NT && CPT >= 16 && CPT <= 32 && NW >= 1, "staging shares");
-    extern __shared__ uint4 smem[];
-    int* rid = reinterpret_cast<int*>(smem + 2 * (BM + BN) * 8);      // [BM] adapter of a row, or -1
-    float* rf = reinterpret_cast<float*>(rid + BM);                   // [BM] factor of the adapter's sums
-    float* ro = rf + BM;                                              // [BM] factor of the finished row
-    int* list = reinterpret_cast<int*>(ro + BM);                      // [BM] distinct adapters
-    int* nlist = list + BM;
+template <int BITS, int BM, int BN, int WM, int WN, int ST>
+__global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_gemm_kernel(LoraArgs a, int lg) {
+    constexpr int WMW = BM / (32 * WM), NW_ = WMW * (BN / (32 * WN)), NT = NW_ * 64;
+    constexpr int CA = BM / (8 * NW_);                     // x loads of a wave and step, eight rows each
+    constexpr int P = NT / BN >= 4 ? 4 : NT / BN >= 2 ? 2 : 1, CPT = 64 / P, NW = BITS * CPT / 32;
+    static_assert(CA >= 1 && BM % (8 * NW_) == 0 && NT >= BN && CPT <= 32 && NW >= 1, "staging shares");
+    constexpr int XB = BM * 8, WB = BN * 8;                // 16-byte chunks of a stage
+    extern __shared__ uint4 smem[];                        // x [ST][BM][8], weights [2][BN][8], then the rows' 2^-e
+    uint4* wsm = smem + ST * XB;
+    float* ro = reinterpret_cast<float*>(wsm + 2 * WB);
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % WMW, wn = wave / WMW;
-    const int mtiles = (a.M + BM - 1) / BM;
-    const int m0 = blockIdx.x % mtiles * BM, n0 = blockIdx.x / mtiles * BN;
-    const uint16_t* x = a.x16 ? a.x16 : a.x;
+    // the row tiles' columns one after another: rows of many adapters (usually the first) take longer and start first
+    const int ntiles = (a.n + BN - 1) / BN;
+    const int m0 = blockIdx.x / ntiles * BM, n0 = blockIdx.x % ntiles * BN;
     const long ldx = a.x16 ? a.k : a.ldx;
 
-    // staging: rows past M (n) repeat the last one and are dropped at the end
-    const uint16_t* xp[CA];
+    // x goes from memory to LDS without registers, eight rows (1 KB) per load: lane l writes chunk l & 7 of row l >> 3,
+    // so it reads the chunk that belongs there.  Buffer loads: rows past M (n) read zeros, and are dropped at the end.
+    // (Loads to LDS in their global form count as flat ones, and every wait for a register becomes one for all.)
+    const int mrows = min(BM, a.M - m0), nrows = min(BN, a.n - n0), rb = a.k * BITS / 8, ng = a.k >> lg;
+    const Rsrc rx = rsrc((a.x16 ? a.x16 : a.x) + (long)m0 * ldx, (uint32_t)((mrows - 1) * (int)ldx + a.k) * 2u);
+    const Rsrc rc = rsrc(reinterpret_cast<const char*>(a.codes) + (long)n0 * rb, (uint32_t)(nrows * rb));
+    const Rsrc rm = rsrc(a.meta + (long)n0 * ng, (uint32_t)(nrows * ng) * 4u);
+    uint32_t xo[CA];
 #pragma unroll
     for (int i = 0; i < CA; ++i) {
-        const int id = tid + NT * i, row = m0 + (id >> 3);
-        xp[i] = x + (long)(row < a.M ? row : a.M - 1) * ldx + (id & 7) * 8;
+        const int lr = (wave * CA + i) * 8 + (lane >> 3);
+        xo[i] = (uint32_t)lr * (uint32_t)ldx * 2u + (uint32_t)((lane & 7) ^ ((lr >> 1) & 7)) * 16u;
     }
-    const int trow = tid / P, part = tid % P, wrow = n0 + trow < a.n ? n0 + trow : a.n - 1;
-    const uint32_t* crow = a.codes + (long)wrow * (a.k * BITS / 32) + part * NW;
-    const uint32_t* mrow = a.meta + (long)wrow * (a.k / a.g);
-    uint4 xv[CA];
-    uint32_t qw[NW], qm;
-    auto load = [&](int k0) {
+    const int trow = tid / P, part = tid % P;
+    const bool stager = NT == BN * P || tid < BN * P;
+    const uint32_t co = (uint32_t)(trow * rb + part * NW * 4), mo = (uint32_t)(trow * ng + (lg == 5 ? part * CPT >> 5 : 0)) * 4u;
+    struct Q {
+        uint32_t w[NW], m;
+    };
+    auto load_x = [&](int kt, int slot) {
 #pragma unroll
-        for (int i = 0; i < CA; ++i) xv[i] = ld16(xp[i] + k0);
-        const uint32_t* p = crow + k0 * BITS / 32;
+        for (int i = 0; i < CA; ++i)
+            load_to_lds(rx, smem + slot * XB + (wave * CA + i) * 64, xo[i], (uint32_t)kt * 128u);
+    };
+    auto load_w = [&](Q& q, int kt) {
+        const uint32_t so = (uint32_t)kt * 8u * BITS;
         if constexpr (NW == 4) {
-            const uint4 v = ld16(p);
-            qw[0] = v.x; qw[1] = v.y; qw[2] = v.z; qw[3] = v.w;
+            const auto v = __builtin_amdgcn_raw_buffer_load_b128(rc, co, so, 0);
+            q.w[0] = v[0]; q.w[1] = v[1]; q.w[2] = v[2]; q.w[3] = v[3];
         } else if constexpr (NW == 2) {
-            const uint2 v = *reinterpret_cast<const uint2*>(p);
-            qw[0] = v.x; qw[1] = v.y;
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(rc, co, so, 0);
+            q.w[0] = v[0]; q.w[1] = v[1];
         } else {
-            qw[0] = *p;
+            q.w[0] = __builtin_amdgcn_raw_buffer_load_b32(rc, co, so, 0);
         }
-        qm = mrow[(k0 + part * CPT) / a.g];
+        q.m = __builtin_amdgcn_raw_buffer_load_b32(rm, mo, (uint32_t)((kt * 64) >> lg) * 4u, 0);
     };
-    auto store = [&](uint4* buf) {
+    const int nk = a.k / 64;
+    Q q[2];
 #pragma unroll
-        for (int i = 0; i < CA; ++i) {
-            const int id = tid + NT * i;
-            st16(&buf[swz(id >> 3, id & 7)], xv[i]);
-        }
-        dequant_store<BITS, CPT>(buf + BM * 8, qw, qm, trow, part);
-    };
-    load(0);
+    for (int s = 0; s < ST - 1; ++s) {
+        load_x(s < nk ? s : nk - 1, s);
+        if (s < 2)
+            load_w(q[s], s < nk ? s : nk - 1);
+    }
 
     f32x16_t acc[WM][WN];
 #pragma unroll
     for (int i = 0; i < WM; ++i)
 #pragma unroll
         for (int j = 0; j < WN; ++j) acc[i][j] = f32x16_t{};
-    // adapters of the rows and their distinct ones
-    if (tid == 0)
-        *nlist = 0;
-    for (int i = tid; i < BM; i += NT) {
-        const int m = m0 + i;
-        int id = m < a.M && a.T > 0 ? a.ids[m] : -1;
-        id = id < a.T ? id : -1;
-        float top = 0.0f;
-        if (id >= 0)
-            for (int r = 0; r < a.R; r += 4) {
-                const f32x4_t v = *reinterpret_cast<const f32x4_t*>(a.t + (long)m * a.R + r);
-                top = fmaxf(fmaxf(top, fmaxf(fabsf(v[0]), fabsf(v[1]))), fmaxf(fabsf(v[2]), fabsf(v[3])));
-            }
-        const int e = min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 100);
-        const float out = a.x16 && m < a.M ? a.xf[m] : 1.0f;
-        rid[i] = id;
-        rf[i] = a.bf ? 1.0f : __uint_as_float((uint32_t)(127 + e) << 23);
-        ro[i] = out;
-    }
-    __syncthreads();
-    for (int i = tid; i < BM; i += NT) {
-        const int id = rid[i];
-        bool first = id >= 0;
-        for (int k = 0; k < i && first; ++k) first = rid[k] != id;
-        if (first)
-            list[atomicAdd(nlist, 1)] = id;                // the order of the list changes nothing: one adapter per row
-    }
-    __syncthreads();
     const int r = lane & 31, hk = lane >> 5;
-    for (int l = 0; l < *nlist; ++l) {
-        const int id = list[l];
+    for (int i = tid; i < BM; i += NT) ro[i] = a.x16 && m0 + i < a.M ? a.xf[m0 + i] : 1.0f;
+    __syncthreads();
+    // the factor 2^e that takes an adapter's sums to the scale of a bfloat16 row's products
+    auto up = [&](int at) { return __uint_as_float(0x7F000000u - __float_as_uint(ro[at])); };
+    if (a.T > 0) {
+        int id[WM];
+        bool same = true;                                  // this wave's rows have one adapter, or none (or lie past M)
+        const int mf = m0 + wm * 32 * WM;
+        int ad0 = a.ids[mf < a.M ? mf : a.M - 1];
+        ad0 = ad0 >= 0 && ad0 < a.T ? ad0 : -1;
 #pragma unroll
         for (int i = 0; i < WM; ++i) {
-            const int row = wm * 32 * WM + i * 32;
-            const int m = m0 + row + r < a.M ? m0 + row + r : a.M - 1;
-            if (!__any(rid[row + r] == id))
-                continue;
+            const int m = mf + i * 32 + r;
+            const int v = a.ids[m < a.M ? m : a.M - 1];
+            id[i] = v >= 0 && v < a.T && m < a.M ? v : -1;
+            same = same && __all(id[i] == ad0 || m >= a.M);
+        }
+        const uint16_t* tp = a.tb + 8 * hk;
+        const uint16_t* bp = a.B + 8 * hk;
+        const long tlo = (long)a.M * a.R;
+        auto load_b = [&](uint4 (&b)[WN], int ad, int k) {
 #pragma unroll
             for (int j = 0; j < WN; ++j) {
                 const int col = n0 + wn * 32 * WN + j * 32 + r;
-                f32x16_t s{};
-                for (int k = 0; k < a.R; k += 16) {
-                    const int kk = k + 8 * hk;
-                    uint4 t0 = make_uint4(0, 0, 0, 0), t1 = t0, bv = t0;
-                    if (kk < a.R) {
-                        float t[8];
-                        const float* tp = a.t + (long)m * a.R + kk;
+                b[j] = k + 8 * hk < a.R ? ld16(bp + ((long)ad * a.n + (col < a.n ? col : a.n - 1)) * a.R + k) : make_uint4(0, 0, 0, 0);
+            }
+        };
+        auto load_t = [&](uint4& t0, uint4& t1, int i, int k) {
+            const int m = mf + i * 32 + r;
+            const uint16_t* p = tp + (long)(m < a.M ? m : a.M - 1) * a.R + k;
+            const bool live = k + 8 * hk < a.R;
+            t0 = live ? ld16(p) : make_uint4(0, 0, 0, 0);
+            t1 = live ? ld16(p + tlo) : make_uint4(0, 0, 0, 0);
+        };
+        if (same) {
+            if (ad0 >= 0) {
+#pragma unroll 1
+                for (int k = 0; k < a.R; k += 32) {        // all loads of 32 ranks, then the products
+                    uint4 t0[2][WM], t1[2][WM], b0[2][WN], b1;
 #pragma unroll
-                        for (int u = 0; u < 8; ++u) t[u] = tp[u];
-                        adapter_operand(t, rf[row + r], a.bf, t0, t1);
-                        bv = ld16(a.B + ((long)id * a.n + (col < a.n ? col : a.n - 1)) * a.R + kk);
+                    for (int c = 0; c < 2; ++c) {
+                        load_b(b0[c], ad0, k + 16 * c);
+#pragma unroll
+                        for (int i = 0; i < WM; ++i) load_t(t0[c][i], t1[c][i], i, k + 16 * c);
                     }
-                    s = a.bf ? mfma32_bf(t1, bv, mfma32_bf(t0, bv, s)) : mfma32(t0, bv, s);
-                }
 #pragma unroll
-                for (int v = 0; v < 16; ++v) {
-                    const int at = row + acc_row(v, lane);
-                    acc[i][j][v] = rid[at] == id ? s[v] / rf[at] / ro[at] : acc[i][j][v];
+                    for (int c = 0; c < 2; ++c)
+#pragma unroll
+                        for (int j = 0; j < WN; ++j) {
+                            if (!a.bf)
+                                split_f16(b0[c][j], b0[c][j], b1);
+#pragma unroll
+                            for (int i = 0; i < WM; ++i) {
+                                acc[i][j] = mfma32_bf(t1[c][i], b0[c][j], mfma32_bf(t0[c][i], b0[c][j], acc[i][j]));
+                                if (!a.bf)
+                                    acc[i][j] = mfma32_bf(t0[c][i], b1, acc[i][j]);
+                            }
+                        }
+                }
+                if (a.bf)
+#pragma unroll
+                    for (int i = 0; i < WM; ++i)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const float f = up(wm * 32 * WM + i * 32 + acc_row(v, lane));
+#pragma unroll
+                            for (int j = 0; j < WN; ++j) acc[i][j][v] *= f;
+                        }
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < WM; ++i) {
+                const int row = wm * 32 * WM + i * 32, slot = m0 + row < a.M ? a.slots[(m0 + row) / 32] : -1;
+                uint32_t todo = (uint32_t)__ballot(id[i] >= 0);
+                if (slot >= 0) {                           // lora_mixed_kernel has formed these rows' terms
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) {
+                        const int col = n0 + wn * 32 * WN + j * 32 + r;
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const int at = acc_row(v, lane);
+                            acc[i][j][v] = a.mixed[((long)slot * 32 + at) * a.n + (col < a.n ? col : a.n - 1)] * up(row + at);
+                        }
+                    }
+                    continue;
+                }
+#pragma unroll 1
+                while (todo) {
+                    const int ad = __builtin_amdgcn_readlane(id[i], __builtin_ctz(todo));
+                    const uint32_t own = (uint32_t)__ballot(id[i] == ad);
+                    todo &= ~own;
+                    f32x16_t s[WN];
+#pragma unroll
+                    for (int j = 0; j < WN; ++j) s[j] = f32x16_t{};
+#pragma unroll 1
+                    for (int k = 0; k < a.R; k += 32) {
+                        uint4 t0[2], t1[2], b0[2][WN], b1;
+#pragma unroll
+                        for (int c = 0; c < 2; ++c) {
+                            load_b(b0[c], ad, k + 16 * c);
+                            load_t(t0[c], t1[c], i, k + 16 * c);
+                        }
+#pragma unroll
+                        for (int c = 0; c < 2; ++c)
+#pragma unroll
+                            for (int j = 0; j < WN; ++j) {
+                                if (!a.bf)
+                                    split_f16(b0[c][j], b0[c][j], b1);
+                                s[j] = mfma32_bf(t1[c], b0[c][j], mfma32_bf(t0[c], b0[c][j], s[j]));
+                                if (!a.bf)
+                                    s[j] = mfma32_bf(t0[c], b1, s[j]);
+                            }
+                    }
+#pragma unroll
+                    for (int j = 0; j < WN; ++j)
+#pragma unroll
+                        for (int v = 0; v < 16; ++v) {
+                            const int at = acc_row(v, lane);
+                            acc[i][j][v] = own >> at & 1 ? s[j][v] * up(row + at) : acc[i][j][v];
+                        }
                 }
             }
         }
     }
 
-    const int nk = a.k / 64;
-    store(smem);
-    load(nk > 1 ? 64 : 0);
-    for (int kt = 0; kt < nk; ++kt) {
-        __syncthreads();
-        const uint4* xs = smem + (kt & 1) * (BM + BN) * 8;
-        const uint4* ws = xs + BM * 8;
+    // Step kt multiplies slot kt % ST of x and kt & 1 of the weights, while x of step kt + ST - 1 is under way, the
+    // codes of kt + 2 too, and the weights of kt + 1 are unpacked.
+    if (stager)
+        dequant_store<BITS, CPT>(wsm, q[0].w, q[0].m, trow, part);
+    load_w(q[0], nk > 2 ? 2 : nk - 1);
+    int slot = 0;
+    auto step = [&](int kt, Q& qn) {
+        // x of this step has arrived: after it ST - 2 steps' x and at least as many steps' two loads of codes were issued
+        vm_window<(ST - 2) * (CA + 2)>();
+        lds_barrier();
+        const uint4* xs = smem + slot * XB;
+        const uint4* ws = wsm + (kt & 1) * WB;
+        {
+            const int far = slot == 0 ? ST - 1 : slot - 1;
+            load_x(kt + ST - 1 < nk ? kt + ST - 1 : nk - 1, far);
+        }
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             uint4 av[WM], bv[WN];
@@ -239,9 +322,20 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
 #pragma unroll
                 for (int j = 0; j < WN; ++j) acc[i][j] = mfma32(av[i], bv[j], acc[i][j]);
         }
-        store(smem + ((kt + 1) & 1) * (BM + BN) * 8);
-        load((kt + 2 < nk ? kt + 2 : nk - 1) * 64);
+        if (stager)
+            dequant_store<BITS, CPT>(wsm + ((kt + 1) & 1) * WB, qn.w, qn.m, trow, part);
+        __asm__ volatile("" ::: "memory");                 // the codes' registers are free now, not before
+        load_w(qn, kt + 3 < nk ? kt + 3 : nk - 1);
+        slot = slot + 1 == ST ? 0 : slot + 1;
+    };
+    int kt = 0;
+    for (; kt + 1 < nk; kt += 2) {
+        step(kt, q[1]);
+        step(kt + 1, q[0]);
     }
+    if (kt < nk)
+        step(kt, q[1]);
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy into LDS outlives the workgroup
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
         const int col = n0 + wn * 32 * WN + j * 32 + r;
@@ -259,18 +353,21 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
 }  // namespace
 
 hipError_t launch_lora_gemm(const LoraArgs& a, hipStream_t st) {
-    auto run = [&](auto k, int BM, int BN, int nt) {
-        const size_t lds = (size_t)2 * (BM + BN) * 128 + (size_t)BM * 16 + 16;
+    const int lg = a.g == 32 ? 5 : a.g == 64 ? 6 : 7;
+    auto run = [&](auto k, int BM, int BN, int nt, int stages) {
+        const size_t lds = (size_t)(stages * BM + 2 * BN) * 128 + (size_t)BM * 4;
         const hipError_t e = set_lds(k, lds);
         if (e != hipSuccess)
             return e;
         const unsigned grid = (unsigned)(((a.M + BM - 1) / BM) * ((a.n + BN - 1) / BN));
-        k<<<grid, (unsigned)nt, lds, st>>>(a);
+        k<<<grid, (unsigned)nt, lds, st>>>(a, lg);
         return hipGetLastError();
     };
+    if (a.M > 512)
+        return a.bits == 2 ? run(lora_gemm_kernel<2, 256, 192, 2, 3, 3>, 256, 192, 512, 3) : run(lora_gemm_kernel<4, 256, 192, 2, 3, 3>, 256, 192, 512, 3);
     if (a.bits == 2)
-        return run(lora_gemm_kernel<2, 128, 128, 2, 2>, 128, 128, 256);
-    return run(lora_gemm_kernel<4, 128, 128, 2, 2>, 128, 128, 256);
+        return run(lora_gemm_kernel<2, 128, 128, 2, 1, 4>, 128, 128, 512, 4);
+    return run(lora_gemm_kernel<4, 128, 128, 2, 1, 4>, 128, 128, 512, 4);
 }
 
 }  // namespace qmlp

@@ -17,21 +17,29 @@ struct LoraArgs {
     int M, n, k, bits, g, T, R;
     int bf;                              // activations are bfloat16 (else binary16)
     // workspace
-    float* t;                            // [M][R] scale[a] A_a x, fp32; zeros where there is no adapter
+    float* t;                            // up to 16 rows: [M][R] scale[a] A_a x, fp32; zeros where there is no adapter
     uint16_t* x16;                       // bfloat16 rows as binary16 x 2^e (rows k apart), or null
     float* xf;                           // [M] 2^-e, or null
+    uint16_t* tb;                        // more than 16 rows: t as two bfloat16 terms [2][M][R]
+    int* slots;                          // [M / 32, rounded up]: which of the mixed sets, or -1; then [kMixedSets]: their places
+    float* mixed;                        // [kMixedSets 32][n] adapter terms of the mixed sets' rows
 };
+
+// Sets of 32 rows with more than kMixedFrom adapters between them (rows without one
+// count as one more) have their terms formed beforehand, up to kMixedSets of them.
+constexpr int kMixedSets = 16, kMixedFrom = 3;
+inline int lora_mixed_most(int M) { return (M + 31) / 32 < kMixedSets ? (M + 31) / 32 : kMixedSets; }
 
 constexpr int kLoraFewTokens = 16;       // rows of the one-shot kernel (a matrix operand's)
 
-// Whether the one-shot kernel takes the call: its rows fit one operand and its
-// arrays 32-bit offsets.
-inline bool lora_few_fits(const LoraArgs& a) {
-    constexpr long most = 1l << 31;
-    return a.M <= kLoraFewTokens && (long)a.n * a.k * a.bits / 8 < most && (long)a.n * (a.k / a.g) * 4 < most &&
-           (a.x16 ? a.k : a.ldx) < most / 2 / kLoraFewTokens;
+// Whether the one-shot kernel takes M rows: they fit one operand, and W's arrays
+// 32-bit offsets.
+inline bool lora_few_rows(int M, const qmlp_qweight* w) {
+    return M <= kLoraFewTokens && (long)w->n_out * w->k_in * w->bits / 8 < (1l << 31) &&
+           (long)w->n_out * (w->k_in / w->group) * 4 < (1l << 31);
 }
 hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st);
+hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st);
 hipError_t launch_lora_few(const LoraArgs& a, hipStream_t st);
 hipError_t launch_lora_gemm(const LoraArgs& a, hipStream_t st);
 

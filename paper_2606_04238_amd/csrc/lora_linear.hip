@@ -18,9 +18,187 @@
 namespace qmlp {
 namespace {
 
-constexpr int kPrepWaves = 8;
+constexpr int kPrepWaves = 8, kPrepRowGroups = 256;
+constexpr int kLoraPrepRows = 256;       // more rows: lora_prep_many_kernel
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4_t mfma16_bf(const uint4& a, const uint4& b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
+                                                   0, 0);
+}
 
 __device__ __forceinline__ float wave_sum(float v) { return group_sum<64>(v); }
+
+// s[r] += x[k .. k + 7] . (row r of A)[k .. k + 7], eight rows a.k apart.
+__device__ __forceinline__ void rank8_dot(float (&s)[8], const LoraArgs& a, const uint16_t* xr, const uint16_t* ar, int k) {
+    const uint4 xv = *reinterpret_cast<const uint4*>(xr + k);
+    uint4 av[8];
+#pragma unroll
+    for (int r = 0; r < 8; ++r) av[r] = *reinterpret_cast<const uint4*>(ar + (long)r * a.k + k);
+    float x[8];
+    act8(xv, a.bf, x);
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        float v[8];
+        act8(av[r], a.bf, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s[r] = __builtin_fmaf(x[i], v[i], s[r]);
+    }
+}
+
+// Row m as binary16 x 2^e, and 2^-e, by one wave: rows of up to 4096 elements stay
+// in its registers between the two passes.
+__device__ __forceinline__ void convert_row(const LoraArgs& a, int m, int lane) {
+    constexpr int N = 8;
+    const uint16_t* xr = a.x + (long)m * a.ldx;
+    uint16_t* o = a.x16 + (long)m * a.k;
+    uint4 v[N];
+    float top = 0.0f;
+    for (int k0 = 0; k0 < a.k; k0 += N * 512) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int k = k0 + i * 512 + lane * 8;
+            v[i] = k < a.k ? *reinterpret_cast<const uint4*>(xr + k) : make_uint4(0, 0, 0, 0);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float f[8];
+            act8(v[i], true, f);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) top = fmaxf(top, fabsf(f[u]));
+        }
+    }
+#pragma unroll
+    for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s, 64));
+    // top = f 2^E with 1 <= f < 2: e = 14 - E (2^e a normal number: rows whose largest is below 2^-112, or not
+    // finite, keep e = 126 or -114)
+    const int E = (int)(__float_as_uint(top) >> 23) - 127;
+    const int e = min(14 - E, 126);
+    const float up = __uint_as_float((uint32_t)(127 + e) << 23);
+    for (int k0 = 0; k0 < a.k; k0 += N * 512) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const int k = k0 + i * 512 + lane * 8;
+            if (k >= a.k)
+                continue;
+            if (a.k > N * 512)
+                v[i] = *reinterpret_cast<const uint4*>(xr + k);
+            float f[8];
+            act8(v[i], true, f);
+            uint32_t w[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) w[u] = f2h(f[2 * u] * up) | (f2h(f[2 * u + 1] * up) << 16);
+            *reinterpret_cast<uint4*>(o + k) = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+    }
+    if (lane == 0)
+        a.xf[m] = __uint_as_float((uint32_t)(127 - e) << 23);
+}
+
+// t[m][r] as the linear's launch reads it: fp32, or two bfloat16 terms.
+__device__ __forceinline__ void put_t(const LoraArgs& a, int m, int r, float t) {
+    const long at = (long)m * a.R + r;
+    if (a.tb) {
+        const uint32_t hi = act_bits(t, true);
+        a.tb[at] = (uint16_t)hi;
+        a.tb[(long)a.M * a.R + at] = act_bits(t - __uint_as_float(hi << 16), true);
+    } else {
+        a.t[at] = t;
+    }
+}
+
+// slots[s] of every set of 32 rows: its number among those with more than
+// kMixedFrom adapters (none counts as one), -1 past kMixedSets and for the others;
+// where a set has a number, its place at [sets + number].  One workgroup.
+__device__ __forceinline__ void lora_find_mixed(const LoraArgs& a, int tid) {
+    __shared__ int count[kPrepWaves * 64];
+    constexpr int N = kPrepWaves * 64;
+    const int sets = (a.M + 31) / 32, per = (sets + N - 1) / N;           // at most 64: M <= 2^20
+    unsigned long long mine = 0;
+    for (int i = 0; i < per && tid * per + i < sets; ++i) {
+        const int s = tid * per + i, n = min(32, a.M - 32 * s);
+        int v[32];
+#pragma unroll
+        for (int u = 0; u < 32; ++u) v[u] = a.ids[32 * (long)s + (u < n ? u : 0)];
+        // distinct ones, up to kMixedFrom + 1
+        int seen[kMixedFrom], d = 0;
+#pragma unroll
+        for (int u = 0; u < 32; ++u) {
+            const int id = v[u] >= 0 && v[u] < a.T ? v[u] : -1;
+            bool is = false;
+#pragma unroll
+            for (int k = 0; k < kMixedFrom; ++k) is = is || (k < d && seen[k] == id);
+            if (!is) {
+#pragma unroll
+                for (int k = 0; k < kMixedFrom; ++k) seen[k] = k == d ? id : seen[k];
+                ++d;
+            }
+        }
+        mine |= (unsigned long long)(d > kMixedFrom) << i;
+    }
+    const int c = __popcll(mine);
+    count[tid] = c;
+    __syncthreads();
+    for (int o = 1; o < N; o *= 2) {
+        const int v = tid >= o ? count[tid - o] : 0;
+        __syncthreads();
+        count[tid] += v;
+        __syncthreads();
+    }
+    int at = count[tid] - c;
+    for (int i = 0; i < per && tid * per + i < sets; ++i) {
+        const bool m = mine >> i & 1;
+        a.slots[tid * per + i] = m && at < kMixedSets ? at : -1;
+        if (m && at < kMixedSets)
+            a.slots[sets + at] = tid * per + i;
+        at += m;
+    }
+    if (tid >= count[N - 1] && tid < kMixedSets)
+        a.slots[sets + tid] = -1;
+}
+
+// Adapter terms B_a t of the rows of the mixed sets, fp32: a workgroup takes four
+// rows and 256 outputs, a lane R ranks of one output's B.  (In the product's launch itself
+// these rows' adapters, one after another, held their workgroups back: 4096 rows
+// of which 48 decode, rank 64, 391 us instead of 344 with one adapter.)
+__global__ void __launch_bounds__(256) lora_mixed_kernel(LoraArgs a) {
+    const int o = blockIdx.x * 256 + threadIdx.x, set = a.slots[(a.M + 31) / 32 + (blockIdx.y >> 3)];
+    if (set < 0 || o >= a.n)
+        return;
+    const int r0 = 4 * (blockIdx.y & 7), m0 = 32 * set + r0;
+    const long tlo = (long)a.M * a.R;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    int id[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int v = a.ids[m0 + u < a.M ? m0 + u : a.M - 1];
+        id[u] = m0 + u < a.M && v >= 0 && v < a.T ? v : -1;
+    }
+#pragma unroll 2
+    for (int c = 0; c < a.R; c += 8) {
+        uint4 bv[4], t0[4], t1[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (id[u] >= 0) {
+                const uint16_t* tp = a.tb + (long)(m0 + u) * a.R + c;
+                bv[u] = *reinterpret_cast<const uint4*>(a.B + ((long)id[u] * a.n + o) * a.R + c);
+                t0[u] = *reinterpret_cast<const uint4*>(tp);
+                t1[u] = *reinterpret_cast<const uint4*>(tp + tlo);
+            }
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+            if (id[u] >= 0) {
+                float b[8], f0[8], f1[8];
+                act8(bv[u], a.bf, b);
+                act8(t0[u], true, f0);
+                act8(t1[u], true, f1);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[u] = __builtin_fmaf(b[i], f0[i] + f1[i], s[u]);
+            }
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) a.mixed[((long)(blockIdx.y >> 3) * 32 + r0 + u) * a.n + o] = s[u];
+}
 
 // blockIdx.x: token, blockIdx.y: eight ranks of t, or (the last one, where
 // bfloat16) the row's conversion.  t: the waves split k, a lane takes eight
@@ -29,64 +207,27 @@ __device__ __forceinline__ float wave_sum(float v) { return group_sum<64>(v); }
 __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) {
     const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const uint16_t* xr = a.x + (long)m * a.ldx;
     const int ny = a.T > 0 ? a.R / 8 : 0;
-    if ((int)blockIdx.y >= ny) {
-        __shared__ float best[kPrepWaves];
-        float top = 0.0f;
-        for (int k = tid * 8; k < a.k; k += kPrepWaves * 64 * 8) {
-            float f[8];
-            act8(*reinterpret_cast<const uint4*>(xr + k), true, f);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
-        }
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s, 64));
-        if (lane == 0)
-            best[wave] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < kPrepWaves; ++w) top = fmaxf(top, best[w]);
-        // top = f 2^E with 1 <= f < 2: e = 14 - E (2^e a normal number: rows whose largest is below 2^-112, or not
-        // finite, keep e = 126 or -113)
-        const int E = (int)(__float_as_uint(top) >> 23) - 127;
-        const int e = min(14 - E, 126);
-        const float up = __uint_as_float((uint32_t)(127 + e) << 23);
-        for (int k = tid * 8; k < a.k; k += kPrepWaves * 64 * 8) {
-            float f[8];
-            act8(*reinterpret_cast<const uint4*>(xr + k), true, f);
-            uint32_t o[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) o[i] = f2h(f[2 * i] * up) | (f2h(f[2 * i + 1] * up) << 16);
-            *reinterpret_cast<uint4*>(a.x16 + (long)m * a.k + k) = make_uint4(o[0], o[1], o[2], o[3]);
-        }
-        if (tid == 0)
-            a.xf[m] = __uint_as_float((uint32_t)(127 - e) << 23);
+    if (m >= a.M) {
+        if (blockIdx.y == 0)
+            lora_find_mixed(a, tid);
         return;
     }
+    if ((int)blockIdx.y >= ny) {
+        if (wave == 0)
+            convert_row(a, m, lane);
+        return;
+    }
+    const uint16_t* xr = a.x + (long)m * a.ldx;
     const int id = a.ids[m], r0 = blockIdx.y * 8;
     if (id < 0 || id >= a.T) {
         if (tid < 8)
-            a.t[(long)m * a.R + r0 + tid] = 0.0f;
+            put_t(a, m, r0 + tid, 0.0f);
         return;
     }
     const uint16_t* ar = a.A + ((long)id * a.R + r0) * a.k;
     float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int k = tid * 8; k < a.k; k += kPrepWaves * 64 * 8) {
-        const uint4 xv = *reinterpret_cast<const uint4*>(xr + k);
-        uint4 av[8];
-#pragma unroll
-        for (int r = 0; r < 8; ++r) av[r] = *reinterpret_cast<const uint4*>(ar + (long)r * a.k + k);
-        float x[8];
-        act8(xv, a.bf, x);
-#pragma unroll
-        for (int r = 0; r < 8; ++r) {
-            float v[8];
-            act8(av[r], a.bf, v);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s[r] = __builtin_fmaf(x[i], v[i], s[r]);
-        }
-    }
+    for (int k = tid * 8; k < a.k; k += kPrepWaves * 64 * 8) rank8_dot(s, a, xr, ar, k);
     __shared__ float red[kPrepWaves][8];
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
@@ -99,8 +240,161 @@ __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) 
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < kPrepWaves; ++w) v += red[w][tid];
-        a.t[(long)m * a.R + r0 + tid] = (a.scale ? a.scale[id] : 1.0f) * v;
+        put_t(a, m, r0 + tid, (a.scale ? a.scale[id] : 1.0f) * v);
     }
+}
+
+// t of row m by one workgroup: R / 8 sets of waves take eight ranks each and split k.
+__device__ __forceinline__ void lora_row(const LoraArgs& a, int m, int id, float* rs, int tid) {
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int per = kPrepWaves * 8 / a.R, r0 = 8 * (wave / per);
+    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    if (id >= 0) {
+        const uint16_t* xr = a.x + (long)m * a.ldx;
+        const uint16_t* ar = a.A + ((long)id * a.R + r0) * a.k;
+        for (int k = ((wave % per) * 64 + lane) * 8; k < a.k; k += per * 64 * 8) rank8_dot(s, a, xr, ar, k);
+    }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) {
+        const float v = wave_sum(s[r]);
+        if (lane == 0)
+            rs[wave * 8 + r] = v;
+    }
+    __syncthreads();
+    if (tid < a.R) {
+        float v = 0.0f;
+        for (int w = 0; w < per; ++w) v += rs[((tid >> 3) * per + w) * 8 + (tid & 7)];
+        put_t(a, m, tid, id < 0 ? 0.0f : (a.scale ? a.scale[id] : 1.0f) * v);
+    }
+    __syncthreads();
+}
+
+// The adapters of the 16 rows of a tile (lane j: row j): the first, the first that
+// differs, and whether there are more.
+struct TileAds {
+    int id, id0, id1;
+    bool more;
+};
+__device__ __forceinline__ TileAds tile_adapters(const LoraArgs& a, int m0, int j) {
+    const int v = m0 + j < a.M ? a.ids[m0 + j] : -1;
+    TileAds t;
+    t.id = v >= 0 && v < a.T ? v : -1;
+    const uint32_t any = (uint32_t)__ballot(t.id >= 0) & 0xFFFFu;
+    t.id0 = any ? __builtin_amdgcn_readlane(t.id, __builtin_ctz(any)) : -1;
+    const uint32_t rest = any & ~((uint32_t)__ballot(t.id == t.id0) & 0xFFFFu);
+    t.id1 = rest ? __builtin_amdgcn_readlane(t.id, __builtin_ctz(rest)) : -1;
+    t.more = (rest & ~((uint32_t)__ballot(t.id == t.id1) & 0xFFFFu)) != 0;
+    return t;
+}
+
+// The same for many rows, one workgroup after another: one that finds the mixed
+// sets; one per 16 rows, which multiplies them on the matrix cores where they
+// have at most two adapters between them (a prompt); kPrepRowGroups that share
+// the rows of the other tiles, a row at a time; and those that convert.  (A
+// workgroup per row and eight ranks would read x and A R / 8 and M times: at 4096
+// rows of rank 64 200 us.  16 per tile of which most have nothing to do: 115.)
+__global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_many_kernel(LoraArgs a, int tiles, int rowgroups) {
+    __shared__ f32x4_t red[kPrepWaves][4][64];
+    const int tid = threadIdx.x, lane = tid & 63, j = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    int block = blockIdx.x;
+    if (block == 0) {
+        if (tiles > 0)
+            lora_find_mixed(a, tid);
+        return;
+    }
+    block -= 1;
+    if (block < rowgroups) {
+        // sets of kPrepWaves * 4 tiles: a wave looks at four of them, 16 rows each
+        __shared__ unsigned long long flags;
+        int seen = 0;                                      // rows of earlier tiles
+        for (int t0 = 0; t0 < tiles; t0 += 64) {
+            if (tid == 0)
+                flags = 0;
+            __syncthreads();
+            unsigned long long f = 0;
+            for (int u = wave; u < 64 && t0 + u < tiles; u += kPrepWaves)
+                if (tile_adapters(a, 16 * (t0 + u), j).more)
+                    f |= 1ull << u;
+            if (lane == 0 && f)
+                atomicOr(&flags, f);
+            __syncthreads();
+            f = flags;
+            __syncthreads();
+            for (; f; f &= f - 1) {
+                const int m0 = 16 * (t0 + __builtin_ctzll(f));
+                // this workgroup's rows of the 16: numbers block, block + rowgroups, ..
+                for (int p = (block - seen % rowgroups + rowgroups) % rowgroups; p < 16; p += rowgroups) {
+                    const int m = m0 + p;
+                    if (m < a.M) {
+                        const int v = a.ids[m];
+                        lora_row(a, m, v >= 0 && v < a.T ? v : -1, reinterpret_cast<float*>(red), tid);
+                    }
+                }
+                seen += 16;
+            }
+        }
+        return;
+    }
+    block -= rowgroups;
+    if (block >= tiles) {
+        const int m = (block - tiles) * kPrepWaves + wave;
+        if (m < a.M)
+            convert_row(a, m, lane);
+        return;
+    }
+    const int m0 = block * 16;
+    const TileAds t = tile_adapters(a, m0, j);
+    if (t.more)
+        return;
+    const uint16_t* xr = a.x + (long)(m0 + j < a.M ? m0 + j : a.M - 1) * a.ldx + 8 * q;
+    const int rt = (a.R + 15) / 16, n = a.k / 32;
+    f32x4_t out = {0.f, 0.f, 0.f, 0.f};                    // wave w < rt: ranks 16 w ..
+    for (int u = 0; u < 2; ++u) {
+        const int ad = u ? t.id1 : t.id0;
+        if (ad < 0)
+            break;
+        const uint16_t* ar = a.A + (long)ad * a.R * a.k + 8 * q;
+        f32x4_t acc[4];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) acc[c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 2
+        for (int s = wave; s < n; s += kPrepWaves) {
+            const uint4 xv = *reinterpret_cast<const uint4*>(xr + 32 * s);
+            uint4 av[4];
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const int rk = 16 * c + j < a.R ? 16 * c + j : a.R - 1;
+                if (c < rt)
+                    av[c] = *reinterpret_cast<const uint4*>(ar + (long)rk * a.k + 32 * s);
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+                if (c < rt)
+                    acc[c] = a.bf ? mfma16_bf(xv, av[c], acc[c]) : mfma16(xv, av[c], acc[c]);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (c < rt)
+                red[wave][c][lane] = acc[c];
+        __syncthreads();
+        if (wave < rt) {
+            f32x4_t v = red[0][wave][lane];
+#pragma unroll
+            for (int w = 1; w < kPrepWaves; ++w) v += red[w][wave][lane];
+            const float sc = a.scale ? a.scale[ad] : 1.0f;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (__builtin_amdgcn_ds_bpermute(4 * (4 * q + i), t.id) == ad)
+                    out[i] = sc * v[i];
+        }
+    }
+    if (wave < rt && 16 * wave + j < a.R)
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (m0 + 4 * q + i < a.M)
+                put_t(a, m0 + 4 * q + i, 16 * wave + j, out[i]);
 }
 
 // Adds B_a[o][8 c .. 8 c + 7] . t[token][8 c ..] for the lane's row o and its
@@ -174,7 +468,20 @@ hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st) {
     const unsigned ny = (a.T > 0 ? a.R / 8 : 0) + (a.bf ? 1 : 0);
     if (ny == 0)
         return hipSuccess;
-    lora_prep_kernel<<<dim3((unsigned)a.M, ny), kPrepWaves * 64, 0, st>>>(a);
+    if (a.M > kLoraPrepRows) {
+        const int tiles = a.T > 0 ? (a.M + 15) / 16 : 0;
+        const int rowgroups = tiles == 0 ? 0 : 16 * tiles < kPrepRowGroups ? 16 * tiles : kPrepRowGroups;
+        const unsigned convert = a.bf ? (unsigned)(a.M + kPrepWaves - 1) / kPrepWaves : 0u;
+        lora_prep_many_kernel<<<1u + rowgroups + tiles + convert, kPrepWaves * 64, 0, st>>>(a, tiles, rowgroups);
+        return hipGetLastError();
+    }
+    const bool find = a.T > 0 && a.tb;                     // one more column of workgroups looks for the mixed sets
+    lora_prep_kernel<<<dim3((unsigned)a.M + (find ? 1u : 0u), ny), kPrepWaves * 64, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st) {
+    lora_mixed_kernel<<<dim3((unsigned)(a.n + 255) / 256, 8u * (unsigned)lora_mixed_most(a.M)), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 

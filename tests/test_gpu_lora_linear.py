@@ -36,7 +36,8 @@ SHAPES = [
     (4, 128, 272, 17408, 3, 16, 3), (2, 64, 48, 8320, 16, 32, 8),
     (4, 128, 256, 512, 17, 16, 3), (4, 32, 130, 64, 31, 8, 40), (4, 64, 255, 320, 129, 64, 5),
     (2, 32, 1000, 1600, 130, 32, 3), (2, 128, 1, 256, 257, 16, 2), (4, 128, 511, 1152, 64, 32, 70),
-    (2, 64, 640, 4160, 300, 64, 2),
+    (2, 64, 640, 4160, 300, 64, 2), (4, 64, 200, 192, 290, 8, 40), (2, 128, 129, 384, 400, 64, 30),
+    (4, 32, 96, 128, 600, 16, 3), (4, 128, 700, 256, 513, 32, 50), (2, 64, 1030, 192, 1025, 16, 1),
 ]
 
 
