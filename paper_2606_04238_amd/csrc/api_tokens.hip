@@ -47,18 +47,33 @@ qmlp_status check_lora(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qm
     return QMLP_OK;
 }
 
-// Workspace: [t: M x R fp32, or as two bfloat16 terms], past 16 rows [sets of
-// rows with several adapters][their terms, fp32], and for bfloat16 [2^-e: M
-// fp32][x 2^e: M x k binary16].
+// Workspace: [t: M x R fp32, or as two bfloat16 terms][adapters of up to 16 rows,
+// or sets of rows with several][2^-e: M fp32], then up to 16 rows [x in operand
+// order][its group sums], past them [terms of the rows of those sets, fp32] and
+// for bfloat16 [x 2^e: M x k binary16].
 struct LoraSizes {
-    size_t t, slots, mixed, xf, x16;
-    size_t all() const { return t + slots + mixed + xf + x16; }
+    size_t t, slots, xf, xo, xs, mixed, x16;
+    size_t all() const { return t + slots + xf + xo + xs + mixed + x16; }
 };
 LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
-    const bool bf = dtype == QMLP_BF16, some = ad && ad->count > 0, many = some && !lora_few_rows(M, w);
-    return {some ? round256((size_t)M * ad->rank * 4) : 0, many ? round256(((size_t)(M + 31) / 32 + kMixedSets) * 4) : 0,
-            many ? round256((size_t)lora_mixed_most(M) * 32 * w->n_out * 4) : 0, bf ? round256((size_t)M * 4) : 0,
-            bf ? round256((size_t)M * w->k_in * 2) : 0};
+    const bool bf = dtype == QMLP_BF16, some = ad && ad->count > 0, few = lora_few_rows(M, w);
+    LoraSizes z{};
+    if (some) {
+        z.t = round256((size_t)M * ad->rank * 4);
+        z.slots = round256(((size_t)(M + 31) / 32 + kMixedSets) * 4);
+    }
+    if (bf)
+        z.xf = round256((size_t)M * 4);
+    if (few) {
+        z.xo = round256((size_t)M * operand_row(w->k_in, w->bits) * 2);
+        z.xs = round256((size_t)M * operand_sums(w->k_in, w->bits, w->group) * 4);
+    } else {
+        if (some)
+            z.mixed = round256((size_t)lora_mixed_most(M) * 32 * w->n_out * 4);
+        if (bf)
+            z.x16 = round256((size_t)M * w->k_in * 2);
+    }
+    return z;
 }
 
 // ---------------------------------------------------------------- router
@@ -110,16 +125,19 @@ qmlp_status check_moe(const qmlp_moe* l, int M, qmlp_dtype dtype) {
     return QMLP_OK;
 }
 
-// Workspace: [logits fp64][expert of a slot][its weight][blocks][t][h][outputs of the instances, fp32].
+// Workspace: [logits fp64][expert of a slot][its weight][blocks][t][h][outputs of
+// the instances, fp32][x in operand order][its group sums].
 struct MoeSizes {
-    size_t logits, idx, w, blocks, t, h, part;
-    size_t all() const { return logits + idx + w + blocks + t + h + part; }
+    size_t logits, idx, w, blocks, t, h, part, xo, xs;
+    size_t all() const { return logits + idx + w + blocks + t + h + part + xo + xs; }
 };
 MoeSizes moe_sizes(const qmlp_moe* l, int M) {
     const size_t n = (size_t)M * l->topk;
     return {route_bytes(M, l->experts), round256(n * 4), round256(n * 4),
             round256((size_t)(1 + moe_blocks_most((int)n, l->experts)) * kBlkInts * 4),
-            round256(n * 2 * l->mlp.rank * 4), round256(n * l->mlp.down.k_in * 2), round256(n * l->mlp.gate.k_in * 4)};
+            round256(n * 2 * l->mlp.rank * 4), round256(n * operand_row(l->mlp.down.k_in, l->mlp.down.bits) * 2), round256(n * l->mlp.gate.k_in * 4),
+            round256((size_t)M * operand_row(l->mlp.gate.k_in, l->mlp.gate.bits) * 2),
+            round256((size_t)M * operand_sums(l->mlp.gate.k_in, l->mlp.gate.bits, l->mlp.gate.group) * 4)};
 }
 
 }  // namespace
@@ -177,14 +195,20 @@ qmlp_status qmlp_linear_lora(const qmlp_qweight* w, const qmlp_adapters* ad, con
     a.g = w->group;
     a.bf = dtype == QMLP_BF16;
     const bool few = lora_few_rows(M, w);
-    a.t = few ? reinterpret_cast<float*>(base) : nullptr;
-    a.tb = few ? nullptr : reinterpret_cast<uint16_t*>(base);
-    base += z.t;
-    a.slots = reinterpret_cast<int*>(base);
-    a.mixed = reinterpret_cast<float*>(base + z.slots);
-    base += z.slots + z.mixed;
-    a.xf = a.bf ? reinterpret_cast<float*>(base) : nullptr;
-    a.x16 = a.bf ? reinterpret_cast<uint16_t*>(base + z.xf) : nullptr;
+    const auto take = [&](size_t bytes) {
+        char* at = base;
+        base += bytes;
+        return at;
+    };
+    char* t = take(z.t);
+    a.t = few ? reinterpret_cast<float*>(t) : nullptr;
+    a.tb = few ? nullptr : reinterpret_cast<uint16_t*>(t);
+    a.slots = a.known = reinterpret_cast<int*>(take(z.slots));
+    a.xf = reinterpret_cast<float*>(take(z.xf));
+    a.xo = few ? reinterpret_cast<uint16_t*>(take(z.xo)) : nullptr;
+    a.xs = reinterpret_cast<float*>(take(z.xs));
+    a.mixed = reinterpret_cast<float*>(take(z.mixed));
+    a.x16 = z.x16 ? reinterpret_cast<uint16_t*>(take(z.x16)) : nullptr;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e = launch_lora_prep(a, st);
     if (e == hipSuccess && !few && adapters)
@@ -269,10 +293,14 @@ qmlp_status qmlp_moe_layer(const qmlp_moe* layer, const void* x, int M, qmlp_dty
     a.y = static_cast<uint16_t*>(y);
     a.idx = r.idx;
     a.w = r.w;
+    a.logits = r.logits;
+    a.score = r.score;
     a.blocks = reinterpret_cast<int*>(take(z.blocks));
     a.t = reinterpret_cast<float*>(take(z.t));
     a.h = reinterpret_cast<uint16_t*>(take(z.h));
     a.part = reinterpret_cast<float*>(take(z.part));
+    a.xo = reinterpret_cast<uint16_t*>(take(z.xo));
+    a.xs = reinterpret_cast<float*>(take(z.xs));
     a.M = M;
     a.d = r.d;
     a.f = m.down.k_in;
@@ -285,7 +313,7 @@ qmlp_status qmlp_moe_layer(const qmlp_moe* layer, const void* x, int M, qmlp_dty
     a.dg = m.down.group;
     a.lora_scale = m.lora_scale;
     const hipStream_t st = static_cast<hipStream_t>(stream);
-    const hipError_t e = launch_route(r, st);
+    const hipError_t e = launch_route_logits(r, st);
     return from_hip(e != hipSuccess ? e : launch_moe_experts(a, st));
 }
 

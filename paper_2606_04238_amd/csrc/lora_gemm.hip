@@ -38,10 +38,6 @@ __device__ __forceinline__ f32x16_t mfma32_bf(const uint4& a, const uint4& b, co
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c,
                                                    0, 0, 0);
 }
-__device__ __forceinline__ uint4 ld16(const void* p) {
-    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
-    return make_uint4(v.x, v.y, v.z, v.w);
-}
 __device__ __forceinline__ void st16(uint4* p, const uint4& v) { *reinterpret_cast<u32x4*>(p) = u32x4{v.x, v.y, v.z, v.w}; }
 // 16 bytes per lane from memory to LDS, lane l to lds + l.  (The host's pass knows no such builtin.)
 __device__ __forceinline__ void load_to_lds(Rsrc r, uint4* lds, uint32_t voff, uint32_t soff) {

@@ -2,6 +2,7 @@
 // (lora_linear.hip, lora_gemm.hip).
 #pragma once
 
+#include "oneshot_plan.h"
 #include "qmlp_internal.h"
 
 namespace qmlp {
@@ -17,9 +18,12 @@ struct LoraArgs {
     int M, n, k, bits, g, T, R;
     int bf;                              // activations are bfloat16 (else binary16)
     // workspace
+    int* known;                          // up to 16 rows: [16] adapter of a row, -1: none
     float* t;                            // up to 16 rows: [M][R] scale[a] A_a x, fp32; zeros where there is no adapter
-    uint16_t* x16;                       // bfloat16 rows as binary16 x 2^e (rows k apart), or null
-    float* xf;                           // [M] 2^-e, or null
+    uint16_t* xo;                        // up to 16 rows: x in operand order (oneshot.h), or null
+    float* xs;                           // and its group sums
+    uint16_t* x16;                       // more: bfloat16 rows as binary16 x 2^e (rows k apart), or null
+    float* xf;                           // [M] 2^-e (bfloat16)
     uint16_t* tb;                        // more than 16 rows: t as two bfloat16 terms [2][M][R]
     int* slots;                          // [M / 32, rounded up]: which of the mixed sets, or -1; then [kMixedSets]: their places
     float* mixed;                        // [kMixedSets 32][n] adapter terms of the mixed sets' rows

@@ -70,10 +70,7 @@ __device__ __forceinline__ void convert_row(const LoraArgs& a, int m, int lane) 
     }
 #pragma unroll
     for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s, 64));
-    // top = f 2^E with 1 <= f < 2: e = 14 - E (2^e a normal number: rows whose largest is below 2^-112, or not
-    // finite, keep e = 126 or -114)
-    const int E = (int)(__float_as_uint(top) >> 23) - 127;
-    const int e = min(14 - E, 126);
+    const int e = bf16_shift(top);
     const float up = __uint_as_float((uint32_t)(127 + e) << 23);
     for (int k0 = 0; k0 < a.k; k0 += N * 512) {
 #pragma unroll
@@ -200,8 +197,8 @@ __global__ void __launch_bounds__(256) lora_mixed_kernel(LoraArgs a) {
     for (int u = 0; u < 4; ++u) a.mixed[((long)(blockIdx.y >> 3) * 32 + r0 + u) * a.n + o] = s[u];
 }
 
-// blockIdx.x: token, blockIdx.y: eight ranks of t, or (the last one, where
-// bfloat16) the row's conversion.  t: the waves split k, a lane takes eight
+// blockIdx.x: token, blockIdx.y: eight ranks of t, or (the last one) the row's
+// conversion to operands, past 16 rows of bfloat16 to binary16.  t: the waves split k, a lane takes eight
 // elements of x and of eight rows of A at a time, fp32 throughout.  It is one
 // trip to memory of 9 KB a wave; the launch's time is its latency.
 __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) {
@@ -214,12 +211,21 @@ __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) 
         return;
     }
     if ((int)blockIdx.y >= ny) {
-        if (wave == 0)
+        if (a.xo)
+            operands_of_row<kPrepWaves>(a.x + (long)m * a.ldx, a.k, a.bf, a.bits, a.g, a.xo + (long)m * operand_row(a.k, a.bits),
+                                        a.xs + (long)m * operand_sums(a.k, a.bits, a.g), a.xf + m, tid);
+        else if (wave == 0)
             convert_row(a, m, lane);
         return;
     }
     const uint16_t* xr = a.x + (long)m * a.ldx;
     const int id = a.ids[m], r0 = blockIdx.y * 8;
+    if (a.t && blockIdx.y == 0 && tid < 16) {
+        if (tid == m)
+            a.known[m] = id >= 0 && id < a.T ? id : -1;
+        else if (m == 0 && tid >= a.M)
+            a.known[tid] = -1;
+    }
     if (id < 0 || id >= a.T) {
         if (tid < 8)
             put_t(a, m, r0 + tid, 0.0f);
@@ -397,67 +403,104 @@ __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_many_kernel(LoraArg
                 put_t(a, m0 + 4 * q + i, 16 * wave + j, out[i]);
 }
 
-// Adds B_a[o][8 c .. 8 c + 7] . t[token][8 c ..] for the lane's row o and its
-// tokens 4 q + v.  A row with no adapter adds nothing (not 0 B: an adapter
-// that holds infinities belongs to its own rows only).
-__device__ __forceinline__ void lora_rank8(f32x4_t& acc, const LoraArgs& a, int o, int c, int lane) {
+// An item of the adapters' share of RT tiles, it = 4 c + v: eight ranks, 8 c .., for
+// the tokens 4 q + v; B_a[o][8 c ..] of the lane's row o = row0 + 16 t + j.  A row
+// with no adapter adds nothing (not 0 B: an adapter that holds infinities belongs
+// to its own rows only).
+template <int RT>
+struct Rank8 {
+    int id;
+    uint4 b[RT];
+    f32x4_t t[2];
+};
+template <int RT>
+__device__ __forceinline__ void rank8_load(Rank8<RT>& k, const LoraArgs& a, int row0, int it, int lane) {
+    const int q = lane >> 4, j = lane & 15, v = it & 3, c = it >> 2;
+    // uniform addresses: scalar loads, which do not queue behind the weights
+    const int i0 = a.known[v], i1 = a.known[4 + v], i2 = a.known[8 + v], i3 = a.known[12 + v];
+    k.id = q < 2 ? (q == 0 ? i0 : i1) : (q == 2 ? i2 : i3);
+    if (k.id >= 0) {
+        const f32x4_t* tp = reinterpret_cast<const f32x4_t*>(a.t + (long)(4 * q + v) * a.R + 8 * c);
+        k.t[0] = tp[0];
+        k.t[1] = tp[1];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const int tok = 4 * (lane >> 4) + v;
-        const int id = tok < a.M ? a.ids[tok] : -1;
-        if (id >= 0 && id < a.T && o < a.n) {
-            float b[8];
-            act8(*reinterpret_cast<const uint4*>(a.B + ((long)id * a.n + o) * a.R + 8 * c), a.bf, b);
-            const float* t = a.t + (long)tok * a.R + 8 * c;
-            float s = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) s = __builtin_fmaf(b[i], t[i], s);
-            acc[v] += s;
+        for (int t = 0; t < RT; ++t) {
+            const int o = row0 + 16 * t + j < a.n ? row0 + 16 * t + j : a.n - 1;
+            k.b[t] = *reinterpret_cast<const uint4*>(a.B + ((long)k.id * a.n + o) * a.R + 8 * c);
         }
+    }
+}
+template <int RT>
+__device__ __forceinline__ void rank8_add(f32x4_t (&acc)[1][RT], const Rank8<RT>& k, int it, bool bf) {
+#pragma unroll
+    for (int t = 0; t < RT; ++t) {
+        float b[8], s = 0.0f;
+        act8(k.b[t], bf, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) s = __builtin_fmaf(b[i], k.t[i >> 2][i & 3], s);
+        s = k.id >= 0 ? s : 0.0f;
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+            if (v == (it & 3))
+                acc[0][t][v] += s;
     }
 }
 
 // Up to 16 rows of x: a workgroup owns RT tiles of 16 outputs (oneshot.h), the
-// waves share its LoRA terms by eight ranks.
+// waves share its adapters' terms by eight ranks.
 template <int B, int G, int RT>
-__global__ void __launch_bounds__(1024) lora_few_kernel(LoraArgs a, int ns, int kw) {
+__global__ void __launch_bounds__(512) lora_few_kernel(LoraArgs a, int ns, int kw) {
     extern __shared__ uint4 smem[];
     f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);       // [kw][RT][64]
     const int lane = threadIdx.x & 63, j = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int row0 = blockIdx.x * 16 * RT;
     const int rb = a.k * B / 8, ng = a.k / G;
-    const Rsrc rc[1] = {rsrc(a.codes, (uint32_t)a.n * (uint32_t)rb)};
-    const Rsrc rm[1] = {rsrc(a.meta, (uint32_t)a.n * (uint32_t)ng * 4u)};
-    const int ldx = a.x16 ? a.k : (int)a.ldx;
-    const Rsrc rx = rsrc(a.x16 ? a.x16 : a.x, (uint32_t)((a.M - 1) * ldx + a.k) * 2u);
+    OneWork<1> o;
+    o.magic = magic_vgpr();
+    o.rc[0] = rsrc(a.codes, (uint32_t)a.n * (uint32_t)rb);
+    o.rm[0] = rsrc(a.meta, (uint32_t)a.n * (uint32_t)ng * 4u);
+    const uint32_t row = j < a.M ? j : 0, xb = operand_row(a.k, B) * 2u, sb = operand_sums(a.k, B, G) * 4u;
+    o.rx = rsrc(a.xo, (uint32_t)a.M * xb);
+    o.rs = rsrc(a.xs, (uint32_t)a.M * sb);
+    o.xv = row * xb + lane_x<B, G>(lane >> 4);
+    o.sv = row * sb + lane_sums<B, G>(lane >> 4);
+    o.K = a.k;
+    o.N = a.n;
+    o.row0 = blockIdx.x * 16 * RT;
+    const int items = a.T > 0 ? a.R / 2 : 0;
     f32x4_t acc[1][RT];
-    oneshot_products<B, G, 1, RT>(acc, rc, rm, rx, j, j < a.M, ldx, a.k, a.n, row0, wave, ns, kw, lane);
+    Rank8<RT> k8;
+    float f[4] = {1.f, 1.f, 1.f, 1.f};
+    oneshot_products<B, G, 1, RT, false>(acc, o, wave, ns, kw, lane, [&] {
+        if (wave < items)
+            rank8_load<RT>(k8, a, o.row0, wave, lane);
+        if (a.bf)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) f[v] = a.xf[4 * (lane >> 4) + v < a.M ? 4 * (lane >> 4) + v : 0];
+    });
     // the factor of bfloat16 rows, before terms that do not have it
-    float f[4];
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const int tok = 4 * (lane >> 4) + v;
-        f[v] = kTileUnscale * (a.x16 && tok < a.M ? a.xf[tok] : 1.0f);
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) acc[0][t][v] *= kTileUnscale * f[v];
+    if (wave < items)
+        rank8_add<RT>(acc, k8, wave, a.bf);
+    for (int it = wave + kw; it < items; it += kw) {
+        rank8_load<RT>(k8, a, o.row0, it, lane);
+        rank8_add<RT>(acc, k8, it, a.bf);
     }
 #pragma unroll
-    for (int t = 0; t < RT; ++t) {
-#pragma unroll
-        for (int v = 0; v < 4; ++v) acc[0][t][v] *= f[v];
-        if (a.T > 0)
-            for (int c = wave; c < a.R / 8; c += kw) lora_rank8(acc[0][t], a, row0 + 16 * t + j, c, lane);
-        red[(wave * RT + t) * 64 + lane] = acc[0][t];
-    }
+    for (int t = 0; t < RT; ++t) red[(wave * RT + t) * 64 + lane] = acc[0][t];
     __syncthreads();
     for (int t = wave; t < RT; t += kw) {
         f32x4_t s = red[t * 64 + lane];
         for (int w = 1; w < kw; ++w) s += red[(w * RT + t) * 64 + lane];
-        const int o = row0 + 16 * t + j;
+        const int n = o.row0 + 16 * t + j;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
             const int tok = 4 * (lane >> 4) + v;
-            if (tok < a.M && o < a.n)
-                a.y[(long)tok * a.ldy + o] = act_bits(s[v], a.bf);
+            if (tok < a.M && n < a.n)
+                a.y[(long)tok * a.ldy + n] = act_bits(s[v], a.bf);
         }
     }
 }
@@ -465,7 +508,7 @@ __global__ void __launch_bounds__(1024) lora_few_kernel(LoraArgs a, int ns, int 
 }  // namespace
 
 hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st) {
-    const unsigned ny = (a.T > 0 ? a.R / 8 : 0) + (a.bf ? 1 : 0);
+    const unsigned ny = (a.T > 0 ? a.R / 8 : 0) + (a.bf || a.xo ? 1 : 0);
     if (ny == 0)
         return hipSuccess;
     if (a.M > kLoraPrepRows) {
@@ -488,15 +531,18 @@ hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st) {
 hipError_t launch_lora_few(const LoraArgs& a, hipStream_t st) {
     if (a.M < 1 || a.M > kLoraFewTokens)
         return hipErrorInvalidValue;
-    constexpr int RT = 1;
-    const int ns = oneshot_steps(a.k, a.bits), kw = oneshot_waves(ns, 16);
-    const unsigned grid = (unsigned)((a.n + 16 * RT - 1) / (16 * RT));
-    const size_t lds = (size_t)kw * RT * 1024;
-#define QMLP_LF(B_, G_)                                                              \
-    if (a.bits == B_ && a.g == G_) {                                                 \
-        lora_few_kernel<B_, G_, RT><<<grid, (unsigned)kw * 64, lds, st>>>(a, ns, kw); \
-        return hipGetLastError();                                                    \
-    }
+    // Two tiles of a workgroup share its operands, one tile makes twice the workgroups: one where those are no more
+    // than the compute units (us, 4 bits, one and two tiles: 2560 x 2560, 160 tiles, M = 1 4.9 and 6.1, M = 16 7.1 and
+    // 8.4; 6144 x 4096, 384 tiles, 9.5 and 8.9, 16.4 and 12.0; 28672 x 4096 25.9 and 24.9, 51.9 and 38.9).
+    const int rt = (a.n + 15) / 16 <= 256 ? 1 : 2, ns = oneshot_steps(a.k, a.bits), kw = oneshot_waves(ns);
+    const unsigned grid = (unsigned)((a.n + 16 * rt - 1) / (16 * rt));
+    auto run = [&](auto k) {
+        k<<<grid, (unsigned)kw * 64, (size_t)kw * rt * 1024, st>>>(a, ns, kw);
+        return hipGetLastError();
+    };
+#define QMLP_LF(B_, G_)            \
+    if (a.bits == B_ && a.g == G_) \
+        return rt == 1 ? run(lora_few_kernel<B_, G_, 1>) : run(lora_few_kernel<B_, G_, 2>);
     QMLP_LF(2, 32) QMLP_LF(2, 64) QMLP_LF(2, 128) QMLP_LF(4, 32) QMLP_LF(4, 64) QMLP_LF(4, 128)
     return hipErrorInvalidValue;
 }

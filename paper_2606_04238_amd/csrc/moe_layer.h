@@ -2,6 +2,7 @@
 // (moe_route.hip, moe_layer.hip).
 #pragma once
 
+#include "oneshot_plan.h"
 #include "qmlp_internal.h"
 
 namespace qmlp {
@@ -18,6 +19,7 @@ struct RouteArgs {
     int M, d, E, k, score, bf;
 };
 hipError_t launch_route(const RouteArgs& a, hipStream_t st);
+hipError_t launch_route_logits(const RouteArgs& a, hipStream_t st);
 
 // A block of work of the experts' launches: up to 16 instances (a token and one
 // of its slots) of one expert.
@@ -28,17 +30,21 @@ struct MoeArgs {
     const uint16_t *Ag, *Bg, *Au, *Bu;                       // [E][r][d], [E][f][r], or null
     const uint16_t* x;
     uint16_t* y;
-    const int32_t* idx;      // [M][k], -1: slot not used
-    const float* w;
-    int* blocks;             // [0] count, then from kBlkInts on the blocks
+    int32_t* idx;            // [M][k], -1: slot not used
+    float* w;
+    const double* logits;    // [M][E]
+    int* blocks;             // moe_blocks_most() blocks, those past the last with no instances
     float* t;                // [M k][2 r]
-    uint16_t* h;             // [M k][f]
+    uint16_t* h;             // [M k][operand_row(f)] in operand order (oneshot.h)
+    uint16_t* xo;            // x in operand order
+    float* xs;               // and its group sums
     float* part;             // [M k][d]
-    int M, d, f, r, E, k, gb, gg, db, dg;
+    int M, d, f, r, E, k, score, gb, gg, db, dg;
     float lora_scale;
 };
 // The most blocks n instances of E experts can make.
-inline int moe_blocks_most(int n, int E) { return n < E + n / 16 ? n : E + n / 16; }
+__host__ __device__ inline int moe_blocks_most(int n, int E) { return n < E + n / 16 ? n : E + n / 16; }
+// Behind launch_route_logits: chooses, runs the experts and adds up.
 hipError_t launch_moe_experts(const MoeArgs& a, hipStream_t st);
 
 }  // namespace qmlp

@@ -3,143 +3,228 @@
 // instance; the instances of an expert run side by side, up to 16 of them as
 // the rows of a matrix operand, so an expert is read once per 16.
 //
-// Launches: LoRA-A of every instance together with the grouping of the
-// instances by expert; gate/up with SiLU(G) * U; down; the routing-weighted
-// sum.  Gate/up and down have a workgroup per block of instances and few weight
-// rows, each wave one piece of K (oneshot.h).
+// Launches: the router's logits (moe_route.hip); the choice, the grouping of the
+// instances by expert and x in operand order; LoRA-A of each block of
+// instances; gate/up with SiLU(G) * U; down; the routing-weighted sum.  Gate/up
+// and down have a workgroup per block of instances and few weight rows
+// (oneshot.h).
 #include "moe_layer.h"
 #include "decode_launch.h"
+#include "moe_select.h"
 #include "oneshot.h"
 
 namespace qmlp {
 namespace {
 
-constexpr int kGroupWaves = 8;
-constexpr int kMaxInst = kMoeTokens * kMoeTopk;
+constexpr int kChooseWaves = 16;
 
-// Workgroup 0: the blocks, experts ascending, instances ascending.
+// Workgroup 0: every token's experts, and the blocks, experts ascending, tokens
+// ascending.  A token chooses an expert at most once, so a 64-bit mask of tokens is
+// an expert's list, and an instance's place the number of bits below its own.
 __device__ __forceinline__ void moe_group(const MoeArgs& a, int tid) {
-    __shared__ int16_t ids[kMaxInst];
-    __shared__ int sum[kMoeExperts];
-    static_assert(kGroupWaves * 64 >= kMoeExperts, "a thread per expert");
-    const int n = a.M * a.k;
-    for (int i = tid; i < n; i += kGroupWaves * 64) ids[i] = (int16_t)a.idx[i];
-    __syncthreads();
-    int c = 0;
-    if (tid < a.E)
-        for (int i = 0; i < n; ++i) c += ids[i] == tid;
-    const int nb = (c + 15) >> 4;
+    __shared__ uint32_t list[kMoeExperts][2];
+    __shared__ int16_t ids[kMoeTokens * kMoeTopk], start[kMoeExperts];
+    __shared__ int sums[kMoeExperts / 64];
+    static_assert(kChooseWaves * 64 >= kMoeExperts && kChooseWaves * 64 >= kMoeTokens * kMoeTopk, "a thread per expert, and per instance");
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), n = a.M * a.k;
     if (tid < kMoeExperts)
-        sum[tid] = nb;
+        list[tid][0] = list[tid][1] = 0;
     __syncthreads();
-    for (int o = 1; o < kMoeExperts; o *= 2) {             // inclusive sums
-        const int v = tid < kMoeExperts && tid >= o ? sum[tid - o] : 0;
-        __syncthreads();
-        if (tid < kMoeExperts)
-            sum[tid] += v;
-        __syncthreads();
-    }
-    if (tid == 0)
-        a.blocks[0] = sum[kMoeExperts - 1];
-    if (tid < a.E && c > 0) {
-        int* b = a.blocks + kBlkInts * (1 + sum[tid] - nb);
-        int at = 0;
-        for (int i = 0; i < n; ++i)
-            if (ids[i] == tid) {
-                int* blk = b + (at >> 4) * kBlkInts;
-                blk[kBlkInst + (at & 15)] = i;
-                blk[kBlkTok + (at & 15)] = i / a.k;
-                ++at;
-            }
-        for (int s = 0; s < nb; ++s) {
-            b[s * kBlkInts] = tid;
-            b[s * kBlkInts + 1] = min(16, c - 16 * s);
+    for (int m = wave; m < a.M; m += kChooseWaves) {
+        const Chosen c = route_select(a.logits + (long)m * a.E, a.E, a.k, a.score, lane);
+        if (lane < a.k) {
+            const int i = m * a.k + lane;
+            a.idx[i] = c.e;
+            a.w[i] = c.w;
+            ids[i] = (int16_t)c.e;
+            if (c.e >= 0)
+                atomicOr(&list[c.e][m >> 5], 1u << (m & 31));
         }
+    }
+    __syncthreads();
+    int c = 0, nb = 0, at = 0;
+    if (tid < kMoeExperts) {                               // blocks of expert tid, and of the experts before it
+        c = __popc(list[tid][0]) + __popc(list[tid][1]);
+        at = nb = (c + 15) >> 4;
+#pragma unroll
+        for (int o = 1; o < 64; o *= 2) {
+            const int v = __shfl_up(at, o, 64);
+            at += lane >= o ? v : 0;
+        }
+        if (lane == 63)
+            sums[wave] = at;
+    }
+    __syncthreads();
+    int all = 0;
+#pragma unroll
+    for (int w = 0; w < kMoeExperts / 64; ++w) {
+        if (w < wave)
+            at += sums[w];
+        all += sums[w];
+    }
+    if (tid < kMoeExperts) {
+        at -= nb;
+        start[tid] = (int16_t)at;
+        for (int s = 0; s < nb; ++s) {
+            a.blocks[(at + s) * kBlkInts] = tid;
+            a.blocks[(at + s) * kBlkInts + 1] = min(16, c - 16 * s);
+        }
+    }
+    for (int b = all + tid; b < moe_blocks_most(n, a.E); b += kChooseWaves * 64) a.blocks[b * kBlkInts + 1] = 0;
+    __syncthreads();
+    if (tid < n && ids[tid] >= 0) {
+        const int e = ids[tid], m = tid / a.k;
+        const uint64_t before = ((uint64_t)list[e][1] << 32 | list[e][0]) & ((1ull << m) - 1);
+        const int p = __popcll(before);
+        int* b = a.blocks + (start[e] + (p >> 4)) * kBlkInts + (p & 15);
+        b[kBlkInst] = tid;
+        b[kBlkTok] = m;
     }
 }
 
-// Workgroup 0 groups; workgroup 1 + (instance, eight rows of [A_g; A_u]): t.
-__global__ void __launch_bounds__(kGroupWaves * 64) moe_prep_kernel(MoeArgs a) {
-    const int tid = threadIdx.x, lane = tid & 63;
+// Workgroup 0 chooses and groups; the others bring a row of x into operand order
+// each, and clear what pads the rows of h to whole steps.
+__global__ void __launch_bounds__(kChooseWaves * 64) moe_choose_kernel(MoeArgs a) {
+    const int tid = threadIdx.x;
     if (blockIdx.x == 0) {
         moe_group(a, tid);
         return;
     }
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int nc = 2 * a.r / 8, i = (blockIdx.x - 1) / nc, c = (blockIdx.x - 1) - i * nc;
-    const int e = a.idx[i];
-    if (e < 0)
+    const int m = blockIdx.x - 1, row = operand_row(a.f, a.db), pad = row - a.f;
+    for (int i = tid; i < a.k * pad; i += kChooseWaves * 64) a.h[(long)(m * a.k + i / pad) * row + a.f + i % pad] = 0;
+    operands_of_row<kChooseWaves>(a.x + (long)m * a.d, a.d, false, a.gb, a.gg, a.xo + (long)m * operand_row(a.d, a.gb),
+                                  a.xs + (long)m * operand_sums(a.d, a.gb, a.gg), nullptr, tid);
+}
+
+// A block of the table in registers: expert and instances are uniform (scalar
+// loads), the lane's own instance and token come with one vector load each.
+struct Block {
+    int e, n, inst, tok;
+};
+__device__ __forceinline__ Block block_of(const MoeArgs& a, int b, int lane) {
+    const int* p = a.blocks + kBlkInts * b;
+    const int n = p[1], l = (lane & 15) < n ? lane & 15 : 0;
+    return {p[0], n, p[kBlkInst + l], p[kBlkTok + l]};
+}
+
+// t of one block of instances: 16 rows of the expert's [A_g; A_u], whose 2 r rows
+// are a multiple of 16, by x as they lie in memory; the waves split d.
+constexpr int kShrinkWaves = 8;
+__global__ void __launch_bounds__(kShrinkWaves * 64) moe_shrink_kernel(MoeArgs a) {
+    constexpr int N = 4;
+    __shared__ f32x4_t red[kShrinkWaves][64];
+    const int lane = threadIdx.x & 63, j = lane & 15, q = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Block bl = block_of(a, blockIdx.y, lane);
+    if (bl.n == 0)
         return;
-    const uint16_t* ar = 8 * c < a.r ? a.Ag + ((long)e * a.r + 8 * c) * a.d : a.Au + ((long)e * a.r + 8 * c - a.r) * a.d;
-    const uint16_t* xr = a.x + (long)(i / a.k) * a.d;
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int k = tid * 8; k < a.d; k += kGroupWaves * 64 * 8) {
-        const uint4 xv = *reinterpret_cast<const uint4*>(xr + k);
-        uint4 av[8];
+    const int row = blockIdx.x * 16 + j;
+    const uint16_t* ar = (row < a.r ? a.Ag + ((long)bl.e * a.r + row) * a.d : a.Au + ((long)bl.e * a.r + row - a.r) * a.d) + 8 * q;
+    const uint16_t* xr = a.x + (long)bl.tok * a.d + 8 * q;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    for (int k = wave * 32; k < a.d; k += N * kShrinkWaves * 32) {
+        uint4 xv[N], av[N];
 #pragma unroll
-        for (int r = 0; r < 8; ++r) av[r] = *reinterpret_cast<const uint4*>(ar + (long)r * a.d + k);
+        for (int i = 0; i < N; ++i)
+            if (k + i * kShrinkWaves * 32 < a.d) {
+                xv[i] = ld16(xr + k + i * kShrinkWaves * 32);
+                av[i] = ld16(ar + k + i * kShrinkWaves * 32);
+            }
 #pragma unroll
-        for (int r = 0; r < 8; ++r)
-            s[r] = dot2(xv.w, av[r].w, dot2(xv.z, av[r].z, dot2(xv.y, av[r].y, dot2(xv.x, av[r].x, s[r]))));
+        for (int i = 0; i < N; ++i)
+            if (k + i * kShrinkWaves * 32 < a.d)
+                acc = mfma16(xv[i], av[i], acc);
     }
-    __shared__ float red[kGroupWaves][8];
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-        const float v = group_sum<64>(s[r]);
-        if (lane == 0)
-            red[wave][r] = v;
-    }
+    red[wave][lane] = acc;
     __syncthreads();
-    if (tid < 8) {
-        float v = 0.0f;
+    if (wave == 0) {
 #pragma unroll
-        for (int w = 0; w < kGroupWaves; ++w) v += red[w][tid];
-        a.t[(long)i * 2 * a.r + 8 * c + tid] = a.lora_scale * v;
+        for (int w = 1; w < kShrinkWaves; ++w) acc += red[w][lane];
+#pragma unroll
+        for (int v = 0; v < 4; ++v) {
+            const int i = __shfl(bl.inst, 4 * q + v, 64);
+            if (4 * q + v < bl.n)
+                a.t[(long)i * 2 * a.r + row] = a.lora_scale * acc[v];
+        }
     }
 }
 
-// Gate and up rows of one block of instances -> h.
+// Gate and up rows of one block of instances -> h.  Eight ranks of one matrix's
+// LoRA-B are two v_mfma_f32_16x16x4_f32 with t as the other operand, ranks 2 q and
+// 2 q + 1 of them in lane quarter q.
 template <int B, int G, int RT>
-__global__ void __launch_bounds__(1024) moe_gateup_kernel(MoeArgs a, int ns, int kw) {
-    if ((int)blockIdx.y >= a.blocks[0])
-        return;
+__global__ void __launch_bounds__(512) moe_gateup_kernel(MoeArgs a, int ns, int kw) {
     extern __shared__ uint4 smem[];
     f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);       // [kw][2][RT][64]
-    const int lane = threadIdx.x & 63, j = lane & 15;
+    const int lane = threadIdx.x & 63, j = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int* blk = a.blocks + kBlkInts * (1 + blockIdx.y);
-    const int e = blk[0], n = blk[1], row0 = blockIdx.x * 16 * RT;
+    const Block bl = block_of(a, blockIdx.y, lane);
+    if (bl.n == 0)
+        return;
     const int rb = a.d * B / 8, ng = a.d / G;
     const long wb = (long)a.f * rb, mb = (long)a.f * ng * 4;
     const char *cg = reinterpret_cast<const char*>(a.cg), *cu = reinterpret_cast<const char*>(a.cu);
     const char *mg = reinterpret_cast<const char*>(a.mg), *mu = reinterpret_cast<const char*>(a.mu);
-    const Rsrc rc[2] = {rsrc(cg + e * wb, (uint32_t)wb), rsrc(cu + e * wb, (uint32_t)wb)};
-    const Rsrc rm[2] = {rsrc(mg + e * mb, (uint32_t)mb), rsrc(mu + e * mb, (uint32_t)mb)};
-    const Rsrc rx = rsrc(a.x, (uint32_t)(a.M * a.d) * 2u);
+    OneWork<2> o;
+    o.magic = magic_vgpr();
+    o.rc[0] = rsrc(cg + bl.e * wb, (uint32_t)wb);
+    o.rc[1] = rsrc(cu + bl.e * wb, (uint32_t)wb);
+    o.rm[0] = rsrc(mg + bl.e * mb, (uint32_t)mb);
+    o.rm[1] = rsrc(mu + bl.e * mb, (uint32_t)mb);
+    const bool live = j < bl.n;
+    const uint32_t xb = operand_row(a.d, B) * 2u, sb = operand_sums(a.d, B, G) * 4u;
+    o.rx = rsrc(a.xo, (uint32_t)a.M * xb);
+    o.rs = rsrc(a.xs, (uint32_t)a.M * sb);
+    o.xv = (uint32_t)bl.tok * xb + lane_x<B, G>(q);
+    o.sv = (uint32_t)bl.tok * sb + lane_sums<B, G>(q);
+    o.K = a.d;
+    o.N = a.f;
+    o.row0 = blockIdx.x * 16 * RT;
+    // rank chunk c of matrix m: item 2 c + m
+    const int items = a.r / 4;
+    struct {
+        float t[2];
+        uint32_t b[RT];
+    } k8;
+    auto rank_load = [&](int it) {
+        const int m = it & 1, at = 8 * (it >> 1) + 2 * q;
+        const float* tp = a.t + (long)(live ? bl.inst : 0) * 2 * a.r + m * a.r + at;
+        k8.t[0] = tp[0];
+        k8.t[1] = tp[1];
+#pragma unroll
+        for (int t = 0; t < RT; ++t) {
+            const int n = o.row0 + 16 * t + j < a.f ? o.row0 + 16 * t + j : a.f - 1;
+            k8.b[t] = *reinterpret_cast<const uint32_t*>((m ? a.Bu : a.Bg) + ((long)bl.e * a.f + n) * a.r + at);
+        }
+    };
     f32x4_t acc[2][RT];
-    oneshot_products<B, G, 2, RT>(acc, rc, rm, rx, j < n ? blk[kBlkTok + j] : 0, j < n, a.d, a.d, a.f, row0, wave, ns, kw, lane);
+    auto rank_add = [&](int it) {
+        const float t0 = live ? k8.t[0] : 0.0f, t1 = live ? k8.t[1] : 0.0f;
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+            if (m == (it & 1))
+#pragma unroll
+                for (int t = 0; t < RT; ++t)
+                    acc[m][t] = mfma4(t1, h2f(k8.b[t] >> 16), mfma4(t0, h2f(k8.b[t] & 0xFFFFu), acc[m][t]));
+    };
+    oneshot_products<B, G, 2, RT, false>(acc, o, wave, ns, kw, lane, [&] {
+        if (wave < items)
+            rank_load(wave);
+    });
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            f32x4_t v = acc[m][t] * kTileUnscale;
-            const int o = row0 + 16 * t + j;
-            for (int c = wave; c < a.r / 8; c += kw)
-                if (o < a.f) {
-                    float b[8];
-                    act8(*reinterpret_cast<const uint4*>((m ? a.Bu : a.Bg) + ((long)e * a.f + o) * a.r + 8 * c), false, b);
+        for (int t = 0; t < RT; ++t) acc[m][t] *= kTileUnscale;
+    if (wave < items)
+        rank_add(wave);
+    for (int it = wave + kw; it < items; it += kw) {       // few waves: short rows
+        rank_load(it);
+        rank_add(it);
+    }
 #pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const int i = 4 * (lane >> 4) + u;
-                        if (i < n) {
-                            const float* tt = a.t + (long)blk[kBlkInst + i] * 2 * a.r + m * a.r + 8 * c;
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-                            for (int z = 0; z < 8; ++z) v[u] = __builtin_fmaf(b[z], tt[z], v[u]);
-                        }
-                    }
-                }
-            red[((wave * 2 + m) * RT + t) * 64 + lane] = v;
-        }
+        for (int t = 0; t < RT; ++t) red[((wave * 2 + m) * RT + t) * 64 + lane] = acc[m][t];
     __syncthreads();
     for (int t = wave; t < RT; t += kw) {
         f32x4_t g = red[t * 64 + lane], u = red[(RT + t) * 64 + lane];
@@ -147,60 +232,76 @@ __global__ void __launch_bounds__(1024) moe_gateup_kernel(MoeArgs a, int ns, int
             g += red[(w * 2 * RT + t) * 64 + lane];
             u += red[((w * 2 + 1) * RT + t) * 64 + lane];
         }
-        const int o = row0 + 16 * t + j;
+        const int n = o.row0 + 16 * t + j, at = operand_at(n, a.db, a.dg), hrow = operand_row(a.f, a.db);
+        const float scale = operand_scale(n, a.db, a.dg);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int i = 4 * (lane >> 4) + v;
-            if (i < n && o < a.f)
-                a.h[(long)blk[kBlkInst + i] * a.f + o] = (uint16_t)f2h(g[v] / (1.0f + __expf(-g[v])) * u[v]);
+            const int i = __shfl(bl.inst, 4 * q + v, 64);
+            if (4 * q + v < bl.n && n < a.f)               // h rounded to binary16, then its operand's power of two
+                a.h[(long)i * hrow + at] = (uint16_t)f2h(h2f(f2h(g[v] / (1.0f + __expf(-g[v])) * u[v])) * scale);
         }
     }
 }
 
 // Down rows of one block of instances -> fp32 outputs of each instance.
 template <int B, int G, int RT>
-__global__ void __launch_bounds__(1024) moe_down_kernel(MoeArgs a, int ns, int kw) {
-    if ((int)blockIdx.y >= a.blocks[0])
-        return;
+__global__ void __launch_bounds__(512) moe_down_kernel(MoeArgs a, int ns, int kw) {
     extern __shared__ uint4 smem[];
     f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);       // [kw][RT][64]
-    const int lane = threadIdx.x & 63, j = lane & 15;
+    const int lane = threadIdx.x & 63, j = lane & 15, q = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int* blk = a.blocks + kBlkInts * (1 + blockIdx.y);
-    const int e = blk[0], n = blk[1], row0 = blockIdx.x * 16 * RT;
+    const Block bl = block_of(a, blockIdx.y, lane);
+    if (bl.n == 0)
+        return;
     const int rb = a.f * B / 8, ng = a.f / G;
     const long wb = (long)a.d * rb, mb = (long)a.d * ng * 4;
-    const Rsrc rc[1] = {rsrc(reinterpret_cast<const char*>(a.cd) + e * wb, (uint32_t)wb)};
-    const Rsrc rm[1] = {rsrc(reinterpret_cast<const char*>(a.md) + e * mb, (uint32_t)mb)};
-    const Rsrc rx = rsrc(a.h, (uint32_t)(a.M * a.k * a.f) * 2u);
+    OneWork<1> o;
+    o.magic = magic_vgpr();
+    o.rc[0] = rsrc(reinterpret_cast<const char*>(a.cd) + bl.e * wb, (uint32_t)wb);
+    o.rm[0] = rsrc(reinterpret_cast<const char*>(a.md) + bl.e * mb, (uint32_t)mb);
+    const uint32_t hb = operand_row(a.f, B) * 2u;
+    o.rx = rsrc(a.h, (uint32_t)(a.M * a.k) * hb);
+    o.xv = (uint32_t)bl.inst * hb + lane_x<B, G>(q);
+    o.K = a.f;
+    o.N = a.d;
+    o.row0 = blockIdx.x * 16 * RT;
     f32x4_t acc[1][RT];
-    oneshot_products<B, G, 1, RT>(acc, rc, rm, rx, j < n ? blk[kBlkInst + j] : 0, j < n, a.f, a.f, a.d, row0, wave, ns, kw, lane);
+    oneshot_products<B, G, 1, RT, true>(acc, o, wave, ns, kw, lane, [] {});
 #pragma unroll
     for (int t = 0; t < RT; ++t) red[(wave * RT + t) * 64 + lane] = acc[0][t] * kTileUnscale;
     __syncthreads();
     for (int t = wave; t < RT; t += kw) {
         f32x4_t s = red[t * 64 + lane];
         for (int w = 1; w < kw; ++w) s += red[(w * RT + t) * 64 + lane];
-        const int o = row0 + 16 * t + j;
+        const int n = o.row0 + 16 * t + j;
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int i = 4 * (lane >> 4) + v;
-            if (i < n && o < a.d)
-                a.part[(long)blk[kBlkInst + i] * a.d + o] = s[v];
+            const int i = __shfl(bl.inst, 4 * q + v, 64);
+            if (4 * q + v < bl.n && n < a.d)
+                a.part[(long)i * a.d + n] = s[v];
         }
     }
 }
 
-// y[m] = sum of w[m][j] part[m k + j], j ascending; slots without an expert add nothing.
+// y[m] = sum of w[m][j] part[m k + j], j ascending; slots without an expert add
+// nothing (their parts, which no launch wrote, are loaded all the same: a load
+// behind a load of the slot's expert would wait for it).
 __global__ void __launch_bounds__(256) moe_combine_kernel(MoeArgs a) {
+    constexpr int N = 8;
     const int m = blockIdx.y, c = (blockIdx.x * 256 + threadIdx.x) * 4;
     if (c >= a.d)
         return;
     f32x4_t s = {0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < a.k; ++j) {
-        const int i = m * a.k + j;
-        if (a.idx[i] >= 0)
-            s += a.w[i] * *reinterpret_cast<const f32x4_t*>(a.part + (long)i * a.d + c);
+    for (int j0 = 0; j0 < a.k; j0 += N) {
+        f32x4_t p[N];
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j0 + j < a.k)
+                p[j] = *reinterpret_cast<const f32x4_t*>(a.part + (long)(m * a.k + j0 + j) * a.d + c);
+#pragma unroll
+        for (int j = 0; j < N; ++j)
+            if (j0 + j < a.k && a.idx[m * a.k + j0 + j] >= 0)
+                s += a.w[m * a.k + j0 + j] * p[j];
     }
     *reinterpret_cast<uint2*>(a.y + (long)m * a.d + c) = make_uint2(f2h(s[0]) | f2h(s[1]) << 16, f2h(s[2]) | f2h(s[3]) << 16);
 }
@@ -209,29 +310,38 @@ __global__ void __launch_bounds__(256) moe_combine_kernel(MoeArgs a) {
 
 hipError_t launch_moe_experts(const MoeArgs& a, hipStream_t st) {
     const int n = a.M * a.k, nb = moe_blocks_most(n, a.E);
-    moe_prep_kernel<<<(unsigned)(1 + n * (2 * a.r / 8)), kGroupWaves * 64, 0, st>>>(a);
+    moe_choose_kernel<<<1u + (unsigned)a.M, kChooseWaves * 64, 0, st>>>(a);
     hipError_t err = hipGetLastError();
     if (err != hipSuccess)
         return err;
-    auto run = [&](auto k, int K, int rows, int bits, int nm, int rt) {
-        const int ns = oneshot_steps(K, bits), kw = oneshot_waves(ns, 16);
-        const size_t lds = (size_t)kw * nm * rt * 1024;
-        hipError_t e = set_lds(k, lds);
-        if (e != hipSuccess)
-            return e;
-        k<<<dim3((unsigned)(rows + 16 * rt - 1) / (16 * rt), (unsigned)nb), (unsigned)kw * 64, lds, st>>>(a, ns, kw);
+    if (a.r > 0) {
+        moe_shrink_kernel<<<dim3((unsigned)a.r / 8, (unsigned)nb), kShrinkWaves * 64, 0, st>>>(a);
+        if ((err = hipGetLastError()) != hipSuccess)
+            return err;
+    }
+    auto run = [&](auto k, int K, int bits, int rows, int nm, int rt) {
+        const int ns = oneshot_steps(K, bits), kw = oneshot_waves(ns);
+        k<<<dim3((unsigned)(rows + 16 * rt - 1) / (16 * rt), (unsigned)nb), (unsigned)kw * 64, (size_t)kw * nm * rt * 1024, st>>>(a, ns, kw);
         return hipGetLastError();
     };
-    constexpr int RT = 1;
+    // Two tiles of gate and up share a workgroup's operands; one where that left compute units without a workgroup
+    // (us, 4 bits, d = 4096, f = 1536, one token's 2 experts: one tile 8.4, two 13.1), and for 2 bits, whose two tiles
+    // leave registers for two waves a SIMD, up to an average of two instances an expert (d = f = 2880, 4 of 32 experts,
+    // one tile and two: M = 1 10.6 and 12.7, 8 37.3 and 40.4, 16 52.3 and 52.9, 32 65.0 and 62.7, 64 80.5 and 68.8;
+    // 4 bits, d = 2048, f = 768, 8 of 128: M = 4 18.0 and 16.8, 13 37.2 and 35.3, 64 71.0 and 62.8).  Down takes two
+    // (M = 1 7.2 and 8.3, 8 29.6 and 25.5, 64 59.2 and 47.9).
+    const bool two = (long)n * (a.f / 32) >= 256 && (a.gb == 4 || n > 2 * a.E);
     err = hipErrorInvalidValue;
-#define QMLP_MG(B_, G_) \
-    if (a.gb == B_ && a.gg == G_) err = run(moe_gateup_kernel<B_, G_, RT>, a.d, a.f, B_, 2, RT);
+#define QMLP_MG(B_, G_)                                                                             \
+    if (a.gb == B_ && a.gg == G_)                                                                   \
+        err = two ? run(moe_gateup_kernel<B_, G_, 2>, a.d, B_, a.f, 2, 2) : run(moe_gateup_kernel<B_, G_, 1>, a.d, B_, a.f, 2, 1);
     QMLP_MG(2, 32) QMLP_MG(2, 64) QMLP_MG(2, 128) QMLP_MG(4, 32) QMLP_MG(4, 64) QMLP_MG(4, 128)
     if (err != hipSuccess)
         return err;
     err = hipErrorInvalidValue;
-#define QMLP_MD(B_, G_) \
-    if (a.db == B_ && a.dg == G_) err = run(moe_down_kernel<B_, G_, RT>, a.f, a.d, B_, 1, RT);
+#define QMLP_MD(B_, G_)           \
+    if (a.db == B_ && a.dg == G_) \
+        err = run(moe_down_kernel<B_, G_, 2>, a.f, B_, a.d, 1, 2);
     QMLP_MD(2, 32) QMLP_MD(2, 64) QMLP_MD(2, 128) QMLP_MD(4, 32) QMLP_MD(4, 64) QMLP_MD(4, 128)
     if (err != hipSuccess)
         return err;

@@ -5,134 +5,151 @@
 // split, and binary16 or bfloat16 products are exact in fp64, so two experts
 // trade places only where their logits agree to about 2^-50 of sum |x w|.
 #include "moe_layer.h"
-#include "decode_launch.h"
+#include "moe_select.h"
 #include "oneshot.h"
-
-#include <float.h>
 
 namespace qmlp {
 namespace {
 
-constexpr int kRouteTok = 8;
+typedef double f64x4_t __attribute__((ext_vector_type(4)));
 
-// A wave: one expert, eight tokens; lanes split d.
-__global__ void __launch_bounds__(256) route_logits_kernel(RouteArgs a) {
-    const int lane = threadIdx.x & 63, e = blockIdx.x * 4 + (threadIdx.x >> 6), m0 = blockIdx.y * kRouteTok;
-    if (e >= a.E)
-        return;
+constexpr int kRouteTok = 8, kRouteWaves = 4;
+
+// Few tokens: a workgroup owns an expert and eight tokens and issues all its loads,
+// 16 bytes a lane, before the first product.
+__global__ void __launch_bounds__(kRouteWaves * 64) route_few_kernel(RouteArgs a) {
+    constexpr int N = 2, step = kRouteWaves * 64 * 8;
+    __shared__ double red[kRouteWaves][kRouteTok];
+    const int tid = threadIdx.x, e = blockIdx.x, m0 = blockIdx.y * kRouteTok, nt = min(kRouteTok, a.M - m0);
+    const uint16_t *wr = a.router + (long)e * a.d, *xr = a.x + (long)m0 * a.d;
+    const double bias = a.bias ? (double)a.bias[e] : 0.0;
     double s[kRouteTok] = {};
-    for (int c = lane * 8; c < a.d; c += 512) {
-        float w[8];
-        act8(*reinterpret_cast<const uint4*>(a.router + (long)e * a.d + c), a.bf, w);
+    for (int c = tid * 8; c < a.d; c += N * step) {
+        uint4 wv[N], xv[N][kRouteTok];
 #pragma unroll
-        for (int t = 0; t < kRouteTok; ++t) {
-            if (m0 + t < a.M) {
-                float x[8];
-                act8(*reinterpret_cast<const uint4*>(a.x + (long)(m0 + t) * a.d + c), a.bf, x);
+        for (int i = 0; i < N; ++i)
+            if (c + i * step < a.d) {
+                wv[i] = ld16(wr + c + i * step);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) s[t] = __builtin_fma((double)x[i], (double)w[i], s[t]);
+                for (int t = 0; t < kRouteTok; ++t)
+                    if (t < nt)
+                        xv[i][t] = ld16(xr + (long)t * a.d + c + i * step);
             }
-        }
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (c + i * step < a.d) {
+                float w[8];
+                act8(wv[i], a.bf, w);
+#pragma unroll
+                for (int t = 0; t < kRouteTok; ++t)
+                    if (t < nt) {
+                        float x[8];
+                        act8(xv[i][t], a.bf, x);
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) s[t] = __builtin_fma((double)x[k], (double)w[k], s[t]);
+                    }
+            }
     }
 #pragma unroll
-    for (int t = 0; t < kRouteTok; ++t) {
-        double v = s[t];
+    for (int t = 0; t < kRouteTok; ++t)
+        if (t < nt) {
+            const double v = wave_sum(s[t]);
+            if ((tid & 63) == 0)
+                red[tid >> 6][t] = v;
+        }
+    __syncthreads();
+    if (tid < nt) {
+        double v = red[0][tid];
 #pragma unroll
-        for (int o = 32; o; o >>= 1) v += __shfl_xor(v, o, 64);
-        if (lane == 0 && m0 + t < a.M)
-            a.logits[(long)(m0 + t) * a.E + e] = v + (a.bias ? (double)a.bias[e] : 0.0);
+        for (int w = 1; w < kRouteWaves; ++w) v += red[w][tid];
+        a.logits[(long)(m0 + tid) * a.E + e] = v + bias;
     }
 }
 
-// The k largest of a token's logits by one wave, expert e in lane e & 63: ties
-// to the lower expert; NaN and -inf are never chosen, +inf counts as the
-// largest fp32.  Slots that find nothing: expert -1, weight 0.
-__device__ __forceinline__ void route_select(const double* l, int E, int k, int score, int32_t* idx, float* w, int lane) {
-    constexpr int N = kMoeExperts / 64;
-    const double none = -__builtin_inf();
-    double v[N];
-    double top = none;
+// Many tokens: a workgroup owns 32 tokens and 32 experts, its waves split d, and
+// each step of 32 elements is 8 k-steps of v_mfma_f64_16x16x4_f64: lane 16 q + j
+// loads 8 elements of row j from 8 q on and gives them one after another (the
+// same order on both sides, so which k-step an element lands in does not matter).
+constexpr int kManyWaves = 8;
+__global__ void __launch_bounds__(kManyWaves * 64) route_many_kernel(RouteArgs a) {
+    __shared__ double red[kManyWaves][4][64][4];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, j = lane & 15, q = lane >> 4;
+    const int m0 = blockIdx.y * 32, e0 = blockIdx.x * 32;
+    const uint16_t *xr[2], *wr[2];
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int e = lane + 64 * i;
-        v[i] = e < E ? l[e] : none;
-        v[i] = v[i] != v[i] ? none : fmin(v[i], (double)FLT_MAX);
-        top = fmax(top, v[i]);
+    for (int i = 0; i < 2; ++i) {
+        xr[i] = a.x + (long)min(m0 + 16 * i + j, a.M - 1) * a.d;
+        wr[i] = a.router + (long)min(e0 + 16 * i + j, a.E - 1) * a.d;
     }
+    f64x4_t acc[2][2] = {};
+    uint4 xv[2], wv[2];
+    auto load = [&](int k) {
 #pragma unroll
-    for (int o = 32; o; o >>= 1) top = fmax(top, __shfl_xor(top, o, 64));
-    float all = 0.0f;
-    if (score == QMLP_SCORE_SOFTMAX) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) all += v[i] == none ? 0.0f : expf((float)(v[i] - top));
-#pragma unroll
-        for (int o = 32; o; o >>= 1) all += __shfl_xor(all, o, 64);
-    }
-    double mine = none;                                    // lane j: the j-th chosen
-    int me = -1;
-    for (int j = 0; j < k; ++j) {
-        double b = none;
-        int be = kMoeExperts;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (v[i] > b) {
-                b = v[i];
-                be = lane + 64 * i;
-            }
-#pragma unroll
-        for (int o = 32; o; o >>= 1) {
-            const double ob = __shfl_xor(b, o, 64);
-            const int oe = __shfl_xor(be, o, 64);
-            if (ob > b || (ob == b && oe < be)) {
-                b = ob;
-                be = oe;
-            }
+        for (int i = 0; i < 2; ++i) {
+            xv[i] = k < a.d ? ld16(xr[i] + k) : make_uint4(0, 0, 0, 0);
+            wv[i] = k < a.d ? ld16(wr[i] + k) : make_uint4(0, 0, 0, 0);
         }
-        if (b == none)
-            break;
-        if (lane == j) {
-            mine = b;
-            me = be;
+    };
+    load(wave * 32 + 8 * q);
+    for (int k = wave * 32; k < a.d; k += kManyWaves * 32) {
+        float x[2][8], w[2][8];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            act8(xv[i], a.bf, x[i]);
+            act8(wv[i], a.bf, w[i]);
         }
+        load(k + kManyWaves * 32 + 8 * q);
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (be == lane + 64 * i)
-                v[i] = none;
+        for (int s = 0; s < 8; ++s)
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+#pragma unroll
+                for (int n = 0; n < 2; ++n)
+                    acc[i][n] = __builtin_amdgcn_mfma_f64_16x16x4f64((double)x[i][s], (double)w[n][s], acc[i][n], 0, 0, 0);
     }
-    // weights: a softmax of z over the chosen ones, z the logit or log sigmoid(logit); or over all experts
-    float g = 0.0f;
-    if (score == QMLP_SCORE_SOFTMAX) {
-        g = me >= 0 ? expf((float)(mine - top)) / all : 0.0f;
-    } else {
-        double z = mine;
-        if (score == QMLP_SCORE_SIGMOID && me >= 0)
-            z = fmin(mine, 0.0) - (double)log1pf(expf(-(float)fabs(mine)));
-        double zt = me >= 0 ? z : none;
 #pragma unroll
-        for (int o = 32; o; o >>= 1) zt = fmax(zt, __shfl_xor(zt, o, 64));
-        g = me >= 0 ? expf((float)(z - zt)) : 0.0f;
-        float sum = g;
+    for (int i = 0; i < 2; ++i)
 #pragma unroll
-        for (int o = 32; o; o >>= 1) sum += __shfl_xor(sum, o, 64);
-        g = me >= 0 ? g / sum : 0.0f;
-    }
-    if (lane < k) {
-        idx[lane] = me;
-        w[lane] = g;
+        for (int n = 0; n < 2; ++n)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) red[wave][2 * i + n][lane][v] = acc[i][n][v];
+    __syncthreads();
+    // item: token 16 i + 4 v + q, expert 16 n + j
+    for (int it = tid; it < 1024; it += kManyWaves * 64) {
+        const int c = it >> 8, l = it & 63, v = (it >> 6) & 3;
+        double s = red[0][c][l][v];
+#pragma unroll
+        for (int w = 1; w < kManyWaves; ++w) s += red[w][c][l][v];
+        const int m = m0 + 16 * (c >> 1) + 4 * v + (l >> 4), e = e0 + 16 * (c & 1) + (l & 15);
+        if (m < a.M && e < a.E)
+            a.logits[(long)m * a.E + e] = s + (a.bias ? (double)a.bias[e] : 0.0);
     }
 }
 
 __global__ void __launch_bounds__(256) route_select_kernel(RouteArgs a) {
-    const int m = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (m < a.M)
-        route_select(a.logits + (long)m * a.E, a.E, a.k, a.score, a.idx + (long)m * a.k, a.w + (long)m * a.k, threadIdx.x & 63);
+    const int m = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (m >= a.M)
+        return;
+    const Chosen c = route_select(a.logits + (long)m * a.E, a.E, a.k, a.score, lane);
+    if (lane < a.k) {
+        a.idx[(long)m * a.k + lane] = c.e;
+        a.w[(long)m * a.k + lane] = c.w;
+    }
 }
 
 }  // namespace
 
+hipError_t launch_route_logits(const RouteArgs& a, hipStream_t st) {
+    // (us, few and many: d = 4096, E = 128: M = 64 14.9 and 48.4, 256 42.6 and 48.4, 2048 262 and 50.8; d = 2880,
+    // E = 32: M = 256 13.6 and 36.1, 2048 66.1 and 36.2)
+    if (a.M < 512)
+        route_few_kernel<<<dim3((unsigned)a.E, (unsigned)(a.M + kRouteTok - 1) / kRouteTok), kRouteWaves * 64, 0, st>>>(a);
+    else
+        route_many_kernel<<<dim3((unsigned)(a.E + 31) / 32, (unsigned)(a.M + 31) / 32), kManyWaves * 64, 0, st>>>(a);
+    return hipGetLastError();
+}
 hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
-    route_logits_kernel<<<dim3((unsigned)(a.E + 3) / 4, (unsigned)(a.M + kRouteTok - 1) / kRouteTok), 256, 0, st>>>(a);
-    const hipError_t e = hipGetLastError();
+    const hipError_t e = launch_route_logits(a, st);
     if (e != hipSuccess)
         return e;
     route_select_kernel<<<(unsigned)(a.M + 3) / 4, 256, 0, st>>>(a);

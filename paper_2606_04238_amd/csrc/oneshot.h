@@ -3,71 +3,388 @@
 // adapters (lora_linear.hip) and the experts of a whole MoE layer
 // (moe_layer.hip).
 //
-// Split.  A workgroup owns RT tiles of 16 weight rows (of one matrix, or of
-// gate and up); its waves split K, wave w takes the steps w, w + KW, .. of 128
-// bytes per row.  A wave issues the loads of its activations and then all its
-// weights at once, converts the activations while the weights are under way,
+// Split.  A workgroup owns RT tiles of 16 weight rows (of one matrix, or of gate
+// and up); its waves split K, wave w takes the steps w, w + KW, .. of 64 bytes per
+// row.  A wave issues the loads of its activations and its weights at once,
 // multiplies and leaves its sums in LDS, where they meet behind one barrier.
 // There is no loop over tiles: the launch has a workgroup for each, and the
 // hardware starts the next one where one ends.  Reading 92 MB in 8 KB pieces,
 // one per wave, took 15.3 us on this card against 17.3 to 21 with persistent
-// waves that prefetch, and 16 MB 4.1 against 5.2 to 9.6 (loads only, whole
-// 128-byte lines of 8 rows per instruction, launch included): a persistent
-// wave ramps its stream up once and waits for its slowest piece at the end.
+// waves that prefetch, and 16 MB 4.1 against 5.2 to 9.6 (loads only, launch
+// included): a persistent wave ramps its stream up once and waits for its
+// slowest piece at the end.  What hides a workgroup's start and end is another
+// one beside it, so registers count: a step of 128 bytes holds twice the operands.
 #pragma once
 
+#include "oneshot_plan.h"
 #include "tile_step.h"
 
 namespace qmlp {
 namespace {
 
-// Sums of this wave's steps: acc[m][t] of matrix m and the 16 rows from
-// row0 + 16 t on (rows past N give zeros).  The tokens are the operand's rows:
-// lane j = lane & 15 supplies row `xrow` of rx (ldx elements apart; zeros
-// where it is not `live`).  K % 64 == 0.  Not yet scaled by kTileUnscale.
-template <int B, int G, int NM, int RT>
-__device__ __forceinline__ void oneshot_products(f32x4_t (&acc)[NM][RT], const Rsrc (&rc)[NM], const Rsrc (&rm)[NM],
-                                                 Rsrc rx, int xrow, bool live, int ldx, int K, int N, int row0,
-                                                 int first, int ns, int kw, int lane) {
+// A step is 64 bytes of each of a tile's 16 rows.  Lane l = 16 q + j loads unit
+// perm(q) (16 bytes) of row j, and E4 and E5 (mfma_tile.h) bring quarter q its words
+// of every group, as in the first half of a tile kernel's step.  Activations come in
+// the operands' order (operand16 below): an operand is one 16-byte load, in which
+// only lanes that have a row take part.  Their group sums come with them
+// (SUMS = false) or are formed here.  Rows that no lane supplies are left as the
+// registers are: a matrix product keeps rows apart, and theirs are dropped.
+template <int B, int G>
+struct OneLay {
     typedef Lay<B, G> Y;
-    const int rb = K * B / 8, ng = K / G;
+    static constexpr int CPS = 512 / B;                    // codes per row and step
+    static constexpr int GS = Y::GSU / 2;                  // groups per step: 1, 2, 4 or 8
+    static constexpr int NA = Y::NA / 2;                   // operands per step
+    static constexpr int NW = GS == 2 || GS == 8 ? 2 : 1;  // (scale | zero) words of a lane
+    static constexpr int NC = GS == 8 ? 2 : 1;             // pairs of group sums of a lane
+};
+template <int B, int G, int NM, int RT>
+struct OneStep {
+    float kc[OneLay<B, G>::NC], kx[OneLay<B, G>::NC];
+    uint4 w[NM * RT];
+    uint32_t m[NM * RT][OneLay<B, G>::NW];
+};
+// What a wave multiplies: rows row0 .. of NM matrices [N][K] with the rows of the
+// activations (lane j: at rows x and sums, where it is `live`).  K % 64 == 0;
+// weight rows past N give zeros.
+template <int NM>
+struct OneWork {
+    Rsrc rc[NM], rm[NM];
+    Rsrc rx, rs;                                           // operands, group sums
+    uint32_t xv, sv;                                       // this lane's place in them at step 0
+    int K, N, row0;
+    uint32_t magic;                                        // magic_vgpr(), taken at the kernel's start
+};
+// (That constant is made at the start, and kept: an instruction written by hand
+// gets no distance from matrix instructions, and one among them that shared a
+// register with an unused part of a running one's result was overwritten by it.)
+
+// A register that holds anything.
+__device__ __forceinline__ uint32_t anything() {
+    uint32_t v;
+    __asm__ volatile("" : "=v"(v));
+    return v;
+}
+
+// Operands of a wave's steps in the order they are used, kOneAhead of them in
+// registers: the weights take their time, and the activations, which many
+// workgroups share, come from the caches while earlier operands are multiplied.
+constexpr int kOneAhead = 4;
+struct OneRing {
+    uint4 a[kOneAhead];
+};
+// A lane's place in a row of operands and of group sums, in bytes.
+template <int B, int G>
+__device__ __forceinline__ uint32_t lane_x(int q) {
+    typedef Lay<B, G> Y;
+    return Y::HALF ? (uint32_t)(64 / B * (q >> 1) + 16 * (q & 1)) : (uint32_t)(64 / B * quarter_word<Y::QW>(q));
+}
+template <int B, int G>
+__device__ __forceinline__ uint32_t lane_sums(int q) {
+    typedef OneLay<B, G> L;
+    return 4u * (L::GS == 1 ? q & 1 : L::GS == 2 ? 2 * (q & 1) + (q >> 1) : 2 * q * L::NC);
+}
+template <int B, int G, int NM, bool SUMS>
+__device__ __forceinline__ void one_operand(uint4& a, const OneWork<NM>& o, int gs, int i, int lane) {
+    typedef Lay<B, G> Y;
+    constexpr int CW = 32 / B, PER = Y::HALF || B == 4 ? 1 : 2;           // codes and operands per word
+    const int w = i / PER, at = Y::HALF ? 2 * w : (w / Y::QW) * Y::WPG + w % Y::QW;
+    a = bload16<0>(o.rx, o.xv, (uint32_t)(CW * 2 * (gs * 16 + at) + 16 * (i % PER)));
+}
+
+template <int B, int G, int NM, int RT, bool SUMS>
+__device__ __forceinline__ void one_load(OneStep<B, G, NM, RT>& s, const OneWork<NM>& o, int gs, int lane) {
+    typedef Lay<B, G> Y;
+    typedef OneLay<B, G> L;
+    const int rb = o.K * B / 8, ng = o.K / G, q = lane >> 4, j = lane & 15;
+    if constexpr (!SUMS) {
+        const uint32_t at = (uint32_t)(gs * L::GS * 8);
+        if constexpr (L::GS <= 2) {
+            s.kc[0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(o.rs, o.sv, at, 0));
+        } else {
+#pragma unroll
+            for (int i = 0; i < L::NC; ++i) {
+                const uint2 v = bload8(o.rs, o.sv, at + 8u * i);
+                s.kc[i] = __uint_as_float(v.x);
+                s.kx[i] = __uint_as_float(v.y);
+            }
+        }
+    }
+    const int b4 = q & 1, b5 = q >> 1, u = gs * 4 + (Y::QW == 4 ? 2 * b5 + b4 : 2 * b4 + b5);
+    const int g0 = gs * L::GS + (L::GS <= 2 ? 0 : q * (L::GS / 4));
+    const bool in = 16 * u < rb, gin = g0 < ng;
+#pragma unroll
+    for (int t = 0; t < RT; ++t)
+#pragma unroll
+        for (int m = 0; m < NM; ++m) {
+            const int row = o.row0 + 16 * t + j;
+            const bool real = row < o.N;
+            s.w[t * NM + m] = bload16<0>(o.rc[m], real && in ? (uint32_t)row * (uint32_t)rb + 16u * (uint32_t)u : kPastEnd, 0);
+            const uint32_t mo = real && gin ? ((uint32_t)row * (uint32_t)ng + (uint32_t)g0) * 4u : kPastEnd;
+            uint32_t(&mw)[L::NW] = s.m[t * NM + m];
+            if constexpr (L::NW == 2) {
+                const uint2 v = bload8(o.rm[m], mo, 0);
+                mw[0] = v.x;
+                mw[1] = v.y;
+            } else {
+                mw[0] = __builtin_amdgcn_raw_buffer_load_b32(o.rm[m], mo, 0, 0);
+            }
+        }
+}
+
+// acc[m][t] += the step's products: the arithmetic of tile_step.h, with the tiles
+// side by side and a group's products added one group later, so that a matrix
+// instruction is not waited for at once.
+template <int B, int G, int NM, int RT, bool SUMS, typename NEXT>
+__device__ __forceinline__ void one_multiply(f32x4_t (&acc)[NM][RT], OneStep<B, G, NM, RT>& s, const OneWork<NM>& o,
+                                             int gs, int lane, NEXT next) {
+    typedef Lay<B, G> Y;
+    typedef OneLay<B, G> L;
+    constexpr int N = NM * RT;
+    const uint32_t mv = o.magic;
+    const int q = lane >> 4, left = o.K / G - gs * L::GS;  // groups of the row from this step on
+    const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int c = 0; c < N; ++c) {
+        if constexpr (Y::QW != 4) {                        // E4, E5
+            swap16(s.w[c].x, s.w[c].z);
+            swap16(s.w[c].y, s.w[c].w);
+        }
+        if constexpr (Y::QW == 1) {
+            swap32(s.w[c].x, s.w[c].y);
+            swap32(s.w[c].z, s.w[c].w);
+        }
+        if (left < L::GS) {
+#pragma unroll
+            for (int e = 0; e < L::NW; ++e)
+                if ((L::GS <= 2 ? 0 : q * (L::GS / 4)) + e >= left)
+                    s.m[c][e] = 0;
+        }
+    }
+    // a group's sums from its operands, kept where its offset and zero-point terms want them
+    const uint4 one = make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u);
+    f32x4_t gc = zero, gx = zero;
+    auto sum_up = [&](int i, int m, const uint4& a) {
+        if constexpr (SUMS) {
+            gc = mfma16(one, a, m == 0 ? zero : gc);
+            gx = mfma16(unscale_pairs<B, Y::HALF>(B == 2 && !Y::HALF ? m & 1 : 0), a, m == 0 ? zero : gx);
+            if (m + 1 < Y::MPG)
+                return;
+            if constexpr (L::GS == 1) {
+                s.kc[0] = (q & 1) ? -gx[0] : -1024.0f * gc[0];
+            } else if constexpr (L::GS == 2) {
+                if (i == 0 || (q & 1)) s.kc[0] = q < 2 ? -1024.0f * gc[0] : -gx[0];
+            } else if (i < L::NC || q == i / L::NC) {
+                s.kc[i % L::NC] = -1024.0f * gc[0];
+                s.kx[i % L::NC] = -gx[0];
+            }
+        }
+    };
+    f32x4_t before[N];
+    float by[N];
+    bool some = false;
+    auto add = [&] {
+        if (some)
+#pragma unroll
+            for (int c = 0; c < N; ++c) acc[c % NM][c / NM] += by[c] * before[c];
+        some = true;
+    };
+    float sc[N][L::NW][4];
+    if constexpr (L::GS == 1 || L::GS == 2) {
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+#pragma unroll
+            for (int e = 0; e < L::NW; ++e) sc[c][0][e] = h2f(s.m[c][e] & 0xFFFFu);
+    } else {
+#pragma unroll
+        for (int c = 0; c < N; ++c)
+#pragma unroll
+            for (int e = 0; e < L::NW; ++e) meta_spread(s.m[c][e], sc[c][e]);
+    }
+    if constexpr (Y::HALF) {                               // eight groups: unit u holds groups 2 u and 2 u + 1
+        const uint32_t sel = (q & 1) ? 0x0C030C02u : 0x0C010C00u;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            uint32_t wd[N][2];
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                uint32_t x = word_of(s.w[c], u), y = x;
+                swap16(x, y);
+                wd[c][0] = __builtin_amdgcn_perm(0u, x, sel);
+                wd[c][1] = __builtin_amdgcn_perm(0u, y, sel);
+            }
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                f32x4_t p[N];
+                const uint4 av = next(2 * u + h);
+                sum_up(2 * u + h, 0, av);
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    const uint32_t v = wd[c][h], v4 = v << 4;
+                    p[c] = mfma16(av, make_uint4(magic(v4, 0x00300030u, mv), magic(v4, 0x00C000C0u, mv),
+                                                             magic(v, 0x00300030u, mv), magic(v, 0x00C000C0u, mv)), zero);
+                }
+                add();
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    before[c] = p[c];
+                    by[c] = sc[c][h][u];
+                }
+            }
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < L::GS; ++i) {
+            f32x4_t p[N];
+#pragma unroll
+            for (int c = 0; c < N; ++c) p[c] = zero;
+#pragma unroll
+            for (int ww = 0; ww < Y::QW; ++ww) {
+                const uint4 a0 = next(B == 2 ? i * Y::MPG + 2 * ww : i * Y::MPG + ww);
+                sum_up(i, B == 2 ? 2 * ww : ww, a0);
+                uint4 a1 = a0;
+                if constexpr (B == 2) {
+                    a1 = next(i * Y::MPG + 2 * ww + 1);
+                    sum_up(i, 2 * ww + 1, a1);
+                }
+#pragma unroll
+                for (int c = 0; c < N; ++c) {
+                    const uint32_t v = word_of(s.w[c], i * Y::QW + ww);
+                    if constexpr (B == 2) {
+                        uint32_t x[8];
+                        extract_w2(v, x, mv);
+                        p[c] = mfma16(a0, make_uint4(x[0], x[1], x[2], x[3]), p[c]);
+                        p[c] = mfma16(a1, make_uint4(x[4], x[5], x[6], x[7]), p[c]);
+                    } else {
+                        uint32_t x[4];
+                        extract_w4(v, x, mv);
+                        p[c] = mfma16(a0, make_uint4(x[0], x[1], x[2], x[3]), p[c]);
+                    }
+                }
+            }
+            add();
+#pragma unroll
+            for (int c = 0; c < N; ++c) {
+                before[c] = p[c];
+                by[c] = sc[c][0][i];
+            }
+        }
+    }
+    add();
+    // the offset and zero-point terms
+#pragma unroll
+    for (int e = 0; e < L::NC; ++e)
+#pragma unroll
+        for (int c = 0; c < N; ++c) {
+            f32x4_t& ac = acc[c % NM][c / NM];
+            const uint32_t mw = L::GS == 2 && (q & 1) ? s.m[c][L::NW - 1] : s.m[c][e];
+            const float sc = h2f(mw & 0xFFFFu), sz = sc * h2f(mw >> 16);
+            if constexpr (L::GS == 1) {
+                ac = mfma4(s.kc[0], q == 0 ? sc : q == 1 ? sz : 0.0f, ac);
+            } else if constexpr (L::GS == 2) {
+                ac = mfma4(s.kc[0], q < 2 ? sc : sz, ac);
+            } else {
+                ac = mfma4(s.kc[e], sc, ac);
+                ac = mfma4(s.kx[e], sz, ac);
+            }
+        }
+}
+// Sums of the wave's steps first, first + kw, .. below ns: acc[m][t] of matrix m and
+// the 16 rows from row0 + 16 t on, not yet scaled by kTileUnscale.  S steps' loads
+// go out at once; `more` issues what else the wave will need behind them.  LOOP:
+// more than S steps per wave, the next S under way while S are multiplied.
+template <int B, int G, int NM, int RT, bool SUMS, typename MORE>
+__device__ __forceinline__ void oneshot_products(f32x4_t (&acc)[NM][RT], const OneWork<NM>& o, int first, int ns, int kw,
+                                                 int lane, MORE more) {
 #pragma unroll
     for (int m = 0; m < NM; ++m)
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[m][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-    for (int gs = first; gs < ns; gs += kw) {
-        AOps<B, G> a;
-        act_load<B, G>(a, rx, gs, live ? xrow : 0, 1 << 30, ldx, live, lane);
-        const int u = gs * 8 + lane_unit<Y::QW == 4>(lane);
-        const uint32_t ol = 16 * u < rb ? (uint32_t)((lane & 7) * rb + 16 * u) : kPastEnd;
-        const uint32_t ml = (uint32_t)((lane & 15) * ng + gs * Y::GSU + meta_first<Y::GSU>(lane >> 4)) * 4u;
-        TileW<B, G> w[NM][RT];
+    constexpr int NA = OneLay<B, G>::NA;
+    static_assert(NA % kOneAhead == 0 || kOneAhead % NA == 0, "a ring slot is known at compile time");
+    OneStep<B, G, NM, RT> s;
+    OneRing r;
+    int gs = first;                                        // < ns
+    one_load<B, G, NM, RT, SUMS>(s, o, gs, lane);
+    more();
 #pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int m = 0; m < NM; ++m) {
-                const int row = row0 + 16 * t;
-                w_load<B, G>(w[m][t], rc[m], rm[m], ol, ml, 8u * (uint32_t)rb,
-                             row < N ? (uint32_t)row * (uint32_t)rb : kPastEnd,
-                             row < N ? (uint32_t)row * (uint32_t)ng * 4u : kPastEnd);
-            }
-        Corr<B, G> cr;
-        act_mask<B, G>(a, gs, K, lane);
-        act_convert<B, G>(a);
-        group_sums<B, G>(a, cr, lane);
-#pragma unroll
-        for (int t = 0; t < RT; ++t)
-#pragma unroll
-            for (int m = 0; m < NM; ++m) tile_step<B, G>(w[m][t], a, cr, acc[m][t], ng - gs * Y::GSU, lane);
+    for (int n = 0; n < kOneAhead && n < NA; ++n) one_operand<B, G, NM, SUMS>(r.a[n], o, gs, n, lane);
+    __builtin_amdgcn_sched_barrier(0);                     // every load above is issued before the first is waited for
+    auto multiply = [&](bool last) {
+        one_multiply<B, G, NM, RT, SUMS>(acc, s, o, gs, lane, [&](int n) {
+            const int f = n + kOneAhead;
+            const uint4 a = r.a[n % kOneAhead];
+            if (!last || f < NA)
+                one_operand<B, G, NM, SUMS>(r.a[n % kOneAhead], o, f < NA ? gs : gs + kw, f % NA, lane);
+            return a;
+        });
+    };
+    for (; gs + kw < ns; gs += kw) {
+        OneStep<B, G, NM, RT> n;
+        one_load<B, G, NM, RT, SUMS>(n, o, gs + kw, lane);
+        __builtin_amdgcn_sched_barrier(0);
+        multiply(false);
+        s = n;
     }
+    multiply(true);
 }
 
-// Steps of a row, and the waves that share them evenly (at most `most`).
-inline int oneshot_steps(int K, int bits) { return (K * bits + 1023) / 1024; }
-inline int oneshot_waves(int ns, int most) {
-    const int per = (ns + most - 1) / most;
-    return (ns + per - 1) / per;
+// ---- activations in the operands' order, for the launch before
+// Where element e of a row goes (within its block of 16), and the power of two it
+// is multiplied by, as act_convert would.
+__device__ __forceinline__ int operand_at(int e, int bits, int g) {
+    return bits == 2 && g != 32 ? (e & ~15) + 2 * (e & 7) + ((e >> 3) & 1) : (e & ~7) + 2 * (e & 3) + ((e >> 2) & 1);
+}
+__device__ __forceinline__ float operand_scale(int e, int bits, int g) {
+    int p;                                                 // fraction position of the element's pair
+    if (bits == 4)
+        p = (e & 3) < 2 ? 4 : 6;
+    else if (g == 32 || (e & 7) < 4)
+        p = (e & 1) ? 6 : 4;
+    else
+        p = (e & 3) == 1 ? 4 : (e & 3) == 2 ? 6 : 8;
+    return __uint_as_float((uint32_t)(127 + kPosMin - p) << 23);
+}
+// Sixteen elements of a row (fp32, already binary16 values) as two operands, and the
+// group sums -1024 C and -X (group_sums) of the group they are in: lanes whose
+// blocks share a group lie side by side, and each gets the sums.
+__device__ __forceinline__ void operand16(const float (&f)[16], int bits, int g, uint4 (&o)[2], float& c, float& x) {
+    uint32_t w[8];
+    c = x = 0.0f;
+    const bool across = bits == 2 && g != 32;              // pairs (e, 8 + e) of 16, or (e, 4 + e) of 8
+#pragma unroll
+    for (int p = 0; p < 8; ++p) {
+        const int e0 = across ? p : (p & 3) + 8 * (p >> 2), e1 = across ? 8 + p : e0 + 4;
+        const float f0 = across ? f[p] : f[(p & 3) + 8 * (p >> 2)], f1 = across ? f[8 + p] : f[(p & 3) + 8 * (p >> 2) + 4];
+        const uint32_t h0 = f2h(f0 * operand_scale(e0, bits, g)), h1 = f2h(f1 * operand_scale(e1, bits, g));
+        w[p] = h0 | h1 << 16;
+        c += h2f(h0) + h2f(h1);
+        x += f0 + f1;
+    }
+    c = -1024.0f * c;
+    x = -16.0f * x;
+    if (g == 32) {
+        c = group_sum<2>(c);
+        x = group_sum<2>(x);
+    } else if (g == 64) {
+        c = group_sum<4>(c);
+        x = group_sum<4>(x);
+    } else {
+        c = group_sum<8>(c);
+        x = group_sum<8>(x);
+    }
+    o[0] = make_uint4(w[0], w[1], w[2], w[3]);
+    o[1] = make_uint4(w[4], w[5], w[6], w[7]);
+}
+
+// The e of a bfloat16 row whose largest element is top = f 2^E, 1 <= f < 2: 14 - E,
+// with 2^e a normal number (a row whose largest is below 2^-112, or not finite,
+// keeps 126 or -114).
+__device__ __forceinline__ int bf16_shift(float top) { return min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126); }
+
+__device__ __forceinline__ uint4 ld16(const void* p) {
+    const u32x4 v = *reinterpret_cast<const u32x4*>(p);
+    return make_uint4(v.x, v.y, v.z, v.w);
 }
 
 // Eight values of the activation type (binary16, or bfloat16 where bf) as fp32.
@@ -86,6 +403,88 @@ __device__ __forceinline__ uint16_t act_bits(float v, bool bf) {
         return (uint16_t)f2h(v);
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
+
+// A row of K binary16 or (bf) bfloat16 elements in operand order, padded with zeros,
+// and its group sums, by a workgroup of W waves; bfloat16 times 2^e, 2^-e to *back.
+// 16 elements per lane; the first N pieces of a wave stay in its registers between
+// the two passes that bfloat16 takes.
+template <int W>
+__device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool bf, int bits, int g, uint16_t* o, float* sums,
+                                                float* back, int tid) {
+    constexpr int N = 3;
+    __shared__ float best[W];
+    const int lane = tid & 63, wave = tid >> 6, len = operand_row(K, bits);
+    uint4 v[N][2];
+    auto load = [&](uint4 (&r)[2], int e) {
+        const uint4 z = make_uint4(0, 0, 0, 0);
+        r[0] = e < K ? *reinterpret_cast<const uint4*>(x + e) : z;
+        r[1] = e < K ? *reinterpret_cast<const uint4*>(x + e + 8) : z;
+    };
+    auto widen = [&](const uint4 (&r)[2], float (&f)[16]) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            float t[8];
+            act8(r[h], bf, t);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) f[8 * h + i] = t[i];
+        }
+    };
+    const int first = (wave * 64 + lane) * 16, step = W * 1024;
+#pragma unroll
+    for (int i = 0; i < N; ++i) load(v[i], first + i * step);
+    float up = 1.0f;
+    if (bf) {
+        float top = 0.0f, f[16];
+        auto most = [&](const uint4 (&r)[2]) {
+            widen(r, f);
+#pragma unroll
+            for (int u = 0; u < 16; ++u) top = fmaxf(top, fabsf(f[u]));
+        };
+#pragma unroll
+        for (int i = 0; i < N; ++i) most(v[i]);
+        for (int e = first + N * step; e < K; e += step) {
+            uint4 r[2];
+            load(r, e);
+            most(r);
+        }
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s, 64));
+        if (lane == 0)
+            best[wave] = top;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < W; ++w) top = fmaxf(top, best[w]);
+        const int e = bf16_shift(top);
+        up = __uint_as_float((uint32_t)(127 + e) << 23);
+        if (tid == 0)
+            *back = __uint_as_float((uint32_t)(127 - e) << 23);
+    }
+    auto put = [&](const uint4 (&r)[2], int e) {
+        float f[16], c, xs;
+        uint4 w[2];
+        widen(r, f);
+        if (bf)
+#pragma unroll
+            for (int u = 0; u < 16; ++u) f[u] = h2f(f2h(f[u] * up));
+        operand16(f, bits, g, w, c, xs);
+        if (e < len) {
+            reinterpret_cast<uint4*>(o + e)[0] = w[0];
+            reinterpret_cast<uint4*>(o + e)[1] = w[1];
+            if (e % g == 0)
+                *reinterpret_cast<float2*>(sums + e / g * 2) = make_float2(c, xs);
+        }
+    };
+#pragma unroll
+    for (int i = 0; i < N; ++i) put(v[i], first + i * step);
+    for (int e0 = N * step; e0 < len; e0 += step) {
+        const int e = first + e0;
+        uint4 r[2];
+        load(r, e);
+        put(r, e);
+    }
+}
+
+
 
 }  // namespace
 }  // namespace qmlp
