@@ -86,7 +86,8 @@ qmlp_status check_route(int M, int d, int E, int k, int score, qmlp_dtype dtype)
         return QMLP_ERR_UNSUPPORTED;
     return QMLP_OK;
 }
-size_t route_bytes(int M, int E) { return round256((size_t)M * E * 8); }
+// [logits fp64][norms of the rows of x][of the router's], the norms for many tokens
+size_t route_bytes(int M, int E) { return round256((size_t)M * E * 8 + ((size_t)M + E) * 4); }
 
 // ---------------------------------------------------------------- MoE layer
 
@@ -236,8 +237,9 @@ qmlp_status qmlp_moe_route(const void* router, const float* bias, const void* x,
         return QMLP_ERR_ALIGN;
     if (!ws || ws_bytes < route_bytes(M, E))
         return QMLP_ERR_WORKSPACE;
+    float* norms = reinterpret_cast<float*>(static_cast<double*>(ws) + (size_t)M * E);
     const RouteArgs a{static_cast<const uint16_t*>(x), static_cast<const uint16_t*>(router), bias, topk_idx, topk_w,
-                      static_cast<double*>(ws), M, d, E, k, score, dtype == QMLP_BF16};
+                      static_cast<double*>(ws), norms, norms + M, M, d, E, k, score, dtype == QMLP_BF16};
     return from_hip(launch_route(a, static_cast<hipStream_t>(stream)));
 }
 

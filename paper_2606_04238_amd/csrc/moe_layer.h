@@ -15,7 +15,8 @@ struct RouteArgs {
     const float* bias;       // [E] or null
     int32_t* idx;            // [M][k]
     float* w;                // [M][k]
-    double* logits;          // [M][E] workspace
+    double* logits;          // workspace: [M][E], and for many tokens the rows' norms [M], [E]
+    float *xnorm, *wnorm;
     int M, d, E, k, score, bf;
 };
 hipError_t launch_route(const RouteArgs& a, hipStream_t st);

@@ -11,109 +11,207 @@ namespace qmlp {
 namespace {
 
 // v of the lane that DPP control CTRL names, or v itself where it names none.
-template <int CTRL, int ROWS>
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false);
+}
+template <int CTRL>
 __device__ __forceinline__ double dpp_f64(double v) {
     const uint2 u = __builtin_bit_cast(uint2, v);
-    return __builtin_bit_cast(double, make_uint2((uint32_t)__builtin_amdgcn_update_dpp((int)u.x, (int)u.x, CTRL, ROWS, 0xF, false),
-                                                 (uint32_t)__builtin_amdgcn_update_dpp((int)u.y, (int)u.y, CTRL, ROWS, 0xF, false)));
+    return __builtin_bit_cast(double, make_uint2(dpp_u32<CTRL>(u.x), dpp_u32<CTRL>(u.y)));
 }
 __device__ __forceinline__ double lane_f64(double v, int lane) {
     const uint2 u = __builtin_bit_cast(uint2, v);
     return __builtin_bit_cast(double, make_uint2((uint32_t)__builtin_amdgcn_readlane((int)u.x, lane),
                                                  (uint32_t)__builtin_amdgcn_readlane((int)u.y, lane)));
 }
-// Over the wave: the largest v (none NaN), and the sum.
-__device__ __forceinline__ double wave_max(double v) {
-    v = fmax(v, dpp_f64<0xB1, 0xF>(v));                    // quad_perm: lanes 1 and 2 away
-    v = fmax(v, dpp_f64<0x4E, 0xF>(v));
-    v = fmax(v, dpp_f64<0x141, 0xF>(v));                   // row_half_mirror, row_mirror
-    v = fmax(v, dpp_f64<0x140, 0xF>(v));
-    v = fmax(v, dpp_f64<0x142, 0xF>(v));                   // row_bcast 15 and 31: into the rows that follow
-    v = fmax(v, dpp_f64<0x143, 0xF>(v));
-    return lane_f64(v, 63);
+// Over the wave, the same in every lane: the largest v; the sum of v.  (quad_perm for
+// lanes 1 and 2 away, row_half_mirror, row_mirror; row_bcast 15 and 31.)
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = max(v, dpp_u32<0xB1>(v));
+    v = max(v, dpp_u32<0x4E>(v));
+    v = max(v, dpp_u32<0x141>(v));
+    v = max(v, dpp_u32<0x140>(v));
+    v = max(v, dpp_u32<0x142>(v));
+    v = max(v, dpp_u32<0x143>(v));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
 }
 __device__ __forceinline__ double wave_sum(double v) {
-    v += dpp_f64<0xB1, 0xF>(v);
-    v += dpp_f64<0x4E, 0xF>(v);
-    v += dpp_f64<0x141, 0xF>(v);
-    v += dpp_f64<0x140, 0xF>(v);
+    v += dpp_f64<0xB1>(v);
+    v += dpp_f64<0x4E>(v);
+    v += dpp_f64<0x141>(v);
+    v += dpp_f64<0x140>(v);
     return (lane_f64(v, 0) + lane_f64(v, 16)) + (lane_f64(v, 32) + lane_f64(v, 48));
 }
+
+// Logits as 64-bit keys in their order, in two halves; 0 for what is never chosen,
+// NaN and -inf.  +inf counts as the largest fp32.
+struct Key {
+    uint32_t hi, lo;
+};
+__device__ __forceinline__ Key key_of(double v) {
+    const uint2 u = __builtin_bit_cast(uint2, fmin(v, (double)FLT_MAX));
+    const bool neg = (int)u.y < 0, any = v > -__builtin_inf();
+    return {any ? (neg ? ~u.y : u.y | 0x80000000u) : 0u, any ? (neg ? ~u.x : u.x) : 0u};
+}
+__device__ __forceinline__ double value_of(uint32_t hi, uint32_t lo) {
+    const bool neg = (int)hi >= 0;
+    return __builtin_bit_cast(double, neg ? make_uint2(~lo, ~hi) : make_uint2(lo, hi & 0x7FFFFFFFu));
+}
+constexpr int kRouteN = kMoeExperts / 64;
 
 // Lane j < k: the j-th chosen expert and its weight; -1 and 0 where there is none.
 struct Chosen {
     int e;
     float w;
 };
-// The k largest of the logits l[0 .. E): expert e in lane e & 63; ties to the
-// lower expert; NaN and -inf are never chosen, +inf counts as the largest fp32.
-__device__ __forceinline__ Chosen route_select(const double* l, int E, int k, int score, int lane) {
-    constexpr int N = kMoeExperts / 64;
-    const double none = -__builtin_inf();
-    double v[N];
+// The largest of the keys (expert e in lane e & 63, place e / 64), taken out: its
+// expert, lower ones first among equals, and its halves; -1 where none is left.
+// The high halves decide, the low ones only between equal high ones.
+__device__ __forceinline__ int take_largest(Key (&key)[kRouteN], int E, int lane, uint32_t& hi, uint32_t& lo) {
+    uint32_t t = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const int e = lane + 64 * i;
-        v[i] = none;
+    for (int i = 0; i < kRouteN; ++i)
         if (64 * i < E)                                    // (the same for every lane: no turns are spent past E)
-            v[i] = e < E ? l[e] : none;
-    }
-    double top = none;
+            t = max(t, key[i].hi);
+    hi = wave_max(t);
+    lo = 0;
+    if (hi == 0)
+        return -1;
+    int e = -1, n = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
+    for (int i = 0; i < kRouteN; ++i)
         if (64 * i < E) {
-            v[i] = v[i] != v[i] ? none : fmin(v[i], (double)FLT_MAX);
-            top = fmax(top, v[i]);
-        }
-    float all = 0.0f;
-    if (score == QMLP_SCORE_SOFTMAX) {
-        const double first = wave_max(top);
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (64 * i < E)
-                all += v[i] == none ? 0.0f : expf((float)(v[i] - first));
-        all = group_sum<64>(all);
-    }
-    double mine = none, best = none;                       // lane j: the j-th chosen
-    int me = -1;
-    for (int j = 0; j < k; ++j) {
-        const double b = wave_max(top);
-        if (b == none)
-            break;
-        if (j == 0)
-            best = b;
-        int e = -1;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (64 * i < E && e < 0) {
-                const uint64_t at = __ballot(v[i] == b);
-                if (at) {
-                    e = 64 * i + __builtin_ctzll(at);
-                    if (lane == (e & 63))
-                        v[i] = none;
-                }
+            const uint64_t at = __ballot(key[i].hi == hi);
+            if (at && e < 0) {
+                e = 64 * i + __builtin_ctzll(at);
+                lo = (uint32_t)__builtin_amdgcn_readlane((int)key[i].lo, e & 63);
             }
-        if (lane == (e & 63)) {
-            top = none;
+            n += __builtin_popcountll(at);
+        }
+    if (n > 1) {
+        t = 0;
 #pragma unroll
-            for (int i = 0; i < N; ++i)
-                if (64 * i < E)
-                    top = fmax(top, v[i]);
-        }
-        if (lane == j) {
-            mine = b;
-            me = e;
-        }
+        for (int i = 0; i < kRouteN; ++i)
+            if (64 * i < E)
+                t = max(t, key[i].hi == hi ? key[i].lo : 0u);
+        lo = wave_max(t);
+        e = -1;
+#pragma unroll
+        for (int i = 0; i < kRouteN; ++i)
+            if (64 * i < E && e < 0) {
+                const uint64_t at = __ballot(key[i].hi == hi && key[i].lo == lo);
+                if (at)
+                    e = 64 * i + __builtin_ctzll(at);
+            }
     }
-    // weights: a softmax of z over the chosen ones, z the logit or log sigmoid(logit), both largest for the
-    // first; or a softmax over all experts
-    if (score == QMLP_SCORE_SOFTMAX)
-        return {me, me >= 0 ? expf((float)(mine - best)) / all : 0.0f};
+#pragma unroll
+    for (int i = 0; i < kRouteN; ++i)
+        if (64 * i < E && e == 64 * i + lane)
+            key[i].hi = key[i].lo = 0;
+    return e;
+}
+
+// The k largest of the logits v (expert e in lane e & 63, place e / 64; anything past
+// E).  Where SURE is false the logits may be off by `off`, and where that could change
+// the choice or its order, the experts in question (all, where off is not finite)
+// are written to list (E entries, this wave's), from which exact(n, put) forms their
+// logits and hands each to put(expert, logit).
+template <bool SURE, typename EXACT>
+__device__ __forceinline__ Chosen route_select(double (&v)[kRouteN], int E, int k, int score, int lane, double off, int16_t* list,
+                                               EXACT exact) {
+    const double none = -__builtin_inf();
+    Key key[kRouteN];
+    double mine = none, first = none;                      // lane j: the j-th chosen
+    int me = -1;
+    bool sure = SURE || off == 0.0;
+    uint32_t in = ~0u;                                     // bit i: expert lane + 64 i may be chosen
+#pragma unroll
+    for (int i = 0; i < kRouteN; ++i)
+        if (64 * i < E && lane + 64 * i >= E)
+            v[i] = none;
+    for (;;) {
+#pragma unroll
+        for (int i = 0; i < kRouteN; ++i)
+            if (64 * i < E)
+                key[i] = key_of(SURE || (in >> i & 1) ? v[i] : none);
+        mine = first = none;
+        me = -1;
+        for (int j = 0; j < (sure ? k : k + 1); ++j) {
+            uint32_t hi, lo;
+            const int e = take_largest(key, E, lane, hi, lo);
+            if (e < 0)
+                break;
+            const double b = value_of(hi, lo);
+            if (j == 0)
+                first = b;
+            if (lane == j) {
+                mine = b;
+                me = e;
+            }
+        }
+        if constexpr (SURE)
+            break;
+        // pairs that are too close: chosen experts beside one are in question, and, where it is the k-th and the
+        // next, every expert down to 2 off below the k-th
+        const bool all = !(off < __builtin_inf());
+        const double above = __shfl_up(mine, 1, 64), edge = lane_f64(mine, k - 1), from = edge - 2.0 * off;
+        const uint64_t pairs = __ballot(lane > 0 && lane <= k && me >= 0 && above - mine <= 2.0 * off);
+        if (sure || (!all && pairs == 0))
+            break;
+        sure = true;
+        uint32_t redo = 0;
+        for (uint64_t at = (pairs | pairs >> 1) & ((1ull << k) - 1); at; at &= at - 1) {
+            const int e = __builtin_amdgcn_readlane(me, __builtin_ctzll(at));
+            redo |= lane == (e & 63) ? 1u << (e >> 6) : 0u;
+        }
+        int n = 0;
+#pragma unroll
+        for (int i = 0; i < kRouteN; ++i)
+            if (64 * i < E) {
+                const double u = fmin(v[i], (double)FLT_MAX);
+                const bool near = u >= from;
+                const bool q = lane + 64 * i < E && (all || (redo >> i & 1) || ((pairs >> k & 1) && near && u <= edge));
+                const uint64_t at = __ballot(q);
+                if (q)
+                    list[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0))] = (int16_t)(lane + 64 * i);
+                n += __builtin_popcountll(at);
+                in = all || near ? in : in & ~(1u << i);
+            }
+        __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the list is this wave's own)
+        exact(n, [&](int e, double s) {
+#pragma unroll
+            for (int i = 0; i < kRouteN; ++i)
+                if (64 * i < E && e == lane + 64 * i)
+                    v[i] = s;
+        });
+    }
+    me = lane < k ? me : -1;
+    // weights: a softmax over all experts, or of z over the chosen ones, z the logit or log sigmoid(logit);
+    // both are largest for the first
+    if (score == QMLP_SCORE_SOFTMAX) {
+        float all = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kRouteN; ++i)
+            if (64 * i < E)
+                all += v[i] > none ? expf((float)(fmin(v[i], (double)FLT_MAX) - first)) : 0.0f;
+        all = group_sum<64>(all);
+        return {me, me >= 0 ? expf((float)(mine - first)) / all : 0.0f};
+    }
     auto z = [&](double t) {
         return score == QMLP_SCORE_SIGMOID ? fmin(t, 0.0) - (double)log1pf(expf(-(float)fabs(t))) : t;
     };
-    const float g = me >= 0 ? expf((float)(z(mine) - z(best))) : 0.0f, sum = group_sum<64>(g);
+    const float g = me >= 0 ? expf((float)(z(mine) - z(first))) : 0.0f, sum = group_sum<64>(g);
     return {me, me >= 0 ? g / sum : 0.0f};
+}
+// Of logits that are right.
+__device__ __forceinline__ Chosen route_select(const double* l, int E, int k, int score, int lane) {
+    double v[kRouteN];
+#pragma unroll
+    for (int i = 0; i < kRouteN; ++i)
+        if (64 * i < E)
+            v[i] = l[min(lane + 64 * i, E - 1)];
+    return route_select<true>(v, E, k, score, lane, 0.0, nullptr, [](int, auto) {});
 }
 
 }  // namespace
