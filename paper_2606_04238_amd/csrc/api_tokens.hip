@@ -49,11 +49,11 @@ qmlp_status check_lora(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qm
 
 // Workspace: [t: M x R fp32, or as two bfloat16 terms][adapters of up to 16 rows,
 // or sets of rows with several][2^-e: M fp32], then up to 16 rows [x in operand
-// order][its group sums], past them [terms of the rows of those sets, fp32] and
-// for bfloat16 [x 2^e: M x k binary16].
+// order][its group sums], past them [sums of shares of k, fp32] or [terms of
+// the rows of those sets, fp32], and for bfloat16 [x 2^e: M x k binary16].
 struct LoraSizes {
-    size_t t, slots, xf, xo, xs, mixed, x16;
-    size_t all() const { return t + slots + xf + xo + xs + mixed + x16; }
+    size_t t, slots, xf, xo, xs, mixed, parts, x16;
+    size_t all() const { return t + slots + xf + xo + xs + mixed + parts + x16; }
 };
 LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
     const bool bf = dtype == QMLP_BF16, some = ad && ad->count > 0, few = lora_few_rows(M, w);
@@ -68,7 +68,9 @@ LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp
         z.xo = round256((size_t)M * operand_row(w->k_in, w->bits) * 2);
         z.xs = round256((size_t)M * operand_sums(w->k_in, w->bits, w->group) * 4);
     } else {
-        if (some)
+        if (const size_t shares = lora_shares(M, w->n_out, w->k_in); shares > 1)
+            z.parts = round256(shares * M * w->n_out * 4);
+        else if (some)
             z.mixed = round256((size_t)lora_mixed_most(M) * 32 * w->n_out * 4);
         if (bf)
             z.x16 = round256((size_t)M * w->k_in * 2);
@@ -209,14 +211,16 @@ qmlp_status qmlp_linear_lora(const qmlp_qweight* w, const qmlp_adapters* ad, con
     a.xo = few ? reinterpret_cast<uint16_t*>(take(z.xo)) : nullptr;
     a.xs = reinterpret_cast<float*>(take(z.xs));
     a.mixed = reinterpret_cast<float*>(take(z.mixed));
+    a.parts = z.parts ? reinterpret_cast<float*>(take(z.parts)) : nullptr;
     a.x16 = z.x16 ? reinterpret_cast<uint16_t*>(take(z.x16)) : nullptr;
     const hipStream_t st = static_cast<hipStream_t>(stream);
     hipError_t e = launch_lora_prep(a, st);
-    if (e == hipSuccess && !few && adapters)
+    if (e == hipSuccess && !few && adapters && !a.parts)
         e = launch_lora_mixed(a, st);
     if (e != hipSuccess)
         return QMLP_ERR_HIP;
-    return from_hip(few ? launch_lora_few(a, st) : launch_lora_gemm(a, st));
+    e = few ? launch_lora_few(a, st) : launch_lora_gemm(a, st);
+    return from_hip(e == hipSuccess && a.parts ? launch_lora_join(a, st) : e);
 }
 
 size_t qmlp_moe_route_workspace_bytes(int E, int M) {

@@ -6,7 +6,10 @@
 // v_mfma_f32_32x32x16_f16.  bfloat16 rows come as binary16 times a power of two
 // (lora_linear.hip), so both types run the same products.
 //
-// Adapters first: the accumulators start as B_a t of each row.  Where a wave's rows
+// Few tiles: k is split into shares, which leave their sums in memory;
+// lora_join_kernel adds them and the adapters' terms.
+//
+// Otherwise adapters first: the accumulators start as B_a t of each row.  Where a wave's rows
 // all have one adapter (a prompt), its products go there directly.  Sets of 32 rows
 // with many (decoding sequences) find their terms ready in memory
 // (lora_mixed_kernel; kMixedSets of them, the first in the call); for the others,
@@ -18,7 +21,7 @@
 //
 // Tile engine: BM rows x BN outputs per workgroup, K in steps of 64 staged in
 // LDS, chunk c of row r at c ^ ((r >> 1) & 7).  x is copied to LDS by the memory
-// system (ST slots, ST - 1 steps ahead); codes are in registers two steps ahead
+// system (ST slots, ST - 1 steps ahead); codes are in registers QA steps ahead
 // and unpacked into two buffers, one step ahead; one barrier per step.
 #include "lora_linear.h"
 #include "decode_launch.h"
@@ -95,12 +98,13 @@ __device__ __forceinline__ void split_f16(const uint4& v, uint4& hi, uint4& lo) 
     lo = make_uint4(l[0], l[1], l[2], l[3]);
 }
 
-template <int BITS, int BM, int BN, int WM, int WN, int ST>
+template <int BITS, int BM, int BN, int WM, int WN, int ST, bool SPLIT>
 __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_gemm_kernel(LoraArgs a, int lg) {
     constexpr int WMW = BM / (32 * WM), NW_ = WMW * (BN / (32 * WN)), NT = NW_ * 64;
     constexpr int CA = BM / (8 * NW_);                     // x loads of a wave and step, eight rows each
     constexpr int P = NT / BN >= 4 ? 4 : NT / BN >= 2 ? 2 : 1, CPT = 64 / P, NW = BITS * CPT / 32;
     static_assert(CA >= 1 && BM % (8 * NW_) == 0 && NT >= BN && CPT <= 32 && NW >= 1, "staging shares");
+    constexpr int QA = ST > 3 ? 4 : 2;                     // steps whose codes are in registers or under way
     constexpr int XB = BM * 8, WB = BN * 8;                // 16-byte chunks of a stage
     extern __shared__ uint4 smem[];                        // x [ST][BM][8], weights [2][BN][8], then the rows' 2^-e
     uint4* wsm = smem + ST * XB;
@@ -110,7 +114,10 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
     const int wm = wave % WMW, wn = wave / WMW;
     // the row tiles' columns one after another: rows of many adapters (usually the first) take longer and start first
     const int ntiles = (a.n + BN - 1) / BN;
-    const int m0 = blockIdx.x / ntiles * BM, n0 = blockIdx.x % ntiles * BN;
+    const int m0 = (int)blockIdx.x / ntiles * BM, n0 = (int)blockIdx.x % ntiles * BN;
+    // the steps of 64 this workgroup multiplies: all, or its share of k (lora_join_kernel adds shares and adapters)
+    const int steps = a.k / 64, share = blockIdx.y, kb = SPLIT ? share * steps / (int)gridDim.y : 0;
+    const int nk = SPLIT ? (share + 1) * steps / (int)gridDim.y - kb : steps;
     const long ldx = a.x16 ? a.k : a.ldx;
 
     // x goes from memory to LDS without registers, eight rows (1 KB) per load: lane l writes chunk l & 7 of row l >> 3,
@@ -135,10 +142,10 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
     auto load_x = [&](int kt, int slot) {
 #pragma unroll
         for (int i = 0; i < CA; ++i)
-            load_to_lds(rx, smem + slot * XB + (wave * CA + i) * 64, xo[i], (uint32_t)kt * 128u);
+            load_to_lds(rx, smem + slot * XB + (wave * CA + i) * 64, xo[i], (uint32_t)(kb + kt) * 128u);
     };
     auto load_w = [&](Q& q, int kt) {
-        const uint32_t so = (uint32_t)kt * 8u * BITS;
+        const uint32_t so = (uint32_t)(kb + kt) * 8u * BITS;
         if constexpr (NW == 4) {
             const auto v = __builtin_amdgcn_raw_buffer_load_b128(rc, co, so, 0);
             q.w[0] = v[0]; q.w[1] = v[1]; q.w[2] = v[2]; q.w[3] = v[3];
@@ -148,14 +155,14 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
         } else {
             q.w[0] = __builtin_amdgcn_raw_buffer_load_b32(rc, co, so, 0);
         }
-        q.m = __builtin_amdgcn_raw_buffer_load_b32(rm, mo, (uint32_t)((kt * 64) >> lg) * 4u, 0);
+        q.m = __builtin_amdgcn_raw_buffer_load_b32(rm, mo, (uint32_t)(((kb + kt) * 64) >> lg) * 4u, 0);
     };
-    const int nk = a.k / 64;
-    Q q[2];
+    Q q[QA];
 #pragma unroll
-    for (int s = 0; s < ST - 1; ++s) {
-        load_x(s < nk ? s : nk - 1, s);
-        if (s < 2)
+    for (int s = 0; s < ST - 1 || s < QA; ++s) {
+        if (s < ST - 1)
+            load_x(s < nk ? s : nk - 1, s);
+        if (s < QA)
             load_w(q[s], s < nk ? s : nk - 1);
     }
 
@@ -169,7 +176,7 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
     __syncthreads();
     // the factor 2^e that takes an adapter's sums to the scale of a bfloat16 row's products
     auto up = [&](int at) { return __uint_as_float(0x7F000000u - __float_as_uint(ro[at])); };
-    if (a.T > 0) {
+    if (!SPLIT && a.T > 0) {
         int id[WM];
         bool same = true;                                  // this wave's rows have one adapter, or none (or lie past M)
         const int mf = m0 + wm * 32 * WM;
@@ -294,7 +301,7 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
     // codes of kt + 2 too, and the weights of kt + 1 are unpacked.
     if (stager)
         dequant_store<BITS, CPT>(wsm, q[0].w, q[0].m, trow, part);
-    load_w(q[0], nk > 2 ? 2 : nk - 1);
+    load_w(q[0], nk > QA ? QA : nk - 1);
     int slot = 0;
     auto step = [&](int kt, Q& qn) {
         // x of this step has arrived: after it ST - 2 steps' x and at least as many steps' two loads of codes were issued
@@ -321,16 +328,17 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
         if (stager)
             dequant_store<BITS, CPT>(wsm + ((kt + 1) & 1) * WB, qn.w, qn.m, trow, part);
         __asm__ volatile("" ::: "memory");                 // the codes' registers are free now, not before
-        load_w(qn, kt + 3 < nk ? kt + 3 : nk - 1);
+        load_w(qn, kt + 1 + QA < nk ? kt + 1 + QA : nk - 1);
         slot = slot + 1 == ST ? 0 : slot + 1;
     };
     int kt = 0;
-    for (; kt + 1 < nk; kt += 2) {
-        step(kt, q[1]);
-        step(kt + 1, q[0]);
-    }
-    if (kt < nk)
-        step(kt, q[1]);
+    for (; kt + QA <= nk; kt += QA)
+#pragma unroll
+        for (int i = 0; i < QA; ++i) step(kt + i, q[(i + 1) % QA]);
+#pragma unroll
+    for (int i = 0; i < QA - 1; ++i)
+        if (kt + i < nk)
+            step(kt + i, q[(i + 1) % QA]);
     __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy into LDS outlives the workgroup
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
@@ -340,8 +348,12 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
 #pragma unroll
             for (int v = 0; v < 16; ++v) {
                 const int at = wm * 32 * WM + i * 32 + acc_row(v, lane), m = m0 + at;
-                if (m < a.M && col < a.n)
-                    a.y[(long)m * a.ldy + col] = act_bits(acc[i][j][v] * ro[at], a.bf);
+                if (m < a.M && col < a.n) {
+                    if (SPLIT)
+                        a.parts[((long)share * a.M + m) * a.n + col] = acc[i][j][v] * ro[at];
+                    else
+                        a.y[(long)m * a.ldy + col] = act_bits(acc[i][j][v] * ro[at], a.bf);
+                }
             }
     }
 }
@@ -350,20 +362,24 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
 
 hipError_t launch_lora_gemm(const LoraArgs& a, hipStream_t st) {
     const int lg = a.g == 32 ? 5 : a.g == 64 ? 6 : 7;
+    const unsigned shares = (unsigned)lora_shares(a.M, a.n, a.k);
     auto run = [&](auto k, int BM, int BN, int nt, int stages) {
         const size_t lds = (size_t)(stages * BM + 2 * BN) * 128 + (size_t)BM * 4;
         const hipError_t e = set_lds(k, lds);
         if (e != hipSuccess)
             return e;
         const unsigned grid = (unsigned)(((a.M + BM - 1) / BM) * ((a.n + BN - 1) / BN));
-        k<<<grid, (unsigned)nt, lds, st>>>(a, lg);
+        k<<<dim3(grid, shares), (unsigned)nt, lds, st>>>(a, lg);
         return hipGetLastError();
     };
+    if (shares > 1)
+        return a.bits == 2 ? run(lora_gemm_kernel<2, 128, 128, 2, 1, 4, true>, 128, 128, 512, 4)
+                           : run(lora_gemm_kernel<4, 128, 128, 2, 1, 4, true>, 128, 128, 512, 4);
     if (a.M > 512)
-        return a.bits == 2 ? run(lora_gemm_kernel<2, 256, 192, 2, 3, 3>, 256, 192, 512, 3) : run(lora_gemm_kernel<4, 256, 192, 2, 3, 3>, 256, 192, 512, 3);
-    if (a.bits == 2)
-        return run(lora_gemm_kernel<2, 128, 128, 2, 1, 4>, 128, 128, 512, 4);
-    return run(lora_gemm_kernel<4, 128, 128, 2, 1, 4>, 128, 128, 512, 4);
+        return a.bits == 2 ? run(lora_gemm_kernel<2, 256, 192, 2, 3, 3, false>, 256, 192, 512, 3)
+                           : run(lora_gemm_kernel<4, 256, 192, 2, 3, 3, false>, 256, 192, 512, 3);
+    return a.bits == 2 ? run(lora_gemm_kernel<2, 128, 128, 2, 1, 4, false>, 128, 128, 512, 4)
+                       : run(lora_gemm_kernel<4, 128, 128, 2, 1, 4, false>, 128, 128, 512, 4);
 }
 
 }  // namespace qmlp

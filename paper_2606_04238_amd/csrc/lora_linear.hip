@@ -154,47 +154,107 @@ __device__ __forceinline__ void lora_find_mixed(const LoraArgs& a, int tid) {
         a.slots[sets + tid] = -1;
 }
 
-// Adapter terms B_a t of the rows of the mixed sets, fp32: a workgroup takes four
-// rows and 256 outputs, a lane R ranks of one output's B.  (In the product's launch itself
-// these rows' adapters, one after another, held their workgroups back: 4096 rows
-// of which 48 decode, rank 64, 391 us instead of 344 with one adapter.)
+// Adapter terms B_a t of four rows and 256 outputs by a workgroup, past 16 rows: RC
+// neighbouring lanes take a row of B (8 RC ranks), so that its lines are read whole,
+// and everything is loaded before the first product.  (A lane a row of B, 64 ranks,
+// 48 rows of 4096, n = 6144: 19.5 us instead of 13.8.)
+constexpr int kTermRows = 4;
+template <int RC>
+struct Terms {
+    static constexpr int PC = 256 / RC;                    // columns of a pass, RC passes
+    int ad[kTermRows];
+    uint4 b[kTermRows][RC], t0[kTermRows], t1[kTermRows];
+    __device__ __forceinline__ void load(const LoraArgs& a, int m0, int c0, int tid) {
+        const int k = 8 * (tid % RC);
+#pragma unroll
+        for (int r = 0; r < kTermRows; ++r) {
+            const int m = min(m0 + r, a.M - 1), v = a.ids[m];
+            ad[r] = m0 + r < a.M && v >= 0 && v < a.T ? v : -1;
+            t0[r] = ld16(a.tb + (long)m * a.R + k);
+            t1[r] = ld16(a.tb + ((long)a.M + m) * a.R + k);
+        }
+#pragma unroll
+        for (int r = 0; r < kTermRows; ++r)
+#pragma unroll
+            for (int p = 0; p < RC; ++p)
+                b[r][p] = ld16(a.B + ((long)max(ad[r], 0) * a.n + min(c0 + p * PC + tid / RC, a.n - 1)) * a.R + k);
+    }
+    // s[r] += row r's term of column c0 + tid (not 0 B where there is no adapter: one's infinities are its own rows')
+    __device__ __forceinline__ void add(float (&s)[kTermRows], float (&at)[kTermRows][256], bool bf, int tid) const {
+#pragma unroll
+        for (int r = 0; r < kTermRows; ++r) {
+            float t[8], lo[8];
+            act8(t0[r], true, t);
+            act8(t1[r], true, lo);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) t[i] += lo[i];
+#pragma unroll
+            for (int p = 0; p < RC; ++p) {
+                float w[8], u = 0.0f;
+                act8(b[r][p], bf, w);
+#pragma unroll
+                for (int i = 0; i < 8; ++i) u = __builtin_fmaf(t[i], w[i], u);
+                if constexpr (RC > 1)
+                    u = group_sum<RC>(u);
+                if (tid % RC == 0)
+                    at[r][p * PC + tid / RC] = u;
+            }
+        }
+        __syncthreads();
+#pragma unroll
+        for (int r = 0; r < kTermRows; ++r)
+            if (ad[r] >= 0)
+                s[r] += at[r][tid];
+    }
+};
+
+// The terms of the rows of the mixed sets.  (In the product's launch itself these rows'
+// adapters, one after another, held their workgroups back: 4096 rows of which 48
+// decode, rank 64, 391 us instead of 344 with one adapter.)
+template <int RC>
 __global__ void __launch_bounds__(256) lora_mixed_kernel(LoraArgs a) {
-    const int o = blockIdx.x * 256 + threadIdx.x, set = a.slots[(a.M + 31) / 32 + (blockIdx.y >> 3)];
-    if (set < 0 || o >= a.n)
+    __shared__ float at[kTermRows][256];
+    const int tid = threadIdx.x, c = blockIdx.x * 256 + tid, set = a.slots[(a.M + 31) / 32 + (blockIdx.y >> 3)];
+    if (set < 0)
         return;
-    const int r0 = 4 * (blockIdx.y & 7), m0 = 32 * set + r0;
-    const long tlo = (long)a.M * a.R;
-    float s[4] = {0.f, 0.f, 0.f, 0.f};
-    int id[4];
+    const int r0 = kTermRows * (blockIdx.y & 7);
+    Terms<RC> x;
+    x.load(a, 32 * set + r0, blockIdx.x * 256, tid);
+    float s[kTermRows] = {};
+    x.add(s, at, a.bf, tid);
+    if (c < a.n)
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int v = a.ids[m0 + u < a.M ? m0 + u : a.M - 1];
-        id[u] = m0 + u < a.M && v >= 0 && v < a.T ? v : -1;
+        for (int u = 0; u < kTermRows; ++u) a.mixed[((long)(blockIdx.y >> 3) * 32 + r0 + u) * a.n + c] = s[u];
+}
+
+// y = the sum of the shares of k, in their order, and the adapters' terms.
+template <int RC>
+__global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs a, int shares) {
+    constexpr int P = 8;                                   // shares loaded at once
+    __shared__ float at[kTermRows][256];
+    const int tid = threadIdx.x, m0 = blockIdx.y * kTermRows, c = blockIdx.x * 256 + tid;
+    Terms<RC> x;
+    if (a.T > 0)
+        x.load(a, m0, blockIdx.x * 256, tid);
+    float s[kTermRows] = {};
+    for (int i0 = 0; i0 < shares; i0 += P) {
+        float p[P][kTermRows];
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int r = 0; r < kTermRows; ++r)
+                p[i][r] = a.parts[((long)min(i0 + i, shares - 1) * a.M + min(m0 + r, a.M - 1)) * a.n + min(c, a.n - 1)];
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int r = 0; r < kTermRows; ++r) s[r] += i0 + i < shares ? p[i][r] : 0.0f;
     }
-#pragma unroll 2
-    for (int c = 0; c < a.R; c += 8) {
-        uint4 bv[4], t0[4], t1[4];
+    if (a.T > 0)
+        x.add(s, at, a.bf, tid);
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (id[u] >= 0) {
-                const uint16_t* tp = a.tb + (long)(m0 + u) * a.R + c;
-                bv[u] = *reinterpret_cast<const uint4*>(a.B + ((long)id[u] * a.n + o) * a.R + c);
-                t0[u] = *reinterpret_cast<const uint4*>(tp);
-                t1[u] = *reinterpret_cast<const uint4*>(tp + tlo);
-            }
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-            if (id[u] >= 0) {
-                float b[8], f0[8], f1[8];
-                act8(bv[u], a.bf, b);
-                act8(t0[u], true, f0);
-                act8(t1[u], true, f1);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[u] = __builtin_fmaf(b[i], f0[i] + f1[i], s[u]);
-            }
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) a.mixed[((long)(blockIdx.y >> 3) * 32 + r0 + u) * a.n + o] = s[u];
+    for (int r = 0; r < kTermRows; ++r)
+        if (m0 + r < a.M && c < a.n)
+            a.y[(long)(m0 + r) * a.ldy + c] = act_bits(s[r], a.bf);
 }
 
 // blockIdx.x: token, blockIdx.y: eight ranks of t, or (the last one) the row's
@@ -518,13 +578,20 @@ hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st) {
         lora_prep_many_kernel<<<1u + rowgroups + tiles + convert, kPrepWaves * 64, 0, st>>>(a, tiles, rowgroups);
         return hipGetLastError();
     }
-    const bool find = a.T > 0 && a.tb;                     // one more column of workgroups looks for the mixed sets
+    const bool find = a.T > 0 && a.tb && !a.parts;                     // one more column of workgroups looks for the mixed sets
     lora_prep_kernel<<<dim3((unsigned)a.M + (find ? 1u : 0u), ny), kPrepWaves * 64, 0, st>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st) {
-    lora_mixed_kernel<<<dim3((unsigned)(a.n + 255) / 256, 8u * (unsigned)lora_mixed_most(a.M)), 256, 0, st>>>(a);
+    auto k = a.R == 8 ? lora_mixed_kernel<1> : a.R == 16 ? lora_mixed_kernel<2> : a.R == 32 ? lora_mixed_kernel<4> : lora_mixed_kernel<8>;
+    k<<<dim3((unsigned)(a.n + 255) / 256, 8u * (unsigned)lora_mixed_most(a.M)), 256, 0, st>>>(a);
+    return hipGetLastError();
+}
+
+hipError_t launch_lora_join(const LoraArgs& a, hipStream_t st) {
+    auto k = a.T == 0 || a.R == 8 ? lora_join_kernel<1> : a.R == 16 ? lora_join_kernel<2> : a.R == 32 ? lora_join_kernel<4> : lora_join_kernel<8>;
+    k<<<dim3((unsigned)(a.n + 255) / 256, (unsigned)(a.M + kTermRows - 1) / kTermRows), 256, 0, st>>>(a, lora_shares(a.M, a.n, a.k));
     return hipGetLastError();
 }
 
