@@ -68,8 +68,8 @@ LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp
         z.xo = round256((size_t)M * operand_row(w->k_in, w->bits) * 2);
         z.xs = round256((size_t)M * operand_sums(w->k_in, w->bits, w->group) * 4);
     } else {
-        if (const size_t shares = lora_shares(M, w->n_out, w->k_in); shares > 1)
-            z.parts = round256(shares * M * w->n_out * 4);
+        if (lora_join(M, w->n_out, w->k_in, some))
+            z.parts = round256((size_t)lora_shares(M, w->n_out, w->k_in) * M * w->n_out * 4);
         else if (some)
             z.mixed = round256((size_t)lora_mixed_most(M) * 32 * w->n_out * 4);
         if (bf)

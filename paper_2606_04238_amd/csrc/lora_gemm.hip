@@ -358,11 +358,138 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
     }
 }
 
+// 17 to 64 rows: a workgroup owns 32 WM rows and 128 outputs, a wave all of the rows
+// and 32 outputs, whose weights go from memory to its registers and are unpacked
+// there: in a step of 64 lane 32 h + r takes the 32 codes of row r from 32 h on, and
+// multiplies them with chunk 4 h + s of x in product s.  Only x is staged; the codes
+// are kMidAhead steps ahead.  (us, and by the tiles of lora_gemm_kernel: 17 x 6144 x
+// 4096 11.2 and 14.0, 32 x 28672 x 4096 35 and 50; at 67 rows 17.2 and 16.4, at 333 x
+// 9728 x 2560 40 and 38: rows are staged again for every 128 outputs.  Eight steps
+// ahead, of x or the codes, took 3 to 10 % more.)
+constexpr int kMidSlots = 4, kMidAhead = 4;
+template <int BITS, int WM>
+__global__ void __launch_bounds__(256) lora_mid_kernel(LoraArgs a, int lg) {
+    constexpr int BM = 32 * WM, XB = BM * 8, ST = kMidSlots, QA = kMidAhead, NW = BITS;
+    extern __shared__ uint4 smem[];                        // x [ST][BM][8], then the rows' 2^-e
+    float* ro = reinterpret_cast<float*>(smem + ST * XB);
+    const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, hk = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int ntiles = (a.n + 127) / 128, m0 = (int)blockIdx.x / ntiles * BM, n0 = (int)blockIdx.x % ntiles * 128 + 32 * wave;
+    // this workgroup's share of k, in steps of 64
+    const int steps = a.k / 64, share = blockIdx.y, kb = share * steps / (int)gridDim.y, nk = (share + 1) * steps / (int)gridDim.y - kb;
+    const long ldx = a.x16 ? a.k : a.ldx;
+    const int mrows = min(BM, a.M - m0), nrows = max(0, min(32, a.n - n0)), rb = a.k * BITS / 8, ng = a.k >> lg;
+    const Rsrc rx = rsrc((a.x16 ? a.x16 : a.x) + (long)m0 * ldx, (uint32_t)((mrows - 1) * (int)ldx + a.k) * 2u);
+    const Rsrc rc = rsrc(reinterpret_cast<const char*>(a.codes) + (long)n0 * rb, (uint32_t)(nrows * rb));
+    const Rsrc rm = rsrc(a.meta + (long)n0 * ng, (uint32_t)(nrows * ng) * 4u);
+    uint32_t xo[WM];
+#pragma unroll
+    for (int i = 0; i < WM; ++i) {
+        const int lr = (wave * WM + i) * 8 + (lane >> 3);
+        xo[i] = (uint32_t)lr * (uint32_t)ldx * 2u + (uint32_t)((lane & 7) ^ ((lr >> 1) & 7)) * 16u;
+    }
+    const uint32_t co = (uint32_t)(r * rb + hk * 4 * BITS), mo = (uint32_t)(r * ng) * 4u;
+    struct Q {
+        uint32_t w[NW], m;
+    };
+    auto load_x = [&](int kt, int slot) {
+#pragma unroll
+        for (int i = 0; i < WM; ++i)
+            load_to_lds(rx, smem + slot * XB + (wave * WM + i) * 64, xo[i], (uint32_t)(kb + kt) * 128u);
+    };
+    auto load_w = [&](Q& q, int kt) {
+        const uint32_t so = (uint32_t)(kb + kt) * 8u * BITS;
+        if constexpr (NW == 4) {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b128(rc, co, so, 0);
+            q.w[0] = v[0]; q.w[1] = v[1]; q.w[2] = v[2]; q.w[3] = v[3];
+        } else {
+            const auto v = __builtin_amdgcn_raw_buffer_load_b64(rc, co, so, 0);
+            q.w[0] = v[0]; q.w[1] = v[1];
+        }
+        q.m = __builtin_amdgcn_raw_buffer_load_b32(rm, mo + (uint32_t)(((kb + kt) * 64 + 32 * hk) >> lg) * 4u, 0, 0);
+    };
+    // eight codes of product s as binary16 scale * (q - zero), rounded once
+    auto unpack = [&](const Q& q, uint32_t s2, uint32_t off, int s) {
+        constexpr int PW = 16 / BITS;                      // pairs (c_i, c_{PW + i}) of a word
+        constexpr uint32_t mask = BITS == 2 ? 0x00030003u : 0x000F000Fu;
+        const uint32_t w = q.w[BITS == 2 ? s >> 1 : s];
+        uint32_t v[PW];
+#pragma unroll
+        for (int p = 0; p < PW; ++p) v[p] = pk_mul(pk_add(((w >> (BITS * p)) & mask) | 0x64006400u, off), s2);
+        if constexpr (BITS == 2)
+            return (s & 1) ? make_uint4(pair_hi(v[0], v[1]), pair_hi(v[2], v[3]), pair_hi(v[4], v[5]), pair_hi(v[6], v[7]))
+                           : make_uint4(pair_lo(v[0], v[1]), pair_lo(v[2], v[3]), pair_lo(v[4], v[5]), pair_lo(v[6], v[7]));
+        else
+            return make_uint4(pair_lo(v[0], v[1]), pair_lo(v[2], v[3]), pair_hi(v[0], v[1]), pair_hi(v[2], v[3]));
+    };
+    Q q[QA];
+#pragma unroll
+    for (int s = 0; s < QA; ++s) {
+        if (s < ST - 1)
+            load_x(s < nk ? s : nk - 1, s);
+        load_w(q[s], s < nk ? s : nk - 1);
+    }
+    f32x16_t acc[WM];
+#pragma unroll
+    for (int i = 0; i < WM; ++i) acc[i] = f32x16_t{};
+    for (int i = tid; i < BM; i += 256) ro[i] = a.x16 && m0 + i < a.M ? a.xf[m0 + i] : 1.0f;
+    int slot = 0;
+    // Step kt multiplies slot kt % ST of x, while x of step kt + ST - 1 and the codes up to kt + QA are under way.
+    auto step = [&](int kt, Q& c) {
+        // x of this step has arrived: after it ST - 2 steps' x and codes (two loads) were issued, and more
+        vm_window<(ST - 2) * (WM + 2)>();
+        lds_barrier();
+        const uint4* xs = smem + slot * XB;
+        load_x(kt + ST - 1 < nk ? kt + ST - 1 : nk - 1, slot == 0 ? ST - 1 : slot - 1);
+        const uint32_t s2 = __builtin_amdgcn_perm(0u, c.m, 0x01000100u);
+        const uint32_t off = pk_add(0xE400E400u, __builtin_amdgcn_perm(0u, c.m, 0x03020302u) ^ 0x80008000u);   // -1024 - z
+#pragma unroll
+        for (int s = 0; s < 4; ++s) {
+            const uint4 wv = unpack(c, s2, off, s);
+#pragma unroll
+            for (int i = 0; i < WM; ++i) acc[i] = mfma32(ld16(&xs[swz(i * 32 + r, 4 * hk + s)]), wv, acc[i]);
+        }
+        __asm__ volatile("" ::: "memory");                 // the codes' registers are free now, not before
+        load_w(c, kt + QA < nk ? kt + QA : nk - 1);
+        slot = slot + 1 == ST ? 0 : slot + 1;
+    };
+    int kt = 0;
+    for (; kt + QA <= nk; kt += QA)
+#pragma unroll
+        for (int i = 0; i < QA; ++i) step(kt + i, q[i]);
+#pragma unroll
+    for (int i = 0; i < QA - 1; ++i)
+        if (kt + i < nk)
+            step(kt + i, q[i]);
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy into LDS outlives the workgroup
+    const int col = n0 + r;
+#pragma unroll
+    for (int i = 0; i < WM; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int at = i * 32 + acc_row(v, lane), m = m0 + at;
+            if (m < a.M && col < a.n) {
+                if (a.parts)
+                    a.parts[((long)share * a.M + m) * a.n + col] = acc[i][v] * ro[at];
+                else
+                    a.y[(long)m * a.ldy + col] = act_bits(acc[i][v] * ro[at], a.bf);
+            }
+        }
+}
+
 }  // namespace
 
 hipError_t launch_lora_gemm(const LoraArgs& a, hipStream_t st) {
     const int lg = a.g == 32 ? 5 : a.g == 64 ? 6 : 7;
     const unsigned shares = (unsigned)lora_shares(a.M, a.n, a.k);
+    if (a.M <= kLoraMidRows) {
+        const int wm = (a.M + 31) / 32;
+        const unsigned grid = (unsigned)(a.n + 127) / 128;
+        const size_t lds = (size_t)kMidSlots * wm * 4096 + wm * 128;
+        auto k = a.bits == 2 ? (wm == 1 ? lora_mid_kernel<2, 1> : lora_mid_kernel<2, 2>) : (wm == 1 ? lora_mid_kernel<4, 1> : lora_mid_kernel<4, 2>);
+        k<<<dim3(grid, shares), 256, lds, st>>>(a, lg);
+        return hipGetLastError();
+    }
     auto run = [&](auto k, int BM, int BN, int nt, int stages) {
         const size_t lds = (size_t)(stages * BM + 2 * BN) * 128 + (size_t)BM * 4;
         const hipError_t e = set_lds(k, lds);

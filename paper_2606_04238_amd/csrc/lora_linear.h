@@ -26,7 +26,7 @@ struct LoraArgs {
     float* xf;                           // [M] 2^-e (bfloat16)
     uint16_t* tb;                        // more than 16 rows: t as two bfloat16 terms [2][M][R]
     int* slots;                          // [M / 32, rounded up]: which of the mixed sets, or -1; then [kMixedSets]: their places
-    float* parts;                        // [shares][M][n] sums of lora_shares() shares of k, where there are several
+    float* parts;                        // [shares][M][n] sums of lora_shares() shares of k, where lora_join() adds up; or null
     float* mixed;                        // [kMixedSets 32][n] adapter terms of the mixed sets' rows
 };
 
@@ -35,11 +35,13 @@ struct LoraArgs {
 constexpr int kMixedSets = 16, kMixedFrom = 3;
 inline int lora_mixed_most(int M) { return (M + 31) / 32 < kMixedSets ? (M + 31) / 32 : kMixedSets; }
 
-// Shares of k for 17 to 512 rows, where tiles of 128 x 128 leave half the compute
-// units or more without one: as many as there are units for, of at least eight steps
-// of 64.  (us, the product's launches with one share and with the rule's: 67 x 6144 x
-// 4096, 48 tiles, 50.5 and 23.4; 200 x 2560 x 2560 36.9 and 20.6; 128 x 2560 x 9728
-// 97 and 26; rank 64: 256 x 4096 x 4096 67 and 52, 512 84 and 67.)
+constexpr int kLoraMidRows = 64;         // rows up to which lora_mid_kernel multiplies
+// Shares of k for 17 to 512 rows, where tiles of 128 outputs (and 128 rows) leave half
+// the compute units or more without one: as many as there are units for, of at
+// least eight steps of 64.  (us, the product's launches with one share and with
+// the rule's: 17 x 6144 x 4096, 48 tiles, 35.7 and 16.9; 67 rows 50.5 and 23.4; 200 x
+// 2560 x 2560 36.9 and 20.6; 128 x 2560 x 9728 97 and 26; rank 64: 256 x 4096 x 4096
+// 67 and 52, 512 84 and 71.)
 inline int lora_shares(int M, int n, int k) {
     const long tiles = (long)((M + 127) / 128) * ((n + 127) / 128);
     if (M > 512 || tiles > 128)
@@ -55,10 +57,14 @@ inline bool lora_few_rows(int M, const qmlp_qweight* w) {
     return M <= kLoraFewTokens && (long)w->n_out * w->k_in * w->bits / 8 < (1l << 31) &&
            (long)w->n_out * (w->k_in / w->group) * 4 < (1l << 31);
 }
+// Whether launch_lora_join follows the product, for several shares or for the adapters.
+inline bool lora_join(int M, int n, int k, bool adapters) {
+    return M > kLoraFewTokens && (lora_shares(M, n, k) > 1 || (M <= kLoraMidRows && adapters));
+}
 hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st);
 hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st);
 hipError_t launch_lora_few(const LoraArgs& a, hipStream_t st);
-// (With several shares of k: into parts, and without the adapters; launch_lora_join adds up.)
+// (Into parts, and without the adapters, where those are not null: launch_lora_join adds up.)
 hipError_t launch_lora_gemm(const LoraArgs& a, hipStream_t st);
 hipError_t launch_lora_join(const LoraArgs& a, hipStream_t st);
 

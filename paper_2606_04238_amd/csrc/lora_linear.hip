@@ -230,11 +230,12 @@ __global__ void __launch_bounds__(256) lora_mixed_kernel(LoraArgs a) {
 // y = the sum of the shares of k, in their order, and the adapters' terms.
 template <int RC>
 __global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs a, int shares) {
+    constexpr bool ADS = RC > 0;                           // (0: no adapters)
     constexpr int P = 8;                                   // shares loaded at once
     __shared__ float at[kTermRows][256];
     const int tid = threadIdx.x, m0 = blockIdx.y * kTermRows, c = blockIdx.x * 256 + tid;
-    Terms<RC> x;
-    if (a.T > 0)
+    Terms<ADS ? RC : 1> x;
+    if constexpr (ADS)
         x.load(a, m0, blockIdx.x * 256, tid);
     float s[kTermRows] = {};
     for (int i0 = 0; i0 < shares; i0 += P) {
@@ -249,7 +250,7 @@ __global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs a, int shares) 
 #pragma unroll
             for (int r = 0; r < kTermRows; ++r) s[r] += i0 + i < shares ? p[i][r] : 0.0f;
     }
-    if (a.T > 0)
+    if constexpr (ADS)
         x.add(s, at, a.bf, tid);
 #pragma unroll
     for (int r = 0; r < kTermRows; ++r)
@@ -590,7 +591,7 @@ hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st) {
 }
 
 hipError_t launch_lora_join(const LoraArgs& a, hipStream_t st) {
-    auto k = a.T == 0 || a.R == 8 ? lora_join_kernel<1> : a.R == 16 ? lora_join_kernel<2> : a.R == 32 ? lora_join_kernel<4> : lora_join_kernel<8>;
+    auto k = a.T == 0 ? lora_join_kernel<0> : a.R == 8 ? lora_join_kernel<1> : a.R == 16 ? lora_join_kernel<2> : a.R == 32 ? lora_join_kernel<4> : lora_join_kernel<8>;
     k<<<dim3((unsigned)(a.n + 255) / 256, (unsigned)(a.M + kTermRows - 1) / kTermRows), 256, 0, st>>>(a, lora_shares(a.M, a.n, a.k));
     return hipGetLastError();
 }
