@@ -198,8 +198,11 @@ __global__ void __launch_bounds__(kManyWaves * 64) route_many_kernel(RouteArgs a
 }
 
 // A workgroup: one token, whose logits may be off by 2^-18 |x| max |w|.  Its first
-// wave chooses; the logits it asks for are formed by all four, which share d.
+// wave chooses; the logits it asks for are formed by all four, which share d.  (Eight
+// waves a SIMD: 2048 tokens of 128 experts 23 us, 28 with three and no register
+// in memory; a token a wave, which formed its logits alone, 38.)
 constexpr int kChooseWaves = 4;
+template <int N>
 __global__ void __launch_bounds__(kChooseWaves * 64, 8) route_choose_kernel(RouteArgs a) {
     constexpr int P = 2;                                   // experts side by side
     __shared__ double part[kChooseWaves][kMoeExperts];
@@ -240,15 +243,14 @@ __global__ void __launch_bounds__(kChooseWaves * 64, 8) route_choose_kernel(Rout
         }
         return;
     }
-    double v[kRouteN];
+    double v[N];
     uint32_t wn = 0;
 #pragma unroll
-    for (int i = 0; i < kRouteN; ++i)
-        if (64 * i < a.E) {
-            const int e = min(lane + 64 * i, a.E - 1);
-            v[i] = a.logits[(long)m * a.E + e];
-            wn = max(wn, __float_as_uint(a.wnorm[e]));     // (not negative: in the order of their bits, NaN last)
-        }
+    for (int i = 0; i < N; ++i) {
+        const int e = min(lane + 64 * i, a.E - 1);
+        v[i] = a.logits[(long)m * a.E + e];
+        wn = max(wn, __float_as_uint(a.wnorm[e]));         // (not negative: in the order of their bits, NaN last)
+    }
     // (past 2^126 the fp32 sums could overflow where the logit does not)
     const double norms = (double)a.xnorm[m] * (double)__uint_as_float(wave_max(wn));
     const double off = norms < 0x1p126 ? 0x1p-18 * norms : __builtin_inf();
@@ -295,9 +297,10 @@ hipError_t launch_route_logits(const RouteArgs& a, hipStream_t st) {
     return hipGetLastError();
 }
 hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
-    // (us, few and many, the choice included: d = 4096, E = 128: M = 64 19.7 and 33.5, 256 40.3 and 35.0, 2048 231 and
-    // 44.2; d = 2880, E = 32: M = 256 16.1 and 26.2, 2048 57.5 and 29.6)
-    const bool few = (long)a.M * a.E < 32768;
+    // (us, few and many, the choice included: d = 4096, E = 128: M = 128 25.8 and 28.3, 256 39.5 and 28.4, 2048 244
+    // and 35.4; d = 2880, E = 32: M = 256 16.2 and 20.8, 512 23.3 and 21.6, 2048 60.6 and 22.3; d = 2048, E = 512:
+    // M = 16 14.7 and 21.2, 64 29.6 and 28.2)
+    const bool few = (long)a.M * a.E <= 16384;
     hipError_t e;
     if (few) {
         e = launch_route_logits(a, st);
@@ -311,7 +314,8 @@ hipError_t launch_route(const RouteArgs& a, hipStream_t st) {
     if (few)
         route_select_kernel<<<(unsigned)(a.M + 3) / 4, 256, 0, st>>>(a);
     else
-        route_choose_kernel<<<(unsigned)a.M, kChooseWaves * 64, 0, st>>>(a);
+        (a.E <= 64 ? route_choose_kernel<1> : a.E <= 128 ? route_choose_kernel<2> : route_choose_kernel<kMoeExperts / 64>)
+            <<<(unsigned)a.M, kChooseWaves * 64, 0, st>>>(a);
     return hipGetLastError();
 }
 
