@@ -57,9 +57,9 @@ inline bool lora_few_rows(int M, const qmlp_qweight* w) {
     return M <= kLoraFewTokens && (long)w->n_out * w->k_in * w->bits / 8 < (1l << 31) &&
            (long)w->n_out * (w->k_in / w->group) * 4 < (1l << 31);
 }
-// Whether launch_lora_join follows the product, for several shares or for the adapters.
+// Whether launch_lora_join follows launch_lora_gemm, for several shares or for the adapters.
 inline bool lora_join(int M, int n, int k, bool adapters) {
-    return M > kLoraFewTokens && (lora_shares(M, n, k) > 1 || (M <= kLoraMidRows && adapters));
+    return lora_shares(M, n, k) > 1 || (M <= kLoraMidRows && adapters);
 }
 hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st);
 hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st);

@@ -149,3 +149,36 @@ def test_workspace_contents_and_streams(q, M):
         torch.cuda.synchronize()
         got = y.clone()
         assert torch.equal(got, q.linear_lora(w, ad, ids, x, ws=ws)), i
+
+
+@pytest.mark.parametrize("M", [17, 32, 33, 64, 65, 128])
+@pytest.mark.parametrize("bits,g,n,k", [(4, 128, 130, 1152), (2, 32, 257, 2624), (4, 32, 384, 64), (2, 128, 33, 4096),
+                                        (4, 64, 5000, 576)])
+def test_shares_of_long_and_short_rows(q, M, bits, g, n, k):
+    """17 to 128 rows, k from one step to many shares, outputs that end inside a tile; y's neighbours stay."""
+    w, x, A, B, sc, ids = make(q, bits, g, n, k, M, 16, 5, BF16)
+    buf = torch.full((M, n + 3), 7.0, dtype=BF16).cuda()
+    y = q.linear_lora(w, q.Adapters(A, B, sc), ids, x, buf[:, :n])
+    assert bool((buf[:, n:] == 7.0).all())
+    ref, bound = lora_ref(w, x, A, B, sc, ids)
+    check(y, ref, bound, BF16)
+
+
+@pytest.mark.parametrize("M", [5, 40])
+def test_codes_past_32_bits(q, M):
+    """Codes of 2^31 bytes and more: rows at both ends and around the 2^31st byte, of few rows and of more."""
+    n, k, bits, g = 2 ** 18 + 40, 16384, 4, 128
+    gen = torch.Generator(device="cuda").manual_seed(71)
+    codes = torch.randint(-2 ** 31, 2 ** 31, (n * k // 8,), generator=gen, device="cuda", dtype=torch.int64).to(torch.int32)
+    one = torch.tensor([2.0 ** -7, 8.0], dtype=F16).view(torch.int32).cuda()
+    meta = one.expand(n * (k // g)).contiguous()
+    w = q.QWeight(bits, n, k, g, codes, meta)
+    rnd = lambda *s: torch.randn(*s, generator=gen, device="cuda")
+    A, B, sc = (rnd(3, 8, k) * 0.01).to(F16), rnd(3, n, 8).to(F16), None
+    x = rnd(M, k).to(F16)
+    ids = (torch.arange(M) % 4 - 1).to(torch.int32).cuda()
+    y = q.linear_lora(w, q.Adapters(A, B, sc), ids, x)
+    for lo in (0, 2 ** 18 - 16, 2 ** 18, n - 16):
+        part = q.QWeight(bits, 16, k, g, codes[lo * k // 8:(lo + 16) * k // 8], meta[:16 * (k // g)])
+        ref, bound = lora_ref(part, x, A, B[:, lo:lo + 16], sc, ids)
+        check(y[:, lo:lo + 16], ref, bound, F16)

@@ -195,3 +195,77 @@ def test_projection_router_and_layer_together(q):
     ref, _ = lora_ref(w, x, A, B, None, ids)
     assert float((u.double().cpu() - ref).norm() / ref.norm()) <= 2.0 ** -11
     _check_layer(q, moe, u, y)
+
+
+MANY = 300                                                 # tokens past which 70 experts take the many-token path
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("score", SCORES)
+@pytest.mark.parametrize("M,d,E,k", [(300, 8, 70, 3), (300, 2888, 70, 4), (2049, 264, 9, 2), (40, 512, 512, 16), (1025, 4096, 17, 16)])
+def test_route_of_many_tokens(q, M, d, E, k, score, dtype):
+    print("\n[case]", M, d, E, k, score, dtype, flush=True)
+    x, r = _rnd(81, M, d).to(dtype).cuda(), _rnd(82, E, d, std=0.05).to(dtype).cuda()
+    bias = _rnd(83, E, std=0.3).cuda() if M % 2 else None
+    _check_route(q.moe_route(x, r, k, bias, score), route_ref(x, r, bias, k, score))
+
+
+@pytest.mark.parametrize("score", SCORES)
+def test_route_of_many_near_ties(q, score):
+    """Experts that differ by one step of one weight, equal ones, and padding rows of zeros: the order is that of fp64."""
+    E, d, k = 70, 1024, 6
+    x = _rnd(84, MANY, d).to(F16)
+    x[50:60] = 0.0
+    r = _rnd(85, 1, d, std=0.1).expand(E, d).clone().to(F16)
+    for e in range(E):
+        if e % 3:
+            r.view(torch.int16)[e, e] += 1 if e % 3 == 1 else 40
+    x, r = x.cuda(), r.cuda()
+    for bias in (None, (torch.arange(E) % 5 * 2.0 ** -20).cuda()):
+        _check_route(q.moe_route(x, r, k, bias, score), route_ref(x, r, bias, k, score))
+
+
+@pytest.mark.parametrize("score", SCORES)
+def test_route_of_many_masks_and_bad_rows(q, score):
+    E, d, k = 70, 192, 6
+    x, r = _rnd(86, MANY, d).to(F16).cuda(), _rnd(87, E, d, std=0.1).to(F16).cuda()
+    bias = torch.full((E,), -float("inf")).cuda()
+    bias[[11, 50, 69]] = torch.tensor([0.5, 0.0, 0.0]).cuda()
+    bias[7] = float("nan")
+    idx, w = q.moe_route(x, r, k, bias, score)
+    _check_route((idx, w), route_ref(x, r, bias, k, score))
+    assert bool((idx[:, 3:] == -1).all()) and bool((w[:, 3:] == 0).all())
+    good = q.moe_route(x, r, k, None, score)
+    x[3, 5], x[100, 0] = float("nan"), float("inf")
+    idx, w = q.moe_route(x, r, k, None, score)
+    ref = route_ref(x, r, None, k, score)
+    assert bool((idx[3] == -1).all()) and torch.equal(idx.cpu(), ref[0])
+    rest = torch.tensor([m for m in range(MANY) if m not in (3, 100)])
+    assert torch.equal(idx.cpu()[rest], good[0].cpu()[rest]) and torch.equal(w.cpu()[rest], good[1].cpu()[rest])
+
+
+@pytest.mark.parametrize("dtype,mag", [(F16, 2.0 ** -20), (BF16, 2.0 ** -70), (BF16, 2.0 ** 60), (BF16, 2.0 ** 100)])
+def test_route_of_many_small_and_large(q, dtype, mag):
+    """Rows below binary16's normal numbers, and bfloat16 rows whose squares leave fp32."""
+    E, d, k = 70, 256, 4
+    x, r = (_rnd(88, MANY, d) * mag).to(dtype).cuda(), _rnd(89, E, d).to(dtype).cuda()
+    x[::2] += (_rnd(90, MANY, d) * (1.0 if dtype == F16 else mag)).to(dtype).cuda()[::2]
+    idx, w = q.moe_route(x, r, k)
+    _check_route((idx, w), route_ref(x, r, None, k, "topk_softmax"))
+
+
+@pytest.mark.parametrize("f,M", [(320, 7), (448, 40)])
+def test_layer_bad_tokens_stay_alone(q, f, M):
+    """A token of infinities and one of NaN leave the others' outputs as they were, bit for bit (f ends inside a step,
+    so an instance's padding lies beside the next one's row)."""
+    moe = make(q, 6, 256, f, 8, 2, db=4, dg=64)
+    x = _rnd(91, M, 256).to(F16).cuda()
+    ws = q.moe_layer_workspace(moe, M)
+    ws.fill_(255)
+    y = q.moe_layer(moe, x, ws=ws)
+    _check_layer(q, moe, x, y)
+    x[1], x[4, 3] = 60000.0, float("nan")
+    z = q.moe_layer(moe, x, ws=ws)
+    rest = torch.tensor([m for m in range(M) if m not in (1, 4)])
+    assert torch.equal(y.cpu()[rest], z.cpu()[rest])
+    assert bool((z[4] == 0).all())                         # a token of NaN logits chooses nothing
