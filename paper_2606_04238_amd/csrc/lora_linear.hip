@@ -30,15 +30,16 @@ __device__ __forceinline__ f32x4_t mfma16_bf(const uint4& a, const uint4& b, f32
 __device__ __forceinline__ float wave_sum(float v) { return group_sum<64>(v); }
 
 // s[r] += x[k .. k + 7] . (row r of A)[k .. k + 7], eight rows a.k apart.
-__device__ __forceinline__ void rank8_dot(float (&s)[8], const LoraArgs& a, const uint16_t* xr, const uint16_t* ar, int k) {
+template <int NR>
+__device__ __forceinline__ void ranks_dot(float (&s)[NR], const LoraArgs& a, const uint16_t* xr, const uint16_t* ar, int k) {
     const uint4 xv = *reinterpret_cast<const uint4*>(xr + k);
-    uint4 av[8];
+    uint4 av[NR];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) av[r] = *reinterpret_cast<const uint4*>(ar + (long)r * a.k + k);
+    for (int r = 0; r < NR; ++r) av[r] = *reinterpret_cast<const uint4*>(ar + (long)r * a.k + k);
     float x[8];
     act8(xv, a.bf, x);
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < NR; ++r) {
         float v[8];
         act8(av[r], a.bf, v);
 #pragma unroll
@@ -258,14 +259,17 @@ __global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs a, int shares) 
             a.y[(long)(m0 + r) * a.ldy + c] = act_bits(s[r], a.bf);
 }
 
-// blockIdx.x: token, blockIdx.y: eight ranks of t, or (the last one) the row's
-// conversion to operands, past 16 rows of bfloat16 to binary16.  t: the waves split k, a lane takes eight
-// elements of x and of eight rows of A at a time, fp32 throughout.  It is one
-// trip to memory of 9 KB a wave; the launch's time is its latency.
+// blockIdx.x: token, blockIdx.y: NR ranks of t, or (the last one) the row's conversion
+// to operands, past 16 rows of bfloat16 to binary16.  t: the waves split k, a lane
+// takes eight elements of x and of NR rows of A at a time, fp32 throughout.  Eight
+// ranks share a read of x; two where that leaves few workgroups, each of
+// which reads no more than one compute unit can (us: one row of 17408, rank 16 7.8
+// with two, 14.0 with eight; of 9728, rank 64 6.0 and 9.9).
+template <int NR>
 __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) {
     const int m = blockIdx.x, tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int ny = a.T > 0 ? a.R / 8 : 0;
+    const int ny = a.T > 0 ? a.R / NR : 0;
     if (m >= a.M) {
         if (blockIdx.y == 0)
             lora_find_mixed(a, tid);
@@ -280,7 +284,7 @@ __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) 
         return;
     }
     const uint16_t* xr = a.x + (long)m * a.ldx;
-    const int id = a.ids[m], r0 = blockIdx.y * 8;
+    const int id = a.ids[m], r0 = blockIdx.y * NR;
     if (a.t && blockIdx.y == 0 && tid < 16) {
         if (tid == m)
             a.known[m] = id >= 0 && id < a.T ? id : -1;
@@ -288,22 +292,22 @@ __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) 
             a.known[tid] = -1;
     }
     if (id < 0 || id >= a.T) {
-        if (tid < 8)
+        if (tid < NR)
             put_t(a, m, r0 + tid, 0.0f);
         return;
     }
     const uint16_t* ar = a.A + ((long)id * a.R + r0) * a.k;
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int k = tid * 8; k < a.k; k += kPrepWaves * 64 * 8) rank8_dot(s, a, xr, ar, k);
-    __shared__ float red[kPrepWaves][8];
+    float s[NR] = {};
+    for (int k = tid * 8; k < a.k; k += kPrepWaves * 64 * 8) ranks_dot<NR>(s, a, xr, ar, k);
+    __shared__ float red[kPrepWaves][NR];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
+    for (int r = 0; r < NR; ++r) {
         const float v = wave_sum(s[r]);
         if (lane == 0)
             red[wave][r] = v;
     }
     __syncthreads();
-    if (tid < 8) {
+    if (tid < NR) {
         float v = 0.0f;
 #pragma unroll
         for (int w = 0; w < kPrepWaves; ++w) v += red[w][tid];
@@ -319,7 +323,7 @@ __device__ __forceinline__ void lora_row(const LoraArgs& a, int m, int id, float
     if (id >= 0) {
         const uint16_t* xr = a.x + (long)m * a.ldx;
         const uint16_t* ar = a.A + ((long)id * a.R + r0) * a.k;
-        for (int k = ((wave % per) * 64 + lane) * 8; k < a.k; k += per * 64 * 8) rank8_dot(s, a, xr, ar, k);
+        for (int k = ((wave % per) * 64 + lane) * 8; k < a.k; k += per * 64 * 8) ranks_dot<8>(s, a, xr, ar, k);
     }
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
@@ -569,7 +573,8 @@ __global__ void __launch_bounds__(512) lora_few_kernel(LoraArgs a, int ns, int k
 }  // namespace
 
 hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st) {
-    const unsigned ny = (a.T > 0 ? a.R / 8 : 0) + (a.bf || a.xo ? 1 : 0);
+    const int nr = (long)a.M * a.R / 8 < 128 ? 2 : 8;
+    const unsigned ny = (a.T > 0 ? a.R / nr : 0) + (a.bf || a.xo ? 1 : 0);
     if (ny == 0)
         return hipSuccess;
     if (a.M > kLoraPrepRows) {
@@ -580,7 +585,7 @@ hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st) {
         return hipGetLastError();
     }
     const bool find = a.T > 0 && a.tb && !a.parts;                     // one more column of workgroups looks for the mixed sets
-    lora_prep_kernel<<<dim3((unsigned)a.M + (find ? 1u : 0u), ny), kPrepWaves * 64, 0, st>>>(a);
+    (nr == 2 ? lora_prep_kernel<2> : lora_prep_kernel<8>)<<<dim3((unsigned)a.M + (find ? 1u : 0u), ny), kPrepWaves * 64, 0, st>>>(a);
     return hipGetLastError();
 }
 
