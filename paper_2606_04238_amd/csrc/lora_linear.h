@@ -20,7 +20,7 @@ struct LoraArgs {
     // workspace
     int* known;                          // up to 16 rows: [16] adapter of a row, -1: none
     float* t;                            // up to 16 rows: [M][R] scale[a] A_a x, fp32; zeros where there is no adapter
-    uint16_t* xo;                        // up to 16 rows: x in operand order (oneshot.h), or null
+    uint16_t* xo;                        // up to 16 rows: x in operand order, rows side by side (oneshot.h), or null
     float* xs;                           // and its group sums
     uint16_t* x16;                       // more: bfloat16 rows as binary16 x 2^e (rows k apart), or null
     float* xf;                           // [M] 2^-e (bfloat16)

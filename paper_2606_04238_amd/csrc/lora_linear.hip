@@ -277,8 +277,8 @@ __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) 
     }
     if ((int)blockIdx.y >= ny) {
         if (a.xo)
-            operands_of_row<kPrepWaves>(a.x + (long)m * a.ldx, a.k, a.bf, a.bits, a.g, a.xo + (long)m * operand_row(a.k, a.bits),
-                                        a.xs + (long)m * operand_sums(a.k, a.bits, a.g), a.xf + m, tid);
+            operands_of_row<kPrepWaves>(a.x + (long)m * a.ldx, a.k, a.bf, a.bits, a.g, reinterpret_cast<uint4*>(a.xo) + m,
+                                        reinterpret_cast<float2*>(a.xs) + m, a.M, a.xf + m, tid);
         else if (wave == 0)
             convert_row(a, m, lane);
         return;
@@ -524,11 +524,10 @@ __global__ void __launch_bounds__(512) lora_few_kernel(LoraArgs a, int ns, int k
     o.magic = magic_vgpr();
     o.rc[0] = rsrc(a.codes, (uint32_t)a.n * (uint32_t)rb);
     o.rm[0] = rsrc(a.meta, (uint32_t)a.n * (uint32_t)ng * 4u);
-    const uint32_t row = j < a.M ? j : 0, xb = operand_row(a.k, B) * 2u, sb = operand_sums(a.k, B, G) * 4u;
-    o.rx = rsrc(a.xo, (uint32_t)a.M * xb);
-    o.rs = rsrc(a.xs, (uint32_t)a.M * sb);
-    o.xv = row * xb + lane_x<B, G>(lane >> 4);
-    o.sv = row * sb + lane_sums<B, G>(lane >> 4);
+    o.rows = (uint32_t)a.M;
+    o.rx = rsrc(a.xo, (uint32_t)a.M * operand_row(a.k, B) * 2u);
+    o.rs = rsrc(a.xs, (uint32_t)a.M * operand_sums(a.k, B, G) * 4u);
+    place<B, G>(o, 16u * j, 8u * j, j < a.M, lane >> 4);
     o.K = a.k;
     o.N = a.n;
     o.row0 = blockIdx.x * 16 * RT;

@@ -24,7 +24,7 @@ hipError_t launch_route_logits(const RouteArgs& a, hipStream_t st);
 
 // A block of work of the experts' launches: up to 16 instances (a token and one
 // of its slots) of one expert.
-constexpr int kBlkInts = 64, kBlkInst = 16, kBlkTok = 32;    // ints: [0] expert, [1] instances, [16..] their numbers, [32..] their tokens
+constexpr int kBlkInts = 64, kBlkInst = 16, kBlkTok = 32;    // ints: [0] expert, [1] instances, [2] its first row of h, [16..] their numbers, [32..] their tokens
 
 struct MoeArgs {
     const uint32_t *cg, *mg, *cu, *mu, *cd, *md;             // [E] matrices each, one after another
@@ -36,7 +36,7 @@ struct MoeArgs {
     const double* logits;    // [M][E]
     int* blocks;             // moe_blocks_most() blocks, those past the last with no instances
     float* t;                // [M k][2 r]
-    uint16_t* h;             // [M k][operand_row(f)] in operand order (oneshot.h)
+    uint16_t* h;             // M k rows in operand order, those of a block side by side (oneshot.h), in the blocks' order
     uint16_t* xo;            // x in operand order
     float* xs;               // and its group sums
     float* part;             // [M k][d]

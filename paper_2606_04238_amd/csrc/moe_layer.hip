@@ -42,10 +42,11 @@ __device__ __forceinline__ void moe_group(const MoeArgs& a, int tid) {
         }
     }
     __syncthreads();
-    int c = 0, nb = 0, at = 0;
-    if (tid < kMoeExperts) {                               // blocks of expert tid, and of the experts before it
+    int c = 0, nb = 0, at = 0;                             // of expert tid: instances, blocks; both of those up to it
+    if (tid < kMoeExperts) {
         c = __popc(list[tid][0]) + __popc(list[tid][1]);
-        at = nb = (c + 15) >> 4;
+        nb = (c + 15) >> 4;
+        at = c << 16 | nb;
 #pragma unroll
         for (int o = 1; o < 64; o *= 2) {
             const int v = __shfl_up(at, o, 64);
@@ -63,14 +64,16 @@ __device__ __forceinline__ void moe_group(const MoeArgs& a, int tid) {
         all += sums[w];
     }
     if (tid < kMoeExperts) {
-        at -= nb;
-        start[tid] = (int16_t)at;
+        const int first = (at & 0xFFFF) - nb, place = (at >> 16) - c;
+        start[tid] = (int16_t)first;
         for (int s = 0; s < nb; ++s) {
-            a.blocks[(at + s) * kBlkInts] = tid;
-            a.blocks[(at + s) * kBlkInts + 1] = min(16, c - 16 * s);
+            int* b = a.blocks + (first + s) * kBlkInts;
+            b[0] = tid;
+            b[1] = min(16, c - 16 * s);
+            b[2] = place + 16 * s;
         }
     }
-    for (int b = all + tid; b < moe_blocks_most(n, a.E); b += kChooseWaves * 64) a.blocks[b * kBlkInts + 1] = 0;
+    for (int b = (all & 0xFFFF) + tid; b < moe_blocks_most(n, a.E); b += kChooseWaves * 64) a.blocks[b * kBlkInts + 1] = 0;
     __syncthreads();
     if (tid < n && ids[tid] >= 0) {
         const int e = ids[tid], m = tid / a.k;
@@ -83,28 +86,30 @@ __device__ __forceinline__ void moe_group(const MoeArgs& a, int tid) {
 }
 
 // Workgroup 0 chooses and groups; the others bring a row of x into operand order
-// each, and clear what pads the rows of h to whole steps.
+// each.  (Side by side with the others' a token's row would bring their lines along:
+// a block's tokens are any of them, and few.  Gate and up of 21 experts of 2880,
+// eight tokens 37.4 us and 41.4, 64 68.6 and 77.5.)
 __global__ void __launch_bounds__(kChooseWaves * 64) moe_choose_kernel(MoeArgs a) {
     const int tid = threadIdx.x;
     if (blockIdx.x == 0) {
         moe_group(a, tid);
         return;
     }
-    const int m = blockIdx.x - 1, row = operand_row(a.f, a.db), pad = row - a.f;
-    for (int i = tid; i < a.k * pad; i += kChooseWaves * 64) a.h[(long)(m * a.k + i / pad) * row + a.f + i % pad] = 0;
-    operands_of_row<kChooseWaves>(a.x + (long)m * a.d, a.d, false, a.gb, a.gg, a.xo + (long)m * operand_row(a.d, a.gb),
-                                  a.xs + (long)m * operand_sums(a.d, a.gb, a.gg), nullptr, tid);
+    const int m = blockIdx.x - 1;
+    operands_of_row<kChooseWaves>(a.x + (long)m * a.d, a.d, false, a.gb, a.gg,
+                                  reinterpret_cast<uint4*>(a.xo) + (long)m * (operand_row(a.d, a.gb) / 8),
+                                  reinterpret_cast<float2*>(a.xs) + (long)m * (operand_sums(a.d, a.gb, a.gg) / 2), 1, nullptr, tid);
 }
 
 // A block of the table in registers: expert and instances are uniform (scalar
 // loads), the lane's own instance and token come with one vector load each.
 struct Block {
-    int e, n, inst, tok;
+    int e, n, at, inst, tok;
 };
 __device__ __forceinline__ Block block_of(const MoeArgs& a, int b, int lane) {
     const int* p = a.blocks + kBlkInts * b;
     const int n = p[1], l = (lane & 15) < n ? lane & 15 : 0;
-    return {p[0], n, p[kBlkInst + l], p[kBlkTok + l]};
+    return {p[0], n, p[2], p[kBlkInst + l], p[kBlkTok + l]};
 }
 
 // t of one block of instances: 16 rows of the expert's [A_g; A_u], whose 2 r rows
@@ -173,10 +178,10 @@ __global__ void __launch_bounds__(512) moe_gateup_kernel(MoeArgs a, int ns, int 
     o.rm[1] = rsrc(mu + bl.e * mb, (uint32_t)mb);
     const bool live = j < bl.n;
     const uint32_t xb = operand_row(a.d, B) * 2u, sb = operand_sums(a.d, B, G) * 4u;
+    o.rows = 1;
     o.rx = rsrc(a.xo, (uint32_t)a.M * xb);
     o.rs = rsrc(a.xs, (uint32_t)a.M * sb);
-    o.xv = (uint32_t)bl.tok * xb + lane_x<B, G>(q);
-    o.sv = (uint32_t)bl.tok * sb + lane_sums<B, G>(q);
+    place<B, G>(o, (uint32_t)bl.tok * xb, (uint32_t)bl.tok * sb, live, q);
     o.K = a.d;
     o.N = a.f;
     o.row0 = blockIdx.x * 16 * RT;
@@ -226,19 +231,22 @@ __global__ void __launch_bounds__(512) moe_gateup_kernel(MoeArgs a, int ns, int 
 #pragma unroll
         for (int t = 0; t < RT; ++t) red[((wave * 2 + m) * RT + t) * 64 + lane] = acc[m][t];
     __syncthreads();
+    const int hrow = operand_row(a.f, a.db);
+    uint16_t* h = a.h + (long)bl.at * hrow;                // the block's rows, side by side
+    if (blockIdx.x == 0)                                   // and what pads them to whole steps
+        for (int i = threadIdx.x; i < (hrow - a.f) * bl.n; i += kw * 64) h[a.f * bl.n + i] = 0;
     for (int t = wave; t < RT; t += kw) {
         f32x4_t g = red[t * 64 + lane], u = red[(RT + t) * 64 + lane];
         for (int w = 1; w < kw; ++w) {
             g += red[(w * 2 * RT + t) * 64 + lane];
             u += red[((w * 2 + 1) * RT + t) * 64 + lane];
         }
-        const int n = o.row0 + 16 * t + j, at = operand_at(n, a.db, a.dg), hrow = operand_row(a.f, a.db);
+        const int n = o.row0 + 16 * t + j, at = operand_at(n, a.db, a.dg);
         const float scale = operand_scale(n, a.db, a.dg);
 #pragma unroll
         for (int v = 0; v < 4; ++v) {
-            const int i = __shfl(bl.inst, 4 * q + v, 64);
             if (4 * q + v < bl.n && n < a.f)               // h rounded to binary16, then its operand's power of two
-                a.h[(long)i * hrow + at] = (uint16_t)f2h(h2f(f2h(g[v] / (1.0f + __expf(-g[v])) * u[v])) * scale);
+                h[((at >> 3) * bl.n + 4 * q + v) * 8 + (at & 7)] = (uint16_t)f2h(h2f(f2h(g[v] / (1.0f + __expf(-g[v])) * u[v])) * scale);
         }
     }
 }
@@ -259,9 +267,10 @@ __global__ void __launch_bounds__(512) moe_down_kernel(MoeArgs a, int ns, int kw
     o.magic = magic_vgpr();
     o.rc[0] = rsrc(reinterpret_cast<const char*>(a.cd) + bl.e * wb, (uint32_t)wb);
     o.rm[0] = rsrc(reinterpret_cast<const char*>(a.md) + bl.e * mb, (uint32_t)mb);
-    const uint32_t hb = operand_row(a.f, B) * 2u;
-    o.rx = rsrc(a.h, (uint32_t)(a.M * a.k) * hb);
-    o.xv = (uint32_t)bl.inst * hb + lane_x<B, G>(q);
+    const int hrow = operand_row(a.f, B);
+    o.rows = (uint32_t)bl.n;
+    o.rx = rsrc(a.h + (long)bl.at * hrow, o.rows * (uint32_t)hrow * 2u);
+    place<B, G>(o, 16u * j, 0u, j < bl.n, q);
     o.K = a.f;
     o.N = a.d;
     o.row0 = blockIdx.x * 16 * RT;

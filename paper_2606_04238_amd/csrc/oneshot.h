@@ -5,15 +5,24 @@
 //
 // Split.  A workgroup owns RT tiles of 16 weight rows (of one matrix, or of gate
 // and up); its waves split K, wave w takes the steps w, w + KW, .. of 64 bytes per
-// row.  A wave issues the loads of its activations and its weights at once,
-// multiplies and leaves its sums in LDS, where they meet behind one barrier.
+// row.  A wave has the next step's weights and the next operands under way while
+// it multiplies, and leaves its sums in LDS, where they meet behind one barrier.
 // There is no loop over tiles: the launch has a workgroup for each, and the
 // hardware starts the next one where one ends.  Reading 92 MB in 8 KB pieces,
 // one per wave, took 15.3 us on this card against 17.3 to 21 with persistent
 // waves that prefetch, and 16 MB 4.1 against 5.2 to 9.6 (loads only, launch
 // included): a persistent wave ramps its stream up once and waits for its
-// slowest piece at the end.  What hides a workgroup's start and end is another
-// one beside it, so registers count: a step of 128 bytes holds twice the operands.
+// slowest piece at the end.
+//
+// Activations.  What bounded these kernels were the vector caches' tag lookups: with
+// a row after the other in memory an operand's 64 lanes read 64 places (a
+// bfloat16 7 x 5120 x 17408 product: 459 lookups a step, 62 400 a compute unit in
+// 70 000 cycles).  So the launch before lays the rows side by side: 16 bytes of
+// every row, then the next 16; an operand is four runs of up to 256 bytes.  (us, rows
+// one after the other and side by side: that product 30.0 and 25.6, 16 x 6144 x
+// 4096 13.9 and 10.9, 16 x 5120 x 17408 40.6 and 30.4, one row 8.7 and 8.7; down of 32
+// experts, 8 rows each, 47.8 and 44.4.)  Copying codes and (scale | zero) words to
+// LDS in whole lines first did not pay: 42 against 41 for gate and up.
 #pragma once
 
 #include "oneshot_plan.h"
@@ -25,10 +34,9 @@ namespace {
 // A step is 64 bytes of each of a tile's 16 rows.  Lane l = 16 q + j loads unit
 // perm(q) (16 bytes) of row j, and E4 and E5 (mfma_tile.h) bring quarter q its words
 // of every group, as in the first half of a tile kernel's step.  Activations come in
-// the operands' order (operand16 below): an operand is one 16-byte load, in which
-// only lanes that have a row take part.  Their group sums come with them
-// (SUMS = false) or are formed here.  Rows that no lane supplies are left as the
-// registers are: a matrix product keeps rows apart, and theirs are dropped.
+// the operands' order (operand16 below): an operand is one 16-byte load, and lanes
+// without a row read past the end, zeros.  Their group sums come with them
+// (SUMS = false) or are formed here.
 template <int B, int G>
 struct OneLay {
     typedef Lay<B, G> Y;
@@ -45,26 +53,20 @@ struct OneStep {
     uint32_t m[NM * RT][OneLay<B, G>::NW];
 };
 // What a wave multiplies: rows row0 .. of NM matrices [N][K] with the rows of the
-// activations (lane j: at rows x and sums, where it is `live`).  K % 64 == 0;
-// weight rows past N give zeros.
+// activations (a lane's row: place() of it).  K % 64 == 0; weight rows past N give
+// zeros.
 template <int NM>
 struct OneWork {
     Rsrc rc[NM], rm[NM];
     Rsrc rx, rs;                                           // operands, group sums
-    uint32_t xv, sv;                                       // this lane's place in them at step 0
+    uint32_t xv, sv;                                       // this lane's place in them at step 0, or kPastEnd
+    uint32_t rows;                                         // rows side by side there
     int K, N, row0;
     uint32_t magic;                                        // magic_vgpr(), taken at the kernel's start
 };
 // (That constant is made at the start, and kept: an instruction written by hand
 // gets no distance from matrix instructions, and one among them that shared a
 // register with an unused part of a running one's result was overwritten by it.)
-
-// A register that holds anything.
-__device__ __forceinline__ uint32_t anything() {
-    uint32_t v;
-    __asm__ volatile("" : "=v"(v));
-    return v;
-}
 
 // Operands of a wave's steps in the order they are used, kOneAhead of them in
 // registers: the weights take their time, and the activations, which many
@@ -73,23 +75,23 @@ constexpr int kOneAhead = 4;
 struct OneRing {
     uint4 a[kOneAhead];
 };
-// A lane's place in a row of operands and of group sums, in bytes.
-template <int B, int G>
-__device__ __forceinline__ uint32_t lane_x(int q) {
+// A lane's place in the operands and the group sums of a row that begins there at
+// bytes x and sums.
+template <int B, int G, int NM>
+__device__ __forceinline__ void place(OneWork<NM>& o, uint32_t x, uint32_t sums, bool live, int q) {
     typedef Lay<B, G> Y;
-    return Y::HALF ? (uint32_t)(64 / B * (q >> 1) + 16 * (q & 1)) : (uint32_t)(64 / B * quarter_word<Y::QW>(q));
-}
-template <int B, int G>
-__device__ __forceinline__ uint32_t lane_sums(int q) {
     typedef OneLay<B, G> L;
-    return 4u * (L::GS == 1 ? q & 1 : L::GS == 2 ? 2 * (q & 1) + (q >> 1) : 2 * q * L::NC);
+    const uint32_t chunk = Y::HALF ? 4 / B * (q >> 1) + (q & 1) : 4 / B * quarter_word<Y::QW>(q);
+    const uint32_t group = L::GS == 1 ? 0 : L::GS == 2 ? q & 1 : q * L::NC, part = L::GS == 1 ? q & 1 : L::GS == 2 ? q >> 1 : 0;
+    o.xv = live ? x + chunk * o.rows * 16u : kPastEnd;
+    o.sv = live ? sums + group * o.rows * 8u + 4u * part : kPastEnd;
 }
 template <int B, int G, int NM, bool SUMS>
 __device__ __forceinline__ void one_operand(uint4& a, const OneWork<NM>& o, int gs, int i, int lane) {
     typedef Lay<B, G> Y;
     constexpr int CW = 32 / B, PER = Y::HALF || B == 4 ? 1 : 2;           // codes and operands per word
     const int w = i / PER, at = Y::HALF ? 2 * w : (w / Y::QW) * Y::WPG + w % Y::QW;
-    a = bload16<0>(o.rx, o.xv, (uint32_t)(CW * 2 * (gs * 16 + at) + 16 * (i % PER)));
+    a = bload16<0>(o.rx, o.xv, (uint32_t)(CW / 8 * (gs * 16 + at) + i % PER) * o.rows * 16u);
 }
 
 template <int B, int G, int NM, int RT, bool SUMS>
@@ -98,13 +100,13 @@ __device__ __forceinline__ void one_load(OneStep<B, G, NM, RT>& s, const OneWork
     typedef OneLay<B, G> L;
     const int rb = o.K * B / 8, ng = o.K / G, q = lane >> 4, j = lane & 15;
     if constexpr (!SUMS) {
-        const uint32_t at = (uint32_t)(gs * L::GS * 8);
+        const uint32_t at = (uint32_t)(gs * L::GS) * o.rows * 8u;
         if constexpr (L::GS <= 2) {
             s.kc[0] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(o.rs, o.sv, at, 0));
         } else {
 #pragma unroll
             for (int i = 0; i < L::NC; ++i) {
-                const uint2 v = bload8(o.rs, o.sv, at + 8u * i);
+                const uint2 v = bload8(o.rs, o.sv, at + 8u * o.rows * i);
                 s.kc[i] = __uint_as_float(v.x);
                 s.kx[i] = __uint_as_float(v.y);
             }
@@ -405,12 +407,12 @@ __device__ __forceinline__ uint16_t act_bits(float v, bool bf) {
 }
 
 // A row of K binary16 or (bf) bfloat16 elements in operand order, padded with zeros,
-// and its group sums, by a workgroup of W waves; bfloat16 times 2^e, 2^-e to *back.
-// 16 elements per lane; the first N pieces of a wave stay in its registers between
+// and its group sums, by a workgroup of W waves, at o and sums among `rows` rows
+// side by side; bfloat16 times 2^e, 2^-e to *back.  16 elements per lane; the first N pieces of a wave stay in its registers between
 // the two passes that bfloat16 takes.
 template <int W>
-__device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool bf, int bits, int g, uint16_t* o, float* sums,
-                                                float* back, int tid) {
+__device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool bf, int bits, int g, uint4* o, float2* sums,
+                                                int rows, float* back, int tid) {
     constexpr int N = 3;
     __shared__ float best[W];
     const int lane = tid & 63, wave = tid >> 6, len = operand_row(K, bits);
@@ -468,10 +470,10 @@ __device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool b
             for (int u = 0; u < 16; ++u) f[u] = h2f(f2h(f[u] * up));
         operand16(f, bits, g, w, c, xs);
         if (e < len) {
-            reinterpret_cast<uint4*>(o + e)[0] = w[0];
-            reinterpret_cast<uint4*>(o + e)[1] = w[1];
+            o[(long)(e / 8) * rows] = w[0];
+            o[(long)(e / 8 + 1) * rows] = w[1];
             if (e % g == 0)
-                *reinterpret_cast<float2*>(sums + e / g * 2) = make_float2(c, xs);
+                sums[(long)(e / g) * rows] = make_float2(c, xs);
         }
     };
 #pragma unroll
