@@ -396,8 +396,10 @@ typedef struct {
  * a result nor written.  t = A x is formed in one launch (with bfloat16 rows
  * rewritten as binary16 times a power of two per row, which keeps every element
  * down to 2^-28 of its row's largest exactly; a row that holds an infinity or
- * NaN gives infinities or NaNs), the linear in a second: up to 16 rows on the
- * weight stream (oneshot.h), more as a dense product.
+ * NaN gives infinities or NaNs), the linear in a second: up to 16 rows with
+ * weights as exact codes, more as a dense product of weights rounded once to
+ * binary16, whose shares of k and adapters a third launch adds up where tiles
+ * are few, or whose rows of many adapters one between the two prepares.
  * ws/ws_bytes: at least qmlp_linear_lora_workspace_bytes(...), any contents,
  * nothing is kept between calls; one call at a time per workspace.
  * M == 0 enqueues nothing.  Nothing is written outside y's M rows and ws.
@@ -472,8 +474,11 @@ int qmlp_moe_lanes(int d, int f, int gu_bits, int dn_bits, int M, int k, int cus
  *   SOFTMAX       softmax over all E logits, taken at the chosen (not
  *                 normalised again);
  *   SIGMOID       sigmoid(l) over the sum of the k chosen sigmoids.
- * Logits are summed in fp64 (products of two 16-bit floats are exact there), so
- * the choice does not depend on how the work was split.  An expert whose logit
+ * The choice is that of logits summed in fp64 (products of two 16-bit floats are
+ * exact there), so it does not depend on how the work was split.  For many
+ * tokens only the logits that could change places are formed so; the others, and
+ * with them the weights, carry the rounding of fp32 sums of 32 products each, at
+ * most 2^-18 |x| |w| of a logit and ordinarily 2^-23 of it.  An expert whose logit
  * is NaN or -inf (a bias of -inf masks it) is never chosen; +inf counts as the
  * largest fp32.  Where fewer than k experts are left, the remaining slots hold
  * expert -1 and weight 0.  topk_idx int32 [M][k] and topk_w fp32 [M][k] are what
