@@ -182,3 +182,16 @@ def test_codes_past_32_bits(q, M):
         part = q.QWeight(bits, 16, k, g, codes[lo * k // 8:(lo + 16) * k // 8], meta[:16 * (k // g)])
         ref, bound = lora_ref(part, x, A, B[:, lo:lo + 16], sc, ids)
         check(y[:, lo:lo + 16], ref, bound, F16)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("bits,g,n,k,M,R,T", [(4, 64, 7700, 192, 1100, 16, 40), (2, 32, 4001, 128, 2100, 64, 3),
+                                              (4, 128, 7688, 384, 1150, 32, 400)])
+def test_many_tiles(q, bits, g, n, k, M, R, T, dtype):
+    """Enough tiles of 128 x 128 for three rounds: the larger ones, whose rows have one adapter, few and many."""
+    w, x, A, B, sc, ids = make(q, bits, g, n, k, M, R, T, dtype)
+    ids[100:900] = 1
+    ids[900:932] = (torch.arange(32) % 3).to(torch.int32).cuda()
+    y = q.linear_lora(w, q.Adapters(A, B, sc), ids, x)
+    ref, bound = lora_ref(w, x, A, B, sc, ids)
+    check(y, ref, bound, dtype)
