@@ -68,13 +68,15 @@ struct OneWork {
 // gets no distance from matrix instructions, and one among them that shared a
 // register with an unused part of a running one's result was overwritten by it.)
 
-// Operands of a wave's steps in the order they are used, kOneAhead of them in
-// registers: the weights take their time, and the activations, which many
-// workgroups share, come from the caches while earlier operands are multiplied.
-constexpr int kOneAhead = 4;
-struct OneRing {
-    uint4 a[kOneAhead];
-};
+// The operands of a step are loaded while the step before is multiplied, each into
+// the register of the one it follows: loads come back in order, and one behind the
+// next step's weights would wait for them (2 bits, four of eight operands so: gate
+// and up of one token 10.3 us instead of 9.7; groups of 32 keep four, whose scales
+// take the registers).
+template <int B, int G>
+constexpr int one_ahead() {
+    return Lay<B, G>::HALF ? 4 : OneLay<B, G>::NA;
+}
 // A lane's place in the operands and the group sums of a row that begins there at
 // bytes x and sums.
 template <int B, int G, int NM>
@@ -303,21 +305,22 @@ __device__ __forceinline__ void oneshot_products(f32x4_t (&acc)[NM][RT], const O
 #pragma unroll
         for (int t = 0; t < RT; ++t) acc[m][t] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     constexpr int NA = OneLay<B, G>::NA;
-    static_assert(NA % kOneAhead == 0 || kOneAhead % NA == 0, "a ring slot is known at compile time");
+    constexpr int AH = one_ahead<B, G>();
+    static_assert(NA % AH == 0, "a ring slot is known at compile time");
     OneStep<B, G, NM, RT> s;
-    OneRing r;
+    uint4 r[AH];
     int gs = first;                                        // < ns
     one_load<B, G, NM, RT, SUMS>(s, o, gs, lane);
     more();
 #pragma unroll
-    for (int n = 0; n < kOneAhead && n < NA; ++n) one_operand<B, G, NM, SUMS>(r.a[n], o, gs, n, lane);
+    for (int n = 0; n < AH; ++n) one_operand<B, G, NM, SUMS>(r[n], o, gs, n, lane);
     __builtin_amdgcn_sched_barrier(0);                     // every load above is issued before the first is waited for
     auto multiply = [&](bool last) {
         one_multiply<B, G, NM, RT, SUMS>(acc, s, o, gs, lane, [&](int n) {
-            const int f = n + kOneAhead;
-            const uint4 a = r.a[n % kOneAhead];
+            const int f = n + AH;
+            const uint4 a = r[n % AH];
             if (!last || f < NA)
-                one_operand<B, G, NM, SUMS>(r.a[n % kOneAhead], o, f < NA ? gs : gs + kw, f % NA, lane);
+                one_operand<B, G, NM, SUMS>(r[n % AH], o, f < NA ? gs : gs + kw, f % NA, lane);
             return a;
         });
     };

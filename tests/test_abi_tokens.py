@@ -160,3 +160,20 @@ def test_moe_layer_refusals(q, lib):
     assert lib.qmlp_moe_layer_workspace_bytes(ctypes.byref(_moe(q)), 65, 0) == 0
     sizes = [lib.qmlp_moe_layer_workspace_bytes(ctypes.byref(_moe(q)), M, 0) for M in range(65)]
     assert sizes == sorted(sizes)
+
+
+def test_binding_refuses_host_tensors():
+    """The kernels run on a device: tensors of the host are an error of the call, not a fault of a kernel."""
+    import torch
+    import paper_2606_04238_amd as qm
+    x, r = torch.zeros(2, 64, dtype=torch.float16), torch.zeros(4, 64, dtype=torch.float16)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    with pytest.raises(ValueError):
+        qm.moe_route(x, r, 2, ws=ws)
+    with pytest.raises(ValueError):
+        qm.Adapters(torch.zeros(1, 8, 64, dtype=torch.float16), torch.zeros(1, 32, 8, dtype=torch.float16))
+    w = qm.QWeight(4, 32, 64, 64, torch.zeros(32 * 8, dtype=torch.int32), torch.zeros(32, dtype=torch.int32))
+    with pytest.raises(ValueError):
+        qm.linear_lora(w, None, None, x, ws=ws)
+    with pytest.raises(ValueError):
+        qm.MoE(r, w, w, w, 2)

@@ -195,3 +195,23 @@ def test_many_tiles(q, bits, g, n, k, M, R, T, dtype):
     y = q.linear_lora(w, q.Adapters(A, B, sc), ids, x)
     ref, bound = lora_ref(w, x, A, B, sc, ids)
     check(y, ref, bound, dtype)
+
+
+@pytest.mark.parametrize("M", [7, 40, 100, 700])
+def test_graph_of_every_path(q, M):
+    """A captured call replayed over new rows and ids gives what an eager one gives, in any workspace."""
+    w, x, A, B, sc, ids = make(q, 4, 64, 640, 1152, M, 16, 6, BF16)
+    ad = q.Adapters(A, B, sc)
+    ws = q.linear_lora_workspace(w, ad, M, BF16)
+    y = torch.empty(M, 640, dtype=BF16, device="cuda")
+    q.linear_lora(w, ad, ids, x, y, ws)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        q.linear_lora(w, ad, ids, x, y, ws)
+    for i in range(3):
+        x.copy_(torch.randn(M, 1152, generator=torch.Generator().manual_seed(80 + i)).to(BF16))
+        ids.copy_((torch.arange(M) * (i + 1) % 8 - 1).to(torch.int32))
+        ws.fill_(255)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, q.linear_lora(w, ad, ids, x))

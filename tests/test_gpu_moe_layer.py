@@ -269,3 +269,29 @@ def test_layer_bad_tokens_stay_alone(q, f, M):
     rest = torch.tensor([m for m in range(M) if m not in (1, 4)])
     assert torch.equal(y.cpu()[rest], z.cpu()[rest])
     assert bool((z[4] == 0).all())                         # a token of NaN logits chooses nothing
+
+
+@pytest.mark.parametrize("M", [5, 300])
+def test_route_streams_and_graph(q, M):
+    """Any workspace contents, another stream, a captured call replayed over new inputs: what an eager call gives."""
+    x, r = _rnd(92, M, 384).to(BF16).cuda(), _rnd(93, 70, 384, std=0.1).to(BF16).cuda()
+    eager = q.moe_route(x, r, 4)
+    ws = q.moe_route_workspace(r, M)
+    ws.fill_(255)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        other = q.moe_route(x, r, 4, ws=ws)
+    torch.cuda.current_stream().wait_stream(s)
+    assert torch.equal(other[0], eager[0]) and torch.equal(other[1], eager[1])
+    xin, idx, w = x.clone(), torch.empty_like(eager[0]), torch.empty_like(eager[1])
+    q.moe_route(xin, r, 4, None, "topk_softmax", idx, w, ws)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        q.moe_route(xin, r, 4, None, "topk_softmax", idx, w, ws)
+    for i in range(3):
+        xin.copy_(_rnd(94 + i, M, 384).to(BF16))
+        g.replay()
+        torch.cuda.synchronize()
+        want = q.moe_route(xin, r, 4)
+        assert torch.equal(idx, want[0]) and torch.equal(w, want[1])
