@@ -462,7 +462,7 @@ class Adapters:
 
 
 def _one_device(*tensors):
-    """The kernels run on the current stream of one device; a tensor elsewhere would fault there."""
+    """The current device, which the kernels run on; a tensor elsewhere would fault there."""
     here = None
     for t in tensors:
         if t is None:
@@ -471,6 +471,13 @@ def _one_device(*tensors):
             here = torch.cuda.current_device()
         if not t.is_cuda or t.get_device() != here:
             raise ValueError("every tensor must be on the current CUDA device")
+    return here
+
+
+def _addr(t):
+    """An address as ctypes takes it where the argument's type is declared (an object of its own costs 0.1 us)."""
+    return None if t is None else t.data_ptr()
+
 
 
 def linear_lora_workspace_bytes(w: QWeight, adapters: Adapters | None, M: int, dtype=torch.float16) -> int:
@@ -508,11 +515,10 @@ def linear_lora(w: QWeight, adapters: Adapters | None, ids: torch.Tensor | None,
         ad = ctypes.byref(adapters._c)
     if ws is None:
         ws = linear_lora_workspace(w, adapters, M, x.dtype, x.device)
-    _one_device(x, y, ids, ws, w.codes, adapters.A if adapters else None)
-    qc = w.c()
-    _check(_lib().qmlp_linear_lora(ctypes.byref(qc), ad, _ptr(ids) if ad else None, _ptr(x), x.stride(0) if M > 1 else k, M,
-                                   code, _ptr(y), y.stride(0) if M > 1 else w.n_out, _ptr(ws), ws.numel(), _stream()),
-           "linear_lora")
+    here = _one_device(x, y, ids, ws, w.codes, adapters.A if adapters else None)
+    _check(_lib().qmlp_linear_lora(ctypes.byref(w.c()), ad, _addr(ids) if ad else None, _addr(x), x.stride(0) if M > 1 else k,
+                                   M, code, _addr(y), y.stride(0) if M > 1 else w.n_out, _addr(ws), ws.numel(),
+                                   torch._C._cuda_getCurrentRawStream(here)), "linear_lora")
     return y
 
 
@@ -588,9 +594,10 @@ def moe_route(x: torch.Tensor, router: torch.Tensor, k: int, bias: torch.Tensor 
         raise ValueError("topk_idx int32 and topk_w float32, both [M][k]")
     if ws is None:
         ws = moe_route_workspace(router, M)
-    _one_device(x, router, bias, topk_idx, topk_w, ws)
-    _check(_lib().qmlp_moe_route(_ptr(router), _ptr(bias), _ptr(x), M, d, router.shape[0], k, SCORES[score], code,
-                                 _ptr(topk_idx), _ptr(topk_w), _ptr(ws), ws.numel(), _stream()), "moe_route")
+    here = _one_device(x, router, bias, topk_idx, topk_w, ws)
+    _check(_lib().qmlp_moe_route(_addr(router), _addr(bias), _addr(x), M, d, router.shape[0], k, SCORES[score], code,
+                                 _addr(topk_idx), _addr(topk_w), _addr(ws), ws.numel(),
+                                 torch._C._cuda_getCurrentRawStream(here)), "moe_route")
     return topk_idx, topk_w
 
 
@@ -653,9 +660,9 @@ def moe_layer(moe: MoE, x: torch.Tensor, y: torch.Tensor | None = None, ws: torc
         raise ValueError("y must be float16 [M][d], contiguous")
     if ws is None:
         ws = moe_layer_workspace(moe, M, x.device)
-    _one_device(x, y, ws, moe.router)
-    _check(_lib().qmlp_moe_layer(ctypes.byref(moe._c), _ptr(x), M, F16, _ptr(y), _ptr(ws), ws.numel(), _stream()),
-           "moe_layer")
+    here = _one_device(x, y, ws, moe.router)
+    _check(_lib().qmlp_moe_layer(ctypes.byref(moe._c), _addr(x), M, F16, _addr(y), _addr(ws), ws.numel(),
+                                 torch._C._cuda_getCurrentRawStream(here)), "moe_layer")
     return y
 
 
