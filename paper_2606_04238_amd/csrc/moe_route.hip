@@ -73,12 +73,14 @@ __global__ void __launch_bounds__(kRouteWaves * 64) route_few_kernel(RouteArgs a
 }
 
 // Many tokens: a workgroup owns 32 tokens and 32 experts, its waves split d in steps
-// of 32, kAhead of them loaded at once: lane 16 q + j takes 8 elements of row j from
+// of 32, kManyAhead of them loaded at once: lane 16 q + j takes 8 elements of row j from
 // 8 q on.  With the logits go the rows' norms, |x| and |w|, which bound what a logit
 // may be off: a sum of 32 products in fp32, however the instruction orders it, by
 // 32 roundings of 2^-23 of sum |x w|, and all of them together by 2^-18 |x| |w|.
-// (fp64 matrix instructions took 50.8 us for 2048 tokens of 4096 and 128 experts.)
-constexpr int kManyWaves = 8, kManyAhead = 4;
+// (2048 tokens of 4096 and 128 experts 21.0 us; fp64 matrix instructions took 50.8,
+// one to four steps ahead, 8 or 16 waves, and tiles of 64 x 64 with d in four shares
+// 20.9 to 22.2.)
+constexpr int kManyWaves = 8, kManyAhead = 2;
 template <bool BF>
 __device__ __forceinline__ float squares(const uint4& v, float s) {
     const uint32_t w[4] = {v.x, v.y, v.z, v.w};
