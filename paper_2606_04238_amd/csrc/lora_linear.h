@@ -32,7 +32,7 @@ struct LoraArgs {
 
 // Sets of 32 rows with more than kMixedFrom adapters between them (rows without one
 // count as one more) have their terms formed beforehand, up to kMixedSets of them.
-constexpr int kMixedSets = 16, kMixedFrom = 3;
+constexpr int kMixedSets = 128, kMixedFrom = 3;
 inline int lora_mixed_most(int M) { return (M + 31) / 32 < kMixedSets ? (M + 31) / 32 : kMixedSets; }
 
 constexpr int kLoraMidRows = 64;         // rows up to which lora_mid_kernel multiplies

@@ -209,23 +209,29 @@ struct Terms {
     }
 };
 
-// The terms of the rows of the mixed sets.  (In the product's launch itself these rows'
-// adapters, one after another, held their workgroups back: 4096 rows of which 48
-// decode, rank 64, 391 us instead of 344 with one adapter.)
+// The terms of the rows of the mixed sets, a workgroup's slots kMixedStride apart (most
+// calls have few).  (In the product's launch itself these rows' adapters, one after
+// another, held their workgroups back: 4096 rows of which 48 decode, rank 64, 391 us
+// instead of 344 with one adapter; 600 rows of 64 adapters, rank 64, three of 19
+// sets there, 1024 x 1024: 115 us, 16.3 without.)
+constexpr int kMixedStride = 16;
 template <int RC>
-__global__ void __launch_bounds__(256) lora_mixed_kernel(LoraArgs a) {
+__global__ void __launch_bounds__(256) lora_mixed_kernel(LoraArgs a, int most) {
     __shared__ float at[kTermRows][256];
-    const int tid = threadIdx.x, c = blockIdx.x * 256 + tid, set = a.slots[(a.M + 31) / 32 + (blockIdx.y >> 3)];
-    if (set < 0)
-        return;
-    const int r0 = kTermRows * (blockIdx.y & 7);
-    Terms<RC> x;
-    x.load(a, 32 * set + r0, blockIdx.x * 256, tid);
-    float s[kTermRows] = {};
-    x.add(s, at, a.bf, tid);
-    if (c < a.n)
+    const int tid = threadIdx.x, c = blockIdx.x * 256 + tid, r0 = kTermRows * (blockIdx.y & 7);
+    for (int slot = blockIdx.y >> 3; slot < most; slot += kMixedStride) {
+        const int set = a.slots[(a.M + 31) / 32 + slot];
+        if (set < 0)
+            return;
+        Terms<RC> x;
+        x.load(a, 32 * set + r0, blockIdx.x * 256, tid);
+        float s[kTermRows] = {};
+        x.add(s, at, a.bf, tid);
+        if (c < a.n)
 #pragma unroll
-        for (int u = 0; u < kTermRows; ++u) a.mixed[((long)(blockIdx.y >> 3) * 32 + r0 + u) * a.n + c] = s[u];
+            for (int u = 0; u < kTermRows; ++u) a.mixed[((long)slot * 32 + r0 + u) * a.n + c] = s[u];
+        __syncthreads();                                   // (at is free again)
+    }
 }
 
 // y = the sum of the shares of k, in their order, and the adapters' terms.
@@ -590,7 +596,8 @@ hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st) {
 
 hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st) {
     auto k = a.R == 8 ? lora_mixed_kernel<1> : a.R == 16 ? lora_mixed_kernel<2> : a.R == 32 ? lora_mixed_kernel<4> : lora_mixed_kernel<8>;
-    k<<<dim3((unsigned)(a.n + 255) / 256, 8u * (unsigned)lora_mixed_most(a.M)), 256, 0, st>>>(a);
+    const int most = lora_mixed_most(a.M);
+    k<<<dim3((unsigned)(a.n + 255) / 256, 8u * (unsigned)(most < kMixedStride ? most : kMixedStride)), 256, 0, st>>>(a, most);
     return hipGetLastError();
 }
 
