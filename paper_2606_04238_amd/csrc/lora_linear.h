@@ -44,7 +44,7 @@ constexpr int kLoraMidRows = 64;         // rows up to which lora_mid_kernel mul
 // 67 and 52, 512 84 and 71.)
 inline int lora_shares(int M, int n, int k) {
     const long tiles = (long)((M + 127) / 128) * ((n + 127) / 128);
-    if (M > 512 || tiles > 128)
+    if (M < 1 || M > 512 || tiles > 128)
         return 1;
     const int most = k / 64 / 8, fill = (int)(256 / tiles);
     return most < 1 ? 1 : fill < most ? fill : most;

@@ -177,3 +177,15 @@ def test_binding_refuses_host_tensors():
         qm.linear_lora(w, None, None, x, ws=ws)
     with pytest.raises(ValueError):
         qm.MoE(r, w, w, w, 2)
+
+
+@pytest.mark.parametrize("bits,n,k", [(4, 256, 512), (4, 1 << 18, 1 << 14), (2, 1 << 20, 1 << 15)])
+def test_no_rows_of_any_weights(q, lib, bits, n, k):
+    """No rows need no work and no division by the tiles of none, also past 2^31 bytes of codes."""
+    w, ad = _w(q, bits, n, k, 128), _ad(q)
+    for a in (None, ad):
+        size = lib.qmlp_linear_lora_workspace_bytes(ctypes.byref(w), None if a is None else ctypes.byref(a), 0, 1)
+        assert 0 <= size < 4096
+        assert _call(lib, w, a, ldx=k, ldy=n, M=0, dt=1) == 0
+    sizes = [lib.qmlp_linear_lora_workspace_bytes(ctypes.byref(w), ctypes.byref(ad), M, 1) for M in (1, 16, 17, 64, 65, 512)]
+    assert all(s > 0 for s in sizes)
