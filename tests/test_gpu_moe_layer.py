@@ -295,3 +295,14 @@ def test_route_streams_and_graph(q, M):
         torch.cuda.synchronize()
         want = q.moe_route(xin, r, 4)
         assert torch.equal(idx, want[0]) and torch.equal(w, want[1])
+
+
+@pytest.mark.parametrize("M", [7, MANY])
+def test_route_bad_router_rows(q, M):
+    """An expert whose row holds NaN is never chosen, one whose row holds an infinity where its logit is +inf; the
+    others keep their order."""
+    x, r = _rnd(97, M, 192).to(F16).cuda(), _rnd(98, 70, 192, std=0.1).to(F16).cuda()
+    r[5, 3], r[9, 0] = float("nan"), float("inf")
+    idx, w = q.moe_route(x, r, 6)
+    ref = route_ref(x, r, None, 6, "topk_softmax")
+    assert torch.equal(idx.cpu(), ref[0]) and not bool((idx == 5).any())
