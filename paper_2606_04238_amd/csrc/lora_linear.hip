@@ -518,7 +518,9 @@ __device__ __forceinline__ void rank8_add(f32x4_t (&acc)[1][RT], const Rank8<RT>
 }
 
 // Up to 16 rows of x: a workgroup owns RT tiles of 16 outputs (oneshot.h), the
-// waves share its adapters' terms by eight ranks.
+// waves share its adapters' terms by eight ranks.  Measured (us, 4 bits): one row of
+// 2560 x 4096 6.6, 16 of 6144 x 4096 with rank 32 11.0, 7 of 5120 x 17408 25.6 (1.9
+// TB/s; its codes alone in the same pieces 16.8).
 template <int B, int G, int RT>
 __global__ void __launch_bounds__(512) lora_few_kernel(LoraArgs a, int ns, int kw) {
     extern __shared__ uint4 smem[];
