@@ -162,12 +162,10 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
     };
     Q q[QA];
 #pragma unroll
-    for (int s = 0; s < ST - 1 || s < QA; ++s) {
-        if (s < ST - 1)
-            load_x(s < nk ? s : nk - 1, s);
-        if (s < QA)
-            load_w(q[s], s < nk ? s : nk - 1);
-    }
+    for (int s = 0; s < ST - 1; ++s) load_x(s < nk ? s : nk - 1, s);
+    __asm__ volatile("" ::: "memory");                     // (the steps' windows below count on this order)
+#pragma unroll
+    for (int s = 0; s < QA; ++s) load_w(q[s], s < nk ? s : nk - 1);
 
     f32x16_t acc[WM][WN];
 #pragma unroll
@@ -307,8 +305,6 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
     load_w(q[0], nk > QA ? QA : nk - 1);
     int slot = 0;
     auto step = [&](int kt, Q& qn) {
-        // x of this step has arrived: after it ST - 2 steps' x and at least as many steps' two loads of codes were issued
-        vm_window<(ST - 2) * (CA + 2)>();
         lds_barrier();
         const uint4* xs = smem + slot * XB;
         const uint4* ws = wsm + (kt & 1) * WB;
@@ -334,14 +330,21 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
         load_w(qn, kt + 1 + QA < nk ? kt + 1 + QA : nk - 1);
         slot = slot + 1 == ST ? 0 : slot + 1;
     };
+    // x of a step has arrived where only what was issued after it is under way: ST - 2 steps' x, and in the loop as many
+    // steps' two loads of codes (in the last steps no codes: the compiler drops loads that no later step uses)
     int kt = 0;
     for (; kt + QA <= nk; kt += QA)
 #pragma unroll
-        for (int i = 0; i < QA; ++i) step(kt + i, q[(i + 1) % QA]);
+        for (int i = 0; i < QA; ++i) {
+            vm_window<(ST - 2) * (CA + 2)>();
+            step(kt + i, q[(i + 1) % QA]);
+        }
 #pragma unroll
     for (int i = 0; i < QA - 1; ++i)
-        if (kt + i < nk)
+        if (kt + i < nk) {
+            vm_window<(ST - 2) * CA>();
             step(kt + i, q[(i + 1) % QA]);
+        }
     __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy into LDS outlives the workgroup
 #pragma unroll
     for (int j = 0; j < WN; ++j) {
@@ -427,11 +430,10 @@ __global__ void __launch_bounds__(256) lora_mid_kernel(LoraArgs a, int lg) {
     };
     Q q[QA];
 #pragma unroll
-    for (int s = 0; s < QA; ++s) {
-        if (s < ST - 1)
-            load_x(s < nk ? s : nk - 1, s);
-        load_w(q[s], s < nk ? s : nk - 1);
-    }
+    for (int s = 0; s < ST - 1; ++s) load_x(s < nk ? s : nk - 1, s);
+    __asm__ volatile("" ::: "memory");
+#pragma unroll
+    for (int s = 0; s < QA; ++s) load_w(q[s], s < nk ? s : nk - 1);
     f32x16_t acc[WM];
 #pragma unroll
     for (int i = 0; i < WM; ++i) acc[i] = f32x16_t{};
@@ -439,8 +441,6 @@ __global__ void __launch_bounds__(256) lora_mid_kernel(LoraArgs a, int lg) {
     int slot = 0;
     // Step kt multiplies slot kt % ST of x, while x of step kt + ST - 1 and the codes up to kt + QA are under way.
     auto step = [&](int kt, Q& c) {
-        // x of this step has arrived: after it ST - 2 steps' x and codes (two loads) were issued, and more
-        vm_window<(ST - 2) * (WM + 2)>();
         lds_barrier();
         const uint4* xs = smem + slot * XB;
         load_x(kt + ST - 1 < nk ? kt + ST - 1 : nk - 1, slot == 0 ? ST - 1 : slot - 1);
@@ -456,14 +456,19 @@ __global__ void __launch_bounds__(256) lora_mid_kernel(LoraArgs a, int lg) {
         load_w(c, kt + QA < nk ? kt + QA : nk - 1);
         slot = slot + 1 == ST ? 0 : slot + 1;
     };
-    int kt = 0;
+    int kt = 0;                                            // (windows as in lora_gemm_kernel)
     for (; kt + QA <= nk; kt += QA)
 #pragma unroll
-        for (int i = 0; i < QA; ++i) step(kt + i, q[i]);
+        for (int i = 0; i < QA; ++i) {
+            vm_window<(ST - 2) * (WM + 2)>();
+            step(kt + i, q[i]);
+        }
 #pragma unroll
     for (int i = 0; i < QA - 1; ++i)
-        if (kt + i < nk)
+        if (kt + i < nk) {
+            vm_window<(ST - 2) * WM>();
             step(kt + i, q[i]);
+        }
     __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");   // no copy into LDS outlives the workgroup
     const int col = n0 + r;
 #pragma unroll

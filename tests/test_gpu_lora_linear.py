@@ -215,3 +215,11 @@ def test_graph_of_every_path(q, M):
         g.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, q.linear_lora(w, ad, ids, x))
+
+
+@pytest.mark.parametrize("M", [40, 70, 300])
+@pytest.mark.parametrize("steps", list(range(1, 13)) + [15, 22, 23, 31])
+def test_every_number_of_steps(q, M, steps):
+    """k of any number of steps of 64, in one share and in several: the last steps follow no full round of the loop."""
+    w, x, A, B, sc, ids = make(q, 4, 64, 160, 64 * steps, M, 8, 4, F16)
+    check(q.linear_lora(w, q.Adapters(A, B, sc), ids, x), *lora_ref(w, x, A, B, sc, ids), F16)
