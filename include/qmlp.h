@@ -400,8 +400,9 @@ typedef struct {
  * weights as exact codes, more as a dense product of weights rounded once to
  * binary16, whose shares of k and adapters a third launch adds up where tiles
  * are few, or whose rows of many adapters one between the two prepares.
- * ws/ws_bytes: at least qmlp_linear_lora_workspace_bytes(...), any contents,
- * nothing is kept between calls; one call at a time per workspace.
+ * ws/ws_bytes: at least qmlp_linear_lora_workspace_bytes(...) of this or any
+ * larger number of rows, any contents, nothing is kept between calls; one call
+ * at a time per workspace.
  * M == 0 enqueues nothing.  Nothing is written outside y's M rows and ws.
  */
 size_t qmlp_linear_lora_workspace_bytes(const qmlp_qweight *w, const qmlp_adapters *adapters, int M,

@@ -78,6 +78,16 @@ LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp
     return z;
 }
 
+// A workspace for any number of rows up to M.  More rows can need less (fewer shares of k, none of them past 512 rows,
+// terms of mixed sets instead), but between these numbers the need grows with M.
+size_t lora_most_bytes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
+    size_t most = lora_sizes(w, ad, M, dtype).all();
+    for (const int m : {kLoraFewTokens, kLoraMidRows, 128, 256, 384, 512})
+        if (m < M && lora_sizes(w, ad, m, dtype).all() > most)
+            most = lora_sizes(w, ad, m, dtype).all();
+    return most;
+}
+
 // ---------------------------------------------------------------- router
 
 qmlp_status check_route(int M, int d, int E, int k, int score, qmlp_dtype dtype) {
@@ -150,7 +160,7 @@ extern "C" {
 size_t qmlp_linear_lora_workspace_bytes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
     if (check_lora(w, ad, M, dtype) != QMLP_OK)
         return 0;
-    return lora_sizes(w, ad, M, dtype).all();
+    return lora_most_bytes(w, ad, M, dtype);
 }
 
 qmlp_status qmlp_linear_lora(const qmlp_qweight* w, const qmlp_adapters* ad, const int32_t* ids, const void* x,

@@ -189,3 +189,16 @@ def test_no_rows_of_any_weights(q, lib, bits, n, k):
         assert _call(lib, w, a, ldx=k, ldy=n, M=0, dt=1) == 0
     sizes = [lib.qmlp_linear_lora_workspace_bytes(ctypes.byref(w), ctypes.byref(ad), M, 1) for M in (1, 16, 17, 64, 65, 512)]
     assert all(s > 0 for s in sizes)
+
+
+@pytest.mark.parametrize("bits,g,n,k", [(4, 128, 6144, 4096), (4, 128, 2560, 9728), (4, 64, 5120, 17408), (2, 32, 9728, 2560),
+                                        (4, 128, 1 << 18, 1 << 14), (4, 64, 100, 64)])
+@pytest.mark.parametrize("dt", [0, 1])
+def test_a_workspace_serves_fewer_rows(q, lib, bits, g, n, k, dt):
+    """What more rows need covers fewer rows, with adapters of every rank and without, over the changes of kernels and
+    shares of k: sizes never fall as rows are added."""
+    w = _w(q, bits, n, k, g)
+    for rank in (None, 8, 64):
+        ad = None if rank is None else ctypes.byref(_ad(q, rank=rank))
+        sizes = [lib.qmlp_linear_lora_workspace_bytes(ctypes.byref(w), ad, M, dt) for M in range(0, 1101)]
+        assert sizes == sorted(sizes), (rank, next(M for M in range(1100) if sizes[M] > sizes[M + 1]))

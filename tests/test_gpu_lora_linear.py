@@ -223,3 +223,16 @@ def test_every_number_of_steps(q, M, steps):
     """k of any number of steps of 64, in one share and in several: the last steps follow no full round of the loop."""
     w, x, A, B, sc, ids = make(q, 4, 64, 160, 64 * steps, M, 8, 4, F16)
     check(q.linear_lora(w, q.Adapters(A, B, sc), ids, x), *lora_ref(w, x, A, B, sc, ids), F16)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("adapters", [True, False])
+def test_one_workspace_for_fewer_rows(q, dtype, adapters):
+    """A workspace for the most rows of a program serves every smaller call: the bits of a workspace of its own."""
+    w, x, A, B, sc, ids = make(q, 4, 128, 640, 2048, 600, 16, 5, dtype)
+    ad = q.Adapters(A, B, sc) if adapters else None
+    ws = q.linear_lora_workspace(w, ad, 600, dtype)
+    for M in (600, 513, 512, 384, 300, 257, 256, 129, 128, 65, 64, 33, 17, 16, 5, 1):
+        want = q.linear_lora(w, ad, ids[:M], x[:M])
+        ws.fill_(255)
+        assert torch.equal(q.linear_lora(w, ad, ids[:M], x[:M], ws=ws), want), M
