@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kChooseWaves * 64) moe_choose_kernel(MoeArgs a
     const int m = blockIdx.x - 1;
     operands_of_row<kChooseWaves>(a.x + (long)m * a.d, a.d, false, a.gb, a.gg,
                                   reinterpret_cast<uint4*>(a.xo) + (long)m * (operand_row(a.d, a.gb) / 8),
-                                  reinterpret_cast<float2*>(a.xs) + (long)m * (operand_sums(a.d, a.gb, a.gg) / 2), 1, nullptr, tid);
+                                  reinterpret_cast<float2*>(a.xs) + (long)m * (operand_sums(a.d, a.gb, a.gg) / 2), 1, a.xf + m, tid);
 }
 
 // A block of the table in registers: expert and instances are uniform (scalar
@@ -217,14 +217,20 @@ __global__ void __launch_bounds__(512) moe_gateup_kernel(MoeArgs a, int ns, int 
                 for (int t = 0; t < RT; ++t)
                     acc[m][t] = mfma4(t1, h2f(k8.b[t] >> 16), mfma4(t0, h2f(k8.b[t] & 0xFFFFu), acc[m][t]));
     };
+    float back = 0.0f;                                     // 2^-e of the lane's own token
     oneshot_products<B, G, 2, RT, false>(acc, o, wave, ns, kw, lane, [&] {
         if (wave < items)
             rank_load(wave);
+        back = a.xf[bl.tok];
     });
 #pragma unroll
-    for (int m = 0; m < 2; ++m)
+    for (int v = 0; v < 4; ++v) {
+        const float f = kTileUnscale * __shfl(back, 4 * q + v, 64);
 #pragma unroll
-        for (int t = 0; t < RT; ++t) acc[m][t] *= kTileUnscale;
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+            for (int t = 0; t < RT; ++t) acc[m][t][v] *= f;
+    }
     if (wave < items)
         rank_add(wave);
     for (int it = wave + kw; it < items; it += kw) {       // few waves: short rows

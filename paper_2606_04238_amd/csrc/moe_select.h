@@ -10,11 +10,6 @@
 namespace qmlp {
 namespace {
 
-// v of the lane that DPP control CTRL names, or v itself where it names none.
-template <int CTRL>
-__device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
-    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false);
-}
 template <int CTRL>
 __device__ __forceinline__ double dpp_f64(double v) {
     const uint2 u = __builtin_bit_cast(uint2, v);
@@ -25,22 +20,12 @@ __device__ __forceinline__ double lane_f64(double v, int lane) {
     return __builtin_bit_cast(double, make_uint2((uint32_t)__builtin_amdgcn_readlane((int)u.x, lane),
                                                  (uint32_t)__builtin_amdgcn_readlane((int)u.y, lane)));
 }
-// Over the wave, the same in every lane: the largest v; the sum of v.  (quad_perm for
-// lanes 1 and 2 away, row_half_mirror, row_mirror; row_bcast 15 and 31.)
-__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
-    v = max(v, dpp_u32<0xB1>(v));
-    v = max(v, dpp_u32<0x4E>(v));
-    v = max(v, dpp_u32<0x141>(v));
-    v = max(v, dpp_u32<0x140>(v));
-    v = max(v, dpp_u32<0x142>(v));
-    v = max(v, dpp_u32<0x143>(v));
-    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
-}
+// Over the wave, the same in every lane: the sum of v.
 __device__ __forceinline__ double wave_sum(double v) {
-    v += dpp_f64<0xB1>(v);
-    v += dpp_f64<0x4E>(v);
-    v += dpp_f64<0x141>(v);
-    v += dpp_f64<0x140>(v);
+    v += dpp_f64<DPP_QUAD_XOR1>(v);
+    v += dpp_f64<DPP_QUAD_XOR2>(v);
+    v += dpp_f64<DPP_HALF_MIRROR>(v);
+    v += dpp_f64<DPP_MIRROR>(v);
     return (lane_f64(v, 0) + lane_f64(v, 16)) + (lane_f64(v, 32) + lane_f64(v, 48));
 }
 

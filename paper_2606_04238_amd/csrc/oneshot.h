@@ -382,10 +382,10 @@ __device__ __forceinline__ void operand16(const float (&f)[16], int bits, int g,
     o[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// The e of a bfloat16 row whose largest element is top = f 2^E, 1 <= f < 2: 14 - E,
-// with 2^e a normal number (a row whose largest is below 2^-112, or not finite,
-// keeps 126 or -114).
-__device__ __forceinline__ int bf16_shift(float top) { return min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126); }
+// The e of a row whose largest element is top = f 2^E, 1 <= f < 2: 14 - E, with 2^e a
+// normal number (a row whose largest is below 2^-112, or not finite, keeps 126 or
+// -114).
+__device__ __forceinline__ int row_shift(float top) { return min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126); }
 
 __device__ __forceinline__ uint4 ld16(const void* p) {
     const u32x4 v = *reinterpret_cast<const u32x4*>(p);
@@ -409,15 +409,20 @@ __device__ __forceinline__ uint16_t act_bits(float v, bool bf) {
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// A row of K binary16 or (bf) bfloat16 elements in operand order, padded with zeros,
-// and its group sums, by a workgroup of W waves, at o and sums among `rows` rows
-// side by side; bfloat16 times 2^e, 2^-e to *back.  16 elements per lane; the first N pieces of a wave stay in its registers between
-// the two passes that bfloat16 takes.
+// A row of K binary16 or (bf) bfloat16 elements times 2^e in operand order, padded
+// with zeros, and its group sums, by a workgroup of W waves, at o and sums among
+// `rows` rows side by side; 2^-e to *back.  The power of two puts the row's largest
+// element into [2^14, 2^15): an operand is another 2^0 to 2^-4 times its element, and
+// small rows as they are would become subnormal numbers (rows of 1e-4 at 2 bits were
+// off by 1.5e-3).  So binary16 elements down to 2^-24 of the row's largest are exact,
+// bfloat16 down to 2^-27, and what is lost below that is under 2^-35 of the largest.
+// 16 elements per lane; the first N pieces of a wave stay in its registers between the
+// two passes.
 template <int W>
 __device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool bf, int bits, int g, uint4* o, float2* sums,
                                                 int rows, float* back, int tid) {
     constexpr int N = 3;
-    __shared__ float best[W];
+    __shared__ uint32_t best[W];
     const int lane = tid & 63, wave = tid >> 6, len = operand_row(K, bits);
     uint4 v[N][2];
     auto load = [&](uint4 (&r)[2], int e) {
@@ -437,40 +442,40 @@ __device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool b
     const int first = (wave * 64 + lane) * 16, step = W * 1024;
 #pragma unroll
     for (int i = 0; i < N; ++i) load(v[i], first + i * step);
-    float up = 1.0f;
-    if (bf) {
-        float top = 0.0f, f[16];
-        auto most = [&](const uint4 (&r)[2]) {
-            widen(r, f);
+    // the largest magnitude by its bits, two at a time (a NaN is the largest: its row is lost in any case)
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    u16x2_t mag = {0, 0};
+    auto most = [&](const uint4 (&r)[2]) {
 #pragma unroll
-            for (int u = 0; u < 16; ++u) top = fmaxf(top, fabsf(f[u]));
-        };
+        for (int h = 0; h < 2; ++h) {
+            const uint32_t w[4] = {r[h].x, r[h].y, r[h].z, r[h].w};
 #pragma unroll
-        for (int i = 0; i < N; ++i) most(v[i]);
-        for (int e = first + N * step; e < K; e += step) {
-            uint4 r[2];
-            load(r, e);
-            most(r);
+            for (int u = 0; u < 4; ++u) mag = __builtin_elementwise_max(mag, __builtin_bit_cast(u16x2_t, w[u] & 0x7FFF7FFFu));
         }
+    };
 #pragma unroll
-        for (int s = 1; s < 64; s *= 2) top = fmaxf(top, __shfl_xor(top, s, 64));
-        if (lane == 0)
-            best[wave] = top;
-        __syncthreads();
-#pragma unroll
-        for (int w = 0; w < W; ++w) top = fmaxf(top, best[w]);
-        const int e = bf16_shift(top);
-        up = __uint_as_float((uint32_t)(127 + e) << 23);
-        if (tid == 0)
-            *back = __uint_as_float((uint32_t)(127 - e) << 23);
+    for (int i = 0; i < N; ++i) most(v[i]);
+    for (int e = first + N * step; e < K; e += step) {
+        uint4 r[2];
+        load(r, e);
+        most(r);
     }
+    uint32_t top = wave_max(max((uint32_t)mag.x, (uint32_t)mag.y));
+    if (lane == 0)
+        best[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w) top = max(top, best[w]);
+    const int shift = row_shift(bf ? __uint_as_float(top << 16) : h2f(top));
+    const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
+    if (tid == 0)
+        *back = __uint_as_float((uint32_t)(127 - shift) << 23);
     auto put = [&](const uint4 (&r)[2], int e) {
         float f[16], c, xs;
         uint4 w[2];
         widen(r, f);
-        if (bf)
 #pragma unroll
-            for (int u = 0; u < 16; ++u) f[u] = h2f(f2h(f[u] * up));
+        for (int u = 0; u < 16; ++u) f[u] = h2f(f2h(f[u] * up));
         operand16(f, bits, g, w, c, xs);
         if (e < len) {
             o[(long)(e / 8) * rows] = w[0];
@@ -480,7 +485,9 @@ __device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool b
         }
     };
 #pragma unroll
-    for (int i = 0; i < N; ++i) put(v[i], first + i * step);
+    for (int i = 0; i < N; ++i)
+        if (wave * 1024 + i * step < len)                  // (waves past the row's end have nothing to write)
+            put(v[i], first + i * step);
     for (int e0 = N * step; e0 < len; e0 += step) {
         const int e = first + e0;
         uint4 r[2];

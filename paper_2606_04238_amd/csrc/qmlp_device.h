@@ -128,6 +128,27 @@ constexpr int DPP_QUAD_XOR1 = 0xB1;     // quad_perm [1,0,3,2]
 constexpr int DPP_QUAD_XOR2 = 0x4E;     // quad_perm [2,3,0,1]
 constexpr int DPP_HALF_MIRROR = 0x141;  // lane i <- lane 7 - i within 8
 constexpr int DPP_MIRROR = 0x140;       // lane i <- lane 15 - i within 16
+constexpr int DPP_BCAST15 = 0x142;      // lane 15 of a row -> the next row
+constexpr int DPP_BCAST31 = 0x143;      // lane 31 -> rows 2 and 3
+
+// v of the lane that DPP control CTRL names, or v itself where it names none.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_u32(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xF, 0xF, false);
+}
+// The largest v of a row of 16 lanes, in each of them; of the wave, in every lane.
+__device__ __forceinline__ uint32_t row16_max(uint32_t v) {
+    v = max(v, dpp_u32<DPP_QUAD_XOR1>(v));
+    v = max(v, dpp_u32<DPP_QUAD_XOR2>(v));
+    v = max(v, dpp_u32<DPP_HALF_MIRROR>(v));
+    return max(v, dpp_u32<DPP_MIRROR>(v));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    v = row16_max(v);
+    v = max(v, dpp_u32<DPP_BCAST15>(v));
+    v = max(v, dpp_u32<DPP_BCAST31>(v));
+    return (uint32_t)__builtin_amdgcn_readlane((int)v, 63);
+}
 
 // Sum over the WIDTH consecutive lanes sharing an output row (every lane of
 // the group ends with the total).  Within 16 lanes the steps are DPP moves

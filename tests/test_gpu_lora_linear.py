@@ -236,3 +236,22 @@ def test_one_workspace_for_fewer_rows(q, dtype, adapters):
         want = q.linear_lora(w, ad, ids[:M], x[:M])
         ws.fill_(255)
         assert torch.equal(q.linear_lora(w, ad, ids[:M], x[:M], ws=ws), want), M
+
+
+@pytest.mark.parametrize("M", [1, 16, 17, 100])
+@pytest.mark.parametrize("bits,g", [(2, 32), (2, 128), (4, 64)])
+@pytest.mark.parametrize("mag", [1e-3, 1e-4, 1e-5])
+def test_binary16_rows_of_any_magnitude(q, M, bits, g, mag):
+    """Small rows (down to subnormal elements) are as right as ordinary ones, and as right with 16 rows as with 17; rows
+    of very different magnitudes, and one of zeros, side by side.  Weights of 0.5 keep y a normal number mostly."""
+    w, x, A, B, sc, ids = make(q, bits, g, 192, 1024, M, 16, 3, F16, std=0.5)
+    x = (x.float() * mag).to(F16)
+    if M > 1:
+        x[0] = (x[0].float() / mag * 1000).to(F16)
+        x[M - 1] = 0
+    ref, bound = lora_ref(w, x, A, B, sc, ids)
+    y = q.linear_lora(w, q.Adapters(A, B, sc), ids, x)
+    small = slice(1 if M > 1 else 0, None)
+    check(y[small], ref[small], bound[small], F16)
+    check(y[:1], ref[:1], bound[:1], F16)
+    assert M == 1 or bool((y[M - 1] == 0).all())

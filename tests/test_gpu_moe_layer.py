@@ -306,3 +306,20 @@ def test_route_bad_router_rows(q, M):
     idx, w = q.moe_route(x, r, 6)
     ref = route_ref(x, r, None, 6, "topk_softmax")
     assert torch.equal(idx.cpu(), ref[0]) and not bool((idx == 5).any())
+
+
+@pytest.mark.parametrize("M", [1, 9, 40])
+@pytest.mark.parametrize("gb,gg", [(2, 32), (2, 64), (4, 128)])
+@pytest.mark.parametrize("mag", [1e-2, 1e-4])
+def test_layer_of_small_tokens(q, M, gb, gg, mag):
+    """Small tokens beside weights that bring gate and up back to about 1: as right as ordinary ones."""
+    E, d, f = 6, 512, 256
+    pack = {2: q.pack_w2, 4: q.pack_w4}
+    g, u = (pack[gb](_rnd(s, E * f, d, std=0.05 / mag).cuda(), gg) for s in (101, 102))
+    moe = q.MoE(_rnd(103, E, d, std=0.05 / mag).to(F16).cuda(), g, u, pack[4](_rnd(104, E * d, f, std=0.05).cuda(), 64), 2)
+    x = (_rnd(105 + M, M, d) * mag).to(F16).cuda()
+    if M > 1:
+        x[M // 2] = 0
+    y = q.moe_layer(moe, x)
+    _check_layer(q, moe, x, y)
+    assert M == 1 or bool((y[M // 2] == 0).all())
