@@ -393,11 +393,11 @@ typedef struct {
  * w: 2 or 4 bits, any group, k % 64 == 0, any n.  x [M][k] and y [M][n] are
  * binary16 or bfloat16, 0 <= M <= 2^20, with rows ldx >= k (a multiple of 8)
  * and ldy >= n elements apart; elements between the rows are neither read into
- * a result nor written.  t = A x is formed in one launch (with bfloat16 rows, and
- * up to 16 binary16 ones, rewritten as binary16 times a power of two per row,
- * which keeps a bfloat16 element down to 2^-27 of its row's largest and a
- * binary16 one down to 2^-24 exactly; a row that holds an infinity or NaN gives
- * infinities or NaNs), the linear in a second: up to 16 rows with weights as exact codes, more as a dense product of weights rounded once to
+ * a result nor written.  t = A x is formed in one launch (with bfloat16 rows
+ * rewritten as binary16 times a power of two per row, which keeps every element
+ * down to 2^-28 of its row's largest exactly; a row that holds an infinity or
+ * NaN gives infinities or NaNs), the linear in a second: up to 16 rows with
+ * weights as exact codes, more as a dense product of weights rounded once to
  * binary16, whose shares of k and adapters a third launch adds up where tiles
  * are few, or whose rows of many adapters one between the two prepares.
  * ws/ws_bytes: at least qmlp_linear_lora_workspace_bytes(...) of this or any

@@ -62,7 +62,7 @@ LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp
         z.t = round256((size_t)M * ad->rank * 4);
         z.slots = round256(((size_t)(M + 31) / 32 + kMixedSets) * 4);
     }
-    if (bf || few)
+    if (bf)
         z.xf = round256((size_t)M * 4);
     if (few) {
         z.xo = round256((size_t)M * operand_row(w->k_in, w->bits) * 2);
@@ -139,10 +139,10 @@ qmlp_status check_moe(const qmlp_moe* l, int M, qmlp_dtype dtype) {
 }
 
 // Workspace: [logits fp64][expert of a slot][its weight][blocks][t][h][outputs of
-// the instances, fp32][x 2^e in operand order][its group sums][2^-e].
+// the instances, fp32][x in operand order][its group sums].
 struct MoeSizes {
-    size_t logits, idx, w, blocks, t, h, part, xo, xs, xf;
-    size_t all() const { return logits + idx + w + blocks + t + h + part + xo + xs + xf; }
+    size_t logits, idx, w, blocks, t, h, part, xo, xs;
+    size_t all() const { return logits + idx + w + blocks + t + h + part + xo + xs; }
 };
 MoeSizes moe_sizes(const qmlp_moe* l, int M) {
     const size_t n = (size_t)M * l->topk;
@@ -150,8 +150,7 @@ MoeSizes moe_sizes(const qmlp_moe* l, int M) {
             round256((size_t)(1 + moe_blocks_most((int)n, l->experts)) * kBlkInts * 4),
             round256(n * 2 * l->mlp.rank * 4), round256(n * operand_row(l->mlp.down.k_in, l->mlp.down.bits) * 2), round256(n * l->mlp.gate.k_in * 4),
             round256((size_t)M * operand_row(l->mlp.gate.k_in, l->mlp.gate.bits) * 2),
-            round256((size_t)M * operand_sums(l->mlp.gate.k_in, l->mlp.gate.bits, l->mlp.gate.group) * 4),
-            round256((size_t)M * 4)};
+            round256((size_t)M * operand_sums(l->mlp.gate.k_in, l->mlp.gate.bits, l->mlp.gate.group) * 4)};
 }
 
 }  // namespace
@@ -318,7 +317,6 @@ qmlp_status qmlp_moe_layer(const qmlp_moe* layer, const void* x, int M, qmlp_dty
     a.part = reinterpret_cast<float*>(take(z.part));
     a.xo = reinterpret_cast<uint16_t*>(take(z.xo));
     a.xs = reinterpret_cast<float*>(take(z.xs));
-    a.xf = reinterpret_cast<float*>(take(z.xf));
     a.M = M;
     a.d = r.d;
     a.f = m.down.k_in;

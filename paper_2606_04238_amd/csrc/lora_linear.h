@@ -23,7 +23,7 @@ struct LoraArgs {
     uint16_t* xo;                        // up to 16 rows: x in operand order, rows side by side (oneshot.h), or null
     float* xs;                           // and its group sums
     uint16_t* x16;                       // more: bfloat16 rows as binary16 x 2^e (rows k apart), or null
-    float* xf;                           // [M] 2^-e (bfloat16, and up to 16 rows binary16)
+    float* xf;                           // [M] 2^-e (bfloat16)
     uint16_t* tb;                        // more than 16 rows: t as two bfloat16 terms [2][M][R]
     int* slots;                          // [M / 32, rounded up]: which of the mixed sets, or -1; then [kMixedSets]: their places
     float* parts;                        // [shares][M][n] sums of lora_shares() shares of k, where lora_join() adds up; or null

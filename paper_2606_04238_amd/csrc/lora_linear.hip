@@ -5,12 +5,12 @@
 // This file: the preparation launch (t = s_a A_a x, and bfloat16 rows as
 // binary16) and the linear of up to 16 rows; lora_gemm.hip has more rows.
 //
-// Powers of two.  The matrix-core arithmetic on packed codes is binary16
-// (tile_step.h), so a bfloat16 row, and up to 16 rows a binary16 one too, enters as
-// x 2^e with the largest |x| in [2^14, 2^15), and its finished sums leave times 2^-e.
-// Past 16 rows that is exact for every bfloat16 element down to 2^-28 of the row's
-// largest (binary16 keeps 11 bits of its 8 down to 2^-14), and what is lost below is
-// under 2^-39 of the largest; up to 16 rows see operands_of_row.
+// bfloat16 rows.  The matrix-core arithmetic on packed codes is binary16
+// (oneshot.h, lora_gemm.hip), so a bfloat16 row enters as x 2^e with the largest |x| in
+// [2^14, 2^15) and its finished sums leave times 2^-e.  Both are exact for
+// every element down to 2^-28 of the row's largest (binary16 keeps 11 bits of
+// a bfloat16's 8 down to 2^-14); what is lost below that is under 2^-39 of the
+// largest element.
 #include "lora_linear.h"
 #include "decode_launch.h"
 #include "oneshot.h"
@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(512) lora_few_kernel(LoraArgs a, int ns, int k
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int rb = a.k * B / 8, ng = a.k / G;
     OneWork<1> o;
-    o.magic = magic_vgpr();
+    one_magic(o);
     o.rc[0] = rsrc(a.codes, (uint32_t)a.n * (uint32_t)rb);
     o.rm[0] = rsrc(a.meta, (uint32_t)a.n * (uint32_t)ng * 4u);
     o.rows = (uint32_t)a.M;
@@ -542,14 +542,15 @@ __global__ void __launch_bounds__(512) lora_few_kernel(LoraArgs a, int ns, int k
     const int items = a.T > 0 ? a.R / 2 : 0;
     f32x4_t acc[1][RT];
     Rank8<RT> k8;
-    float f[4];
+    float f[4] = {1.f, 1.f, 1.f, 1.f};
     oneshot_products<B, G, 1, RT, false>(acc, o, wave, ns, kw, lane, [&] {
         if (wave < items)
             rank8_load<RT>(k8, a, o.row0, wave, lane);
+        if (a.bf)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) f[v] = a.xf[4 * (lane >> 4) + v < a.M ? 4 * (lane >> 4) + v : 0];
+            for (int v = 0; v < 4; ++v) f[v] = a.xf[4 * (lane >> 4) + v < a.M ? 4 * (lane >> 4) + v : 0];
     });
-    // the rows' factors, before terms that do not have them
+    // the factor of bfloat16 rows, before terms that do not have it
 #pragma unroll
     for (int t = 0; t < RT; ++t)
 #pragma unroll

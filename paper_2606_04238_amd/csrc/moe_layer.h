@@ -37,9 +37,8 @@ struct MoeArgs {
     int* blocks;             // moe_blocks_most() blocks, those past the last with no instances
     float* t;                // [M k][2 r]
     uint16_t* h;             // M k rows in operand order, those of a block side by side (oneshot.h), in the blocks' order
-    uint16_t* xo;            // x 2^e in operand order
+    uint16_t* xo;            // x in operand order
     float* xs;               // and its group sums
-    float* xf;               // [M] 2^-e
     float* part;             // [M k][d]
     int M, d, f, r, E, k, score, gb, gg, db, dg;
     float lora_scale;

@@ -98,7 +98,7 @@ __global__ void __launch_bounds__(kChooseWaves * 64) moe_choose_kernel(MoeArgs a
     const int m = blockIdx.x - 1;
     operands_of_row<kChooseWaves>(a.x + (long)m * a.d, a.d, false, a.gb, a.gg,
                                   reinterpret_cast<uint4*>(a.xo) + (long)m * (operand_row(a.d, a.gb) / 8),
-                                  reinterpret_cast<float2*>(a.xs) + (long)m * (operand_sums(a.d, a.gb, a.gg) / 2), 1, a.xf + m, tid);
+                                  reinterpret_cast<float2*>(a.xs) + (long)m * (operand_sums(a.d, a.gb, a.gg) / 2), 1, nullptr, tid);
 }
 
 // A block of the table in registers: expert and instances are uniform (scalar
@@ -176,7 +176,7 @@ __global__ void __launch_bounds__(512) moe_gateup_kernel(MoeArgs a, int ns, int 
     const char *cg = reinterpret_cast<const char*>(a.cg), *cu = reinterpret_cast<const char*>(a.cu);
     const char *mg = reinterpret_cast<const char*>(a.mg), *mu = reinterpret_cast<const char*>(a.mu);
     OneWork<2> o;
-    o.magic = magic_vgpr();
+    one_magic(o);
     o.rc[0] = rsrc(cg + bl.e * wb, (uint32_t)wb);
     o.rc[1] = rsrc(cu + bl.e * wb, (uint32_t)wb);
     o.rm[0] = rsrc(mg + bl.e * mb, (uint32_t)mb);
@@ -217,20 +217,14 @@ __global__ void __launch_bounds__(512) moe_gateup_kernel(MoeArgs a, int ns, int 
                 for (int t = 0; t < RT; ++t)
                     acc[m][t] = mfma4(t1, h2f(k8.b[t] >> 16), mfma4(t0, h2f(k8.b[t] & 0xFFFFu), acc[m][t]));
     };
-    float back = 0.0f;                                     // 2^-e of the lane's own token
     oneshot_products<B, G, 2, RT, false>(acc, o, wave, ns, kw, lane, [&] {
         if (wave < items)
             rank_load(wave);
-        back = a.xf[bl.tok];
     });
 #pragma unroll
-    for (int v = 0; v < 4; ++v) {
-        const float f = kTileUnscale * __shfl(back, 4 * q + v, 64);
+    for (int m = 0; m < 2; ++m)
 #pragma unroll
-        for (int m = 0; m < 2; ++m)
-#pragma unroll
-            for (int t = 0; t < RT; ++t) acc[m][t][v] *= f;
-    }
+        for (int t = 0; t < RT; ++t) acc[m][t] *= kTileUnscale;
     if (wave < items)
         rank_add(wave);
     for (int it = wave + kw; it < items; it += kw) {       // few waves: short rows
@@ -253,12 +247,12 @@ __global__ void __launch_bounds__(512) moe_gateup_kernel(MoeArgs a, int ns, int 
             u += red[((w * 2 + 1) * RT + t) * 64 + lane];
         }
         const int n = o.row0 + 16 * t + j, at = operand_at(n, a.db, a.dg);
-        const float scale = operand_scale(n, a.db, a.dg);
+        // h is rounded to binary16, which down's matrix instructions take: half a step of each element, as the
+        // output's own rounding (the layer is 2.9e-4 off 64 bits with it, the output's rounding alone 2.1e-4)
 #pragma unroll
-        for (int v = 0; v < 4; ++v) {
-            if (4 * q + v < bl.n && n < a.f)               // h rounded to binary16, then its operand's power of two
-                h[((at >> 3) * bl.n + 4 * q + v) * 8 + (at & 7)] = (uint16_t)f2h(h2f(f2h(g[v] / (1.0f + __expf(-g[v])) * u[v])) * scale);
-        }
+        for (int v = 0; v < 4; ++v)
+            if (4 * q + v < bl.n && n < a.f)
+                h[((at >> 3) * bl.n + 4 * q + v) * 8 + (at & 7)] = (uint16_t)f2h(g[v] / (1.0f + __expf(-g[v])) * u[v]);
     }
 }
 
@@ -276,7 +270,7 @@ __global__ void __launch_bounds__(512) moe_down_kernel(MoeArgs a, int ns, int kw
     const int rb = a.f * B / 8, ng = a.f / G;
     const long wb = (long)a.d * rb, mb = (long)a.d * ng * 4;
     OneWork<1> o;
-    o.magic = magic_vgpr();
+    one_magic(o);
     o.rc[0] = rsrc(reinterpret_cast<const char*>(a.cd) + bl.e * wb, (uint32_t)wb);
     o.rm[0] = rsrc(reinterpret_cast<const char*>(a.md) + bl.e * mb, (uint32_t)mb);
     const int hrow = operand_row(a.f, B);

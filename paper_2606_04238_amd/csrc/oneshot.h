@@ -23,6 +23,13 @@
 // 4096 13.9 and 10.9, 16 x 5120 x 17408 40.6 and 30.4, one row 8.7 and 8.7; down of 32
 // experts, 8 rows each, 47.8 and 44.4.)  Copying codes and (scale | zero) words to
 // LDS in whole lines first did not pay: 42 against 41 for gate and up.
+//
+// Arithmetic.  That of decode_tile.hip but for the powers of two: a code at fraction
+// bits j.. of a binary16 2^(14 - j) reads 2^(14 - j) + 16 q, whatever j is, so the
+// activations are operands as they are.  (Beside 1024 + q 2^j they would be multiplied
+// by 2^(4 - j), j up to 8, and rounded to binary16 again: rows of 1e-4 were off by
+// 1.4e-3 at 2 bits and 5.7e-4 at 4, where the output's own rounding is 2.8e-4.)  The
+// offsets' sum is C = sum of 2^(14 - j) x, that of the zero points X = 16 sum of x.
 #pragma once
 
 #include "oneshot_plan.h"
@@ -62,11 +69,41 @@ struct OneWork {
     uint32_t xv, sv;                                       // this lane's place in them at step 0, or kPastEnd
     uint32_t rows;                                         // rows side by side there
     int K, N, row0;
-    uint32_t magic;                                        // magic_vgpr(), taken at the kernel's start
+    uint32_t magic[3];                                     // pairs of 2^(14 - j), j = 4, 6 and 8, made at the kernel's start
 };
-// (That constant is made at the start, and kept: an instruction written by hand
+// (Those constants are made at the start, and kept: an instruction written by hand
 // gets no distance from matrix instructions, and one among them that shared a
 // register with an unused part of a running one's result was overwritten by it.)
+template <int NM>
+__device__ __forceinline__ void one_magic(OneWork<NM>& o) {
+    o.magic[0] = magic_vgpr();
+    o.magic[1] = o.magic[0] - 0x08000800u;
+    o.magic[2] = o.magic[0] - 0x10001000u;
+}
+// The code pairs of extract_w4 and extract_w2 (qmlp_device.h), each above its own power of two.
+__device__ __forceinline__ void one_extract_w4(uint32_t w, uint32_t (&e)[4], const uint32_t (&m)[3]) {
+    e[0] = magic(w << 4, 0x00F000F0u, m[0]);
+    e[1] = magic(w, 0x00F000F0u, m[0]);
+    e[2] = magic(w >> 2, 0x03C003C0u, m[1]);
+    e[3] = magic(w >> 6, 0x03C003C0u, m[1]);
+}
+__device__ __forceinline__ void one_extract_w2(uint32_t w, uint32_t (&e)[8], const uint32_t (&m)[3]) {
+    const uint32_t l = w << 4, r = w >> 6;
+    e[0] = magic(l, 0x00300030u, m[0]);
+    e[1] = magic(l, 0x00C000C0u, m[1]);
+    e[2] = magic(w, 0x00300030u, m[0]);
+    e[3] = magic(w, 0x00C000C0u, m[1]);
+    e[4] = magic(w, 0x03000300u, m[2]);
+    e[5] = magic(r, 0x00300030u, m[0]);
+    e[6] = magic(r, 0x00C000C0u, m[1]);
+    e[7] = magic(r, 0x03000300u, m[2]);
+}
+// 2^(4 - j) of the pairs of an operand: 2^-10 of the codes' offsets.
+template <int B, bool HALF>
+__device__ __forceinline__ uint4 offset_pairs(int h) {
+    return make_uint4(pow2_pair(kPosMin - pair_pos<B, HALF>(h, 0)), pow2_pair(kPosMin - pair_pos<B, HALF>(h, 1)),
+                      pow2_pair(kPosMin - pair_pos<B, HALF>(h, 2)), pow2_pair(kPosMin - pair_pos<B, HALF>(h, 3)));
+}
 
 // The operands of a step are loaded while the step before is multiplied, each into
 // the register of the one it follows: loads come back in order, and one behind the
@@ -145,7 +182,6 @@ __device__ __forceinline__ void one_multiply(f32x4_t (&acc)[NM][RT], OneStep<B, 
     typedef Lay<B, G> Y;
     typedef OneLay<B, G> L;
     constexpr int N = NM * RT;
-    const uint32_t mv = o.magic;
     const int q = lane >> 4, left = o.K / G - gs * L::GS;  // groups of the row from this step on
     const f32x4_t zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -166,12 +202,13 @@ __device__ __forceinline__ void one_multiply(f32x4_t (&acc)[NM][RT], OneStep<B, 
         }
     }
     // a group's sums from its operands, kept where its offset and zero-point terms want them
-    const uint4 one = make_uint4(0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u);
+    constexpr uint32_t k16 = pow2_pair(kPosMin);
+    const uint4 sixteen = make_uint4(k16, k16, k16, k16);
     f32x4_t gc = zero, gx = zero;
     auto sum_up = [&](int i, int m, const uint4& a) {
         if constexpr (SUMS) {
-            gc = mfma16(one, a, m == 0 ? zero : gc);
-            gx = mfma16(unscale_pairs<B, Y::HALF>(B == 2 && !Y::HALF ? m & 1 : 0), a, m == 0 ? zero : gx);
+            gc = mfma16(offset_pairs<B, Y::HALF>(B == 2 && !Y::HALF ? m & 1 : 0), a, m == 0 ? zero : gc);
+            gx = mfma16(sixteen, a, m == 0 ? zero : gx);
             if (m + 1 < Y::MPG)
                 return;
             if constexpr (L::GS == 1) {
@@ -225,8 +262,8 @@ __device__ __forceinline__ void one_multiply(f32x4_t (&acc)[NM][RT], OneStep<B, 
 #pragma unroll
                 for (int c = 0; c < N; ++c) {
                     const uint32_t v = wd[c][h], v4 = v << 4;
-                    p[c] = mfma16(av, make_uint4(magic(v4, 0x00300030u, mv), magic(v4, 0x00C000C0u, mv),
-                                                             magic(v, 0x00300030u, mv), magic(v, 0x00C000C0u, mv)), zero);
+                    p[c] = mfma16(av, make_uint4(magic(v4, 0x00300030u, o.magic[0]), magic(v4, 0x00C000C0u, o.magic[1]),
+                                                 magic(v, 0x00300030u, o.magic[0]), magic(v, 0x00C000C0u, o.magic[1])), zero);
                 }
                 add();
 #pragma unroll
@@ -256,12 +293,12 @@ __device__ __forceinline__ void one_multiply(f32x4_t (&acc)[NM][RT], OneStep<B, 
                     const uint32_t v = word_of(s.w[c], i * Y::QW + ww);
                     if constexpr (B == 2) {
                         uint32_t x[8];
-                        extract_w2(v, x, mv);
+                        one_extract_w2(v, x, o.magic);
                         p[c] = mfma16(a0, make_uint4(x[0], x[1], x[2], x[3]), p[c]);
                         p[c] = mfma16(a1, make_uint4(x[4], x[5], x[6], x[7]), p[c]);
                     } else {
                         uint32_t x[4];
-                        extract_w4(v, x, mv);
+                        one_extract_w4(v, x, o.magic);
                         p[c] = mfma16(a0, make_uint4(x[0], x[1], x[2], x[3]), p[c]);
                     }
                 }
@@ -335,12 +372,12 @@ __device__ __forceinline__ void oneshot_products(f32x4_t (&acc)[NM][RT], const O
 }
 
 // ---- activations in the operands' order, for the launch before
-// Where element e of a row goes (within its block of 16), and the power of two it
-// is multiplied by, as act_convert would.
+// Where element e of a row goes (within its block of 16), and 2^-10 of the offset of
+// the codes that it meets.
 __device__ __forceinline__ int operand_at(int e, int bits, int g) {
     return bits == 2 && g != 32 ? (e & ~15) + 2 * (e & 7) + ((e >> 3) & 1) : (e & ~7) + 2 * (e & 3) + ((e >> 2) & 1);
 }
-__device__ __forceinline__ float operand_scale(int e, int bits, int g) {
+__device__ __forceinline__ float operand_offset(int e, int bits, int g) {
     int p;                                                 // fraction position of the element's pair
     if (bits == 4)
         p = (e & 3) < 2 ? 4 : 6;
@@ -351,8 +388,8 @@ __device__ __forceinline__ float operand_scale(int e, int bits, int g) {
     return __uint_as_float((uint32_t)(127 + kPosMin - p) << 23);
 }
 // Sixteen elements of a row (fp32, already binary16 values) as two operands, and the
-// group sums -1024 C and -X (group_sums) of the group they are in: lanes whose
-// blocks share a group lie side by side, and each gets the sums.
+// sums -C and -X of the group they are in: lanes whose blocks share a group lie side
+// by side, and each gets the sums.
 __device__ __forceinline__ void operand16(const float (&f)[16], int bits, int g, uint4 (&o)[2], float& c, float& x) {
     uint32_t w[8];
     c = x = 0.0f;
@@ -361,9 +398,8 @@ __device__ __forceinline__ void operand16(const float (&f)[16], int bits, int g,
     for (int p = 0; p < 8; ++p) {
         const int e0 = across ? p : (p & 3) + 8 * (p >> 2), e1 = across ? 8 + p : e0 + 4;
         const float f0 = across ? f[p] : f[(p & 3) + 8 * (p >> 2)], f1 = across ? f[8 + p] : f[(p & 3) + 8 * (p >> 2) + 4];
-        const uint32_t h0 = f2h(f0 * operand_scale(e0, bits, g)), h1 = f2h(f1 * operand_scale(e1, bits, g));
-        w[p] = h0 | h1 << 16;
-        c += h2f(h0) + h2f(h1);
+        w[p] = f2h(f0) | f2h(f1) << 16;
+        c += f0 * operand_offset(e0, bits, g) + f1 * operand_offset(e1, bits, g);
         x += f0 + f1;
     }
     c = -1024.0f * c;
@@ -382,9 +418,9 @@ __device__ __forceinline__ void operand16(const float (&f)[16], int bits, int g,
     o[1] = make_uint4(w[4], w[5], w[6], w[7]);
 }
 
-// The e of a row whose largest element is top = f 2^E, 1 <= f < 2: 14 - E, with 2^e a
-// normal number (a row whose largest is below 2^-112, or not finite, keeps 126 or
-// -114).
+// The e of a bfloat16 row whose largest element is top = f 2^E, 1 <= f < 2: 14 - E,
+// with 2^e a normal number (a row whose largest is below 2^-112, or not finite,
+// keeps 126 or -114).
 __device__ __forceinline__ int row_shift(float top) { return min(14 - ((int)(__float_as_uint(top) >> 23) - 127), 126); }
 
 __device__ __forceinline__ uint4 ld16(const void* p) {
@@ -409,15 +445,10 @@ __device__ __forceinline__ uint16_t act_bits(float v, bool bf) {
     return __builtin_bit_cast(uint16_t, (__bf16)v);
 }
 
-// A row of K binary16 or (bf) bfloat16 elements times 2^e in operand order, padded
-// with zeros, and its group sums, by a workgroup of W waves, at o and sums among
-// `rows` rows side by side; 2^-e to *back.  The power of two puts the row's largest
-// element into [2^14, 2^15): an operand is another 2^0 to 2^-4 times its element, and
-// small rows as they are would become subnormal numbers (rows of 1e-4 at 2 bits were
-// off by 1.5e-3).  So binary16 elements down to 2^-24 of the row's largest are exact,
-// bfloat16 down to 2^-27, and what is lost below that is under 2^-35 of the largest.
-// 16 elements per lane; the first N pieces of a wave stay in its registers between the
-// two passes.
+// A row of K binary16 or (bf) bfloat16 elements in operand order, padded with zeros,
+// and its group sums, by a workgroup of W waves, at o and sums among `rows` rows
+// side by side; bfloat16 times 2^e, 2^-e to *back.  16 elements per lane; the first N
+// pieces of a wave stay in its registers between the two passes that bfloat16 takes.
 template <int W>
 __device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool bf, int bits, int g, uint4* o, float2* sums,
                                                 int rows, float* back, int tid) {
@@ -442,40 +473,44 @@ __device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool b
     const int first = (wave * 64 + lane) * 16, step = W * 1024;
 #pragma unroll
     for (int i = 0; i < N; ++i) load(v[i], first + i * step);
-    // the largest magnitude by its bits, two at a time (a NaN is the largest: its row is lost in any case)
-    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
-    u16x2_t mag = {0, 0};
-    auto most = [&](const uint4 (&r)[2]) {
+    float up = 1.0f;
+    if (bf) {
+        // the largest magnitude by its bits, two at a time (a NaN is the largest: its row is lost in any case)
+        typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+        u16x2_t mag = {0, 0};
+        auto most = [&](const uint4 (&r)[2]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const uint32_t w[4] = {r[h].x, r[h].y, r[h].z, r[h].w};
+            for (int h = 0; h < 2; ++h) {
+                const uint32_t w[4] = {r[h].x, r[h].y, r[h].z, r[h].w};
 #pragma unroll
-            for (int u = 0; u < 4; ++u) mag = __builtin_elementwise_max(mag, __builtin_bit_cast(u16x2_t, w[u] & 0x7FFF7FFFu));
+                for (int u = 0; u < 4; ++u) mag = __builtin_elementwise_max(mag, __builtin_bit_cast(u16x2_t, w[u] & 0x7FFF7FFFu));
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < N; ++i) most(v[i]);
+        for (int e = first + N * step; e < K; e += step) {
+            uint4 r[2];
+            load(r, e);
+            most(r);
         }
-    };
+        uint32_t top = wave_max(max((uint32_t)mag.x, (uint32_t)mag.y));
+        if (lane == 0)
+            best[wave] = top;
+        __syncthreads();
 #pragma unroll
-    for (int i = 0; i < N; ++i) most(v[i]);
-    for (int e = first + N * step; e < K; e += step) {
-        uint4 r[2];
-        load(r, e);
-        most(r);
+        for (int w = 0; w < W; ++w) top = max(top, best[w]);
+        const int e = row_shift(__uint_as_float(top << 16));
+        up = __uint_as_float((uint32_t)(127 + e) << 23);
+        if (tid == 0)
+            *back = __uint_as_float((uint32_t)(127 - e) << 23);
     }
-    uint32_t top = wave_max(max((uint32_t)mag.x, (uint32_t)mag.y));
-    if (lane == 0)
-        best[wave] = top;
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < W; ++w) top = max(top, best[w]);
-    const int shift = row_shift(bf ? __uint_as_float(top << 16) : h2f(top));
-    const float up = __uint_as_float((uint32_t)(127 + shift) << 23);
-    if (tid == 0)
-        *back = __uint_as_float((uint32_t)(127 - shift) << 23);
     auto put = [&](const uint4 (&r)[2], int e) {
         float f[16], c, xs;
         uint4 w[2];
         widen(r, f);
+        if (bf)
 #pragma unroll
-        for (int u = 0; u < 16; ++u) f[u] = h2f(f2h(f[u] * up));
+            for (int u = 0; u < 16; ++u) f[u] = h2f(f2h(f[u] * up));
         operand16(f, bits, g, w, c, xs);
         if (e < len) {
             o[(long)(e / 8) * rows] = w[0];

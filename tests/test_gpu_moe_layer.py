@@ -323,3 +323,24 @@ def test_layer_of_small_tokens(q, M, gb, gg, mag):
     y = q.moe_layer(moe, x)
     _check_layer(q, moe, x, y)
     assert M == 1 or bool((y[M // 2] == 0).all())
+
+
+@pytest.mark.parametrize("M", [1, 9, 40])
+@pytest.mark.parametrize("db,dg", [(2, 32), (2, 64), (2, 128), (4, 32), (4, 64), (4, 128)])
+def test_layer_of_small_h(q, M, db, dg):
+    """Gate and up of about 0.008 give an h of 3e-5, partly subnormal: off by no more than its own rounding, 2^-25
+    (5e-4 of it in the norm, beside 3e-4 of ordinary h and y: under 2^-10).  Every other token's h is a thousand
+    times larger."""
+    E, d, f = 6, 512, 256
+    pack = {2: q.pack_w2, 4: q.pack_w4}
+    g, u = (q.pack_w4(_rnd(s, E * f, d, std=0.008 / d ** 0.5).cuda(), 64) for s in (111, 112))
+    moe = q.MoE(_rnd(113, E, d, std=0.05).to(F16).cuda(), g, u, pack[db](_rnd(114, E * d, f).cuda(), dg), 2)
+    x = _rnd(115 + M, M, d).cuda()
+    x[1::2] *= 100.0
+    x = x.to(F16)
+    y = q.moe_layer(moe, x)
+    idx, w = route_ref(x, moe.router, None, 2, "topk_softmax")
+    ref = moe_ref(moe, x, idx, w)
+    err = (y.double().cpu() - ref).norm(dim=1) / ref.norm(dim=1)
+    print("rel %.2e" % float(err.max()))
+    assert bool((err <= 2.0 ** -10).all())
