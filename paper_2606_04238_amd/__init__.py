@@ -613,11 +613,13 @@ class MoE:
         f = down.k_in
         _router_args(router, bias, gate.k_in, torch.float16)
         rank = 0
-        if A_gate is not None:
+        if any(t is not None for t in (A_gate, B_gate, A_up, B_up)):
+            if A_gate is None or A_gate.dim() != 3:
+                raise ValueError("adapters must be float16, A [E][rank][d] and B [E][f][rank], all four or none")
             rank = int(A_gate.shape[1])
             for t, s in ((A_gate, (E, rank, d)), (A_up, (E, rank, d)), (B_gate, (E, f, rank)), (B_up, (E, f, rank))):
                 if t is None or t.dtype != torch.float16 or tuple(t.shape) != s or not t.is_contiguous():
-                    raise ValueError("adapters must be float16, A [E][rank][d] and B [E][f][rank]")
+                    raise ValueError("adapters must be float16, A [E][rank][d] and B [E][f][rank], all four or none")
         _one_device(router, bias, gate.codes, up.codes, down.codes, A_gate, B_gate, A_up, B_up)
         self.router, self.gate, self.up, self.down, self.bias = router, gate, up, down, bias
         self.adapters = (A_gate, B_gate, A_up, B_up)

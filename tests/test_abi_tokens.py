@@ -202,3 +202,15 @@ def test_a_workspace_serves_fewer_rows(q, lib, bits, g, n, k, dt):
         ad = None if rank is None else ctypes.byref(_ad(q, rank=rank))
         sizes = [lib.qmlp_linear_lora_workspace_bytes(ctypes.byref(w), ad, M, dt) for M in range(0, 1101)]
         assert sizes == sorted(sizes), (rank, next(M for M in range(1100) if sizes[M] > sizes[M + 1]))
+
+
+@pytest.mark.parametrize("have", [(0, 1, 1, 1), (1, 0, 1, 1), (1, 1, 0, 1), (1, 1, 1, 0), (0, 0, 0, 1), (1, 0, 0, 0)])
+def test_moe_adapters_come_together(q, have):
+    """Some of the four adapters without the others are refused, not left out."""
+    import torch
+    E, d, f, r = 2, 64, 64, 8
+    ad = [torch.zeros(*s, dtype=torch.float16) if h else None
+          for h, s in zip(have, [(E, r, d), (E, f, r), (E, r, d), (E, f, r)])]
+    w = q.QWeight(4, E * f, d, 64, torch.zeros(E * f * 8, dtype=torch.int32), torch.zeros(E * f, dtype=torch.int32))
+    with pytest.raises(ValueError, match="adapters"):
+        q.MoE(torch.zeros(E, d, dtype=torch.float16), w, w, w, 1, *ad)
