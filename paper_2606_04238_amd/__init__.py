@@ -515,7 +515,7 @@ def linear_lora(w: QWeight, adapters: Adapters | None, ids: torch.Tensor | None,
         ad = ctypes.byref(adapters._c)
     if ws is None:
         ws = linear_lora_workspace(w, adapters, M, x.dtype, x.device)
-    here = _one_device(x, y, ids, ws, w.codes, adapters.A if adapters else None)
+    here = _one_device(x, y, ids, ws, w.codes, w.meta, adapters.A if adapters else None)
     _check(_lib().qmlp_linear_lora(ctypes.byref(w.c()), ad, _addr(ids) if ad else None, _addr(x), x.stride(0) if M > 1 else k,
                                    M, code, _addr(y), y.stride(0) if M > 1 else w.n_out, _addr(ws), ws.numel(),
                                    torch._C._cuda_getCurrentRawStream(here)), "linear_lora")
@@ -620,7 +620,7 @@ class MoE:
             for t, s in ((A_gate, (E, rank, d)), (A_up, (E, rank, d)), (B_gate, (E, f, rank)), (B_up, (E, f, rank))):
                 if t is None or t.dtype != torch.float16 or tuple(t.shape) != s or not t.is_contiguous():
                     raise ValueError("adapters must be float16, A [E][rank][d] and B [E][f][rank], all four or none")
-        _one_device(router, bias, gate.codes, up.codes, down.codes, A_gate, B_gate, A_up, B_up)
+        _one_device(router, bias, gate.codes, gate.meta, up.codes, up.meta, down.codes, down.meta, A_gate, B_gate, A_up, B_up)
         self.router, self.gate, self.up, self.down, self.bias = router, gate, up, down, bias
         self.adapters = (A_gate, B_gate, A_up, B_up)
         self.experts, self.topk, self.d, self.f, self.rank = int(E), int(topk), int(d), int(f), rank

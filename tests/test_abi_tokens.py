@@ -214,3 +214,26 @@ def test_moe_adapters_come_together(q, have):
     w = q.QWeight(4, E * f, d, 64, torch.zeros(E * f * 8, dtype=torch.int32), torch.zeros(E * f, dtype=torch.int32))
     with pytest.raises(ValueError, match="adapters"):
         q.MoE(torch.zeros(E, d, dtype=torch.float16), w, w, w, 1, *ad)
+
+
+def test_scales_are_checked_like_codes(q, monkeypatch):
+    """The device of a matrix' scales is checked with that of its codes, before anything is launched."""
+    import torch
+
+    class Seen(Exception):
+        pass
+
+    def look(*tensors):
+        raise Seen([id(t) for t in tensors])
+
+    monkeypatch.setattr(q, "_one_device", look)
+    E, d, f = 2, 64, 64
+    w = [q.QWeight(4, E * f, d, 64, torch.zeros(E * f * 8, dtype=torch.int32), torch.zeros(E * f, dtype=torch.int32))
+         for _ in range(3)]
+    x = torch.zeros(3, d, dtype=torch.float16)
+    with pytest.raises(Seen) as e:
+        q.linear_lora(w[0], None, None, x, ws=torch.zeros(1 << 16, dtype=torch.uint8))
+    assert {id(w[0].codes), id(w[0].meta), id(x)} <= set(e.value.args[0])
+    with pytest.raises(Seen) as e:
+        q.MoE(torch.zeros(E, d, dtype=torch.float16), *w, 1)
+    assert {id(t) for v in w for t in (v.codes, v.meta)} <= set(e.value.args[0])
