@@ -255,3 +255,18 @@ def test_binary16_rows_of_any_magnitude(q, M, bits, g, mag):
     check(y[small], ref[small], bound[small], F16)
     check(y[:1], ref[:1], bound[:1], F16)
     assert M == 1 or bool((y[M - 1] == 0).all())
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("M,n", [(4715, 130), (4715, 7700), (16515, 130)])
+def test_more_mixed_sets_than_are_formed_beforehand(q, M, n, dtype):
+    """More than 128 sets of 32 rows with many adapters, single-adapter sets and ones without adapters between them, in
+    tiles of 128 x 128 and 256 x 192; past 16384 rows a thread of the search has several sets."""
+    w, x, A, B, sc, ids = make(q, 4, 64, n, 64, M, 8, 40, dtype)
+    for s in range(0, M // 32, 12):
+        ids[32 * s:32 * s + 32] = s % 41 - 1
+    sets = ids[:M // 32 * 32].view(-1, 32).cpu()
+    assert sum(len(set(v.tolist())) > 3 for v in sets) > 128
+    y = q.linear_lora(w, q.Adapters(A, B, sc), ids, x)
+    ref, bound = lora_ref(w, x, A, B, sc, ids)
+    check(y, ref, bound, dtype)
