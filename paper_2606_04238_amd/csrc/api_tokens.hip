@@ -68,8 +68,9 @@ LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp
         z.xo = round256((size_t)M * operand_row(w->k_in, w->bits) * 2);
         z.xs = round256((size_t)M * operand_sums(w->k_in, w->bits, w->group) * 4);
     } else {
-        if (lora_join(M, w->n_out, w->k_in, some))
-            z.parts = round256((size_t)lora_shares(M, w->n_out, w->k_in) * M * w->n_out * 4);
+        const int shares = lora_shares(M, w->n_out, w->k_in, plan_cus());
+        if (lora_join(M, shares, some))
+            z.parts = round256((size_t)shares * M * w->n_out * 4);
         else if (some)
             z.mixed = round256((size_t)lora_mixed_most(M) * 32 * w->n_out * 4);
         if (bf)
@@ -207,6 +208,8 @@ qmlp_status qmlp_linear_lora(const qmlp_qweight* w, const qmlp_adapters* ad, con
     a.bits = w->bits;
     a.g = w->group;
     a.bf = dtype == QMLP_BF16;
+    a.cus = plan_cus();
+    a.shares = lora_shares(M, a.n, a.k, a.cus);
     const bool few = lora_few_rows(M, w);
     const auto take = [&](size_t bytes) {
         char* at = base;

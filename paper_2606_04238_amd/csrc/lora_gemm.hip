@@ -489,7 +489,7 @@ __global__ void __launch_bounds__(256) lora_mid_kernel(LoraArgs a, int lg) {
 
 hipError_t launch_lora_gemm(const LoraArgs& a, hipStream_t st) {
     const int lg = a.g == 32 ? 5 : a.g == 64 ? 6 : 7;
-    const unsigned shares = (unsigned)lora_shares(a.M, a.n, a.k);
+    const unsigned shares = (unsigned)a.shares;
     if (a.M <= kLoraMidRows) {
         const int wm = (a.M + 31) / 32;
         const unsigned grid = (unsigned)(a.n + 127) / 128;
@@ -510,11 +510,7 @@ hipError_t launch_lora_gemm(const LoraArgs& a, hipStream_t st) {
     if (shares > 1)
         return a.bits == 2 ? run(lora_gemm_kernel<2, 128, 128, 2, 1, 4, true>, 128, 128, 512, 4)
                            : run(lora_gemm_kernel<4, 128, 128, 2, 1, 4, true>, 128, 128, 512, 4);
-    // Tiles of 256 x 192 take 2.2 times as long as those of 128 x 128 for three times the work; both run in rounds over
-    // the compute units (us, large and small: 600 x 2560 x 9728 236 and 116, 1024 x 6144 x 4096 141 and 117, 2048 x 2560 x
-    // 2560 110 and 86, 512 x 28672 x 4096 218 and 202; 4096 x 2560 x 2560 123 and 153, 520 x 14336 x 4096 114 and 146).
-    auto rounds = [&](int BM, int BN) { return ((long)((a.M + BM - 1) / BM) * ((a.n + BN - 1) / BN) + 255) / 256; };
-    if (11 * rounds(256, 192) < 5 * rounds(128, 128))
+    if (lora_large_tiles(a.M, a.n, a.cus))
         return a.bits == 2 ? run(lora_gemm_kernel<2, 256, 192, 2, 3, 3, false>, 256, 192, 512, 3)
                            : run(lora_gemm_kernel<4, 256, 192, 2, 3, 3, false>, 256, 192, 512, 3);
     return a.bits == 2 ? run(lora_gemm_kernel<2, 128, 128, 2, 1, 4, false>, 128, 128, 512, 4)

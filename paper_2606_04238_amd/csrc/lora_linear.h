@@ -4,6 +4,7 @@
 
 #include "oneshot_plan.h"
 #include "qmlp_internal.h"
+#include "tokens_plan.h"
 
 namespace qmlp {
 
@@ -17,6 +18,7 @@ struct LoraArgs {
     long ldx, ldy;
     int M, n, k, bits, g, T, R;
     int bf;                              // activations are bfloat16 (else binary16)
+    int shares, cus;                     // of k, past 16 rows; compute units of the device
     // workspace
     int* known;                          // up to 16 rows: [16] adapter of a row, -1: none
     float* t;                            // up to 16 rows: [M][R] scale[a] A_a x, fp32; zeros where there is no adapter
@@ -26,7 +28,7 @@ struct LoraArgs {
     float* xf;                           // [M] 2^-e (bfloat16)
     uint16_t* tb;                        // more than 16 rows: t as two bfloat16 terms [2][M][R]
     int* slots;                          // [M / 32, rounded up]: which of the mixed sets, or -1; then [kMixedSets]: their places
-    float* parts;                        // [shares][M][n] sums of lora_shares() shares of k, where lora_join() adds up; or null
+    float* parts;                        // [shares][M][n] sums of the shares of k, where lora_join() adds up; or null
     float* mixed;                        // [kMixedSets 32][n] adapter terms of the mixed sets' rows
 };
 
@@ -35,31 +37,11 @@ struct LoraArgs {
 constexpr int kMixedSets = 128, kMixedFrom = 3;
 inline int lora_mixed_most(int M) { return (M + 31) / 32 < kMixedSets ? (M + 31) / 32 : kMixedSets; }
 
-constexpr int kLoraMidRows = 64;         // rows up to which lora_mid_kernel multiplies
-// Shares of k for 17 to 512 rows, where tiles of 128 outputs (and 128 rows) leave half
-// the compute units or more without one: as many as there are units for, of at
-// least eight steps of 64.  (us, the product's launches with one share and with
-// the rule's: 17 x 6144 x 4096, 48 tiles, 35.7 and 16.9; 67 rows 50.5 and 23.4; 200 x
-// 2560 x 2560 36.9 and 20.6; 128 x 2560 x 9728 97 and 26; rank 64: 256 x 4096 x 4096
-// 67 and 52, 512 84 and 71.)
-inline int lora_shares(int M, int n, int k) {
-    const long tiles = (long)((M + 127) / 128) * ((n + 127) / 128);
-    if (M < 1 || M > 512 || tiles > 128)
-        return 1;
-    const int most = k / 64 / 8, fill = (int)(256 / tiles);
-    return most < 1 ? 1 : fill < most ? fill : most;
-}
-constexpr int kLoraFewTokens = 16;       // rows of the one-shot kernel (a matrix operand's)
-
 // Whether the one-shot kernel takes M rows: they fit one operand, and W's arrays
 // 32-bit offsets.
 inline bool lora_few_rows(int M, const qmlp_qweight* w) {
     return M <= kLoraFewTokens && (long)w->n_out * w->k_in * w->bits / 8 < (1l << 31) &&
            (long)w->n_out * (w->k_in / w->group) * 4 < (1l << 31);
-}
-// Whether launch_lora_join follows launch_lora_gemm, for several shares or for the adapters.
-inline bool lora_join(int M, int n, int k, bool adapters) {
-    return lora_shares(M, n, k) > 1 || (M <= kLoraMidRows && adapters);
 }
 hipError_t launch_lora_prep(const LoraArgs& a, hipStream_t st);
 hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st);

@@ -236,7 +236,7 @@ __global__ void __launch_bounds__(256) lora_mixed_kernel(LoraArgs a, int most) {
 
 // y = the sum of the shares of k, in their order, and the adapters' terms.
 template <int RC>
-__global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs a, int shares) {
+__global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs a) {
     constexpr bool ADS = RC > 0;                           // (0: no adapters)
     constexpr int P = 8;                                   // shares loaded at once
     __shared__ float at[kTermRows][256];
@@ -245,17 +245,17 @@ __global__ void __launch_bounds__(256) lora_join_kernel(LoraArgs a, int shares) 
     if constexpr (ADS)
         x.load(a, m0, blockIdx.x * 256, tid);
     float s[kTermRows] = {};
-    for (int i0 = 0; i0 < shares; i0 += P) {
+    for (int i0 = 0; i0 < a.shares; i0 += P) {
         float p[P][kTermRows];
 #pragma unroll
         for (int i = 0; i < P; ++i)
 #pragma unroll
             for (int r = 0; r < kTermRows; ++r)
-                p[i][r] = a.parts[((long)min(i0 + i, shares - 1) * a.M + min(m0 + r, a.M - 1)) * a.n + min(c, a.n - 1)];
+                p[i][r] = a.parts[((long)min(i0 + i, a.shares - 1) * a.M + min(m0 + r, a.M - 1)) * a.n + min(c, a.n - 1)];
 #pragma unroll
         for (int i = 0; i < P; ++i)
 #pragma unroll
-            for (int r = 0; r < kTermRows; ++r) s[r] += i0 + i < shares ? p[i][r] : 0.0f;
+            for (int r = 0; r < kTermRows; ++r) s[r] += i0 + i < a.shares ? p[i][r] : 0.0f;
     }
     if constexpr (ADS)
         x.add(s, at, a.bf, tid);
@@ -605,17 +605,14 @@ hipError_t launch_lora_mixed(const LoraArgs& a, hipStream_t st) {
 
 hipError_t launch_lora_join(const LoraArgs& a, hipStream_t st) {
     auto k = a.T == 0 ? lora_join_kernel<0> : a.R == 8 ? lora_join_kernel<1> : a.R == 16 ? lora_join_kernel<2> : a.R == 32 ? lora_join_kernel<4> : lora_join_kernel<8>;
-    k<<<dim3((unsigned)(a.n + 255) / 256, (unsigned)(a.M + kTermRows - 1) / kTermRows), 256, 0, st>>>(a, lora_shares(a.M, a.n, a.k));
+    k<<<dim3((unsigned)(a.n + 255) / 256, (unsigned)(a.M + kTermRows - 1) / kTermRows), 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
 hipError_t launch_lora_few(const LoraArgs& a, hipStream_t st) {
     if (a.M < 1 || a.M > kLoraFewTokens)
         return hipErrorInvalidValue;
-    // Two tiles of a workgroup share its operands, one tile makes twice the workgroups: one where those are no more
-    // than the compute units (us, 4 bits, one and two tiles: 2560 x 2560, 160 tiles, M = 1 4.9 and 6.1, M = 16 7.1 and
-    // 8.4; 6144 x 4096, 384 tiles, 9.5 and 8.9, 16.4 and 12.0; 28672 x 4096 25.9 and 24.9, 51.9 and 38.9).
-    const int rt = (a.n + 15) / 16 <= 256 ? 1 : 2, ns = oneshot_steps(a.k, a.bits), kw = oneshot_waves(ns);
+    const int rt = lora_few_tiles(a.n, a.cus), ns = oneshot_steps(a.k, a.bits), kw = oneshot_waves(ns);
     const unsigned grid = (unsigned)((a.n + 16 * rt - 1) / (16 * rt));
     auto run = [&](auto k) {
         k<<<grid, (unsigned)kw * 64, (size_t)kw * rt * 1024, st>>>(a, ns, kw);

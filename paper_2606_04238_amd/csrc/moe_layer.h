@@ -4,6 +4,7 @@
 
 #include "oneshot_plan.h"
 #include "qmlp_internal.h"
+#include "tokens_plan.h"
 
 namespace qmlp {
 

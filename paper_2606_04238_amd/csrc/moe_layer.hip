@@ -339,13 +339,9 @@ hipError_t launch_moe_experts(const MoeArgs& a, hipStream_t st) {
         k<<<dim3((unsigned)(rows + 16 * rt - 1) / (16 * rt), (unsigned)nb), (unsigned)kw * 64, (size_t)kw * nm * rt * 1024, st>>>(a, ns, kw);
         return hipGetLastError();
     };
-    // Two tiles of gate and up share a workgroup's operands; one where that left compute units without a workgroup
-    // (us, 4 bits, d = 4096, f = 1536, one token's 2 experts: one tile 8.4, two 13.1), and for 2 bits, whose two tiles
-    // leave registers for two waves a SIMD, up to an average of two instances an expert (d = f = 2880, 4 of 32 experts,
-    // one tile and two: M = 1 10.6 and 12.7, 8 37.3 and 40.4, 16 52.3 and 52.9, 32 65.0 and 62.7, 64 80.5 and 68.8;
-    // 4 bits, d = 2048, f = 768, 8 of 128: M = 4 18.0 and 16.8, 13 37.2 and 35.3, 64 71.0 and 62.8).  Down takes two
-    // (M = 1 7.2 and 8.3, 8 29.6 and 25.5, 64 59.2 and 47.9).
-    const bool two = (long)n * (a.f / 32) >= 256 && (a.gb == 4 || n > 2 * a.E);
+    // Down takes two tiles (us, d = f = 2880, 4 of 32 experts, one tile and two: M = 1 7.2 and 8.3, 8 29.6 and 25.5, 64
+    // 59.2 and 47.9).
+    const bool two = moe_two_tiles(n, a.E, a.f, a.gb, plan_cus());
     err = hipErrorInvalidValue;
 #define QMLP_MG(B_, G_)                                                                             \
     if (a.gb == B_ && a.gg == G_)                                                                   \

@@ -524,13 +524,6 @@ hipError_t launch_prefill_lora(const uint16_t* Ag, const uint16_t* Au, const uin
     return hipGetLastError();
 }
 
-// Compute units of the plans (without a device, whose launches fail anyway,
-// those of a whole MI355X).
-static int plan_cus() {
-    const int n = device_cus();
-    return n > 0 ? n : 256;
-}
-
 hipError_t launch_prefill_gateup(const uint32_t* cg, const uint32_t* mg, const uint32_t* cu,
                                  const uint32_t* mu, const uint16_t* x, const uint16_t* T,
                                  const uint16_t* Bg, const uint16_t* Bu, uint16_t* h, int M, int d,

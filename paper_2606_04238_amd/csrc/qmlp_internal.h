@@ -18,8 +18,13 @@ size_t forward_least_bytes(const qmlp_mlp* mlp, int M, qmlp_dtype dtype);
 // The structural checks of one packed-weight view (bits 0: any width).
 qmlp_status weight_check(const qmlp_qweight* w, int bits);
 
-// Compute units of the current device (asked once per device), 0 without one.
+// Compute units of the current device (asked once per device), 0 without one; for
+// plans: without a device, whose launches fail anyway, those of a whole MI355X.
 int device_cus();
+inline int plan_cus() {
+    const int n = device_cus();
+    return n > 0 ? n : 256;
+}
 
 // Codes per unit of a row's code stream: 32 at 4 bits and 64 at 2 bits (one
 // 16-byte load); at 3 bits 64 (16 bytes of the 2-bit plane and 8 bytes of
