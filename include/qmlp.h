@@ -396,7 +396,9 @@ typedef struct {
  * a result nor written.  t = A x is formed in one launch (with bfloat16 rows
  * rewritten as binary16 times a power of two per row, which keeps every element
  * down to 2^-28 of its row's largest exactly; a row that holds an infinity or
- * NaN gives infinities or NaNs), the linear in a second: up to 16 rows with
+ * NaN, or whose adapter does, or whose t overflows fp32, gives infinities or
+ * NaNs, and so may a bfloat16 row of more than 16 whose adapter's term exceeds
+ * 2^113 times its largest element), the linear in a second: up to 16 rows with
  * weights as exact codes, more as a dense product of weights rounded once to
  * binary16, whose shares of k and adapters a third launch adds up where tiles
  * are few, or whose rows of many adapters one between the two prepares.

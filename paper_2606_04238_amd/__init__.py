@@ -479,7 +479,6 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
-
 def linear_lora_workspace_bytes(w: QWeight, adapters: Adapters | None, M: int, dtype=torch.float16) -> int:
     qc = w.c()
     return int(_lib().qmlp_linear_lora_workspace_bytes(ctypes.byref(qc), ctypes.byref(adapters.c()) if adapters else None,

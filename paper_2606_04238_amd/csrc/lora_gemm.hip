@@ -21,7 +21,7 @@
 //
 // Tile engine: BM rows x BN outputs per workgroup, K in steps of 64 staged in
 // LDS, chunk c of row r at c ^ ((r >> 1) & 7).  x is copied to LDS by the memory
-// system (ST slots, ST - 1 steps ahead); codes are in registers QA steps ahead
+// system (ST slots, ST - 1 steps ahead); codes are in registers QA + 1 steps ahead
 // and unpacked into two buffers, one step ahead; one barrier per step.  Measured:
 // bfloat16 4096 x 6144 x 4096 with rank 64 252 us (818 TFLOP/s; matrix units busy
 // 40 % of the cycles, 41 % of the waves' time waits), 2-bit 333 x 9728 x 2560 37 us in
@@ -34,7 +34,6 @@ namespace qmlp {
 namespace {
 
 typedef float f32x16_t __attribute__((ext_vector_type(16)));
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ f32x16_t mfma32(const uint4& a, const uint4& b, const f32x16_t& c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0,
@@ -298,8 +297,8 @@ __global__ void __launch_bounds__(BM / (32 * WM) * (BN / (32 * WN)) * 64) lora_g
         }
     }
 
-    // Step kt multiplies slot kt % ST of x and kt & 1 of the weights, while x of step kt + ST - 1 is under way, the
-    // codes of kt + 2 too, and the weights of kt + 1 are unpacked.
+    // Step kt multiplies slot kt % ST of x and kt & 1 of the weights, while x of the steps up to kt + ST - 1 and codes up
+    // to kt + 1 + QA are under way and the weights of kt + 1 are unpacked.
     if (stager)
         dequant_store<BITS, CPT>(wsm, q[0].w, q[0].m, trow, part);
     load_w(q[0], nk > QA ? QA : nk - 1);

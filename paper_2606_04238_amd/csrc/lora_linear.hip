@@ -21,14 +21,6 @@ namespace {
 constexpr int kPrepWaves = 8, kPrepRowGroups = 256;
 constexpr int kLoraPrepRows = 256;       // more rows: lora_prep_many_kernel
 
-typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-__device__ __forceinline__ f32x4_t mfma16_bf(const uint4& a, const uint4& b, f32x4_t c) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
-                                                   0, 0);
-}
-
-__device__ __forceinline__ float wave_sum(float v) { return group_sum<64>(v); }
-
 // s[r] += x[k .. k + 7] . (row r of A)[k .. k + 7], eight rows a.k apart.
 template <int NR>
 __device__ __forceinline__ void ranks_dot(float (&s)[NR], const LoraArgs& a, const uint16_t* xr, const uint16_t* ar, int k) {
@@ -308,7 +300,7 @@ __global__ void __launch_bounds__(kPrepWaves * 64) lora_prep_kernel(LoraArgs a) 
     __shared__ float red[kPrepWaves][NR];
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
-        const float v = wave_sum(s[r]);
+        const float v = group_sum<64>(s[r]);
         if (lane == 0)
             red[wave][r] = v;
     }
@@ -333,7 +325,7 @@ __device__ __forceinline__ void lora_row(const LoraArgs& a, int m, int id, float
     }
 #pragma unroll
     for (int r = 0; r < 8; ++r) {
-        const float v = wave_sum(s[r]);
+        const float v = group_sum<64>(s[r]);
         if (lane == 0)
             rs[wave * 8 + r] = v;
     }

@@ -33,6 +33,11 @@ __device__ __forceinline__ void swap16(uint32_t& a, uint32_t& b) {
 
 // LDS barrier that leaves vector-memory loads in flight: this wave's LDS
 // accesses complete, then the workgroup meets.
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4_t mfma16_bf(const uint4& a, const uint4& b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0,
+                                                   0, 0);
+}
 __device__ __forceinline__ void lds_barrier() {
     __asm__ volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
 }

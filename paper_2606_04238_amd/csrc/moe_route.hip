@@ -14,11 +14,6 @@
 namespace qmlp {
 namespace {
 
-__device__ __forceinline__ f32x4_t mfma16_bf(const uint4& a, const uint4& b, f32x4_t c) {
-    typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
-}
-
 constexpr int kRouteTok = 4, kRouteWaves = 4;
 
 // Few tokens: a workgroup owns an expert and four tokens and issues all its loads,

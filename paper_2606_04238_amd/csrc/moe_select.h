@@ -64,15 +64,14 @@ __device__ __forceinline__ int take_largest(Key (&key)[N], int lane, uint32_t& h
         return -1;
     int e = -1, some = 0;
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-        {
-            const uint64_t at = __ballot(key[i].hi == hi);
-            if (at && e < 0) {
-                e = 64 * i + __builtin_ctzll(at);
-                lo = (uint32_t)__builtin_amdgcn_readlane((int)key[i].lo, e & 63);
-            }
-            some += __builtin_popcountll(at);
+    for (int i = 0; i < N; ++i) {
+        const uint64_t at = __ballot(key[i].hi == hi);
+        if (at && e < 0) {
+            e = 64 * i + __builtin_ctzll(at);
+            lo = (uint32_t)__builtin_amdgcn_readlane((int)key[i].lo, e & 63);
         }
+        some += __builtin_popcountll(at);
+    }
     if (some > 1) {
         t = 0;
 #pragma unroll
@@ -149,17 +148,16 @@ __device__ __forceinline__ Chosen route_select(double (&v)[N], int E, int k, int
         }
         int n = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            {
-                const double u = fmin(v[i], (double)FLT_MAX);
-                const bool near = u >= from;
-                const bool q = lane + 64 * i < E && (all || (redo >> i & 1) || ((pairs >> k & 1) && near && u <= edge));
-                const uint64_t at = __ballot(q);
-                if (q)
-                    list[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0))] = (int16_t)(lane + 64 * i);
-                n += __builtin_popcountll(at);
-                in = all || near ? in : in & ~(1u << i);
-            }
+        for (int i = 0; i < N; ++i) {
+            const double u = fmin(v[i], (double)FLT_MAX);
+            const bool near = u >= from;
+            const bool q = lane + 64 * i < E && (all || (redo >> i & 1) || ((pairs >> k & 1) && near && u <= edge));
+            const uint64_t at = __ballot(q);
+            if (q)
+                list[n + __builtin_amdgcn_mbcnt_hi((uint32_t)(at >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)at, 0))] = (int16_t)(lane + 64 * i);
+            n += __builtin_popcountll(at);
+            in = all || near ? in : in & ~(1u << i);
+        }
         __asm__ volatile("s_waitcnt lgkmcnt(0)" ::: "memory");         // (the list is this wave's own)
         exact(n, [&](int e, double s) {
 #pragma unroll

@@ -125,8 +125,8 @@ __device__ __forceinline__ void place(OneWork<NM>& o, uint32_t x, uint32_t sums,
     o.xv = live ? x + chunk * o.rows * 16u : kPastEnd;
     o.sv = live ? sums + group * o.rows * 8u + 4u * part : kPastEnd;
 }
-template <int B, int G, int NM, bool SUMS>
-__device__ __forceinline__ void one_operand(uint4& a, const OneWork<NM>& o, int gs, int i, int lane) {
+template <int B, int G, int NM>
+__device__ __forceinline__ void one_operand(uint4& a, const OneWork<NM>& o, int gs, int i) {
     typedef Lay<B, G> Y;
     constexpr int CW = 32 / B, PER = Y::HALF || B == 4 ? 1 : 2;           // codes and operands per word
     const int w = i / PER, at = Y::HALF ? 2 * w : (w / Y::QW) * Y::WPG + w % Y::QW;
@@ -331,9 +331,9 @@ __device__ __forceinline__ void one_multiply(f32x4_t (&acc)[NM][RT], OneStep<B, 
         }
 }
 // Sums of the wave's steps first, first + kw, .. below ns: acc[m][t] of matrix m and
-// the 16 rows from row0 + 16 t on, not yet scaled by kTileUnscale.  S steps' loads
-// go out at once; `more` issues what else the wave will need behind them.  LOOP:
-// more than S steps per wave, the next S under way while S are multiplied.
+// the 16 rows from row0 + 16 t on, not yet scaled by kTileUnscale.  The first step's
+// loads go out at once, and `more` issues what else the wave will need behind its
+// weights; then a step's weights are under way while the one before is multiplied.
 template <int B, int G, int NM, int RT, bool SUMS, typename MORE>
 __device__ __forceinline__ void oneshot_products(f32x4_t (&acc)[NM][RT], const OneWork<NM>& o, int first, int ns, int kw,
                                                  int lane, MORE more) {
@@ -350,14 +350,14 @@ __device__ __forceinline__ void oneshot_products(f32x4_t (&acc)[NM][RT], const O
     one_load<B, G, NM, RT, SUMS>(s, o, gs, lane);
     more();
 #pragma unroll
-    for (int n = 0; n < AH; ++n) one_operand<B, G, NM, SUMS>(r[n], o, gs, n, lane);
+    for (int n = 0; n < AH; ++n) one_operand<B, G, NM>(r[n], o, gs, n);
     __builtin_amdgcn_sched_barrier(0);                     // every load above is issued before the first is waited for
     auto multiply = [&](bool last) {
         one_multiply<B, G, NM, RT, SUMS>(acc, s, o, gs, lane, [&](int n) {
             const int f = n + AH;
             const uint4 a = r[n % AH];
             if (!last || f < NA)
-                one_operand<B, G, NM, SUMS>(r[n % AH], o, f < NA ? gs : gs + kw, f % NA, lane);
+                one_operand<B, G, NM>(r[n % AH], o, f < NA ? gs : gs + kw, f % NA);
             return a;
         });
     };
@@ -530,8 +530,6 @@ __device__ __forceinline__ void operands_of_row(const uint16_t* x, int K, bool b
         put(r, e);
     }
 }
-
-
 
 }  // namespace
 }  // namespace qmlp

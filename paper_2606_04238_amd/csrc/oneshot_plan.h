@@ -6,8 +6,9 @@
 
 namespace qmlp {
 
-// Steps of a row (64 bytes of codes), and the waves that share them: as many as leave
-// each at least three, and at most 8.  (us, 4-bit rows of 2880, 23 steps, 21 experts:
+// Steps of a row (64 bytes of codes), and the waves that share them: twice as many as
+// long as a wave would have more than four, up to 8, so two to four steps each and
+// more past 32.  (us, 4-bit rows of 2880, 23 steps, 21 experts:
 // 4 waves 29.2, 6 30.9, 8 25.5; of 768, 6 steps, 104 experts: 2 waves 18.2, 4 20.2,
 // 6 30.7; 2-bit gate and up of 2880, 12 steps, 21 experts: 3 waves 40.2, 4 37.2, 6
 // 46.4, 8 41.5.)

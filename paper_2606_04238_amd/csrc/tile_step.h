@@ -1,5 +1,5 @@
 // One step of a 16-row tile of 2- or 4-bit codes on the matrix cores
-// (decode_tile.hip, select_linear.h): the layout of a step, its
+// (decode_tile.hip, and in half steps oneshot.h): the layout of a step, its
 // activations as matrix operands with their group sums, the weight loads and
 // the products.  The arithmetic is described at the top of decode_tile.hip.
 #pragma once
