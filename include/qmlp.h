@@ -512,6 +512,8 @@ qmlp_status qmlp_moe_route(const void *router, const float *bias, const void *x,
  * weighted sum, slots in order, is rounded once.
  * ws: qmlp_moe_layer_workspace_bytes(...) bytes, any contents, nothing kept
  * between calls; one call at a time per workspace.
+ * Up to four tokens of at most 40 experts qmlp_moe_route and qmlp_forward_moe
+ * are the faster way (one token of the 20B-class layer 26.9 us, here 35.2).
  */
 typedef struct {
     const void *router;      /* [E][d] binary16, 16-byte aligned */

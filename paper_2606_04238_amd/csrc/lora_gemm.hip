@@ -1,8 +1,10 @@
 // The linear with adapters of many requests at more than 16 rows (gfx950),
 // y = x W^T + s_a (x A_a^T) B_a^T, a dense product on the matrix cores:
 // weights are unpacked to binary16 in LDS, scale * (q - zero) rounded once (the
-// value qmlp_dequant gives; 2^-12 relative at most, as much as one rounding of
-// the output, and independent from group to group) and multiplied with
+// value qmlp_dequant gives; 2^-11 relative at most, as much as one rounding of
+// the output, and independent from weight to weight: 4-bit weights take a binary16
+// output from 2.1e-4 off 64 bits to 2.7e-4, and 2-bit ones, whose products with an
+// 11-bit scale mostly fit, leave it) and multiplied with
 // v_mfma_f32_32x32x16_f16.  bfloat16 rows come as binary16 times a power of two
 // (lora_linear.hip), so both types run the same products.
 //
@@ -23,9 +25,9 @@
 // LDS, chunk c of row r at c ^ ((r >> 1) & 7).  x is copied to LDS by the memory
 // system (ST slots, ST - 1 steps ahead); codes are in registers QA + 1 steps ahead
 // and unpacked into two buffers, one step ahead; one barrier per step.  Measured:
-// bfloat16 4096 x 6144 x 4096 with rank 64 252 us (818 TFLOP/s; matrix units busy
-// 40 % of the cycles, 41 % of the waves' time waits), 2-bit 333 x 9728 x 2560 37 us in
-// 228 tiles (1.3 waves a SIMD).
+// bfloat16 4096 x 6144 x 4096 with rank 64 252 to 262 us from run to run (788 to 818
+// TFLOP/s; matrix units busy 39 % of the cycles, 41 % of the waves' time waits), 2-bit
+// 333 x 9728 x 2560 37 us in 228 tiles (1.3 waves a SIMD).
 #include "lora_linear.h"
 #include "decode_launch.h"
 #include "oneshot.h"
