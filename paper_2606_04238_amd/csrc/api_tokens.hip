@@ -17,12 +17,21 @@ inline bool aligned16(const void* p) { return ((uintptr_t)p & 15u) == 0; }
 inline bool aligned4(const void* p) { return ((uintptr_t)p & 3u) == 0; }
 inline size_t round256(size_t v) { return (v + 255) & ~(size_t)255; }
 qmlp_status from_hip(hipError_t e) { return e == hipSuccess ? QMLP_OK : QMLP_ERR_HIP; }
+// An enumeration's number as a C caller passed it, any at all: to be refused it has to be looked at, and reading a
+// number that the enumeration does not have is undefined in C++.
+template <typename E>
+inline int number(const E& e) {
+    static_assert(sizeof(E) == sizeof(int), "an enumeration of the C interface");
+    int v;
+    __builtin_memcpy(&v, &e, sizeof v);
+    return v;
+}
 
 // ---------------------------------------------------------------- linear with adapters
 
 constexpr int kMaxRows = 1 << 20, kMaxStride = 1 << 21;    // 256 rows, or a column of 1024, within 32-bit offsets
 
-qmlp_status check_lora(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
+qmlp_status check_lora(const qmlp_qweight* w, const qmlp_adapters* ad, int M, int dtype) {
     const qmlp_status s = weight_check(w, 0);
     if (s != QMLP_OK)
         return s;
@@ -55,7 +64,7 @@ struct LoraSizes {
     size_t t, slots, xf, xo, xs, mixed, parts, x16;
     size_t all() const { return t + slots + xf + xo + xs + mixed + parts + x16; }
 };
-LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
+LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, int dtype) {
     const bool bf = dtype == QMLP_BF16, some = ad && ad->count > 0, few = lora_few_rows(M, w);
     LoraSizes z{};
     if (some) {
@@ -81,7 +90,7 @@ LoraSizes lora_sizes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp
 
 // A workspace for any number of rows up to M.  More rows can need less (fewer shares of k, none of them past 512 rows,
 // terms of mixed sets instead), but between these numbers the need grows with M.
-size_t lora_most_bytes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
+size_t lora_most_bytes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, int dtype) {
     size_t most = lora_sizes(w, ad, M, dtype).all();
     for (const int m : {kLoraFewTokens, kLoraMidRows, 128, 256, 384, 512})
         if (m < M && lora_sizes(w, ad, m, dtype).all() > most)
@@ -91,7 +100,7 @@ size_t lora_most_bytes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qm
 
 // ---------------------------------------------------------------- router
 
-qmlp_status check_route(int M, int d, int E, int k, int score, qmlp_dtype dtype) {
+qmlp_status check_route(int M, int d, int E, int k, int score, int dtype) {
     if (M < 0 || d <= 0 || E < 1 || k < 1 || k > E || d % 8 != 0)
         return QMLP_ERR_SHAPE;
     if (M > kMaxRows || E > kMoeExperts || k > kMoeTopk || d > (1 << 20) || (dtype != QMLP_F16 && dtype != QMLP_BF16) ||
@@ -104,7 +113,7 @@ size_t route_bytes(int M, int E) { return round256((size_t)M * E * 8 + ((size_t)
 
 // ---------------------------------------------------------------- MoE layer
 
-qmlp_status check_moe(const qmlp_moe* l, int M, qmlp_dtype dtype) {
+qmlp_status check_moe(const qmlp_moe* l, int M, int dtype) {
     if (!l)
         return QMLP_ERR_NULL;
     const qmlp_mlp& m = l->mlp;
@@ -159,15 +168,15 @@ MoeSizes moe_sizes(const qmlp_moe* l, int M) {
 extern "C" {
 
 size_t qmlp_linear_lora_workspace_bytes(const qmlp_qweight* w, const qmlp_adapters* ad, int M, qmlp_dtype dtype) {
-    if (check_lora(w, ad, M, dtype) != QMLP_OK)
+    if (check_lora(w, ad, M, number(dtype)) != QMLP_OK)
         return 0;
-    return lora_most_bytes(w, ad, M, dtype);
+    return lora_most_bytes(w, ad, M, number(dtype));
 }
 
 qmlp_status qmlp_linear_lora(const qmlp_qweight* w, const qmlp_adapters* ad, const int32_t* ids, const void* x,
                              int64_t ldx, int M, qmlp_dtype dtype, void* y, int64_t ldy, void* ws, size_t ws_bytes,
                              qmlp_stream stream) {
-    const qmlp_status s = check_lora(w, ad, M, dtype);
+    const qmlp_status s = check_lora(w, ad, M, number(dtype));
     if (s != QMLP_OK)
         return s;
     if (M == 0)
@@ -243,7 +252,7 @@ size_t qmlp_moe_route_workspace_bytes(int E, int M) {
 qmlp_status qmlp_moe_route(const void* router, const float* bias, const void* x, int M, int d, int E, int k,
                            qmlp_score score, qmlp_dtype dtype, int32_t* topk_idx, float* topk_w, void* ws,
                            size_t ws_bytes, qmlp_stream stream) {
-    const qmlp_status s = check_route(M, d, E, k, score, dtype);
+    const qmlp_status s = check_route(M, d, E, k, number(score), number(dtype));
     if (s != QMLP_OK)
         return s;
     if (M == 0)
@@ -261,12 +270,12 @@ qmlp_status qmlp_moe_route(const void* router, const float* bias, const void* x,
 }
 
 size_t qmlp_moe_layer_workspace_bytes(const qmlp_moe* layer, int M, qmlp_dtype dtype) {
-    return check_moe(layer, M, dtype) != QMLP_OK ? 0 : moe_sizes(layer, M).all();
+    return check_moe(layer, M, number(dtype)) != QMLP_OK ? 0 : moe_sizes(layer, M).all();
 }
 
 qmlp_status qmlp_moe_layer(const qmlp_moe* layer, const void* x, int M, qmlp_dtype dtype, void* y, void* ws,
                            size_t ws_bytes, qmlp_stream stream) {
-    const qmlp_status s = check_moe(layer, M, dtype);
+    const qmlp_status s = check_moe(layer, M, number(dtype));
     if (s != QMLP_OK)
         return s;
     if (M == 0)
