@@ -27,9 +27,10 @@
 // Arithmetic.  That of decode_tile.hip but for the powers of two: a code at fraction
 // bits j.. of a binary16 2^(14 - j) reads 2^(14 - j) + 16 q, whatever j is, so the
 // activations are operands as they are.  (Beside 1024 + q 2^j they would be multiplied
-// by 2^(4 - j), j up to 8, and rounded to binary16 again: rows of 1e-4 were off by
-// 1.4e-3 at 2 bits and 5.7e-4 at 4, where the output's own rounding is 2.8e-4.)  The
-// offsets' sum is C = sum of 2^(14 - j) x, that of the zero points X = 16 sum of x.
+// by 2^(4 - j), j up to 8, and rounded to binary16 again: 16 rows of 1e-4, k = 1024,
+// were 3.4e-3 off 64 bits at 2 bits and 1.3e-3 at 4, where the output's own rounding,
+// all that is left now, is 2.1e-4.)  The offsets' sum is C = sum of 2^(14 - j) x, that
+// of the zero points X = 16 sum of x.
 #pragma once
 
 #include "oneshot_plan.h"
