@@ -527,6 +527,143 @@ size_t qmlp_moe_layer_workspace_bytes(const qmlp_moe *layer, int M, qmlp_dtype d
 qmlp_status qmlp_moe_layer(const qmlp_moe *layer, const void *x, int M, qmlp_dtype dtype, void *y, void *ws,
                            size_t ws_bytes, qmlp_stream stream);
 
+/* ------------------------- attention over a cache of keys and values in 4 bits */
+
+/*
+ * What lies between a decoder layer's q/k/v projection (qmlp_linear_batch,
+ * qmlp_linear_lora) and its output projection, for a batch of requests whose
+ * keys and values stay in a paged cache: the pages of a step's tokens
+ * (qmlp_kv_plan), norm, rotation and the write (qmlp_qk_norm_rope), attention
+ * (qmlp_kv_attention).  Every array is on the device and nothing is read on
+ * the host, so a decoding step, its growth by new pages included, can be
+ * captured once and replayed.
+ *
+ * Storage format of the cache.  A page holds `page` tokens of one layer:
+ *   data [pages][kv_heads][2][page * (head_dim/2 + 4)] bytes, K then V: the
+ * codes of the page's tokens, then binary16 (scale, zero) of each.  One group is
+ * one token's head_dim numbers of one head; its quantizer is that of the
+ * weights at b = 4 (scale and zero as above, value scale * (code - zero)); a
+ * group that holds an infinity or NaN, or whose scale passes 65504, is stored as
+ * scale NaN, zero 0, codes 0 and reads back as NaN.  Eight codes are a 32-bit
+ * word: dims 8w + 0..7 at nibbles 0, 4, 1, 5, 2, 6, 3, 7 of word w.  Words of K
+ * are [token][head_dim/8]; words of V [token / 4][head_dim/8][token % 4].
+ * A slot is page number * page + place in the page; -1 is no slot.
+ * head_dim 64 or 128; page 16, 32, 64, 128 or 256; fewer than 2^31 slots.
+ */
+typedef struct {
+    void *data;             /* qmlp_kv_cache_bytes() bytes, 16-byte aligned */
+    int32_t pages, kv_heads, head_dim, page;
+} qmlp_kv_cache;
+
+/* Bytes of a cache; 0 for one that is not supported. */
+size_t qmlp_kv_cache_bytes(int pages, int kv_heads, int head_dim, int page);
+
+/*
+ * The pages of one step.  Request b has lens[b] tokens in the cache and adds
+ * new_tokens[b]; -1 (or less) ends it.  table [B][W] holds each request's page
+ * numbers in order; free_pages [N] is a stack of unused pages with n_free[0] of
+ * them.  In this order:
+ *  1. the pages of ended requests, ceil(lens/page) each, are pushed on the
+ *     stack, requests and their pages in order (what would pass N is dropped);
+ *  2. a growing request that lacks pages takes them from the top of the stack,
+ *     requests in order, page after page, into its row of the table.  A request gets all it needs or is
+ *     refused: it is refused if its tokens would pass W pages, if the step's tokens up to
+ *     its last pass `tokens`, or if what it and those before it need (the
+ *     ones that lacked pages counted) passes the stack.
+ * starts [B+1]: the first token of each request among the step's, the sums of
+ * the new tokens (refused ones too, ended ones none; at most 2^31 - 1).  positions and
+ * slots [tokens]: place in its request and slot of every token; slot -1 for
+ * the tokens of refused requests; past the last token position 0, slot -1.
+ * lens_out [B]: lens + new, lens for a refused request, 0 for an ended one.
+ * n_free_out[0]; short_out[0]: requests refused.  lens_out may be lens and
+ * n_free_out may be n_free (a chain of steps); otherwise no two arrays overlap.
+ * Entries of the table past a request's pages are left as they are, those of an
+ * ended request too, and stack places that nothing is pushed to: the same
+ * call on the same lens and n_free gives the same again.
+ * lens outside [0, W page] and n_free outside [0, N] are taken as the nearest number inside.
+ * 0 <= B <= 4096, 1 <= W <= 2^20, W * page < 2^31, 0 <= N, 0 <= tokens <= 2^24.  One launch
+ * (none with B = 0: nothing is written).
+ */
+qmlp_status qmlp_kv_plan(const int32_t *lens, const int32_t *new_tokens, int B, int page, int32_t *table, int W,
+                         int32_t *free_pages, int N, const int32_t *n_free, int tokens, int32_t *slots,
+                         int32_t *positions, int32_t *starts, int32_t *lens_out, int32_t *n_free_out,
+                         int32_t *short_out, qmlp_stream stream);
+
+/* Which dims of a head turn together: (i, i + rot/2), or (2i, 2i + 1). */
+typedef enum { QMLP_PAIRS_HALF = 0, QMLP_PAIRS_NEXT = 1 } qmlp_pairs;
+
+/*
+ * Queries and keys of T tokens, one launch: each head x of q and k becomes
+ *   u = x / sqrt(mean(x^2) + eps) * weight      (weight NULL: u = x),
+ *   (u_i, u_j) -> mul (u_i cos a - u_j sin a, u_j cos a + u_i sin a) with
+ *   a = positions[t] inv_freq[p] for the p-th pair of the first `rot` dims
+ *   (inv_freq NULL: no rotation),
+ * rounded once to the activation type; q goes to q_out, k to k_out (or NULL)
+ * and, with a cache, k and v of the tokens with a slot in [0, slots of the cache)
+ * are quantized from the activation type and written there.  q, k and v are
+ * rows ldq, ldk, ldv elements apart with their heads side by side (views of one
+ * q/k/v row, for instance).  q_out may be q and k_out may be k, at the same
+ * address and stride; otherwise outputs overlap nothing.  q arithmetic is fp32 and k's fp64 (a code
+ * hangs on the last bits of numbers next to a border), angles are reduced in fp64.
+ */
+typedef struct {
+    const void *q, *k, *v;              /* [T][heads or kv_heads][head_dim], 16-byte aligned; v only with a cache */
+    int64_t ldq, ldk, ldv;              /* elements from row to row, multiples of 8 */
+    void *q_out, *k_out;
+    int64_t ldq_out, ldk_out;
+    const void *q_weight, *k_weight;    /* [head_dim] activation type, 16-byte aligned, or NULL */
+    const int32_t *positions;           /* [T] (with inv_freq) */
+    const float *inv_freq;              /* [rot/2], or NULL */
+    const int32_t *slots;               /* [T] (with a cache) */
+    int32_t heads, kv_heads, head_dim;  /* head_dim 64 or 128; heads may be 0 (q and q_out unused) */
+    int32_t rot;                        /* a multiple of 16, 16 .. head_dim (with inv_freq) */
+    int32_t pairs;                      /* qmlp_pairs */
+    float eps, mul;                     /* eps >= 0 */
+} qmlp_heads;
+
+/* cache may be NULL (k_out then receives k).  0 <= T <= 2^20.  Two tokens with the same
+ * slot leave a mixture of the two there. */
+qmlp_status qmlp_qk_norm_rope(const qmlp_heads *h, int T, qmlp_dtype dtype, const qmlp_kv_cache *cache,
+                              qmlp_stream stream);
+
+/* What the cache holds at slots [T]: k and v [T][kv_heads][head_dim] (either may be
+ * NULL) rounded once to the type (past its largest number: infinity); zeros for a slot outside the
+ * cache.  T * kv_heads at most 2^27. */
+qmlp_status qmlp_kv_read(const qmlp_kv_cache *cache, const int32_t *slots, int T, qmlp_dtype dtype, void *k, void *v,
+                         qmlp_stream stream);
+
+/*
+ * Causal attention of a step's tokens over the cached keys and values, their
+ * own among them.  Request b has lens[b] tokens in the cache, the last n =
+ * starts[b+1] - starts[b] of them this step's: rows starts[b] + i of q and y,
+ * at position p = lens[b] - n + i (starts NULL: T == B and one row each).
+ * Head g reads K/V head g / (heads / kv_heads):
+ *   y = sum_j w_j V_j / (sum_j w_j + exp(sinks[g])),  w_j = exp(scale q . K_j),
+ * j over max(0, p - window + 1) .. p (window 0: from 0), sinks NULL: no such term.
+ * A row that sees nothing is zeros.  A page number outside the cache hides its tokens.
+ * table [B][W]; lens past W pages count as W pages.  q and y [T][heads][head_dim] in
+ * rows ldq and ldy elements apart.  Rows of y before starts[0] and from starts[B] on
+ * are left as they are (starts has to be rising, 0 <= starts <= T; rows past T are not touched).
+ * Codes enter the products as exact integers; scores, sums and outputs are fp32; weights times the
+ * value's scale are rounded to binary16, with a power of two that keeps 2^-22 of the largest normal.
+ * Keys or values that are NaN, and rows of q with an infinity or NaN, make the rows that
+ * see them NaN and no others.
+ * max_new: the most new tokens of any request, as far as the host knows.  It chooses kernels and sizes
+ * the workspace; a request with more is computed all the same, slower.
+ * heads a multiple of kv_heads, 0 <= B <= 4096, 0 <= T <= 2^20, 1 <= W, W * page < 2^31, scale finite,
+ * window >= 0.
+ * ws: qmlp_kv_attention_workspace_bytes(...) of this or a larger max_new, ZERO before its first call (and after
+ * a call that failed); each call leaves it ready for the next, of any shape it is large enough for.  One call at
+ * a time per workspace.
+ */
+size_t qmlp_kv_attention_workspace_bytes(const qmlp_kv_cache *cache, int heads, int max_new);
+
+qmlp_status qmlp_kv_attention(const qmlp_kv_cache *cache, const void *q, int64_t ldq, int T, int heads,
+                              qmlp_dtype dtype, const int32_t *table, int W, const int32_t *lens,
+                              const int32_t *starts, int B, int max_new, float scale, int window,
+                              const float *sinks, void *y, int64_t ldy, void *ws, size_t ws_bytes,
+                              qmlp_stream stream);
+
 /* ---------------------------------------------- inspection (not timed) */
 
 /*

@@ -15,6 +15,8 @@ Functions keep the names of the C entry points:
 * ``forward_stack``               -- L blocks on a residual stream, x_{l+1} = x_l + block_l(RMSNorm(x_l))
 * ``linear_lora``                 -- a linear with adapters of many requests, y[m] = W x[m] + s_a B_a (A_a x[m])
 * ``moe_route`` / ``moe_layer``   -- a router's top-k choice and weights; a whole MoE layer for a few tokens
+* ``kv_plan`` / ``qk_norm_rope`` / ``kv_read`` / ``kv_attention`` -- a step's pages and slots, head norms and rotation with
+  the write into a 4-bit cache of keys and values, what the cache holds, causal attention over it
 * ``unpack`` / ``dequant``        -- inspection of a packed matrix (not timed)
 """
 from __future__ import annotations
@@ -63,6 +65,19 @@ class MoeC(ctypes.Structure):
                 ("topk", ctypes.c_int32), ("score", ctypes.c_int32), ("mlp", MlpC)]
 
 
+class KVCacheC(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("pages", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page", ctypes.c_int32)]
+
+
+class HeadsC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("q", "k", "v")] + [(n, ctypes.c_int64) for n in ("ldq", "ldk", "ldv")] + \
+               [(n, ctypes.c_void_p) for n in ("q_out", "k_out")] + [(n, ctypes.c_int64) for n in ("ldq_out", "ldk_out")] + \
+               [(n, ctypes.c_void_p) for n in ("q_weight", "k_weight", "positions", "inv_freq", "slots")] + \
+               [(n, ctypes.c_int32) for n in ("heads", "kv_heads", "head_dim", "rot", "pairs")] + \
+               [(n, ctypes.c_float) for n in ("eps", "mul")]
+
+
 _LIB = None
 
 
@@ -78,6 +93,7 @@ def _lib():
         pm = ctypes.POINTER(MlpC)
         po = ctypes.POINTER(MoeC)
         pa, L = ctypes.POINTER(AdaptersC), ctypes.c_int64
+        pc, F = ctypes.POINTER(KVCacheC), ctypes.c_float
         sig = {
             "qmlp_codes_bytes": (Z, [I, I, I]),
             "qmlp_meta_bytes": (Z, [I, I, I]),
@@ -115,6 +131,12 @@ def _lib():
             "qmlp_moe_layer_workspace_bytes": (Z, [po, I, I]),
             "qmlp_moe_layer": (I, [po, P, I, I, P, P, Z, P]),
             "qmlp_linear_lora": (I, [pq, pa, P, P, L, I, I, P, L, P, Z, P]),
+            "qmlp_kv_cache_bytes": (Z, [I, I, I, I]),
+            "qmlp_kv_plan": (I, [P, P, I, I, P, I, P, I, P, I, P, P, P, P, P, P, P]),
+            "qmlp_qk_norm_rope": (I, [ctypes.POINTER(HeadsC), I, I, pc, P]),
+            "qmlp_kv_read": (I, [pc, P, I, I, P, P, P]),
+            "qmlp_kv_attention_workspace_bytes": (Z, [pc, I, I]),
+            "qmlp_kv_attention": (I, [pc, P, L, I, I, I, P, I, P, P, I, I, F, I, P, P, L, P, Z, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(lib, name)
@@ -664,6 +686,207 @@ def moe_layer(moe: MoE, x: torch.Tensor, y: torch.Tensor | None = None, ws: torc
     here = _one_device(x, y, ws, moe.router)
     _check(_lib().qmlp_moe_layer(ctypes.byref(moe._c), _addr(x), M, F16, _addr(y), _addr(ws), ws.numel(),
                                  torch._C._cuda_getCurrentRawStream(here)), "moe_layer")
+    return y
+
+
+class KVCache:
+    """A paged cache of keys and values in 4 bits: ``data`` uint8 [pages][kv_heads][2][page * (head_dim/2 + 4)] on the
+    device (the storage format of qmlp_kv_cache; kv_cache makes an empty one)."""
+
+    def __init__(self, data: torch.Tensor, page: int):
+        if data.dim() != 4 or data.dtype != torch.uint8 or data.shape[2] != 2 or not data.is_contiguous() or \
+                page < 1 or data.shape[3] % page or data.shape[3] // page not in (36, 68):
+            raise ValueError("data must be contiguous uint8 [pages][kv_heads][2][page * (head_dim/2 + 4)], head_dim 64 or 128")
+        self.data, self.page = data, int(page)
+        self.pages, self.kv_heads = int(data.shape[0]), int(data.shape[1])
+        self.head_dim = 2 * (int(data.shape[3]) // self.page - 4)
+        if not _lib().qmlp_kv_cache_bytes(self.pages, self.kv_heads, self.head_dim, self.page):
+            raise QmlpError(4, "KVCache")
+        self._c = KVCacheC(data.data_ptr(), self.pages, self.kv_heads, self.head_dim, self.page)
+
+    def c(self) -> KVCacheC:
+        return self._c
+
+
+def kv_cache(pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> KVCache:
+    """An empty cache (all zeros)."""
+    return KVCache(torch.zeros((pages, kv_heads, 2, page * (head_dim // 2 + 4)), dtype=torch.uint8, device=device), page)
+
+
+def _ints(n, what, *tensors):
+    for t in tensors:
+        if t is not None and (t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous()):
+            raise ValueError("%s must be int32 [%d], contiguous" % (what, n))
+
+
+class KVPlan:
+    """What kv_plan writes for up to ``B`` requests and ``tokens`` new tokens of a step: int32 ``slots`` and ``positions``
+    [tokens], ``starts`` [B + 1], ``lens`` [B], ``n_free`` [1], ``short`` [1] (requests refused)."""
+
+    def __init__(self, B: int, tokens: int, device="cuda", lens: torch.Tensor | None = None,
+                 n_free: torch.Tensor | None = None):
+        new = lambda n: torch.empty(n, dtype=torch.int32, device=device)
+        self.slots, self.positions, self.starts, self.short = new(tokens), new(tokens), new(B + 1), new(1)
+        self.lens, self.n_free = new(B) if lens is None else lens, new(1) if n_free is None else n_free
+        _ints(B, "lens", self.lens)
+        _ints(1, "n_free", self.n_free)
+
+
+def kv_plan(plan: KVPlan, lens: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free: torch.Tensor,
+            n_free: torch.Tensor, page: int) -> KVPlan:
+    """The pages of a step (qmlp_kv_plan): requests with ``lens`` cached tokens add ``new`` (-1: ended, pages back on the
+    stack ``free`` of ``n_free``); ``table`` [B][W] grows in place and ``plan`` takes starts, slots, positions and the new
+    lens and n_free (which may be the same tensors as the old ones).  All int32."""
+    B = lens.shape[0]
+    _ints(B, "lens and new", lens, new, plan.lens)
+    _ints(B + 1, "plan.starts", plan.starts)
+    _ints(1, "n_free", n_free)
+    _ints(free.shape[0], "free", free)
+    if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or not table.is_contiguous():
+        raise ValueError("table must be int32 [B][W], contiguous")
+    here = _one_device(lens, new, table, free, n_free, plan.slots, plan.positions, plan.starts, plan.lens, plan.n_free, plan.short)
+    _check(_lib().qmlp_kv_plan(_addr(lens), _addr(new), B, page, _addr(table), table.shape[1], _addr(free), free.shape[0],
+                               _addr(n_free), plan.slots.shape[0], _addr(plan.slots), _addr(plan.positions),
+                               _addr(plan.starts), _addr(plan.lens), _addr(plan.n_free), _addr(plan.short),
+                               torch._C._cuda_getCurrentRawStream(here)), "kv_plan")
+    return plan
+
+
+PAIRS = {"half": 0, "next": 1}
+
+
+def _head_rows(t, what, T, D, dtype):
+    """The row stride of [T][heads][D] with the heads of a row side by side."""
+    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or t.dtype != dtype:
+        raise ValueError("%s must be [T][heads][head_dim] of q's type" % what)
+    H = t.shape[1]
+    if t.stride(2) != 1 or (H > 1 and t.stride(1) != D):
+        raise ValueError("the heads of a row of %s must lie side by side" % what)
+    return t.stride(0) if T > 1 else H * D
+
+
+def qk_norm_rope(q: torch.Tensor | None, k: torch.Tensor | None, positions: torch.Tensor | None = None,
+                 inv_freq: torch.Tensor | None = None, q_weight: torch.Tensor | None = None,
+                 k_weight: torch.Tensor | None = None, eps: float = 1e-6, pairs: str = "half", mul: float = 1.0,
+                 q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, cache: KVCache | None = None,
+                 v: torch.Tensor | None = None, slots: torch.Tensor | None = None):
+    """RMS norm of each head (with a weight) and rotation by position (with inv_freq float32 [rot/2]; positions int32 [T])
+    of q [T][heads][D] and k [T][kv_heads][D]; with a cache, k and v are quantized into it at slots int32 [T] (negative: not
+    written).  Returns (q_out, k_out); without a cache k_out is made if it is not given, with one it is None unless given.
+    q_out may be q and k_out may be k."""
+    x = q if q is not None else k
+    if x is None or x.dim() != 3:
+        raise ValueError("q or k must be given, [T][heads][head_dim]")
+    T, _, D = x.shape
+    code = _dtype_code(x)
+    h = HeadsC()
+    if q is not None:
+        if q_out is None:
+            q_out = torch.empty((T, q.shape[1], D), dtype=q.dtype, device=q.device)
+        if q_out.shape != q.shape:
+            raise ValueError("q_out must have q's shape")
+        h.ldq, h.ldq_out, h.heads = _head_rows(q, "q", T, D, x.dtype), _head_rows(q_out, "q_out", T, D, x.dtype), q.shape[1]
+        h.q, h.q_out = _addr(q), _addr(q_out)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    if k is not None:
+        if k_out is None and cache is None:
+            k_out = torch.empty((T, k.shape[1], D), dtype=k.dtype, device=k.device)
+        h.ldk, h.kv_heads, h.k = _head_rows(k, "k", T, D, x.dtype), k.shape[1], _addr(k)
+        if k_out is not None:
+            if k_out.shape != k.shape:
+                raise ValueError("k_out must have k's shape")
+            h.ldk_out, h.k_out = _head_rows(k_out, "k_out", T, D, x.dtype), _addr(k_out)
+    elif k_out is not None or cache is not None:
+        raise ValueError("a cache and k_out need k")
+    if (cache is None) != (v is None) or (cache is None) != (slots is None):
+        raise ValueError("cache, v and slots go together")
+    if cache is not None:
+        if v.shape != k.shape:
+            raise ValueError("v must have k's shape")
+        _ints(T, "slots", slots)
+        h.ldv, h.v, h.slots = _head_rows(v, "v", T, D, x.dtype), _addr(v), _addr(slots)
+    if (inv_freq is None) != (positions is None):
+        raise ValueError("positions and inv_freq go together")
+    if inv_freq is not None:
+        _ints(T, "positions", positions)
+        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+            raise ValueError("inv_freq must be float32 [rot/2], contiguous")
+        h.positions, h.inv_freq, h.rot = _addr(positions), _addr(inv_freq), 2 * inv_freq.shape[0]
+    for w in (q_weight, k_weight):
+        if w is not None and (w.dtype != x.dtype or w.shape != (D,) or not w.is_contiguous()):
+            raise ValueError("weights must be [head_dim] of q's type, contiguous")
+    h.q_weight, h.k_weight = _addr(q_weight), _addr(k_weight)
+    h.head_dim, h.pairs, h.eps, h.mul = D, PAIRS[pairs], eps, mul
+    here = _one_device(q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, slots, cache.data if cache else None)
+    _check(_lib().qmlp_qk_norm_rope(ctypes.byref(h), T, code, ctypes.byref(cache._c) if cache else None,
+                                    torch._C._cuda_getCurrentRawStream(here)), "qk_norm_rope")
+    return q_out, k_out
+
+
+def kv_read(cache: KVCache, slots: torch.Tensor, k: torch.Tensor | None = None, v: torch.Tensor | None = None,
+            dtype=torch.float16):
+    """(k, v) [T][kv_heads][head_dim] as the cache holds them at slots int32 [T]; zeros for a slot outside it.  Both are
+    made if neither is given; else the given ones are written."""
+    T, shape = slots.shape[0], (slots.shape[0], cache.kv_heads, cache.head_dim)
+    _ints(T, "slots", slots)
+    if k is None and v is None:
+        k, v = (torch.empty(shape, dtype=dtype, device=slots.device) for _ in range(2))
+    for t in (k, v):
+        if t is not None and (tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != (k if k is not None else v).dtype):
+            raise ValueError("k and v must be [T][kv_heads][head_dim], contiguous and of one type")
+    code = _dtype_code(k if k is not None else v)
+    here = _one_device(slots, k, v, cache.data)
+    _check(_lib().qmlp_kv_read(ctypes.byref(cache._c), _addr(slots), T, code, _addr(k), _addr(v),
+                               torch._C._cuda_getCurrentRawStream(here)), "kv_read")
+    return k, v
+
+
+def kv_attention_workspace_bytes(cache: KVCache, heads: int, max_new: int) -> int:
+    return int(_lib().qmlp_kv_attention_workspace_bytes(ctypes.byref(cache._c), heads, max_new))
+
+
+def kv_attention_workspace(q: torch.Tensor, cache: KVCache, table: torch.Tensor | None = None, max_new: int = 1) -> torch.Tensor:
+    """A zeroed workspace for kv_attention of steps with up to max_new new tokens a request (zero it again after a call
+    that failed)."""
+    return torch.zeros(max(kv_attention_workspace_bytes(cache, q.shape[1], max_new), 256), dtype=torch.uint8, device=q.device)
+
+
+def kv_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: torch.Tensor, starts: torch.Tensor | None = None,
+                 y: torch.Tensor | None = None, max_new: int | None = None, scale: float | None = None, window: int = 0,
+                 sinks: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
+    """y [T][heads][D]: causal attention of a step's rows q over the cache.  Request b has lens[b] cached tokens, pages
+    table[b], and the rows starts[b] .. starts[b+1] (None: one row each), which are its last tokens.  scale: head_dim^-0.5
+    unless given; window: tokens a row sees, itself among them (0: all); sinks float32 [heads] or None.  max_new: the most new tokens of a request
+    (a bound chooses kernels; unless given 1 without starts, T with them).  Rows before starts[0] and from starts[B] on are left as
+    they are (a y made here starts at zeros)."""
+    if q.dim() != 3:
+        raise ValueError("q must be [T][heads][head_dim]")
+    T, H, D = q.shape
+    code = _dtype_code(q)
+    if D != cache.head_dim:
+        raise ValueError("q and the cache differ in head_dim")
+    if y is None:
+        y = torch.zeros((T, H, D), dtype=q.dtype, device=q.device)
+    elif y.shape != q.shape:
+        raise ValueError("y must have q's shape")
+    ldq, ldy = _head_rows(q, "q", T, D, q.dtype), _head_rows(y, "y", T, D, q.dtype)
+    B = lens.shape[0]
+    _ints(B, "lens", lens)
+    _ints(B + 1, "starts", starts)
+    if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or not table.is_contiguous():
+        raise ValueError("table must be int32 [B][W], contiguous")
+    if sinks is not None and (sinks.dtype != torch.float32 or sinks.shape != (H,) or not sinks.is_contiguous()):
+        raise ValueError("sinks must be float32 [heads]")
+    if max_new is None:
+        max_new = T if starts is not None else 1
+    if ws is None:
+        ws = kv_attention_workspace(q, cache, table, max_new)
+    here = _one_device(q, y, table, lens, starts, sinks, ws, cache.data)
+    _check(_lib().qmlp_kv_attention(ctypes.byref(cache._c), _addr(q), ldq, T, H, code, _addr(table), table.shape[1], _addr(lens),
+                                    _addr(starts), B, max_new, D ** -0.5 if scale is None else scale, window, _addr(sinks),
+                                    _addr(y), ldy, _addr(ws), ws.numel(), torch._C._cuda_getCurrentRawStream(here)),
+           "kv_attention")
     return y
 
 
