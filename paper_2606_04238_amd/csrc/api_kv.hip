@@ -91,7 +91,7 @@ qmlp_status qmlp_kv_plan(const int32_t* lens, const int32_t* new_tokens, int B, 
         return QMLP_ERR_UNSUPPORTED;
     if (B < 0 || W < 1 || N < 0 || tokens < 0)
         return QMLP_ERR_SHAPE;
-    if (B > kKvRequests || W > (1 << 20) || (int64_t)W * page >= (1ll << 31) || tokens > (1 << 24))
+    if (B > kKvRequests || W > (1 << 20) || (int64_t)W * page > (1ll << 30) || tokens > (1 << 24))
         return QMLP_ERR_UNSUPPORTED;
     if (B == 0)
         return QMLP_OK;
@@ -220,7 +220,7 @@ qmlp_status qmlp_kv_attention(const qmlp_kv_cache* cache, const void* q, int64_t
         return s;
     if (B < 0 || W < 1 || window < 0 || (!starts && T != B))
         return QMLP_ERR_SHAPE;
-    if (B > kKvRequests || (int64_t)W * cache->page >= (1ll << 31) || !isfinite(scale))
+    if (B > kKvRequests || (int64_t)W * cache->page > (1ll << 30) || !isfinite(scale))
         return QMLP_ERR_UNSUPPORTED;
     if (T == 0 || B == 0)
         return QMLP_OK;

@@ -1,101 +1,387 @@
-// Causal attention over the 4-bit cache (gfx950): the simple form, a workgroup a row and head.
+// Causal attention over the 4-bit cache for a few rows a request (decoding), gfx950.
 //
-// scores s_j = scale q . K_j (log2 units), w_j = 2^(s_j - max), y = sum w_j V_j / (sum w_j + sink),
-// with the maximum and the sum carried along (one pass over the tokens).
-#include "kv_cache.h"
-#include "qmlp_device.h"
+//   s_j = scale q . K_j,  w_j = 2^(s_j log2(e) - m),  y = sum_j w_j V_j / (sum_j w_j + sink)
+//
+// One pass over the tokens, the maximum m and the sum carried along.  What bounds it is reading the cache
+// (D + 8 bytes a token and head), so all heads that share a K/V head, and the rows of a request, are one
+// operand of up to 16 rows, and codes go from the loads to the matrix cores in registers: the cache's layout
+// is the operands'.  K: a lane's D/4 dims of one token, codes as 64 + code; with u = sum q the offset comes off as
+// s = scale_K (sum q (64 + c) - (64 + zero) u).  The product is transposed (tokens down, rows
+// across), so that a lane's eight weights are those of one row and go on as the second product's operand without
+// moving.  V: a lane's words are 4 tokens' same 8 dims; halves of two tokens' words side by side give the pairs.
+// Weights times the values' scales are rounded to binary16 (fp32 sums of exact products after that), and the zeros come
+// off through one more product of the same weights with 64 + zero.
+//
+// The rounding to binary16 is made where weights are at most 2^15 and, when the maximum is taken anew, 2^8: normal
+// numbers down to 2^-22 of the largest.  m moves only when a weight would pass 2^15.
+#include "kv_device.h"
+#include "qmlp_internal.h"
 
 namespace qmlp {
 namespace {
 
+constexpr int kRows = 16, kStep = 128;                    // rows of a tile; tokens of a workgroup's step, 32 a wave
+
+// One tile of 16 tokens as its lanes hold it.
 template <int D>
-__global__ void __launch_bounds__(64) simple_kernel(AttnArgs a) {
-    __shared__ float qs[D], ws[64], os[D];
-    const int t = blockIdx.x, g = blockIdx.y, lane = threadIdx.x, lg = a.cache.page_log2;
-    // the request of row t
-    int b = -1;
-    if (a.starts) {
-        for (int i = 0; i < a.B && b < 0; ++i)
-            if (t >= a.starts[i] && t < a.starts[i + 1])
-                b = i;
+struct Tile {
+    uint32_t k[D / 32];                                   // D/4 dims of token lane & 15
+    uint4 v;                                              // 8 dims of 4 tokens
+    uint4 km, vm;                                         // (scale, zero) of 4 tokens
+};
+
+template <int D>
+__device__ __forceinline__ void load_tile(Tile<D>& t, const AttnArgs& a, int pid, int head, int in_page) {
+    const uint32_t lane = threadIdx.x & 63, h = lane >> 4, r = lane & 15, side = a.cache.side(D);
+    const uint8_t* base = a.cache.at(D, pid, head);
+    const uint8_t* codes = base + (uint32_t)in_page * (D / 2);
+    const uint8_t* meta = base + ((uint32_t)(D / 2) << a.cache.page_log2) + (uint32_t)in_page * 4u;
+    if constexpr (D == 128) {
+        const u32x4 k = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + r * 64u + h * 16u));
+        t.k[0] = k.x;
+        t.k[1] = k.y;
+        t.k[2] = k.z;
+        t.k[3] = k.w;
     } else {
-        b = t;
+        const uint2 k = *reinterpret_cast<const uint2*>(codes + r * 32u + h * 8u);
+        t.k[0] = k.x;
+        t.k[1] = k.y;
     }
-    if (b < 0)
-        return;
-    const int len = min(max(a.lens[b], 0), a.W << lg);
-    const int s0 = a.starts ? a.starts[b] : t, n = a.starts ? a.starts[b + 1] - s0 : 1;
-    const int pos = len - n + t - s0, first = a.window ? max(0, pos - a.window + 1) : 0;
-    for (int i = lane; i < D; i += 64) {
-        const uint32_t v = a.q[t * a.ldq + (long)g * D + i];
-        qs[i] = a.bf ? __uint_as_float(v << 16) : h2f(v);
-        os[i] = 0.0f;
-    }
-    __syncthreads();
-    float m = -1e30f, l = 0.0f, o[D / 64] = {};
-    for (int j0 = first; j0 <= pos; j0 += 64) {
-        const int j = j0 + lane;
-        float s = -INFINITY;
-        int p = -1;
-        if (j <= pos) {
-            p = a.table[(long)b * a.W + (j >> lg)];
-            if (p >= 0 && p < a.cache.pages) {
-                const int in = j & ((1 << lg) - 1);
-                const uint32_t* kw = reinterpret_cast<const uint32_t*>(a.cache.at(D, p, g / a.G));
-                const uint32_t mt = kw[((D / 8) << lg) + in];
-                const float z = h2f(mt >> 16);
-                float acc = 0.0f;
-                for (int w = 0; w < D / 8; ++w) {
-                    const uint32_t c = kw[in * (D / 8) + w];
-                    for (int i = 0; i < 8; ++i)
-                        acc += qs[8 * w + i] * ((float)((c >> (4 * ((i >> 1) + 4 * (i & 1)))) & 15u) - z);
+    t.v = load_stream(reinterpret_cast<const uint4*>(codes + side + h * (2u * D) + (r & (D / 8 - 1)) * 16u));
+    t.km = *reinterpret_cast<const uint4*>(meta + h * 16u);
+    t.vm = *reinterpret_cast<const uint4*>(meta + side + h * 16u);
+}
+
+// Work is cut evenly over the workgroups (see prefix_work): a unit is one step of one item, an item a tile
+// of rows of one K/V head.  A workgroup's range can begin and end inside items; what it has of those goes to the
+// workspace, two places a workgroup, and the last to come to an item (a counter at the item's first workgroup) joins
+// its parts.
+template <int D>
+__global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
+    constexpr int NT = D / 16, LD = D + 4;                // tiles of outputs; row of LDS
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    float* lo = reinterpret_cast<float*>(smem);           // [4][16][LD]
+    __shared__ float lm[4][kRows], ll[4][kRows];
+    __shared__ uint32_t arrived;
+    int64_t* sums = reinterpret_cast<int64_t*>(smem + 4 * kRows * LD * 4);
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 4, col = lane & 15;
+    const int lg = a.cache.page_log2, Hk = a.cache.heads;
+
+    auto first_step = [&](const Request& q) {             // the first token any row sees, in steps
+        const int p = q.len - q.n - a.window + 1;
+        return a.window && p > 0 ? p / kStep : 0;
+    };
+    auto tiles_of = [&](const Request& q) {
+        const long rows = (long)q.n * a.G;
+        return rows > limit ? 0 : (int)((rows + kRows - 1) / kRows);
+    };
+    auto steps_of = [&](const Request& q) { return max(1, (q.len + kStep - 1) / kStep - first_step(q)); };
+    const int64_t total = prefix_work<256>(a.B, sums, [&](int b) {
+        const Request q = request(a, b);
+        return (int64_t)tiles_of(q) * Hk * steps_of(q);
+    });
+    const int64_t share = (total + gridDim.x - 1) / gridDim.x;
+    // workgroups of one XCD take neighbouring ranges
+    const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
+    int64_t at = wg * share;
+    const int64_t end = min(at + share, total), begin = at;
+    const uint32_t mv = magic64();
+
+    while (at < end) {
+        const int b = __builtin_amdgcn_readfirstlane(request_of(sums, a.B, at));
+        const Request q = request(a, b);
+        const int steps = steps_of(q), tiles = tiles_of(q);
+        const int64_t item = (at - sums[b]) / steps, item0 = sums[b] + item * steps;
+        const int head = (int)(item / tiles), tile = (int)(item % tiles);
+        const int s0 = (int)(at - item0), s1 = (int)min((int64_t)steps, end - item0);
+        const int rows = min((int)min((long)q.n * a.G, (long)INT32_MAX) - tile * kRows, kRows);
+        const int row = tile * kRows + col, tok = row / a.G;
+        const int pos = col < rows ? q.len - q.n + tok : -1;
+        const int low = a.window ? max(0, pos - a.window + 1) : 0;
+        // tokens that every row of the tile sees
+        const int all_hi = q.len - q.n + tile * kRows / a.G;
+        const int all_lo = a.window ? q.len - q.n + (tile * kRows + rows - 1) / a.G - a.window + 1 : 0;
+
+        // q as the second operand: lane's row, dims (D/4) h ..
+        uint4 qv[D / 32];
+        float qsum;
+        {
+            const uint16_t* src = a.q + (long)(q.row0 + tok) * a.ldq + ((long)head * a.G + row % a.G) * D + h * (D / 4);
+#pragma unroll
+            for (int i = 0; i < D / 32; ++i)
+                qv[i] = col < rows ? reinterpret_cast<const uint4*>(src)[i] : make_uint4(0, 0, 0, 0);
+        }
+        auto quarters = [](float v) {
+            v += __shfl_xor(v, 16, 64);
+            return v + __shfl_xor(v, 32, 64);
+        };
+        const float scale = a.scale * operand_rows(qv, a.bf, qsum, quarters, [](uint32_t v) {
+            v |= __shfl_xor(v, 16, 64);
+            return v | (uint32_t)__shfl_xor((int)v, 32, 64);
+        });
+
+        f32x4_t o[NT], oz = {0, 0, 0, 0};
+#pragma unroll
+        for (int i = 0; i < NT; ++i)
+            o[i] = f32x4_t{0, 0, 0, 0};
+        float m = kNone, l = 0.0f;
+
+        const int t0 = (first_step(q) + s0) * kStep + wave * 32;     // this wave's tokens: t0 + 128 i ..
+        const int n = s1 - s0;
+        // page numbers of 32 steps: lane 2 i + j has that of step i, tile j
+        int pages = 0;
+        auto load_pages = [&](int i) {
+            const int t = t0 + (i + (lane >> 1)) * kStep + (lane & 1) * 16;     // (below 2^30 + 2^13)
+            pages = a.table[(long)b * a.W + min(t >> lg, a.W - 1)];
+        };
+        Tile<D> cur[2], nxt[2];
+        auto load = [&](Tile<D> (&d)[2], int i) {
+            const int t = t0 + i * kStep;
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                int p = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + j);
+                p = (uint32_t)p < (uint32_t)a.cache.pages ? p : 0;
+                load_tile<D>(d[j], a, p, head, (t + 16 * j) & ((1 << lg) - 1));
+            }
+        };
+        auto hidden = [&](int i, int j) {
+            return (uint32_t)__builtin_amdgcn_readlane(pages, 2 * (i & 31) + j) >= (uint32_t)a.cache.pages;
+        };
+        load_pages(0);
+        load(cur, 0);
+        for (int i = 0; i < n; ++i) {
+            const int t = t0 + i * kStep;
+            const bool hid0 = hidden(i, 0), hid1 = hidden(i, 1);
+            if (i + 1 < n) {
+                if (((i + 1) & 31) == 0)
+                    load_pages(i + 1);
+                load(nxt, i + 1);
+            }
+            const bool full = t >= all_lo && t + 31 <= all_hi && !hid0 && !hid1;
+            if (full || t < q.len) {
+                // scores: tokens 16 j + 4 h + i of row `col`
+                float x[8], sv[8];
+                uint32_t zz[4];
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    f32x4_t acc = {0, 0, 0, 0};
+#pragma unroll
+                    for (int w = 0; w < D / 32; ++w) {
+                        uint32_t e[4];
+                        pairs64(cur[j].k[w], mv, e);
+                        acc = mfma16(make_uint4(e[0], e[1], e[2], e[3]), qv[w], acc);
+                    }
+#pragma unroll
+                    for (int i4 = 0; i4 < 4; ++i4) {
+                        const uint32_t km = comp(cur[j].km, i4);
+                        x[4 * j + i4] = (acc[i4] - (64.0f + h2f(km >> 16)) * qsum) * (h2f(km & 0xFFFFu) * scale);
+                        sv[4 * j + i4] = h2f(comp(cur[j].vm, i4) & 0xFFFFu);
+                    }
+                    zz[2 * j] = add2(highs(cur[j].vm.x, cur[j].vm.y), mv);
+                    zz[2 * j + 1] = add2(highs(cur[j].vm.z, cur[j].vm.w), mv);
                 }
-                s = acc * h2f(mt & 0xFFFFu) * a.scale;
+                uint32_t seen = 0xFFu;
+                if (!full) {
+                    // what a row does not see weighs nothing, whatever lies there
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const int j = t + (k >> 2) * 16 + 4 * h + (k & 3);
+                        const bool there = j < q.len && !(k >> 2 ? hid1 : hid0);
+                        if (!(there && j <= pos && j >= low)) {
+                            seen &= ~(1u << k);
+                            x[k] = -INFINITY;
+                        }
+                        if (!there)
+                            zz[k >> 1] &= k & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+                    }
+                }
+                float e[8], w[8], top = 0.0f, etop = 0.0f;
+                auto weigh = [&] {
+                    top = etop = 0.0f;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        e[k] = exp2_(x[k] - m);
+                        w[k] = e[k] * sv[k];
+                        if (!full)
+                            w[k] = seen >> k & 1 ? w[k] : 0.0f;
+                        top = fmaxf(top, w[k]);
+                        etop = fmaxf(etop, e[k]);
+                    }
+                };
+                weigh();
+                if (__ballot(top > kTop || etop > kTop * kLeast)) {
+                    float best = kNone;
+#pragma unroll
+                    for (int k = 0; k < 8; ++k)
+                        best = fmaxf(best, seen >> k & 1 ? x[k] + log2_(fmaxf(sv[k], 1.0f / kLeast)) : kNone);
+                    best = fmaxf(best, __shfl_xor(best, 16, 64));
+                    best = fmaxf(best, __shfl_xor(best, 32, 64));
+                    const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
+                    m = mn;
+                    l *= f;
+                    oz *= f;
+#pragma unroll
+                    for (int d = 0; d < NT; ++d)
+                        o[d] *= f;
+                    weigh();
+                }
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    l += e[k];
+                const uint4 p = make_uint4(pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7]));
+                oz = mfma16(make_uint4(zz[0], zz[1], zz[2], zz[3]), p, oz);
+                if constexpr (D == 128) {
+                    uint32_t lw[4], hw[4];
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        lw[2 * j] = lows(cur[j].v.x, cur[j].v.y);
+                        lw[2 * j + 1] = lows(cur[j].v.z, cur[j].v.w);
+                        hw[2 * j] = highs(cur[j].v.x, cur[j].v.y);
+                        hw[2 * j + 1] = highs(cur[j].v.z, cur[j].v.w);
+                    }
+                    uint32_t ea[4][4];
+#pragma unroll
+                    for (int c = 0; c < 2; ++c) {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            pairs64(c ? hw[k] : lw[k], mv, ea[k]);
+#pragma unroll
+                        for (int f = 0; f < 4; ++f)
+                            o[2 * f + c] = mfma16(make_uint4(ea[0][f], ea[1][f], ea[2][f], ea[3][f]), p, o[2 * f + c]);
+                    }
+                } else {
+                    // lanes of the upper eight rows take the odd dims of the same words
+                    const uint32_t sel = col & 8 ? 0x07060302u : 0x05040100u;
+                    uint32_t ea[4][4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const uint4& v = cur[k >> 1].v;
+                        pairs64(k & 1 ? __builtin_amdgcn_perm(v.w, v.z, sel) : __builtin_amdgcn_perm(v.y, v.x, sel), mv, ea[k]);
+                    }
+#pragma unroll
+                    for (int f = 0; f < 4; ++f)
+                        o[f] = mfma16(make_uint4(ea[0][f], ea[1][f], ea[2][f], ea[3][f]), p, o[f]);
+                }
+            }
+            cur[0] = nxt[0];
+            cur[1] = nxt[1];
+        }
+
+        // the four waves' parts, by row
+        l = quarters(l);
+        if (h == 0) {
+            lm[wave][col] = m;
+            ll[wave][col] = l;
+        }
+        float* my = lo + (wave * kRows + col) * LD;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = 4 * h + i;
+            if constexpr (D == 128) {
+                *reinterpret_cast<float4*>(my + 8 * r) = make_float4(o[0][i] - oz[i], o[1][i] - oz[i], o[2][i] - oz[i], o[3][i] - oz[i]);
+                *reinterpret_cast<float4*>(my + 8 * r + 4) = make_float4(o[4][i] - oz[i], o[5][i] - oz[i], o[6][i] - oz[i], o[7][i] - oz[i]);
             } else {
-                p = -1;
+#pragma unroll
+                for (int f = 0; f < 4; ++f)
+                    my[8 * (r & 7) + 2 * f + (r >> 3)] = o[f][i] - oz[i];
             }
         }
-        float top = s;
-        for (int d = 1; d < 64; d <<= 1)
-            top = fmaxf(top, __shfl_xor(top, d, 64));
-        const float mn = fmaxf(m, top), al = exp2f(m - mn), e = exp2f(s - mn);
-        m = mn;
-        l = l * al + e;
-        ws[lane] = p >= 0 ? e : 0.0f;
-        for (int k = 0; k < D / 64; ++k) {
-            o[k] *= al;
-            __syncthreads();
-            for (int i = 0; i < 64 && j0 + i <= pos; ++i) {
-                const int pi = a.table[(long)b * a.W + ((j0 + i) >> lg)];
-                if (pi < 0 || pi >= a.cache.pages)
-                    continue;
-                const int in = (j0 + i) & ((1 << lg) - 1), d = lane + 64 * k;
-                const uint32_t* vw = reinterpret_cast<const uint32_t*>(a.cache.at(D, pi, g / a.G) + a.cache.side(D));
-                const uint32_t mt = vw[((D / 8) << lg) + in], c = vw[((in >> 2) * (D / 8) + d / 8) * 4 + (in & 3)];
-                o[k] += ws[i] * (h2f(mt & 0xFFFFu) * ((float)((c >> (4 * (((d & 7) >> 1) + 4 * (d & 1)))) & 15u) - h2f(mt >> 16)));
+        __syncthreads();
+        const bool whole = s0 == 0 && s1 == steps;
+        const uint32_t place = kRows * (D + 2) * 4u;      // bytes of a part: [16][D], m [16], l [16]
+        const uint32_t mine = (uint32_t)(2 * wg + (at == begin ? 0 : 1)) * place;
+        const Rsrc rp = rsrc(a.part, 2 * gridDim.x * place);
+        for (int c = tid; c < rows * (D / 4); c += 256) {
+            const int r = c / (D / 4), d = 4 * (c % (D / 4));
+            float mm = lm[0][r];
+#pragma unroll
+            for (int w = 1; w < 4; ++w)
+                mm = fmaxf(mm, lm[w][r]);
+            float ls = 0.0f, v[4] = {0, 0, 0, 0};
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const float f = exp2_(lm[w][r] - mm);
+                const float4 u = *reinterpret_cast<const float4*>(lo + (w * kRows + r) * LD + d);
+                ls += f * ll[w][r];
+                v[0] += f * u.x;
+                v[1] += f * u.y;
+                v[2] += f * u.z;
+                v[3] += f * u.w;
             }
-            __syncthreads();
+            if (whole) {
+                const int rr = tile * kRows + r, g = head * a.G + rr % a.G;
+                const float f = row_factor(a, g, mm, ls);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[k] = ls == 0.0f ? 0.0f : v[k] * f;
+                store4(a.y + (long)(q.row0 + rr / a.G) * a.ldy + (long)g * D + d, v, a.bf);
+            } else {
+                typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+                const w4 u = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+                __builtin_amdgcn_raw_buffer_store_b128(u, rp, mine + (uint32_t)(r * D + d) * 4u, 0, kDevice);
+                if (d == 0) {
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(mm), rp, mine + (uint32_t)(kRows * D + r) * 4u, 0, kDevice);
+                    __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(ls), rp, mine + (uint32_t)(kRows * D + kRows + r) * 4u, 0, kDevice);
+                }
+            }
         }
-    }
-    for (int d = 1; d < 64; d <<= 1)
-        l += __shfl_xor(l, d, 64);
-    const float den = l + (a.sinks ? exp2f(a.sinks[g] * 1.4426950408889634f - m) : 0.0f);
-    for (int k = 0; k < D / 64; ++k) {
-        const float y = l > 0.0f || l != l ? o[k] / den : 0.0f;
-        a.y[t * a.ldy + (long)g * D + lane + 64 * k] = a.bf ? __builtin_bit_cast(uint16_t, (__bf16)y) : (uint16_t)f2h(y);
+        if (!whole) {
+            // the part is out, then the item's counter: the last to come joins
+            const int w0 = (int)(item0 / share), w1 = (int)((item0 + steps - 1) / share);
+            __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __syncthreads();
+            if (tid == 0)
+                arrived = __hip_atomic_fetch_add(a.done + w0, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            __syncthreads();
+            if (arrived == (uint32_t)(w1 - w0)) {
+                if (tid == 0)
+                    __hip_atomic_store(a.done + w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                // (an item begins at its first workgroup's range or inside it; later ones begin with it)
+                auto part = [&](int w) { return (uint32_t)(2 * w + (w == w0 && item0 != (int64_t)w0 * share ? 1 : 0)) * place; };
+                for (int c = tid; c < rows * (D / 4); c += 256) {
+                    const int r = c / (D / 4), d = 4 * (c % (D / 4));
+                    float mm = kNone, ls = 0.0f, v[4] = {0, 0, 0, 0};
+                    for (int w = w0; w <= w1; ++w) {
+                        const uint32_t at0 = part(w);
+                        const auto u = __builtin_amdgcn_raw_buffer_load_b128(rp, at0 + (uint32_t)(r * D + d) * 4u, 0, kDevice);
+                        const float pm = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at0 + (uint32_t)(kRows * D + r) * 4u, 0, kDevice));
+                        const float pl = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at0 + (uint32_t)(kRows * D + kRows + r) * 4u, 0, kDevice));
+                        const float mn = fmaxf(mm, pm), f0 = exp2_(mm - mn), f1 = exp2_(pm - mn);
+                        mm = mn;
+                        ls = ls * f0 + pl * f1;
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            v[k] = v[k] * f0 + __uint_as_float(u[k]) * f1;
+                    }
+                    const int rr = tile * kRows + r, g = head * a.G + rr % a.G;
+                    const float f = row_factor(a, g, mm, ls);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        v[k] = ls == 0.0f ? 0.0f : v[k] * f;
+                    store4(a.y + (long)(q.row0 + rr / a.G) * a.ldy + (long)g * D + d, v, a.bf);
+                }
+            }
+        }
+        __syncthreads();                                  // LDS is the next item's
+        at = item0 + s1;
     }
 }
 
+constexpr int kPerCu = 2;                                 // workgroups of a compute unit
+int few_grid() { return (plan_cus() * kPerCu + 7) / 8 * 8; }
+
 }  // namespace
 
-size_t kv_attention_bytes(int, int, int) { return 256; }
+size_t kv_attention_bytes(int D, int, int) { return (size_t)few_grid() * 2 * kRows * (D + 2) * 4 + kCounters; }
 
-hipError_t launch_kv_attention(const AttnArgs& a, int, hipStream_t st) {
-    const dim3 grid(a.T, a.Hq);
+hipError_t launch_kv_attention(const AttnArgs& args, int, hipStream_t st) {
+    AttnArgs a = args;
+    a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.done) + kCounters);
+    const size_t lds = (size_t)4 * kRows * (a.D + 4) * 4 + (size_t)a.B * 8;
     if (a.D == 128)
-        simple_kernel<128><<<grid, 64, 0, st>>>(a);
+        few_kernel<128><<<few_grid(), 256, lds, st>>>(a, INT32_MAX);
     else
-        simple_kernel<64><<<grid, 64, 0, st>>>(a);
+        few_kernel<64><<<few_grid(), 256, lds, st>>>(a, INT32_MAX);
     return hipGetLastError();
 }
 

@@ -57,6 +57,7 @@ struct AttnArgs {
     int T, B, W, Hq, G, D, bf, window;
     float scale;                             // times log2(e): scores are powers of two
 };
+constexpr size_t kCounters = 16384;           // bytes of counters at the workspace's start
 size_t kv_attention_bytes(int D, int G, int max_new);
 hipError_t launch_kv_attention(const AttnArgs& a, int max_new, hipStream_t st);
 
