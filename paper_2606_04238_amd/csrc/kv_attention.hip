@@ -14,12 +14,16 @@
 //
 // The rounding to binary16 is made where weights are at most 2^15 and, when the maximum is taken anew, 2^8: normal
 // numbers down to 2^-22 of the largest.  m moves only when a weight would pass 2^15.
-#include "kv_device.h"
 #include "qmlp_internal.h"
+
+#include "decode_launch.h"
+#include "kv_device.h"
 
 namespace qmlp {
 namespace {
 
+typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+constexpr int kAhead = 8;                                 // parts under way where they are joined
 constexpr int kRows = 16, kStep = 128;                    // rows of a tile; tokens of a workgroup's step, 32 a wave
 
 // One tile of 16 tokens as its lanes hold it.
@@ -28,6 +32,13 @@ struct Tile {
     uint32_t k[D / 32];                                   // D/4 dims of token lane & 15
     uint4 v;                                              // 8 dims of 4 tokens
     uint4 km, vm;                                         // (scale, zero) of 4 tokens
+    uint32_t kz;                                          // and of token lane & 15
+};
+
+template <int D>
+struct Step {
+    Tile<D> tile[2];
+    bool hidden[2];                                       // its page is not one of the cache's
 };
 
 template <int D>
@@ -50,20 +61,21 @@ __device__ __forceinline__ void load_tile(Tile<D>& t, const AttnArgs& a, int pid
     t.v = load_stream(reinterpret_cast<const uint4*>(codes + side + h * (2u * D) + (r & (D / 8 - 1)) * 16u));
     t.km = *reinterpret_cast<const uint4*>(meta + h * 16u);
     t.vm = *reinterpret_cast<const uint4*>(meta + side + h * 16u);
+    t.kz = *reinterpret_cast<const uint32_t*>(meta + r * 4u);
 }
 
 // Work is cut evenly over the workgroups (see prefix_work): a unit is one step of one item, an item a tile
 // of rows of one K/V head.  A workgroup's range can begin and end inside items; what it has of those goes to the
 // workspace, two places a workgroup, and the last to come to an item (a counter at the item's first workgroup) joins
 // its parts.
-template <int D>
+template <int D, typename I>
 __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
     constexpr int NT = D / 16, LD = D + 4;                // tiles of outputs; row of LDS
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     float* lo = reinterpret_cast<float*>(smem);           // [4][16][LD]
     __shared__ float lm[4][kRows], ll[4][kRows];
     __shared__ uint32_t arrived;
-    int64_t* sums = reinterpret_cast<int64_t*>(smem + 4 * kRows * LD * 4);
+    Known<I>* known = reinterpret_cast<Known<I>*>(smem + 4 * kRows * LD * 4);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 4, col = lane & 15;
     const int lg = a.cache.page_log2, Hk = a.cache.heads;
 
@@ -76,24 +88,22 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
         return rows > limit ? 0 : (int)((rows + kRows - 1) / kRows);
     };
     auto steps_of = [&](const Request& q) { return max(1, (q.len + kStep - 1) / kStep - first_step(q)); };
-    const int64_t total = prefix_work<256>(a.B, sums, [&](int b) {
-        const Request q = request(a, b);
-        return (int64_t)tiles_of(q) * Hk * steps_of(q);
-    });
-    const int64_t share = (total + gridDim.x - 1) / gridDim.x;
+    const I total = prefix_work<256, I>(a, known, [&](const Request& q) { return (I)tiles_of(q) * Hk * steps_of(q); });
+    const I share = (total + gridDim.x - 1) / gridDim.x;
     // workgroups of one XCD take neighbouring ranges
     const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
-    int64_t at = wg * share;
-    const int64_t end = min(at + share, total), begin = at;
+    const I begin = wg * share, end = min(begin + share, total);
+    I at = begin;
     const uint32_t mv = magic64();
 
     while (at < end) {
-        const int b = __builtin_amdgcn_readfirstlane(request_of(sums, a.B, at));
-        const Request q = request(a, b);
+        const int b = __builtin_amdgcn_readfirstlane(request_of(known, a.B, at));
+        const Request q = known[b].uniform();
+        const I before = known[b].before;
         const int steps = steps_of(q), tiles = tiles_of(q);
-        const int64_t item = (at - sums[b]) / steps, item0 = sums[b] + item * steps;
+        const I item = (at - before) / steps, item0 = before + item * steps;
         const int head = (int)(item / tiles), tile = (int)(item % tiles);
-        const int s0 = (int)(at - item0), s1 = (int)min((int64_t)steps, end - item0);
+        const int s0 = (int)(at - item0), s1 = (int)min((I)steps, end - item0);
         const int rows = min((int)min((long)q.n * a.G, (long)INT32_MAX) - tile * kRows, kRows);
         const int row = tile * kRows + col, tok = row / a.G;
         const int pos = col < rows ? q.len - q.n + tok : -1;
@@ -120,6 +130,12 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
             return v | (uint32_t)__shfl_xor((int)v, 32, 64);
         });
 
+        // minus the row's sum, in the places of the first quarter
+        uint32_t part3[3];
+        three_bf16(-qsum, part3);
+        const uint4 qz = h == 0 ? make_uint4(part3[0] | part3[1] << 16, part3[2], 0, 0) : make_uint4(0, 0, 0, 0);
+        const float away = scale < 0.0f ? INFINITY : -INFINITY;      // a score that weighs nothing
+
         f32x4_t o[NT], oz = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -134,37 +150,32 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
             const int t = t0 + (i + (lane >> 1)) * kStep + (lane & 1) * 16;     // (below 2^30 + 2^13)
             pages = a.table[(long)b * a.W + min(t >> lg, a.W - 1)];
         };
-        Tile<D> cur[2], nxt[2];
-        auto load = [&](Tile<D> (&d)[2], int i) {
+        Step<D> buf[3];                                   // two steps are under way while one is multiplied
+        auto load = [&](Step<D>& d, int i) {
+            if ((i & 31) == 0)
+                load_pages(i);
             const int t = t0 + i * kStep;
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                int p = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + j);
-                p = (uint32_t)p < (uint32_t)a.cache.pages ? p : 0;
-                load_tile<D>(d[j], a, p, head, (t + 16 * j) & ((1 << lg) - 1));
+                const int p = __builtin_amdgcn_readlane(pages, 2 * (i & 31) + j);
+                d.hidden[j] = (uint32_t)p >= (uint32_t)a.cache.pages;
+                load_tile<D>(d.tile[j], a, d.hidden[j] ? 0 : p, head, (t + 16 * j) & ((1 << lg) - 1));
             }
         };
-        auto hidden = [&](int i, int j) {
-            return (uint32_t)__builtin_amdgcn_readlane(pages, 2 * (i & 31) + j) >= (uint32_t)a.cache.pages;
-        };
-        load_pages(0);
-        load(cur, 0);
-        for (int i = 0; i < n; ++i) {
+        auto multiply = [&](const Step<D>& s, int i) {
+            const Tile<D>* cur = s.tile;
+            const bool hid0 = s.hidden[0], hid1 = s.hidden[1];
             const int t = t0 + i * kStep;
-            const bool hid0 = hidden(i, 0), hid1 = hidden(i, 1);
-            if (i + 1 < n) {
-                if (((i + 1) & 31) == 0)
-                    load_pages(i + 1);
-                load(nxt, i + 1);
-            }
             const bool full = t >= all_lo && t + 31 <= all_hi && !hid0 && !hid1;
             if (full || t < q.len) {
                 // scores: tokens 16 j + 4 h + i of row `col`
-                float x[8], sv[8];
-                uint32_t zz[4];
+                float x[8];
+                uint32_t zz[4], sv[8];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
-                    f32x4_t acc = {0, 0, 0, 0};
+                    // the offset and the zero of a token, times the row's sum: one more step, in bfloat16 (64 + zero is exact there)
+                    const uint32_t z = __float_as_uint(fma_hi(cur[j].kz, 1.0f, 64.0f)), zd = __builtin_amdgcn_perm(z, z, 0x03020302u);
+                    f32x4_t acc = mfma16_bf(make_uint4(zd, zd, zd, zd), qz, f32x4_t{0, 0, 0, 0});
 #pragma unroll
                     for (int w = 0; w < D / 32; ++w) {
                         uint32_t e[4];
@@ -173,14 +184,12 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                     }
 #pragma unroll
                     for (int i4 = 0; i4 < 4; ++i4) {
-                        const uint32_t km = comp(cur[j].km, i4);
-                        x[4 * j + i4] = (acc[i4] - (64.0f + h2f(km >> 16)) * qsum) * (h2f(km & 0xFFFFu) * scale);
-                        sv[4 * j + i4] = h2f(comp(cur[j].vm, i4) & 0xFFFFu);
+                        x[4 * j + i4] = fma_lo(comp(cur[j].km, i4), acc[i4], 0.0f);
+                        sv[4 * j + i4] = comp(cur[j].vm, i4);
                     }
                     zz[2 * j] = add2(highs(cur[j].vm.x, cur[j].vm.y), mv);
                     zz[2 * j + 1] = add2(highs(cur[j].vm.z, cur[j].vm.w), mv);
                 }
-                uint32_t seen = 0xFFu;
                 if (!full) {
                     // what a row does not see weighs nothing, whatever lies there
 #pragma unroll
@@ -188,32 +197,31 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                         const int j = t + (k >> 2) * 16 + 4 * h + (k & 3);
                         const bool there = j < q.len && !(k >> 2 ? hid1 : hid0);
                         if (!(there && j <= pos && j >= low)) {
-                            seen &= ~(1u << k);
-                            x[k] = -INFINITY;
+                            x[k] = away;
+                            sv[k] = 0x3C00u;
                         }
                         if (!there)
                             zz[k >> 1] &= k & 1 ? 0x0000FFFFu : 0xFFFF0000u;
                     }
                 }
-                float e[8], w[8], top = 0.0f, etop = 0.0f;
+                float w[8], sum, top;
                 auto weigh = [&] {
-                    top = etop = 0.0f;
+                    sum = 0.0f;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        e[k] = exp2_(x[k] - m);
-                        w[k] = e[k] * sv[k];
-                        if (!full)
-                            w[k] = seen >> k & 1 ? w[k] : 0.0f;
-                        top = fmaxf(top, w[k]);
-                        etop = fmaxf(etop, e[k]);
+                        const float e = exp2_(__builtin_fmaf(x[k], scale, -m));
+                        w[k] = fma_lo(sv[k], e, 0.0f);
+                        sum += e;
                     }
+                    top = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
                 };
                 weigh();
-                if (__ballot(top > kTop || etop > kTop * kLeast)) {
+                // (a scale of 0, as in an empty cache, hides a large weight from the first test)
+                if (__ballot(top > kTop || sum > 8.0f * kTop * kLeast)) {
                     float best = kNone;
 #pragma unroll
                     for (int k = 0; k < 8; ++k)
-                        best = fmaxf(best, seen >> k & 1 ? x[k] + log2_(fmaxf(sv[k], 1.0f / kLeast)) : kNone);
+                        best = fmaxf(best, __builtin_fmaf(x[k], scale, log2_(fmaxf(h2f(sv[k] & 0xFFFFu), 1.0f / kLeast))));
                     best = fmaxf(best, __shfl_xor(best, 16, 64));
                     best = fmaxf(best, __shfl_xor(best, 32, 64));
                     const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
@@ -225,9 +233,7 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                         o[d] *= f;
                     weigh();
                 }
-#pragma unroll
-                for (int k = 0; k < 8; ++k)
-                    l += e[k];
+                l += sum;
                 const uint4 p = make_uint4(pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7]));
                 oz = mfma16(make_uint4(zz[0], zz[1], zz[2], zz[3]), p, oz);
                 if constexpr (D == 128) {
@@ -263,8 +269,18 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                         o[f] = mfma16(make_uint4(ea[0][f], ea[1][f], ea[2][f], ea[3][f]), p, o[f]);
                 }
             }
-            cur[0] = nxt[0];
-            cur[1] = nxt[1];
+        };
+        load(buf[0], 0);
+        if (n > 1)
+            load(buf[1], 1);
+        for (int i = 0; i < n; i += 3) {
+#pragma unroll
+            for (int j = 0; j < 3; ++j)
+                if (i + j < n) {
+                    if (i + j + 2 < n)
+                        load(buf[(j + 2) % 3], i + j + 2);
+                    multiply(buf[j], i + j);
+                }
         }
 
         // the four waves' parts, by row
@@ -316,7 +332,6 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                     v[k] = ls == 0.0f ? 0.0f : v[k] * f;
                 store4(a.y + (long)(q.row0 + rr / a.G) * a.ldy + (long)g * D + d, v, a.bf);
             } else {
-                typedef uint32_t w4 __attribute__((ext_vector_type(4)));
                 const w4 u = {__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
                 __builtin_amdgcn_raw_buffer_store_b128(u, rp, mine + (uint32_t)(r * D + d) * 4u, 0, kDevice);
                 if (d == 0) {
@@ -337,28 +352,55 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                 if (tid == 0)
                     __hip_atomic_store(a.done + w0, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
                 // (an item begins at its first workgroup's range or inside it; later ones begin with it)
-                auto part = [&](int w) { return (uint32_t)(2 * w + (w == w0 && item0 != (int64_t)w0 * share ? 1 : 0)) * place; };
-                for (int c = tid; c < rows * (D / 4); c += 256) {
-                    const int r = c / (D / 4), d = 4 * (c % (D / 4));
+                auto part = [&](int w) { return (uint32_t)(2 * w + (w == w0 && item0 != w0 * share ? 1 : 0)) * place; };
+                // each wave joins every fourth part, four numbers a lane, eight parts under way; then the waves meet in LDS
+                for (int c0 = 0; c0 < rows * (D / 4); c0 += 64) {
+                    const int c = min(c0 + lane, rows * (D / 4) - 1), r = c / (D / 4), d = 4 * (c % (D / 4));
                     float mm = kNone, ls = 0.0f, v[4] = {0, 0, 0, 0};
-                    for (int w = w0; w <= w1; ++w) {
-                        const uint32_t at0 = part(w);
-                        const auto u = __builtin_amdgcn_raw_buffer_load_b128(rp, at0 + (uint32_t)(r * D + d) * 4u, 0, kDevice);
-                        const float pm = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at0 + (uint32_t)(kRows * D + r) * 4u, 0, kDevice));
-                        const float pl = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at0 + (uint32_t)(kRows * D + kRows + r) * 4u, 0, kDevice));
-                        const float mn = fmaxf(mm, pm), f0 = exp2_(mm - mn), f1 = exp2_(pm - mn);
-                        mm = mn;
-                        ls = ls * f0 + pl * f1;
+                    for (int w = w0 + wave; w <= w1; w += 4 * kAhead) {
+                        w4 u[kAhead];
+                        float pm[kAhead], pl[kAhead];
+#pragma unroll
+                        for (int k = 0; k < kAhead; ++k) {
+                            const uint32_t at0 = part(min(w + 4 * k, w1));
+                            u[k] = __builtin_amdgcn_raw_buffer_load_b128(rp, at0 + (uint32_t)(r * D + d) * 4u, 0, kDevice);
+                            pm[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at0 + (uint32_t)(kRows * D + r) * 4u, 0, kDevice));
+                            pl[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at0 + (uint32_t)(kRows * D + kRows + r) * 4u, 0, kDevice));
+                        }
+#pragma unroll
+                        for (int k = 0; k < kAhead; ++k)
+                            if (w + 4 * k <= w1) {
+                                const float mn = fmaxf(mm, pm[k]), f0 = exp2_(mm - mn), f1 = exp2_(pm[k] - mn);
+                                mm = mn;
+                                ls = ls * f0 + pl[k] * f1;
+#pragma unroll
+                                for (int x = 0; x < 4; ++x)
+                                    v[x] = v[x] * f0 + __uint_as_float(u[k][x]) * f1;
+                            }
+                    }
+                    __syncthreads();                      // the last reads of LDS are over
+                    float* my = lo + (wave * 64 + lane) * 8;
+                    *reinterpret_cast<float4*>(my) = make_float4(v[0], v[1], v[2], v[3]);
+                    *reinterpret_cast<float2*>(my + 4) = make_float2(mm, ls);
+                    __syncthreads();
+                    if (wave == 0 && c0 + lane < rows * (D / 4)) {
+#pragma unroll
+                        for (int w = 1; w < 4; ++w) {
+                            const float* o = lo + (w * 64 + lane) * 8;
+                            const float mn = fmaxf(mm, o[4]), f0 = exp2_(mm - mn), f1 = exp2_(o[4] - mn);
+                            mm = mn;
+                            ls = ls * f0 + o[5] * f1;
+#pragma unroll
+                            for (int x = 0; x < 4; ++x)
+                                v[x] = v[x] * f0 + o[x] * f1;
+                        }
+                        const int rr = tile * kRows + r, g = head * a.G + rr % a.G;
+                        const float f = row_factor(a, g, mm, ls);
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            v[k] = v[k] * f0 + __uint_as_float(u[k]) * f1;
+                            v[k] = ls == 0.0f ? 0.0f : v[k] * f;
+                        store4(a.y + (long)(q.row0 + rr / a.G) * a.ldy + (long)g * D + d, v, a.bf);
                     }
-                    const int rr = tile * kRows + r, g = head * a.G + rr % a.G;
-                    const float f = row_factor(a, g, mm, ls);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        v[k] = ls == 0.0f ? 0.0f : v[k] * f;
-                    store4(a.y + (long)(q.row0 + rr / a.G) * a.ldy + (long)g * D + d, v, a.bf);
                 }
             }
         }
@@ -370,6 +412,16 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
 constexpr int kPerCu = 2;                                 // workgroups of a compute unit
 int few_grid() { return (plan_cus() * kPerCu + 7) / 8 * 8; }
 
+template <int D, typename I>
+hipError_t launch_few(const AttnArgs& a, int limit, hipStream_t st) {
+    const size_t lds = (size_t)4 * kRows * (D + 4) * 4 + (size_t)a.B * sizeof(Known<I>);
+    const hipError_t e = set_lds(few_kernel<D, I>, lds + 1024);
+    if (e != hipSuccess)
+        return e;
+    few_kernel<D, I><<<few_grid(), 256, lds, st>>>(a, limit);
+    return hipGetLastError();
+}
+
 }  // namespace
 
 size_t kv_attention_bytes(int D, int, int) { return (size_t)few_grid() * 2 * kRows * (D + 2) * 4 + kCounters; }
@@ -377,12 +429,12 @@ size_t kv_attention_bytes(int D, int, int) { return (size_t)few_grid() * 2 * kRo
 hipError_t launch_kv_attention(const AttnArgs& args, int, hipStream_t st) {
     AttnArgs a = args;
     a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.done) + kCounters);
-    const size_t lds = (size_t)4 * kRows * (a.D + 4) * 4 + (size_t)a.B * 8;
+    // the units of all requests at most: 32 bits hold them but for the longest tables with the most rows
+    const double units = ((double)a.T * a.G / kRows + a.B) * a.cache.heads * (((double)((long)a.W << a.cache.page_log2)) / kStep + 2);
+    const bool wide = units + few_grid() >= 2147483647.0;
     if (a.D == 128)
-        few_kernel<128><<<few_grid(), 256, lds, st>>>(a, INT32_MAX);
-    else
-        few_kernel<64><<<few_grid(), 256, lds, st>>>(a, INT32_MAX);
-    return hipGetLastError();
+        return wide ? launch_few<128, int64_t>(a, INT32_MAX, st) : launch_few<128, int32_t>(a, INT32_MAX, st);
+    return wide ? launch_few<64, int64_t>(a, INT32_MAX, st) : launch_few<64, int32_t>(a, INT32_MAX, st);
 }
 
 }  // namespace qmlp

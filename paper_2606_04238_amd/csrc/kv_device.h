@@ -26,11 +26,19 @@ __device__ __forceinline__ f32x4_t mfma16(const uint4& a, const uint4& b, f32x4_
 __device__ __forceinline__ f32x16_t mfma32(const uint4& a, const uint4& b, f32x16_t c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8_t, a), __builtin_bit_cast(f16x8_t, b), c, 0, 0, 0);
 }
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ f32x4_t mfma16_bf(const uint4& a, const uint4& b, f32x4_t c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8_t, a), __builtin_bit_cast(bf16x8_t, b), c, 0, 0, 0);
+}
 __device__ __forceinline__ Rsrc rsrc(const void* p, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
 }
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
 __device__ __forceinline__ float log2_(float v) { return __builtin_amdgcn_logf(v); }
+
+// The low (high) half of w times v, and c added: the conversion is the instruction's.
+__device__ __forceinline__ float fma_lo(uint32_t w, float v, float c) { return __builtin_fmaf(h2f(w & 0xFFFFu), v, c); }
+__device__ __forceinline__ float fma_hi(uint32_t w, float v, float c) { return __builtin_fmaf(h2f(w >> 16), v, c); }
 
 // Two fp32 to two binary16, each rounded to nearest even.
 __device__ __forceinline__ uint32_t pack2(float a, float b) {
@@ -57,6 +65,15 @@ __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, (half2_t)(__builtin_bit_cast(half2_t, a) + __builtin_bit_cast(half2_t, b)));
 }
 __device__ __forceinline__ uint32_t comp(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+// fp32 as the sum of three bfloat16 numbers (24 bits): what the matrix cores multiply by small integers exactly.
+__device__ __forceinline__ void three_bf16(float v, uint32_t (&p)[3]) {
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        p[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v);
+        v -= __uint_as_float(p[i] << 16);
+    }
+}
 
 // One request of a call.
 struct Request {
@@ -146,42 +163,59 @@ __device__ __forceinline__ float row_factor(const AttnArgs& a, int head, float m
     return l == 0.0f ? 0.0f : 1.0f / d;
 }
 
-// The work of a call is cut evenly over the workgroups: request b stands for `work(b)` units of it, sums[b] those before it.
-// Every workgroup forms the sums itself (the lengths are on the device only).  Returns the total.
-template <int NT, typename F>
-__device__ __forceinline__ int64_t prefix_work(int B, int64_t* sums, F work) {
-    __shared__ int64_t wave_sum[NT / 64];
+// A request as LDS holds it, with the units of work of those before it.
+template <typename I>
+struct Known {
+    I before;
+    Request q;
+    __device__ __forceinline__ Request uniform() const {
+        return Request{__builtin_amdgcn_readfirstlane(q.len), __builtin_amdgcn_readfirstlane(q.n), __builtin_amdgcn_readfirstlane(q.row0)};
+    }
+};
+
+// The work of a call is cut evenly over the workgroups: request b stands for `work` units of it. Every workgroup
+// forms the sums itself (the lengths are on the device only).  Returns the total.
+template <int NT, typename I, typename F>
+__device__ __forceinline__ I prefix_work(const AttnArgs& a, Known<I>* known, F work) {
+    __shared__ I wave_sum[NT / 64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int64_t total = 0;
-    for (int b0 = 0; b0 < B; b0 += NT) {
+    I total = 0;
+    for (int b0 = 0; b0 < a.B; b0 += NT) {
         const int b = b0 + tid;
-        const int64_t v = b < B ? work(b) : 0;
-        int64_t inc = v;
+        Request q{0, 0, 0};
+        I v = 0;
+        if (b < a.B) {
+            q = request(a, b);
+            v = work(q);
+        }
+        I inc = v;
 #pragma unroll
         for (int d = 1; d < 64; d <<= 1) {
-            const int64_t o = __shfl_up(inc, d, 64);
+            const I o = __shfl_up(inc, d, 64);
             inc += lane >= d ? o : 0;
         }
         if (lane == 63)
             wave_sum[wave] = inc;
         __syncthreads();
-        int64_t before = total;
+        I before = total;
+#pragma unroll
         for (int w = 0; w < NT / 64; ++w) {
             before += w < wave ? wave_sum[w] : 0;
             total += wave_sum[w];
         }
-        if (b < B)
-            sums[b] = before + inc - v;
+        if (b < a.B)
+            known[b] = Known<I>{before + inc - v, q};
         __syncthreads();
     }
     return total;
 }
-// The last b in [0, B) with sums[b] <= i: the request with unit i.
-__device__ __forceinline__ int request_of(const int64_t* sums, int B, int64_t i) {
+// The last b in [0, B) with at most i units before it: the request with unit i.
+template <typename I>
+__device__ __forceinline__ int request_of(const Known<I>* known, int B, I i) {
     int lo = 0, hi = B;
     while (hi - lo > 1) {
         const int m = (lo + hi) >> 1;
-        if (sums[m] <= i)
+        if (known[m].before <= i)
             lo = m;
         else
             hi = m;
