@@ -128,7 +128,7 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
         const float scale = a.scale * operand_rows(qv, a.bf, qsum, quarters, [](uint32_t v) {
             v |= __shfl_xor(v, 16, 64);
             return v | (uint32_t)__shfl_xor((int)v, 32, 64);
-        });
+        }, [](uint32_t top) { return top; });
 
         // minus the row's sum, in the places of the first quarter
         uint32_t part3[3];
@@ -424,17 +424,30 @@ hipError_t launch_few(const AttnArgs& a, int limit, hipStream_t st) {
 
 }  // namespace
 
-size_t kv_attention_bytes(int D, int, int) { return (size_t)few_grid() * 2 * kRows * (D + 2) * 4 + kCounters; }
+// Requests of up to this many rows take the kernel above, those with more the one for many rows (kv_attention_rows.hip).
+constexpr int kFewRows = 32;
 
-hipError_t launch_kv_attention(const AttnArgs& args, int, hipStream_t st) {
+size_t kv_attention_bytes(int D, int G, int max_new) {
+    const size_t few = (size_t)few_grid() * 2 * kRows * (D + 2) * 4, many = (long)max_new * G > kFewRows ? kv_rows_bytes(D) : 0;
+    return (few > many ? few : many) + kCounters;
+}
+
+hipError_t launch_kv_attention(const AttnArgs& args, int max_new, hipStream_t st) {
     AttnArgs a = args;
     a.part = reinterpret_cast<float*>(reinterpret_cast<uint8_t*>(a.done) + kCounters);
+    const bool many = (long)max_new * a.G > kFewRows;
+    if (many) {
+        const hipError_t e = launch_kv_rows(a, kFewRows, st);
+        if (e != hipSuccess)
+            return e;
+    }
+    const int limit = many ? kFewRows : INT32_MAX;
     // the units of all requests at most: 32 bits hold them but for the longest tables with the most rows
     const double units = ((double)a.T * a.G / kRows + a.B) * a.cache.heads * (((double)((long)a.W << a.cache.page_log2)) / kStep + 2);
     const bool wide = units + few_grid() >= 2147483647.0;
     if (a.D == 128)
-        return wide ? launch_few<128, int64_t>(a, INT32_MAX, st) : launch_few<128, int32_t>(a, INT32_MAX, st);
-    return wide ? launch_few<64, int64_t>(a, INT32_MAX, st) : launch_few<64, int32_t>(a, INT32_MAX, st);
+        return wide ? launch_few<128, int64_t>(a, limit, st) : launch_few<128, int32_t>(a, limit, st);
+    return wide ? launch_few<64, int64_t>(a, limit, st) : launch_few<64, int32_t>(a, limit, st);
 }
 
 }  // namespace qmlp

@@ -1,0 +1,397 @@
+// Causal attention over the 4-bit cache for many rows a request (prompts and their chunks), gfx950.
+//
+// The mathematics of kv_attention.hip.  With rows to spare what bounds it is arithmetic: the matrix products, and beside
+// them the weights (an exponential and five more operations for each of rows x tokens).  So a
+// workgroup takes 128 rows (of all heads that share a K/V head), unpacks 64 tokens once for all of them into
+// LDS, as exact binary16 integers code - zero, and the scales go on the scores and the weights, which are touched anyway.  A
+// wave owns 32 rows; its products are transposed (tokens or dims down, rows across), so that weights go from one
+// product to the other in registers.  Two stages of LDS: while one is multiplied the next is loaded and unpacked.
+//
+// LDS: K [64 tokens][D], 16-byte pieces (8 dims) at place p ^ (token & 7); V [D dims][64 tokens], a piece being the eight
+// tokens a lane multiplies at once (16 s + 4 h + {0..3, 8..11}), at place p ^ (dim & 7) ^ (dim / 8 & 7), its
+// halves swapped from dim 64 on.  Eight neighbouring lanes so read and write different banks.
+#include "qmlp_internal.h"
+
+#include "decode_launch.h"
+#include "kv_device.h"
+
+namespace qmlp {
+namespace {
+
+constexpr int kTileRows = 128, kTokens = 64, kMostShares = 16;
+
+template <int D>
+struct Stage {
+    uint16_t k[kTokens * D];
+    uint16_t v[D * kTokens];
+    float sk[kTokens], sv[kTokens];
+    uint32_t away[4];                                     // nonzero: a wave met tokens that are not there
+};
+
+// What a thread stages: a piece of K (4 words of a token) and of V (a word of 4 tokens), with their (scale, zero); at
+// D = 64 one of the two.
+template <int D>
+struct Piece {
+    static constexpr bool both = D == 128;
+    uint4 k, v, vm;
+    uint32_t km;
+};
+
+template <int D>
+__global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int target) {
+    constexpr int KS = D / 16, DT = D / 32;
+    extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
+    __shared__ uint32_t arrived, tops[4];
+    Stage<D>* stage = reinterpret_cast<Stage<D>*>(smem);
+    Known<int32_t>* known = reinterpret_cast<Known<int32_t>*>(smem + 2 * sizeof(Stage<D>));
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
+    const int lg = a.cache.page_log2, Hk = a.cache.heads;
+
+    auto tiles_of = [&](const Request& q) {
+        const long rows = (long)q.n * a.G;
+        return rows <= limit ? 0 : (int)((rows + kTileRows - 1) / kTileRows);
+    };
+    const int tiles = prefix_work<256, int32_t>(a, known, [&](const Request& q) { return tiles_of(q); });
+    const int items = tiles * Hk;
+    // few items: the tokens of each are shared by several workgroups
+    const int shares = items ? min(max(target / items, 1), kMostShares) : 1;
+    if ((int)blockIdx.x >= items * shares)
+        return;
+    // neighbouring workgroups (on different XCDs) take different K/V heads; the last tiles of a request, which see most, first
+    const int head = (int)blockIdx.x % Hk, rest = (int)blockIdx.x / Hk, part = rest % shares, nth = rest / shares;
+    const int b = __builtin_amdgcn_readfirstlane(request_of(known, a.B, nth));
+    const Request q = known[b].uniform();
+    const int nt = tiles_of(q), tile = nt - 1 - (nth - __builtin_amdgcn_readfirstlane(known[b].before));
+    const int rows = min((int)((long)q.n * a.G - (long)tile * kTileRows), kTileRows);
+    const int first = q.len - q.n + tile * kTileRows / a.G, last = q.len - q.n + (tile * kTileRows + rows - 1) / a.G;   // positions
+    const int low0 = a.window ? max(0, first - a.window + 1) / kTokens : 0;
+    const int all = max(0, last / kTokens + 1 - low0);    // steps of the tile (last < 0: none)
+    const int i0 = low0 + (int)((long)all * part / shares), i1 = low0 + (last < 0 ? 0 : (int)((long)all * (part + 1) / shares));
+
+    // this lane's row
+    const int r = wave * 32 + col, row = tile * kTileRows + r, tok = row / a.G;
+    const int pos = r < rows ? q.len - q.n + tok : -1;
+    const int low = a.window ? max(0, pos - a.window + 1) : 0;
+    uint4 qv[KS];
+    {
+        const uint16_t* src = a.q + (long)(q.row0 + tok) * a.ldq + ((long)head * a.G + row % a.G) * D + h * 8;
+#pragma unroll
+        for (int i = 0; i < KS; ++i)
+            qv[i] = r < rows ? *reinterpret_cast<const uint4*>(src + 16 * i) : make_uint4(0, 0, 0, 0);
+    }
+
+    // staging
+    const bool has_k = Piece<D>::both || tid < 128, has_v = Piece<D>::both || tid >= 128;
+    const int ktok = D == 128 ? tid >> 2 : (tid & 127) >> 1, kc = D == 128 ? tid & 3 : tid & 1;
+    const int vquad = D == 128 ? tid >> 4 : (tid & 127) >> 3, vword = D == 128 ? tid & 15 : tid & 7;
+    int kpage = 0, vpage = 0;                             // page numbers of the step to be loaded next
+    auto load_pages = [&](int i) {
+        const int32_t* t = a.table + (long)b * a.W;
+        if (has_k)
+            kpage = t[min((i * kTokens + ktok) >> lg, a.W - 1)];
+        if (has_v)
+            vpage = t[min((i * kTokens + 4 * vquad) >> lg, a.W - 1)];
+    };
+    Piece<D> p;
+    bool kthere = false;
+    int vthere = 0;                                       // tokens of the quad that are there
+    auto load = [&](int i) {
+        const uint32_t side = a.cache.side(D), codes = (uint32_t)(D / 2) << lg, in = (1u << lg) - 1u;
+        if (has_k) {
+            const int t = i * kTokens + ktok;
+            kthere = t < q.len && (uint32_t)kpage < (uint32_t)a.cache.pages;
+            const uint8_t* base = a.cache.at(D, kthere ? kpage : 0, head);
+            const uint32_t o = (uint32_t)t & in;
+            p.k = *reinterpret_cast<const uint4*>(base + o * (D / 2) + kc * 16);
+            p.km = *reinterpret_cast<const uint32_t*>(base + codes + o * 4u);
+        }
+        if (has_v) {
+            const int t = i * kTokens + 4 * vquad;
+            const bool there = (uint32_t)vpage < (uint32_t)a.cache.pages;
+            vthere = there ? min(max(q.len - t, 0), 4) : 0;
+            const uint8_t* base = a.cache.at(D, there ? vpage : 0, head) + side;
+            const uint32_t o = (uint32_t)t & in;
+            p.v = *reinterpret_cast<const uint4*>(base + o * (D / 2) + vword * 16);
+            p.vm = *reinterpret_cast<const uint4*>(base + codes + o * 4u);
+        }
+    };
+    float scale = 0.0f;                                   // of a raw score, with the power of two of q
+    const uint32_t mv = magic64();
+    auto put = [&](Stage<D>& s) {
+        if (has_k) {
+            const uint32_t m = kthere ? p.km : 0x3C00u;
+            const uint32_t z = (m >> 16) | (m & 0xFFFF0000u), off = add2(z, mv) ^ 0x80008000u;        // -(64 + zero), twice
+            // (threads of the upper half of a row begin with its second pair of words: see the banks above)
+            const bool turn = D == 128 && (kc & 2);
+            const uint32_t w[4] = {turn ? p.k.z : p.k.x, turn ? p.k.w : p.k.y, turn ? p.k.x : p.k.z, turn ? p.k.y : p.k.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                uint32_t e[4];
+                pairs64(w[i], mv, e);
+                const int piece = 4 * kc + (i ^ (turn ? 2 : 0));
+                *reinterpret_cast<uint4*>(s.k + ktok * D + ((piece ^ (ktok & 7)) << 3)) =
+                    make_uint4(add2(e[0], off), add2(e[1], off), add2(e[2], off), add2(e[3], off));
+            }
+            if (kc == 0)
+                s.sk[ktok] = kthere ? h2f(m & 0xFFFFu) * scale : INFINITY;      // (a scale is never infinite: not there)
+        }
+        if (has_v) {
+            uint32_t m[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                m[i] = i < vthere ? comp(p.vm, i) : 0x3C00u;
+            const uint32_t off[2] = {add2(highs(m[0], m[1]), mv) ^ 0x80008000u, add2(highs(m[2], m[3]), mv) ^ 0x80008000u};
+            const uint32_t src[4] = {p.v.x, p.v.y, p.v.z, p.v.w};
+            uint32_t out[8][2];
+#pragma unroll
+            for (int pr = 0; pr < 2; ++pr) {
+                uint32_t e[4], f[4];
+                pairs64(lows(src[2 * pr], src[2 * pr + 1]), mv, e);
+                pairs64(highs(src[2 * pr], src[2 * pr + 1]), mv, f);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    out[2 * i][pr] = add2(e[i], off[pr]);
+                    out[2 * i + 1][pr] = add2(f[i], off[pr]);
+                }
+            }
+            const int piece = 2 * (vquad >> 2) + (vquad & 1), half = ((vquad >> 1) & 1) ^ (vword >> 3);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                *reinterpret_cast<uint2*>(s.v + (8 * vword + j) * kTokens + ((piece ^ j ^ (vword & 7)) << 3) + 4 * half) =
+                    make_uint2(out[j][0], out[j][1]);
+            if (vword == 0)
+                *reinterpret_cast<float4*>(s.sv + 4 * vquad) =
+                    make_float4(h2f(m[0] & 0xFFFFu), h2f(m[1] & 0xFFFFu), h2f(m[2] & 0xFFFFu), h2f(m[3] & 0xFFFFu));
+        }
+        const bool gone = (has_k && !kthere) || (has_v && vthere < 4);
+        const uint64_t any = __ballot(gone);
+        if (lane == 0)
+            s.away[wave] = any != 0;
+    };
+
+    f32x16_t o[DT];
+#pragma unroll
+    for (int d = 0; d < DT; ++d)
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+            o[d][i] = 0.0f;
+    float m = kNone, l = 0.0f;
+    if (i0 < i1) {
+        load_pages(i0);
+        load(i0);
+        if (i0 + 1 < i1)
+            load_pages(i0 + 1);
+    }
+    float qsum;
+    scale = a.scale * operand_rows(qv, a.bf, qsum, [](float v) { return v + __shfl_xor(v, 32, 64); },
+                                   [](uint32_t v) { return v | (uint32_t)__shfl_xor((int)v, 32, 64); },
+                                   [&](uint32_t top) {
+                                       // one power of two for the workgroup
+                                       if (lane == 0)
+                                           tops[wave] = top;
+                                       __syncthreads();
+                                       return max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+                                   });
+    const bool bad = qsum != qsum;                        // an infinity or NaN in the row
+    if (i0 < i1)
+        put(stage[0]);
+    __syncthreads();
+
+    for (int i = i0; i < i1; ++i) {
+        const Stage<D>& s = stage[(i - i0) & 1];
+        if (i + 1 < i1) {
+            load(i + 1);
+            if (i + 2 < i1)
+                load_pages(i + 2);
+        }
+        const int t = i * kTokens;
+        const uint4 aw = *reinterpret_cast<const uint4*>(s.away);
+        const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w) == 0 && t + kTokens - 1 <= first &&
+                                                         (!a.window || t > last - a.window));
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            // scores: tokens 32 j + 8 (e / 4) + 4 h + e % 4 of row `col`
+            f32x16_t x;
+#pragma unroll
+            for (int e = 0; e < 16; ++e)
+                x[e] = 0.0f;
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                x = mfma32(*reinterpret_cast<const uint4*>(s.k + (32 * j + col) * D + (((2 * k + h) ^ (col & 7)) << 3)), qv[k], x);
+            uint32_t pk[8];
+            float sum, top;
+            auto weigh = [&] {
+                sum = top = 0.0f;
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const float4 sv = *reinterpret_cast<const float4*>(s.sv + 32 * j + 8 * g + 4 * h);
+                    const float v4[4] = {sv.x, sv.y, sv.z, sv.w};
+                    float w[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        const float ex = exp2_(x[4 * g + e] - m);
+                        w[e] = ex * v4[e];
+                        if (!full)
+                            w[e] = x[4 * g + e] == -INFINITY ? 0.0f : w[e];      // (the scale may be NaN)
+                        sum += ex;
+                    }
+                    top = fmaxf(fmaxf(top, fmaxf(w[0], w[1])), fmaxf(w[2], w[3]));
+                    pk[2 * g] = pack2(w[0], w[1]);
+                    pk[2 * g + 1] = pack2(w[2], w[3]);
+                }
+            };
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const int at = 32 * j + 8 * g + 4 * h;
+                const float4 sk = *reinterpret_cast<const float4*>(s.sk + at);
+                const float k4[4] = {sk.x, sk.y, sk.z, sk.w};
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v = x[4 * g + e] * k4[e];
+                    if (!full) {
+                        // what a row does not see weighs nothing, whatever lies there
+                        const int n = t + at + e;
+                        v = n <= pos && n >= low && k4[e] != INFINITY ? v : -INFINITY;
+                    }
+                    x[4 * g + e] = v;
+                }
+            }
+            weigh();
+            if (__ballot(top > kTop || sum > 16.0f * kTop * kLeast)) {
+                float best = kNone;
+#pragma unroll
+                for (int e = 0; e < 16; ++e)
+                    best = fmaxf(best, x[e] + log2_(fmaxf(s.sv[32 * j + 8 * (e >> 2) + 4 * h + (e & 3)], 1.0f / kLeast)));
+                best = fmaxf(best, __shfl_xor(best, 32, 64));
+                const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
+                m = mn;
+                l *= f;
+#pragma unroll
+                for (int d = 0; d < DT; ++d)
+                    o[d] *= f;
+                weigh();
+            }
+            l += sum;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const uint4 w = make_uint4(pk[4 * u], pk[4 * u + 1], pk[4 * u + 2], pk[4 * u + 3]);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    const int dim = 32 * d + col, piece = 2 * (2 * j + u) + h;
+                    uint4 v = *reinterpret_cast<const uint4*>(s.v + dim * kTokens + ((piece ^ (dim & 7) ^ ((dim >> 3) & 7)) << 3));
+                    if (32 * d >= 64)
+                        v = make_uint4(v.z, v.w, v.x, v.y);
+                    o[d] = mfma32(v, w, o[d]);
+                }
+            }
+        }
+        if (i + 1 < i1)
+            put(stage[(i + 1 - i0) & 1]);
+        __syncthreads();
+    }
+    l += __shfl_xor(l, 32, 64);
+    if (bad && l != 0.0f)
+        l = NAN;
+
+    const int g = head * a.G + row % a.G;
+    uint16_t* y = a.y + (long)(q.row0 + tok) * a.ldy + (long)g * D;
+    if (shares == 1) {
+        const float f = row_factor(a, g, m, l);
+        if (r < rows)
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float v[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        v[k] = l == 0.0f ? 0.0f : o[d][4 * e + k] * f;
+                    store4(y + 32 * d + 8 * e + 4 * h, v, a.bf);
+                }
+        return;
+    }
+    // parts of an item: [128][D], then m and l of the rows; the last to come joins them
+    typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+    const int item = nth * Hk + head;
+    const size_t place = (size_t)kTileRows * (D + 2) * 4;
+    uint8_t* parts = reinterpret_cast<uint8_t*>(a.part) + (size_t)item * shares * place;
+    const Rsrc rp = rsrc(parts, (uint32_t)(place * shares));
+    const uint32_t mine = (uint32_t)(part * place);
+    if (r < rows) {
+#pragma unroll
+        for (int d = 0; d < DT; ++d)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const w4 u = {__float_as_uint(o[d][4 * e]), __float_as_uint(o[d][4 * e + 1]), __float_as_uint(o[d][4 * e + 2]),
+                              __float_as_uint(o[d][4 * e + 3])};
+                __builtin_amdgcn_raw_buffer_store_b128(u, rp, mine + (uint32_t)(r * D + 32 * d + 8 * e + 4 * h) * 4u, 0, kDevice);
+            }
+        if (h == 0) {
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(m), rp, mine + (uint32_t)(kTileRows * D + r) * 4u, 0, kDevice);
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(l), rp, mine + (uint32_t)(kTileRows * (D + 1) + r) * 4u, 0, kDevice);
+        }
+    }
+    __asm__ volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __syncthreads();
+    if (tid == 0)
+        arrived = __hip_atomic_fetch_add(a.done + item, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    if (arrived != (uint32_t)shares - 1u)
+        return;
+    if (tid == 0)
+        __hip_atomic_store(a.done + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    for (int c = tid; c < rows * (D / 4); c += 256) {
+        const int jr = c / (D / 4), d = 4 * (c % (D / 4)), rr = tile * kTileRows + jr, gg = head * a.G + rr % a.G;
+        float mm = kNone, ls = 0.0f, v[4] = {0, 0, 0, 0};
+        for (int p0 = 0; p0 < shares; p0 += 4) {
+            w4 u[4];
+            float pm[4], pl[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const uint32_t at = (uint32_t)(min(p0 + k, shares - 1) * place);
+                u[k] = __builtin_amdgcn_raw_buffer_load_b128(rp, at + (uint32_t)(jr * D + d) * 4u, 0, kDevice);
+                pm[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at + (uint32_t)(kTileRows * D + jr) * 4u, 0, kDevice));
+                pl[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at + (uint32_t)(kTileRows * (D + 1) + jr) * 4u, 0, kDevice));
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (p0 + k < shares) {
+                    const float mn = fmaxf(mm, pm[k]), f0 = exp2_(mm - mn), f1 = exp2_(pm[k] - mn);
+                    mm = mn;
+                    ls = ls * f0 + pl[k] * f1;
+#pragma unroll
+                    for (int x = 0; x < 4; ++x)
+                        v[x] = v[x] * f0 + __uint_as_float(u[k][x]) * f1;
+                }
+        }
+        const float f = row_factor(a, gg, mm, ls);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = ls == 0.0f ? 0.0f : v[k] * f;
+        store4(a.y + (long)(q.row0 + rr / a.G) * a.ldy + (long)gg * D + d, v, a.bf);
+    }
+}
+
+int rows_target() { return plan_cus() * 2; }
+
+template <int D>
+hipError_t launch(const AttnArgs& a, int limit, hipStream_t st) {
+    const size_t lds = 2 * sizeof(Stage<D>) + (size_t)a.B * sizeof(Known<int32_t>);
+    const hipError_t e = set_lds(rows_kernel<D>, lds + 1024);
+    if (e != hipSuccess)
+        return e;
+    // tiles of the requests at most: each may have one that is not full
+    const int most = ((int)((long)a.T * a.G / kTileRows) + (a.B < a.T ? a.B : a.T)) * a.cache.heads;
+    rows_kernel<D><<<most > rows_target() ? most : rows_target(), 256, lds, st>>>(a, limit, rows_target());
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t kv_rows_bytes(int D) { return (size_t)rows_target() * kTileRows * (D + 2) * 4; }
+
+hipError_t launch_kv_rows(const AttnArgs& a, int limit, hipStream_t st) {
+    return a.D == 128 ? launch<128>(a, limit, st) : launch<64>(a, limit, st);
+}
+
+}  // namespace qmlp

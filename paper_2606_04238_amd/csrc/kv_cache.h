@@ -59,6 +59,9 @@ struct AttnArgs {
 };
 constexpr size_t kCounters = 16384;           // bytes of counters at the workspace's start
 size_t kv_attention_bytes(int D, int G, int max_new);
+// The kernel for many rows: requests of more than `limit` rows; its part of the workspace.
+hipError_t launch_kv_rows(const AttnArgs& a, int limit, hipStream_t st);
+size_t kv_rows_bytes(int D);
 hipError_t launch_kv_attention(const AttnArgs& a, int max_new, hipStream_t st);
 
 }  // namespace qmlp
