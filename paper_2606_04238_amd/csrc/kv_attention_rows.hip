@@ -18,30 +18,22 @@
 namespace qmlp {
 namespace {
 
-constexpr int kTileRows = 128, kTokens = 64, kMostShares = 16;
+constexpr int kWaves = 8, kTileRows = 32 * kWaves, kThreads = 64 * kWaves, kMostShares = 16;
 
 template <int D>
-struct Stage {
-    uint16_t k[kTokens * D];
-    uint16_t v[D * kTokens];
-    float sk[kTokens], sv[kTokens];
-    uint32_t away[4];                                     // nonzero: a wave met tokens that are not there
-};
-
-// What a thread stages: a piece of K (4 words of a token) and of V (a word of 4 tokens), with their (scale, zero); at
-// D = 64 one of the two.
-template <int D>
-struct Piece {
-    static constexpr bool both = D == 128;
-    uint4 k, v, vm;
-    uint32_t km;
+struct __attribute__((aligned(256))) Stage {
+    static constexpr int tokens = 8192 / D;               // of a step: 64 or 128
+    uint16_t k[tokens * D];
+    uint16_t v[D * tokens];
+    float sk[tokens], sv[tokens];
+    uint32_t away[kWaves];                                // nonzero: a wave met tokens that are not there
 };
 
 template <int D>
-__global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int target) {
-    constexpr int KS = D / 16, DT = D / 32;
+__global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit, int target) {
+    constexpr int KS = D / 16, DT = D / 32, kTokens = Stage<D>::tokens;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    __shared__ uint32_t arrived, tops[4];
+    __shared__ uint32_t arrived, tops[kWaves];
     Stage<D>* stage = reinterpret_cast<Stage<D>*>(smem);
     Known<int32_t>* known = reinterpret_cast<Known<int32_t>*>(smem + 2 * sizeof(Stage<D>));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
@@ -51,7 +43,7 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
         const long rows = (long)q.n * a.G;
         return rows <= limit ? 0 : (int)((rows + kTileRows - 1) / kTileRows);
     };
-    const int tiles = prefix_work<256, int32_t>(a, known, [&](const Request& q) { return tiles_of(q); });
+    const int tiles = prefix_work<kThreads, int32_t>(a, known, [&](const Request& q) { return tiles_of(q); });
     const int items = tiles * Hk;
     // few items: the tokens of each are shared by several workgroups
     const int shares = items ? min(max(target / items, 1), kMostShares) : 1;
@@ -68,7 +60,10 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
     const int all = max(0, last / kTokens + 1 - low0);    // steps of the tile (last < 0: none)
     const int i0 = low0 + (int)((long)all * part / shares), i1 = low0 + (last < 0 ? 0 : (int)((long)all * (part + 1) / shares));
 
-    // this lane's row
+    // the wave's rows' positions, and this lane's row
+    const int wrows = min(rows - wave * 32, 32);
+    const int wfirst = q.len - q.n + (tile * kTileRows + wave * 32) / a.G;
+    const int wlast = wrows > 0 ? q.len - q.n + (tile * kTileRows + wave * 32 + wrows - 1) / a.G : -1;
     const int r = wave * 32 + col, row = tile * kTileRows + r, tok = row / a.G;
     const int pos = r < rows ? q.len - q.n + tok : -1;
     const int low = a.window ? max(0, pos - a.window + 1) : 0;
@@ -80,50 +75,38 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
             qv[i] = r < rows ? *reinterpret_cast<const uint4*>(src + 16 * i) : make_uint4(0, 0, 0, 0);
     }
 
-    // staging
-    const bool has_k = Piece<D>::both || tid < 128, has_v = Piece<D>::both || tid >= 128;
-    const int ktok = D == 128 ? tid >> 2 : (tid & 127) >> 1, kc = D == 128 ? tid & 3 : tid & 1;
-    const int vquad = D == 128 ? tid >> 4 : (tid & 127) >> 3, vword = D == 128 ? tid & 15 : tid & 7;
-    int kpage = 0, vpage = 0;                             // page numbers of the step to be loaded next
-    auto load_pages = [&](int i) {
-        const int32_t* t = a.table + (long)b * a.W;
-        if (has_k)
-            kpage = t[min((i * kTokens + ktok) >> lg, a.W - 1)];
-        if (has_v)
-            vpage = t[min((i * kTokens + 4 * vquad) >> lg, a.W - 1)];
-    };
-    Piece<D> p;
-    bool kthere = false;
-    int vthere = 0;                                       // tokens of the quad that are there
+    // staging: a thread of the lower four waves takes 4 words of a token of K, one of the upper four a word of 4 tokens of V
+    const bool takes_k = wave < 4;
+    const int sid = tid & 255;
+    const int ktok = D == 128 ? sid >> 2 : sid >> 1, kc = D == 128 ? sid & 3 : sid & 1;
+    const int vquad = D == 128 ? sid >> 4 : sid >> 3, vword = D == 128 ? sid & 15 : sid & 7;
+    const int mine0 = takes_k ? ktok : 4 * vquad;         // the first token of it
+    int page = 0;                                         // page number of the step to be loaded next
+    auto load_pages = [&](int i) { page = a.table[(long)b * a.W + min((i * kTokens + mine0) >> lg, a.W - 1)]; };
+    uint4 codes, meta;                                    // (meta of K: one token's, in x)
+    int there = 0;                                        // how many of its tokens are there
     auto load = [&](int i) {
-        const uint32_t side = a.cache.side(D), codes = (uint32_t)(D / 2) << lg, in = (1u << lg) - 1u;
-        if (has_k) {
-            const int t = i * kTokens + ktok;
-            kthere = t < q.len && (uint32_t)kpage < (uint32_t)a.cache.pages;
-            const uint8_t* base = a.cache.at(D, kthere ? kpage : 0, head);
-            const uint32_t o = (uint32_t)t & in;
-            p.k = *reinterpret_cast<const uint4*>(base + o * (D / 2) + kc * 16);
-            p.km = *reinterpret_cast<const uint32_t*>(base + codes + o * 4u);
-        }
-        if (has_v) {
-            const int t = i * kTokens + 4 * vquad;
-            const bool there = (uint32_t)vpage < (uint32_t)a.cache.pages;
-            vthere = there ? min(max(q.len - t, 0), 4) : 0;
-            const uint8_t* base = a.cache.at(D, there ? vpage : 0, head) + side;
-            const uint32_t o = (uint32_t)t & in;
-            p.v = *reinterpret_cast<const uint4*>(base + o * (D / 2) + vword * 16);
-            p.vm = *reinterpret_cast<const uint4*>(base + codes + o * 4u);
-        }
+        const int t = i * kTokens + mine0;
+        const bool known_page = (uint32_t)page < (uint32_t)a.cache.pages;
+        there = known_page ? min(max(q.len - t, 0), takes_k ? 1 : 4) : 0;
+        const uint8_t* base = a.cache.at(D, known_page ? page : 0, head) + (takes_k ? 0u : a.cache.side(D));
+        const uint32_t o = (uint32_t)t & ((1u << lg) - 1u);
+        codes = *reinterpret_cast<const uint4*>(base + o * (D / 2) + (takes_k ? kc : vword) * 16);
+        base += ((uint32_t)(D / 2) << lg) + o * 4u;
+        if (takes_k)
+            meta.x = *reinterpret_cast<const uint32_t*>(base);
+        else
+            meta = *reinterpret_cast<const uint4*>(base);
     };
     float scale = 0.0f;                                   // of a raw score, with the power of two of q
     const uint32_t mv = magic64();
     auto put = [&](Stage<D>& s) {
-        if (has_k) {
-            const uint32_t m = kthere ? p.km : 0x3C00u;
+        if (takes_k) {
+            const uint32_t m = there ? meta.x : 0x3C00u;
             const uint32_t z = (m >> 16) | (m & 0xFFFF0000u), off = add2(z, mv) ^ 0x80008000u;        // -(64 + zero), twice
             // (threads of the upper half of a row begin with its second pair of words: see the banks above)
             const bool turn = D == 128 && (kc & 2);
-            const uint32_t w[4] = {turn ? p.k.z : p.k.x, turn ? p.k.w : p.k.y, turn ? p.k.x : p.k.z, turn ? p.k.y : p.k.w};
+            const uint32_t w[4] = {turn ? codes.z : codes.x, turn ? codes.w : codes.y, turn ? codes.x : codes.z, turn ? codes.y : codes.w};
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 uint32_t e[4];
@@ -133,21 +116,19 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                     make_uint4(add2(e[0], off), add2(e[1], off), add2(e[2], off), add2(e[3], off));
             }
             if (kc == 0)
-                s.sk[ktok] = kthere ? h2f(m & 0xFFFFu) * scale : INFINITY;      // (a scale is never infinite: not there)
-        }
-        if (has_v) {
+                s.sk[ktok] = there ? h2f(m & 0xFFFFu) * scale : INFINITY;       // (a scale is never infinite: not there)
+        } else {
             uint32_t m[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                m[i] = i < vthere ? comp(p.vm, i) : 0x3C00u;
+                m[i] = i < there ? comp(meta, i) : 0x3C00u;
             const uint32_t off[2] = {add2(highs(m[0], m[1]), mv) ^ 0x80008000u, add2(highs(m[2], m[3]), mv) ^ 0x80008000u};
-            const uint32_t src[4] = {p.v.x, p.v.y, p.v.z, p.v.w};
             uint32_t out[8][2];
 #pragma unroll
             for (int pr = 0; pr < 2; ++pr) {
                 uint32_t e[4], f[4];
-                pairs64(lows(src[2 * pr], src[2 * pr + 1]), mv, e);
-                pairs64(highs(src[2 * pr], src[2 * pr + 1]), mv, f);
+                pairs64(lows(comp(codes, 2 * pr), comp(codes, 2 * pr + 1)), mv, e);
+                pairs64(highs(comp(codes, 2 * pr), comp(codes, 2 * pr + 1)), mv, f);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     out[2 * i][pr] = add2(e[i], off[pr]);
@@ -163,10 +144,9 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                 *reinterpret_cast<float4*>(s.sv + 4 * vquad) =
                     make_float4(h2f(m[0] & 0xFFFFu), h2f(m[1] & 0xFFFFu), h2f(m[2] & 0xFFFFu), h2f(m[3] & 0xFFFFu));
         }
-        const bool gone = (has_k && !kthere) || (has_v && vthere < 4);
-        const uint64_t any = __ballot(gone);
+        const uint64_t gone = __ballot(there < (takes_k ? 1 : 4));
         if (lane == 0)
-            s.away[wave] = any != 0;
+            s.away[wave] = gone != 0;
     };
 
     f32x16_t o[DT];
@@ -190,14 +170,20 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                                        if (lane == 0)
                                            tops[wave] = top;
                                        __syncthreads();
-                                       return max(max(tops[0], tops[1]), max(tops[2], tops[3]));
+                                       #pragma unroll
+                                       for (int w = 0; w < kWaves; ++w)
+                                           top = max(top, tops[w]);
+                                       return top;
                                    });
     const bool bad = qsum != qsum;                        // an infinity or NaN in the row
     if (i0 < i1)
         put(stage[0]);
     __syncthreads();
 
+    const uint32_t kplace = (uint32_t)(col * D * 2 + ((h ^ (col & 7)) << 4));
+    const uint32_t vplace = (uint32_t)(offsetof(Stage<D>, v) + col * kTokens * 2 + ((h ^ (col & 7) ^ (col >> 3)) << 4));
     for (int i = i0; i < i1; ++i) {
+        const uint32_t stage_at = (uint32_t)(((i - i0) & 1) * sizeof(Stage<D>));
         const Stage<D>& s = stage[(i - i0) & 1];
         if (i + 1 < i1) {
             load(i + 1);
@@ -205,11 +191,16 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                 load_pages(i + 2);
         }
         const int t = i * kTokens;
-        const uint4 aw = *reinterpret_cast<const uint4*>(s.away);
-        const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w) == 0 && t + kTokens - 1 <= first &&
-                                                         (!a.window || t > last - a.window));
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        const uint4 aw = *reinterpret_cast<const uint4*>(s.away), aw2 = *reinterpret_cast<const uint4*>(s.away + 4);
+        const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w | aw2.x | aw2.y | aw2.z | aw2.w) == 0 &&
+                                                         t + kTokens - 1 <= wfirst && (!a.window || t > wlast - a.window));
+        if (t <= wlast) {
+#pragma unroll 2
+        for (int j = 0; j < kTokens / 32; ++j) {
+            // (places in LDS are formed anew from one number each: kept apart they would take the registers)
+            uint32_t kat = stage_at + kplace + (uint32_t)j * 64u * D, vat = (stage_at + vplace) ^ (uint32_t)(j << 6);
+            pin(kat);
+            pin(vat);
             // scores: tokens 32 j + 8 (e / 4) + 4 h + e % 4 of row `col`
             f32x16_t x;
 #pragma unroll
@@ -217,10 +208,26 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                 x[e] = 0.0f;
 #pragma unroll
             for (int k = 0; k < KS; ++k)
-                x = mfma32(*reinterpret_cast<const uint4*>(s.k + (32 * j + col) * D + (((2 * k + h) ^ (col & 7)) << 3)), qv[k], x);
+                x = mfma32(*reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(k << 5))), qv[k], x);
             uint32_t pk[8];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                const float4 sk = *reinterpret_cast<const float4*>(s.sk + 32 * j + 8 * g + 4 * h);
+                x[4 * g] *= sk.x;
+                x[4 * g + 1] *= sk.y;
+                x[4 * g + 2] *= sk.z;
+                x[4 * g + 3] *= sk.w;
+            }
+            if (!full) {
+                // what a row does not see weighs nothing, whatever lies there
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3), n = t + at;
+                    x[e] = n <= pos && n >= low && s.sk[at] != INFINITY ? x[e] : -INFINITY;
+                }
+            }
             float sum, top;
-            auto weigh = [&] {
+            auto weigh = [&](auto masked) {
                 sum = top = 0.0f;
 #pragma unroll
                 for (int g = 0; g < 4; ++g) {
@@ -231,7 +238,7 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                     for (int e = 0; e < 4; ++e) {
                         const float ex = exp2_(x[4 * g + e] - m);
                         w[e] = ex * v4[e];
-                        if (!full)
+                        if constexpr (decltype(masked)::value)
                             w[e] = x[4 * g + e] == -INFINITY ? 0.0f : w[e];      // (the scale may be NaN)
                         sum += ex;
                     }
@@ -240,23 +247,10 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                     pk[2 * g + 1] = pack2(w[2], w[3]);
                 }
             };
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const int at = 32 * j + 8 * g + 4 * h;
-                const float4 sk = *reinterpret_cast<const float4*>(s.sk + at);
-                const float k4[4] = {sk.x, sk.y, sk.z, sk.w};
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    float v = x[4 * g + e] * k4[e];
-                    if (!full) {
-                        // what a row does not see weighs nothing, whatever lies there
-                        const int n = t + at + e;
-                        v = n <= pos && n >= low && k4[e] != INFINITY ? v : -INFINITY;
-                    }
-                    x[4 * g + e] = v;
-                }
-            }
-            weigh();
+            if (full)
+                weigh(std::false_type{});
+            else
+                weigh(std::true_type{});
             if (__ballot(top > kTop || sum > 16.0f * kTop * kLeast)) {
                 float best = kNone;
 #pragma unroll
@@ -269,7 +263,7 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
 #pragma unroll
                 for (int d = 0; d < DT; ++d)
                     o[d] *= f;
-                weigh();
+                weigh(std::true_type{});
             }
             l += sum;
 #pragma unroll
@@ -277,13 +271,14 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                 const uint4 w = make_uint4(pk[4 * u], pk[4 * u + 1], pk[4 * u + 2], pk[4 * u + 3]);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
-                    const int dim = 32 * d + col, piece = 2 * (2 * j + u) + h;
-                    uint4 v = *reinterpret_cast<const uint4*>(s.v + dim * kTokens + ((piece ^ (dim & 7) ^ ((dim >> 3) & 7)) << 3));
+                    // piece 2 (2 j + u) + h of dim 32 d + col
+                    uint4 v = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)(u << 5 | (d & 1) << 6)) + d * 64 * kTokens);
                     if (32 * d >= 64)
                         v = make_uint4(v.z, v.w, v.x, v.y);
                     o[d] = mfma32(v, w, o[d]);
                 }
             }
+        }
         }
         if (i + 1 < i1)
             put(stage[(i + 1 - i0) & 1]);
@@ -310,7 +305,7 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
                 }
         return;
     }
-    // parts of an item: [128][D], then m and l of the rows; the last to come joins them
+    // parts of an item: [rows][D], then m and l of the rows; the last to come joins them
     typedef uint32_t w4 __attribute__((ext_vector_type(4)));
     const int item = nth * Hk + head;
     const size_t place = (size_t)kTileRows * (D + 2) * 4;
@@ -340,7 +335,7 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
         return;
     if (tid == 0)
         __hip_atomic_store(a.done + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    for (int c = tid; c < rows * (D / 4); c += 256) {
+    for (int c = tid; c < rows * (D / 4); c += kThreads) {
         const int jr = c / (D / 4), d = 4 * (c % (D / 4)), rr = tile * kTileRows + jr, gg = head * a.G + rr % a.G;
         float mm = kNone, ls = 0.0f, v[4] = {0, 0, 0, 0};
         for (int p0 = 0; p0 < shares; p0 += 4) {
@@ -372,7 +367,7 @@ __global__ void __launch_bounds__(256, 2) rows_kernel(AttnArgs a, int limit, int
     }
 }
 
-int rows_target() { return plan_cus() * 2; }
+int rows_target() { return plan_cus(); }
 
 template <int D>
 hipError_t launch(const AttnArgs& a, int limit, hipStream_t st) {
@@ -382,7 +377,7 @@ hipError_t launch(const AttnArgs& a, int limit, hipStream_t st) {
         return e;
     // tiles of the requests at most: each may have one that is not full
     const int most = ((int)((long)a.T * a.G / kTileRows) + (a.B < a.T ? a.B : a.T)) * a.cache.heads;
-    rows_kernel<D><<<most > rows_target() ? most : rows_target(), 256, lds, st>>>(a, limit, rows_target());
+    rows_kernel<D><<<most > rows_target() ? most : rows_target(), kThreads, lds, st>>>(a, limit, rows_target());
     return hipGetLastError();
 }
 
