@@ -49,11 +49,59 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     const int shares = items ? min(max(target / items, 1), kMostShares) : 1;
     if ((int)blockIdx.x >= items * shares)
         return;
-    // neighbouring workgroups (on different XCDs) take different K/V heads; the last tiles of a request, which see most, first
+    // neighbouring workgroups (on different XCDs) take different K/V heads; tiles go by the tokens before their end,
+    // most first, so that the last to be handed out are short (ties: by request)
     const int head = (int)blockIdx.x % Hk, rest = (int)blockIdx.x / Hk, part = rest % shares, nth = rest / shares;
-    const int b = __builtin_amdgcn_readfirstlane(request_of(known, a.B, nth));
+    // tiles of a request with at least s steps before their end
+    auto longer = [&](const Request& q, int s) {
+        const int x = (s - 1) * kTokens - (q.len - q.n), nt = tiles_of(q);
+        return nt == 0 || x > q.n - 1 ? 0 : x <= 0 ? nt : nt - (int)((long)x * a.G / kTileRows);
+    };
+    auto count = [&](int s) {
+        int c = 0;
+        for (int i = lane; i < a.B; i += 64)
+            c += longer(known[i].q, s);
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1)
+            c += __shfl_xor(c, d, 64);
+        return __builtin_amdgcn_readfirstlane(c);
+    };
+    // the most steps that more than nth tiles have, and which of the tiles with just that many
+    // (a request with fewer tokens than rows begins before 0)
+    int lo = -(a.T / kTokens) - 2, hi = (a.W << lg) / kTokens + 2;          // count(lo) > nth >= count(hi)
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (count(mid) > nth)
+            lo = mid;
+        else
+            hi = mid;
+    }
+    int left = nth - count(hi), b = 0, tile = 0;
+    for (int b0 = 0; b0 < a.B; b0 += 64) {
+        int c = 0, c1 = 0;
+        if (b0 + lane < a.B) {
+            c1 = longer(known[b0 + lane].q, hi);
+            c = longer(known[b0 + lane].q, lo) - c1;
+        }
+        int before = c;
+#pragma unroll
+        for (int d = 1; d < 64; d <<= 1) {
+            const int o = __shfl_up(before, d, 64);
+            before += lane >= d ? o : 0;
+        }
+        const int all = __builtin_amdgcn_readlane(before, 63);
+        before -= c;
+        if (left < all) {
+            const int src = __builtin_ctzll(__ballot(left >= before && left < before + c));
+            b = b0 + src;
+            tile = __builtin_amdgcn_readlane(c1, src) + left - __builtin_amdgcn_readlane(before, src);      // from the last
+            break;
+        }
+        left -= all;
+    }
+    b = __builtin_amdgcn_readfirstlane(b);
     const Request q = known[b].uniform();
-    const int nt = tiles_of(q), tile = nt - 1 - (nth - __builtin_amdgcn_readfirstlane(known[b].before));
+    tile = tiles_of(q) - 1 - tile;
     const int rows = min((int)((long)q.n * a.G - (long)tile * kTileRows), kTileRows);
     const int first = q.len - q.n + tile * kTileRows / a.G, last = q.len - q.n + (tile * kTileRows + rows - 1) / a.G;   // positions
     const int low0 = a.window ? max(0, first - a.window + 1) / kTokens : 0;
