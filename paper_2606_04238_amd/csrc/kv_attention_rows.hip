@@ -31,7 +31,7 @@ struct __attribute__((aligned(256))) Stage {
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit, int target) {
-    constexpr int KS = D / 16, DT = D / 32, kTokens = Stage<D>::tokens;
+    constexpr int KS = D / 16, DT = D / 32, kTokens = Stage<D>::tokens, TJ = kTokens / 32;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     __shared__ uint32_t arrived, tops[kWaves];
     Stage<D>* stage = reinterpret_cast<Stage<D>*>(smem);
@@ -224,8 +224,14 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
                                        return top;
                                    });
     const bool bad = qsum != qsum;                        // an infinity or NaN in the row
-    if (i0 < i1)
+    if (i0 < i1) {
         put(stage[0]);
+        if (i0 + 1 < i1) {
+            load(i0 + 1);
+            if (i0 + 2 < i1)
+                load_pages(i0 + 2);
+        }
+    }
     __syncthreads();
 
     const uint32_t kplace = (uint32_t)(col * D * 2 + ((h ^ (col & 7)) << 4));
@@ -233,103 +239,150 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     for (int i = i0; i < i1; ++i) {
         const uint32_t stage_at = (uint32_t)(((i - i0) & 1) * sizeof(Stage<D>));
         const Stage<D>& s = stage[(i - i0) & 1];
-        if (i + 1 < i1) {
-            load(i + 1);
-            if (i + 2 < i1)
-                load_pages(i + 2);
-        }
         const int t = i * kTokens;
         const uint4 aw = *reinterpret_cast<const uint4*>(s.away), aw2 = *reinterpret_cast<const uint4*>(s.away + 4);
         const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w | aw2.x | aw2.y | aw2.z | aw2.w) == 0 &&
                                                          t + kTokens - 1 <= wfirst && (!a.window || t > wlast - a.window));
+        // the next step goes to the other stage, and the one after it is asked for
+        if (i + 1 < i1) {
+            put(stage[(i + 1 - i0) & 1]);
+            if (i + 2 < i1) {
+                load(i + 2);
+                if (i + 3 < i1)
+                    load_pages(i + 3);
+            }
+        }
         if (t <= wlast) {
-#pragma unroll 2
-        for (int j = 0; j < kTokens / 32; ++j) {
+            // Tiles of 32 tokens.  While a tile's weights are formed on the vector units, the matrix cores have the next
+            // tile's scores and the last one's output: a wave issues in order, so their instructions alternate.  Their first
+            // operands come from LDS two turns ahead, the scales half a tile.
+            f32x16_t x[2];                                // scores, tokens 32 j + 8 (e / 4) + 4 h + e % 4 of row `col`
+            uint32_t pk[2][8];                            // weights times scales
+            uint4 kf[3], vf[3];
+            float4 sk[2], sv[2];
             // (places in LDS are formed anew from one number each: kept apart they would take the registers)
-            uint32_t kat = stage_at + kplace + (uint32_t)j * 64u * D, vat = (stage_at + vplace) ^ (uint32_t)(j << 6);
-            pin(kat);
-            pin(vat);
-            // scores: tokens 32 j + 8 (e / 4) + 4 h + e % 4 of row `col`
-            f32x16_t x;
-#pragma unroll
-            for (int e = 0; e < 16; ++e)
-                x[e] = 0.0f;
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-                x = mfma32(*reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(k << 5))), qv[k], x);
-            uint32_t pk[8];
-#pragma unroll
-            for (int g = 0; g < 4; ++g) {
-                const float4 sk = *reinterpret_cast<const float4*>(s.sk + 32 * j + 8 * g + 4 * h);
-                x[4 * g] *= sk.x;
-                x[4 * g + 1] *= sk.y;
-                x[4 * g + 2] *= sk.z;
-                x[4 * g + 3] *= sk.w;
-            }
-            if (!full) {
-                // what a row does not see weighs nothing, whatever lies there
-#pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3), n = t + at;
-                    x[e] = n <= pos && n >= low && s.sk[at] != INFINITY ? x[e] : -INFINITY;
-                }
-            }
-            float sum, top;
-            auto weigh = [&](auto masked) {
-                sum = top = 0.0f;
-#pragma unroll
-                for (int g = 0; g < 4; ++g) {
-                    const float4 sv = *reinterpret_cast<const float4*>(s.sv + 32 * j + 8 * g + 4 * h);
-                    const float v4[4] = {sv.x, sv.y, sv.z, sv.w};
-                    float w[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const float ex = exp2_(x[4 * g + e] - m);
-                        w[e] = ex * v4[e];
-                        if constexpr (decltype(masked)::value)
-                            w[e] = x[4 * g + e] == -INFINITY ? 0.0f : w[e];      // (the scale may be NaN)
-                        sum += ex;
-                    }
-                    top = fmaxf(fmaxf(top, fmaxf(w[0], w[1])), fmaxf(w[2], w[3]));
-                    pk[2 * g] = pack2(w[0], w[1]);
-                    pk[2 * g + 1] = pack2(w[2], w[3]);
+            uint32_t kat = stage_at + kplace, vat = stage_at + vplace, sat = stage_at + (uint32_t)offsetof(Stage<D>, sk) + 16u * h;
+            // turn n: step k of tile n / KS's scores, and of the output of the tile two before it
+            auto fetch = [&](int n) {
+                const int j = n / KS, k = n % KS, u = k / DT, d = k % DT;
+                if (j < TJ)
+                    kf[n % 3] = *reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(k << 5)) + j * 64 * D);
+                if (j >= 2 && j - 2 < TJ)                 // piece 2 (2 (j - 2) + u) + h of dim 32 d + col
+                    vf[n % 3] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)((j - 2) << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
+            };
+            auto scales = [&](int g) {                    // of tokens 8 g + 4 h ..
+                if (g < 4 * TJ) {
+                    sk[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 32 * g);
+                    sv[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 32 * g + 4 * kTokens);
                 }
             };
-            if (full)
-                weigh(std::false_type{});
-            else
-                weigh(std::true_type{});
-            if (__ballot(top > kTop || sum > 16.0f * kTop * kLeast)) {
-                float best = kNone;
+            auto turn = [&](int n) {
+                const int j = n / KS, k = n % KS, u = k / DT, d = k % DT;
+                fetch(n + 2);
+                if (j < TJ) {
+                    f32x16_t& y = x[j & 1];
+                    if (k == 0) {
 #pragma unroll
-                for (int e = 0; e < 16; ++e)
-                    best = fmaxf(best, x[e] + log2_(fmaxf(s.sv[32 * j + 8 * (e >> 2) + 4 * h + (e & 3)], 1.0f / kLeast)));
-                best = fmaxf(best, __shfl_xor(best, 32, 64));
-                const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
-                m = mn;
-                l *= f;
-#pragma unroll
-                for (int d = 0; d < DT; ++d)
-                    o[d] *= f;
-                weigh(std::true_type{});
-            }
-            l += sum;
-#pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const uint4 w = make_uint4(pk[4 * u], pk[4 * u + 1], pk[4 * u + 2], pk[4 * u + 3]);
-#pragma unroll
-                for (int d = 0; d < DT; ++d) {
-                    // piece 2 (2 j + u) + h of dim 32 d + col
-                    uint4 v = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)(u << 5 | (d & 1) << 6)) + d * 64 * kTokens);
-                    if (32 * d >= 64)
-                        v = make_uint4(v.z, v.w, v.x, v.y);
-                    o[d] = mfma32(v, w, o[d]);
+                        for (int e = 0; e < 16; ++e)
+                            y[e] = 0.0f;
+                    }
+                    y = mfma32(kf[n % 3], qv[k], y);
                 }
+                if (j >= 2) {
+                    const uint4 v = 32 * d >= 64 ? make_uint4(vf[n % 3].z, vf[n % 3].w, vf[n % 3].x, vf[n % 3].y) : vf[n % 3];
+                    const uint32_t(&w)[8] = pk[j & 1];
+                    o[d] = mfma32(v, make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]), o[d]);
+                }
+            };
+            fetch(0);
+            fetch(1);
+            scales(0);
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                turn(k);
+#pragma unroll
+            for (int j = 0; j < TJ; ++j) {
+                f32x16_t& xj = x[j & 1];
+                uint32_t(&pj)[8] = pk[j & 1];
+                float sum = 0.0f;
+                uint32_t top = 0;                         // of the rounded weights, two by two
+                // weights of two tokens, scores times their scales (or, where they have been seen to, as they are)
+                auto weigh2 = [&](int e, const float4& ks, const float4& vs, auto raw) {
+                    const float ka = e & 2 ? ks.z : ks.x, kb = e & 2 ? ks.w : ks.y, va = e & 2 ? vs.z : vs.x, vb = e & 2 ? vs.w : vs.y;
+                    float ea, eb, wa, wb;
+                    if constexpr (decltype(raw)::value) {
+                        ea = exp2_(__builtin_fmaf(xj[e], ka, -m));
+                        eb = exp2_(__builtin_fmaf(xj[e + 1], kb, -m));
+                        wa = ea * va;
+                        wb = eb * vb;
+                    } else {
+                        ea = exp2_(xj[e] - m);
+                        eb = exp2_(xj[e + 1] - m);
+                        wa = xj[e] == -INFINITY ? 0.0f : ea * va;            // (the scale may be NaN)
+                        wb = xj[e + 1] == -INFINITY ? 0.0f : eb * vb;
+                    }
+                    sum += ea + eb;
+                    pj[e >> 1] = pack2(wa, wb);
+                    top = max2(top, pj[e >> 1]);
+                };
+                auto weigh = [&] {                        // all of them, as they are
+                    sum = 0.0f;
+                    top = 0;
+#pragma unroll
+                    for (int e = 0; e < 16; e += 2)
+                        weigh2(e, float4{}, *reinterpret_cast<const float4*>(s.sv + 32 * j + 8 * (e >> 2) + 4 * h), std::false_type{});
+                };
+                pin(kat);
+                pin(vat);
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    turn((j + 1) * KS + k);
+                    constexpr int per = 16 / KS;          // weights of a turn
+                    if (per * k % 4 == 0)
+                        scales(4 * j + per * k / 4 + 1);
+#pragma unroll
+                    for (int e = per * k; e < per * (k + 1); e += 2)
+                        weigh2(e, sk[(e >> 2) & 1], sv[(e >> 2) & 1], std::true_type{});
+                    // (they stay here, and are not put off to where it is known that every token is seen)
+                    pin(top);
+                    __asm__ volatile("" : "+v"(sum));
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+                if (!full) {
+                    // what a row does not see weighs nothing, whatever lies there
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3), n = t + at;
+                        const float k1 = s.sk[at];
+                        xj[e] = n <= pos && n >= low && k1 != INFINITY ? xj[e] * k1 : -INFINITY;
+                    }
+                    weigh();
+                }
+                // (a weight that passes binary16 is infinite there)
+                if (__ballot(h2f(top & 0xFFFFu) > kTop || h2f(top >> 16) > kTop || sum > 16.0f * kTop * kLeast)) {
+                    float best = kNone;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
+                        if (full)
+                            xj[e] *= s.sk[at];
+                        best = fmaxf(best, xj[e] + log2_(fmaxf(s.sv[at], 1.0f / kLeast)));
+                    }
+                    best = fmaxf(best, __shfl_xor(best, 32, 64));
+                    const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
+                    m = mn;
+                    l *= f;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+                        o[d] *= f;
+                    weigh();
+                }
+                l += sum;
             }
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+                turn((TJ + 1) * KS + k);
         }
-        }
-        if (i + 1 < i1)
-            put(stage[(i + 1 - i0) & 1]);
         __syncthreads();
     }
     l += __shfl_xor(l, 32, 64);

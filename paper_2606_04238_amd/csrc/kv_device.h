@@ -66,6 +66,9 @@ __device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __bui
 __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, (half2_t)(__builtin_bit_cast(half2_t, a) + __builtin_bit_cast(half2_t, b)));
 }
+__device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(half2_t, a), __builtin_bit_cast(half2_t, b)));
+}
 __device__ __forceinline__ uint32_t comp(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
 // fp32 as the sum of three bfloat16 numbers (24 bits): what the matrix cores multiply by small integers exactly.
