@@ -581,7 +581,7 @@ size_t qmlp_kv_cache_bytes(int pages, int kv_heads, int head_dim, int page);
  * ended request too, and stack places that nothing is pushed to: the same
  * call on the same lens and n_free gives the same again.
  * lens outside [0, W page] and n_free outside [0, N] are taken as the nearest number inside.
- * 0 <= B <= 4096, 1 <= W <= 2^20, W * page <= 2^30, 0 <= N, 0 <= tokens <= 2^24.  One launch
+ * 0 <= B <= 2048, 1 <= W <= 2^20, W * page <= 2^30, 0 <= N, 0 <= tokens <= 2^24.  One launch
  * (none with B = 0: nothing is written).
  */
 qmlp_status qmlp_kv_plan(const int32_t *lens, const int32_t *new_tokens, int B, int page, int32_t *table, int W,
@@ -650,7 +650,7 @@ qmlp_status qmlp_kv_read(const qmlp_kv_cache *cache, const int32_t *slots, int T
  * see them NaN and no others.
  * max_new: the most new tokens of any request, as far as the host knows.  It chooses kernels and sizes
  * the workspace; a request with more is computed all the same, slower.
- * heads a multiple of kv_heads, 0 <= B <= 4096, 0 <= T <= 2^20, 1 <= W, W * page <= 2^30, scale finite,
+ * heads a multiple of kv_heads, 0 <= B <= 2048, 0 <= T <= 2^20, 1 <= W, W * page <= 2^30, scale finite,
  * window >= 0.
  * ws: qmlp_kv_attention_workspace_bytes(...) of this or a larger max_new, ZERO before its first call (and after
  * a call that failed); each call leaves it ready for the next, of any shape it is large enough for.  One call at

@@ -32,10 +32,11 @@ struct __attribute__((aligned(256))) Stage {
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit, int target) {
     constexpr int KS = D / 16, DT = D / 32, kTokens = Stage<D>::tokens, TJ = kTokens / 32;
+    using St = Stage<D>;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
     __shared__ uint32_t arrived, tops[kWaves];
     Stage<D>* stage = reinterpret_cast<Stage<D>*>(smem);
-    Known<int32_t>* known = reinterpret_cast<Known<int32_t>*>(smem + 2 * sizeof(Stage<D>));
+    Known<int32_t>* known = reinterpret_cast<Known<int32_t>*>(smem + 3 * sizeof(Stage<D>));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
     const int lg = a.cache.page_log2, Hk = a.cache.heads;
 
@@ -224,167 +225,202 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
                                        return top;
                                    });
     const bool bad = qsum != qsum;                        // an infinity or NaN in the row
+
+    // Three stages: at step i the matrix cores read stages i and i + 1 and, in the step's first turns, i - 1, whose
+    // place stage i + 2 then takes.  One meeting of the waves a step, after those turns.
     if (i0 < i1) {
         put(stage[0]);
         if (i0 + 1 < i1) {
             load(i0 + 1);
-            if (i0 + 2 < i1)
+            put(stage[1]);
+            if (i0 + 2 < i1) {
                 load_pages(i0 + 2);
+                load(i0 + 2);
+                if (i0 + 3 < i1)
+                    load_pages(i0 + 3);
+            }
         }
     }
     __syncthreads();
 
+    // Tiles of 32 tokens.  While a tile's weights are formed on the vector units, the matrix cores have the next
+    // tile's scores and the last one's output: a wave issues in order, so their instructions alternate.  Their first
+    // operands come from LDS one turn ahead, the scales half a tile.
+    f32x16_t x[2];                                        // scores, tokens 32 j + 8 (e / 4) + 4 h + e % 4 of row `col`
+    uint32_t pk[2][8] = {};                               // weights times scales
+    uint4 kf[2], vf[2];
+    float4 sk[2], sv[2];
     const uint32_t kplace = (uint32_t)(col * D * 2 + ((h ^ (col & 7)) << 4));
     const uint32_t vplace = (uint32_t)(offsetof(Stage<D>, v) + col * kTokens * 2 + ((h ^ (col & 7) ^ (col >> 3)) << 4));
+    const uint32_t splace = (uint32_t)offsetof(Stage<D>, sk) + 16u * h;
+    uint32_t before = 0, now = 0, next = (uint32_t)sizeof(Stage<D>);        // where the stages are (of the first step: no output yet, weights 0)
+    // (places in LDS are formed anew from one number each: kept apart they would take the registers)
+    uint32_t kat = 0, vat = 0, sat = 0;
+    // turn n = 0 .. KS - 1 of tile j: step n of the scores of tile j + 1, and of the output of tile j - 1 (piece 2 (j - 1) + u + h of
+    // dim 32 d + col)
+    auto fetch = [&](int j, int n) {
+        const int jk = (j + 1) % TJ, jv = (j + TJ - 1) % TJ, u = n / DT, d = n % DT;
+        kf[n & 1] = *reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(n << 5)) + jk * 64 * D);
+        vf[n & 1] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)(jv << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
+    };
+    auto scales = [&](int j, int g) {                     // of tokens 32 j + 8 g + 4 h ..
+        sk[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 128 * j + 32 * g);
+        sv[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 128 * j + 32 * g + 4 * kTokens);
+    };
+    auto begin = [&](int j) {                             // of tile j of this step
+        kat = (j + 1 < TJ ? now : next) + kplace;
+        vat = (j > 0 ? now : before) + vplace;
+        sat = now + splace;
+        pin(kat);
+        pin(vat);
+        pin(sat);
+        fetch(j, 0);
+        scales(j, 0);
+    };
+    auto output = [&](int j, int n) {
+        const int u = n / DT, d = n % DT;
+        const uint4 v = 32 * d >= 64 ? make_uint4(vf[n & 1].z, vf[n & 1].w, vf[n & 1].x, vf[n & 1].y) : vf[n & 1];
+        const uint32_t(&w)[8] = pk[(j + 1) & 1];
+        o[d] = mfma32(v, make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]), o[d]);
+    };
+    auto zero = [](f32x16_t& y) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+            y[e] = 0.0f;
+    };
+    auto section = [&](auto tile_of_step, int t, bool full) {
+        constexpr int j = decltype(tile_of_step)::value;
+        f32x16_t &xj = x[j & 1], &y = x[(j + 1) & 1];
+        uint32_t(&pj)[8] = pk[j & 1];
+        const St& s = *reinterpret_cast<const St*>(smem + now);
+        float sum = 0.0f;
+        uint32_t top = 0;                                 // of the rounded weights, two by two
+        // weights of two tokens, scores times their scales (or, where they have been seen to, as they are)
+        auto weigh2 = [&](int e, const float4& ks, const float4& vs, auto raw) {
+            const float ka = e & 2 ? ks.z : ks.x, kb = e & 2 ? ks.w : ks.y, va = e & 2 ? vs.z : vs.x, vb = e & 2 ? vs.w : vs.y;
+            float ea, eb, wa, wb;
+            if constexpr (decltype(raw)::value) {
+                ea = exp2_(__builtin_fmaf(xj[e], ka, -m));
+                eb = exp2_(__builtin_fmaf(xj[e + 1], kb, -m));
+                wa = ea * va;
+                wb = eb * vb;
+            } else {
+                ea = exp2_(xj[e] - m);
+                eb = exp2_(xj[e + 1] - m);
+                wa = xj[e] == -INFINITY ? 0.0f : ea * va;                    // (the scale may be NaN)
+                wb = xj[e + 1] == -INFINITY ? 0.0f : eb * vb;
+            }
+            sum += ea + eb;
+            pj[e >> 1] = pack2(wa, wb);
+            top = max2(top, pj[e >> 1]);
+        };
+        auto weigh = [&] {                                // all of them, as they are
+            sum = 0.0f;
+            top = 0;
+#pragma unroll
+            for (int e = 0; e < 16; e += 2)
+                weigh2(e, float4{}, *reinterpret_cast<const float4*>(s.sv + 32 * j + 8 * (e >> 2) + 4 * h), std::false_type{});
+        };
+        zero(y);
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            constexpr int per = 16 / KS;                  // weights of a turn
+            if (k + 1 < KS)
+                fetch(j, k + 1);
+            y = mfma32(kf[k & 1], qv[k], y);
+            output(j, k);
+            if (per * k % 4 == 0 && per * k / 4 + 1 < 4)
+                scales(j, per * k / 4 + 1);
+#pragma unroll
+            for (int e = per * k; e < per * (k + 1); e += 2)
+                weigh2(e, sk[(e >> 2) & 1], sv[(e >> 2) & 1], std::true_type{});
+            // (they stay here, and are not put off to where it is known that every token is seen)
+            pin(top);
+            __asm__ volatile("" : "+v"(sum));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        if (!full) {
+            // what a row does not see weighs nothing, whatever lies there
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3), n = t + at;
+                const float k1 = s.sk[at];
+                xj[e] = n <= pos && n >= low && k1 != INFINITY ? xj[e] * k1 : -INFINITY;
+            }
+            weigh();
+        }
+        // (a weight that passes binary16 is infinite there)
+        if (__ballot(h2f(top & 0xFFFFu) > kTop || h2f(top >> 16) > kTop || sum > 16.0f * kTop * kLeast)) {
+            float best = kNone;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
+                if (full)
+                    xj[e] *= s.sk[at];
+                best = fmaxf(best, xj[e] + log2_(fmaxf(s.sv[at], 1.0f / kLeast)));
+            }
+            best = fmaxf(best, __shfl_xor(best, 32, 64));
+            const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
+            m = mn;
+            l *= f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d)
+                o[d] *= f;
+            weigh();
+        }
+        l += sum;
+    };
+
+    if (i0 < i1) {                                        // the first tile's scores
+        kat = now + kplace;
+        pin(kat);
+        zero(x[0]);
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+            x[0] = mfma32(*reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(k << 5))), qv[k], x[0]);
+    }
+    auto last_output = [&] {
+        vat = before + vplace;
+        pin(vat);
+#pragma unroll
+        for (int n = 0; n < KS; ++n) {
+            const int u = n / DT, d = n % DT;
+            vf[n & 1] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)((TJ - 1) << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
+            output(0, n);
+        }
+    };
     for (int i = i0; i < i1; ++i) {
-        const uint32_t stage_at = (uint32_t)(((i - i0) & 1) * sizeof(Stage<D>));
-        const Stage<D>& s = stage[(i - i0) & 1];
         const int t = i * kTokens;
+        const St& s = *reinterpret_cast<const St*>(smem + now);
         const uint4 aw = *reinterpret_cast<const uint4*>(s.away), aw2 = *reinterpret_cast<const uint4*>(s.away + 4);
         const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w | aw2.x | aw2.y | aw2.z | aw2.w) == 0 &&
                                                          t + kTokens - 1 <= wfirst && (!a.window || t > wlast - a.window));
-        // the next step goes to the other stage, and the one after it is asked for
-        if (i + 1 < i1) {
-            put(stage[(i + 1 - i0) & 1]);
-            if (i + 2 < i1) {
-                load(i + 2);
-                if (i + 3 < i1)
-                    load_pages(i + 3);
-            }
-        }
-        if (t <= wlast) {
-            // Tiles of 32 tokens.  While a tile's weights are formed on the vector units, the matrix cores have the next
-            // tile's scores and the last one's output: a wave issues in order, so their instructions alternate.  Their first
-            // operands come from LDS two turns ahead, the scales half a tile.
-            f32x16_t x[2];                                // scores, tokens 32 j + 8 (e / 4) + 4 h + e % 4 of row `col`
-            uint32_t pk[2][8];                            // weights times scales
-            uint4 kf[3], vf[3];
-            float4 sk[2], sv[2];
-            // (places in LDS are formed anew from one number each: kept apart they would take the registers)
-            uint32_t kat = stage_at + kplace, vat = stage_at + vplace, sat = stage_at + (uint32_t)offsetof(Stage<D>, sk) + 16u * h;
-            // turn n: step k of tile n / KS's scores, and of the output of the tile two before it
-            auto fetch = [&](int n) {
-                const int j = n / KS, k = n % KS, u = k / DT, d = k % DT;
-                if (j < TJ)
-                    kf[n % 3] = *reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(k << 5)) + j * 64 * D);
-                if (j >= 2 && j - 2 < TJ)                 // piece 2 (2 (j - 2) + u) + h of dim 32 d + col
-                    vf[n % 3] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)((j - 2) << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
-            };
-            auto scales = [&](int g) {                    // of tokens 8 g + 4 h ..
-                if (g < 4 * TJ) {
-                    sk[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 32 * g);
-                    sv[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 32 * g + 4 * kTokens);
-                }
-            };
-            auto turn = [&](int n) {
-                const int j = n / KS, k = n % KS, u = k / DT, d = k % DT;
-                fetch(n + 2);
-                if (j < TJ) {
-                    f32x16_t& y = x[j & 1];
-                    if (k == 0) {
-#pragma unroll
-                        for (int e = 0; e < 16; ++e)
-                            y[e] = 0.0f;
-                    }
-                    y = mfma32(kf[n % 3], qv[k], y);
-                }
-                if (j >= 2) {
-                    const uint4 v = 32 * d >= 64 ? make_uint4(vf[n % 3].z, vf[n % 3].w, vf[n % 3].x, vf[n % 3].y) : vf[n % 3];
-                    const uint32_t(&w)[8] = pk[j & 1];
-                    o[d] = mfma32(v, make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]), o[d]);
-                }
-            };
-            fetch(0);
-            fetch(1);
-            scales(0);
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-                turn(k);
-#pragma unroll
-            for (int j = 0; j < TJ; ++j) {
-                f32x16_t& xj = x[j & 1];
-                uint32_t(&pj)[8] = pk[j & 1];
-                float sum = 0.0f;
-                uint32_t top = 0;                         // of the rounded weights, two by two
-                // weights of two tokens, scores times their scales (or, where they have been seen to, as they are)
-                auto weigh2 = [&](int e, const float4& ks, const float4& vs, auto raw) {
-                    const float ka = e & 2 ? ks.z : ks.x, kb = e & 2 ? ks.w : ks.y, va = e & 2 ? vs.z : vs.x, vb = e & 2 ? vs.w : vs.y;
-                    float ea, eb, wa, wb;
-                    if constexpr (decltype(raw)::value) {
-                        ea = exp2_(__builtin_fmaf(xj[e], ka, -m));
-                        eb = exp2_(__builtin_fmaf(xj[e + 1], kb, -m));
-                        wa = ea * va;
-                        wb = eb * vb;
-                    } else {
-                        ea = exp2_(xj[e] - m);
-                        eb = exp2_(xj[e + 1] - m);
-                        wa = xj[e] == -INFINITY ? 0.0f : ea * va;            // (the scale may be NaN)
-                        wb = xj[e + 1] == -INFINITY ? 0.0f : eb * vb;
-                    }
-                    sum += ea + eb;
-                    pj[e >> 1] = pack2(wa, wb);
-                    top = max2(top, pj[e >> 1]);
-                };
-                auto weigh = [&] {                        // all of them, as they are
-                    sum = 0.0f;
-                    top = 0;
-#pragma unroll
-                    for (int e = 0; e < 16; e += 2)
-                        weigh2(e, float4{}, *reinterpret_cast<const float4*>(s.sv + 32 * j + 8 * (e >> 2) + 4 * h), std::false_type{});
-                };
-                pin(kat);
-                pin(vat);
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    turn((j + 1) * KS + k);
-                    constexpr int per = 16 / KS;          // weights of a turn
-                    if (per * k % 4 == 0)
-                        scales(4 * j + per * k / 4 + 1);
-#pragma unroll
-                    for (int e = per * k; e < per * (k + 1); e += 2)
-                        weigh2(e, sk[(e >> 2) & 1], sv[(e >> 2) & 1], std::true_type{});
-                    // (they stay here, and are not put off to where it is known that every token is seen)
-                    pin(top);
-                    __asm__ volatile("" : "+v"(sum));
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-                if (!full) {
-                    // what a row does not see weighs nothing, whatever lies there
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3), n = t + at;
-                        const float k1 = s.sk[at];
-                        xj[e] = n <= pos && n >= low && k1 != INFINITY ? xj[e] * k1 : -INFINITY;
-                    }
-                    weigh();
-                }
-                // (a weight that passes binary16 is infinite there)
-                if (__ballot(h2f(top & 0xFFFFu) > kTop || h2f(top >> 16) > kTop || sum > 16.0f * kTop * kLeast)) {
-                    float best = kNone;
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
-                        if (full)
-                            xj[e] *= s.sk[at];
-                        best = fmaxf(best, xj[e] + log2_(fmaxf(s.sv[at], 1.0f / kLeast)));
-                    }
-                    best = fmaxf(best, __shfl_xor(best, 32, 64));
-                    const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
-                    m = mn;
-                    l *= f;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d)
-                        o[d] *= f;
-                    weigh();
-                }
-                l += sum;
-            }
-#pragma unroll
-            for (int k = 0; k < KS; ++k)
-                turn((TJ + 1) * KS + k);
-        }
+        begin(0);
+        section(std::integral_constant<int, 0>{}, t, full);
         __syncthreads();
+        begin(1);
+        if (i + 2 < i1) {
+            put(*reinterpret_cast<St*>(smem + (i == i0 ? 2 * (uint32_t)sizeof(St) : before)));
+            if (i + 3 < i1) {
+                load(i + 3);
+                if (i + 4 < i1)
+                    load_pages(i + 4);
+            }
+        }
+        section(std::integral_constant<int, 1>{}, t, full);
+        if constexpr (TJ > 2) {
+            begin(2);
+            section(std::integral_constant<int, 2>{}, t, full);
+            begin(3);
+            section(std::integral_constant<int, 3>{}, t, full);
+        }
+        const uint32_t free = i == i0 ? 2 * (uint32_t)sizeof(St) : before;
+        before = now;
+        now = next;
+        next = free;
     }
+    if (i0 < i1)
+        last_output();
     l += __shfl_xor(l, 32, 64);
     if (bad && l != 0.0f)
         l = NAN;
@@ -472,7 +508,7 @@ int rows_target() { return plan_cus(); }
 
 template <int D>
 hipError_t launch(const AttnArgs& a, int limit, hipStream_t st) {
-    const size_t lds = 2 * sizeof(Stage<D>) + (size_t)a.B * sizeof(Known<int32_t>);
+    const size_t lds = 3 * sizeof(Stage<D>) + (size_t)a.B * sizeof(Known<int32_t>);
     const hipError_t e = set_lds(rows_kernel<D>, lds + 1024);
     if (e != hipSuccess)
         return e;

@@ -9,7 +9,7 @@
 
 namespace qmlp {
 
-constexpr int kKvRequests = 4096;            // most requests of a call: their sums are kept in LDS
+constexpr int kKvRequests = 2048;            // most requests of a call: their sums are kept in LDS
 
 // A cache as the kernels see it.  `side` bytes hold one page of one head's K or V.
 struct KvView {

@@ -12,7 +12,7 @@
 namespace qmlp {
 namespace {
 
-constexpr int kPer = 4;                                   // requests of a thread at most (1024 threads, 4096 requests)
+constexpr int kPer = kKvRequests / 1024;                  // requests of a thread at most
 
 // Exclusive sums over the workgroup's threads of v; the total goes to *all.
 template <int NT>

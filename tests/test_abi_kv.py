@@ -51,7 +51,7 @@ def test_plan_refusals(lib):
     assert _plan(lib, B=-1) == SHAPE and _plan(lib, W=0) == SHAPE and _plan(lib, N=-1) == SHAPE and _plan(lib, tokens=-1) == SHAPE
     for page in (0, 8, 24, 512, -16):
         assert _plan(lib, page=page) == UNSUP
-    assert _plan(lib, B=4097) == UNSUP and _plan(lib, W=(1 << 20) + 1) == UNSUP and _plan(lib, W=1 << 20, page=256) == 0
+    assert _plan(lib, B=2049) == UNSUP and _plan(lib, W=(1 << 20) + 1) == UNSUP and _plan(lib, W=1 << 20, page=256) == 0
     assert _plan(lib, tokens=(1 << 24) + 1) == UNSUP
     for n in ("lens", "new", "table", "free", "n_free", "slots", "positions", "starts", "lens_out", "n_free_out", "short"):
         assert _plan(lib, B=2, **{n: 0}) == NULL, n
@@ -114,7 +114,7 @@ def test_kv_attention_refusals(q, lib):
     assert call() == 0 and call(B=0, T=5) == 0 and call(c=None) == NULL
     assert call(T=-1) == SHAPE and call(T=(1 << 20) + 1) == UNSUP and call(dt=2) == UNSUP
     assert call(heads=0) == SHAPE and call(heads=5) == SHAPE and call(heads=4098) == UNSUP
-    assert call(B=-1) == SHAPE and call(B=4097) == UNSUP and call(W=0) == SHAPE and call(W=1 << 25) == UNSUP
+    assert call(B=-1) == SHAPE and call(B=2049) == UNSUP and call(W=0) == SHAPE and call(W=1 << 25) == UNSUP
     assert call(new=-1) == SHAPE and call(new=(1 << 20) + 1) == UNSUP and call(window=-1) == SHAPE
     assert call(scale=math.nan) == UNSUP and call(scale=math.inf) == UNSUP
     assert call(starts=0, T=3, B=2) == SHAPE

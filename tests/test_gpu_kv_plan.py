@@ -48,7 +48,7 @@ def state(rng, B, W, page, spare, ended, most_new):
 @pytest.mark.parametrize("seed", range(4))
 @pytest.mark.parametrize("B,W,page,spare,ended,most", [
     (1, 1, 16, 0, 0.0, 3), (3, 5, 16, 2, 0.3, 40), (8, 9, 64, 20, 0.0, 1), (37, 12, 32, 9, 0.2, 60), (256, 7, 16, 60, 0.1, 30),
-    (257, 5, 128, 300, 0.05, 200), (1025, 3, 16, 400, 0.3, 20), (4096, 2, 16, 1500, 0.2, 6), (70, 64, 256, 1000, 0.5, 3000)])
+    (257, 5, 128, 300, 0.05, 200), (1025, 3, 16, 400, 0.3, 20), (2048, 3, 16, 1500, 0.2, 6), (70, 64, 256, 1000, 0.5, 3000)])
 def test_against_a_loop(q, B, W, page, spare, ended, most, seed):
     rng = random.Random(1000 * B + seed)
     lens, new, table, free, n = state(rng, B, W, page, spare, ended, most)
