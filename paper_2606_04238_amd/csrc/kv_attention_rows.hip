@@ -8,8 +8,8 @@
 // product to the other in registers.  Two stages of LDS: while one is multiplied the next is loaded and unpacked.
 //
 // LDS: K [64 tokens][D], 16-byte pieces (8 dims) at place p ^ (token & 7); V [D dims][64 tokens], a piece being the eight
-// tokens a lane multiplies at once (16 s + 4 h + {0..3, 8..11}), at place p ^ (dim & 7) ^ (dim / 8 & 7), its
-// halves swapped from dim 64 on.  Eight neighbouring lanes so read and write different banks.
+// tokens a lane multiplies at once (16 s + 4 h + {0..3, 8..11}), at place p ^ (dim & 7) ^ (dim / 8 & 7).  Neighbouring lanes so
+// read and write different banks.
 #include "qmlp_internal.h"
 
 #include "decode_launch.h"
@@ -128,7 +128,9 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     const bool takes_k = wave < 4;
     const int sid = tid & 255;
     const int ktok = D == 128 ? sid >> 2 : sid >> 1, kc = D == 128 ? sid & 3 : sid & 1;
-    const int vquad = D == 128 ? sid >> 4 : sid >> 3, vword = D == 128 ? sid & 15 : sid & 7;
+    // (16 neighbouring threads of V: eight words of the two quads that share pieces)
+    const int vword = (sid & 7) | (D == 128 ? (sid >> 1) & 8 : 0);
+    const int vquad = D == 128 ? ((sid >> 2) & 2) | ((sid >> 5) & 1) | ((sid >> 4) & 12) : ((sid >> 2) & 2) | ((sid >> 4) & 1) | ((sid >> 3) & 28);
     const int mine0 = takes_k ? ktok : 4 * vquad;         // the first token of it
     int page = 0;                                         // page number of the step to be loaded next
     auto load_pages = [&](int i) { page = a.table[(long)b * a.W + min((i * kTokens + mine0) >> lg, a.W - 1)]; };
@@ -184,7 +186,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
                     out[2 * i + 1][pr] = add2(f[i], off[pr]);
                 }
             }
-            const int piece = 2 * (vquad >> 2) + (vquad & 1), half = ((vquad >> 1) & 1) ^ (vword >> 3);
+            const int piece = 2 * (vquad >> 2) + (vquad & 1), half = (vquad >> 1) & 1;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 *reinterpret_cast<uint2*>(s.v + (8 * vword + j) * kTokens + ((piece ^ j ^ (vword & 7)) << 3) + 4 * half) =
@@ -245,10 +247,10 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
 
     // Tiles of 32 tokens.  While a tile's weights are formed on the vector units, the matrix cores have the next
     // tile's scores and the last one's output: a wave issues in order, so their instructions alternate.  Their first
-    // operands come from LDS one turn ahead, the scales half a tile.
+    // operands come from LDS two turns ahead, the scales half a tile.
     f32x16_t x[2];                                        // scores, tokens 32 j + 8 (e / 4) + 4 h + e % 4 of row `col`
     uint32_t pk[2][8] = {};                               // weights times scales
-    uint4 kf[2], vf[2];
+    uint4 kf[3], vf[3];
     float4 sk[2], sv[2];
     const uint32_t kplace = (uint32_t)(col * D * 2 + ((h ^ (col & 7)) << 4));
     const uint32_t vplace = (uint32_t)(offsetof(Stage<D>, v) + col * kTokens * 2 + ((h ^ (col & 7) ^ (col >> 3)) << 4));
@@ -260,28 +262,28 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     // dim 32 d + col)
     auto fetch = [&](int j, int n) {
         const int jk = (j + 1) % TJ, jv = (j + TJ - 1) % TJ, u = n / DT, d = n % DT;
-        kf[n & 1] = *reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(n << 5)) + jk * 64 * D);
-        vf[n & 1] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)(jv << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
+        kf[n % 3] = *reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(n << 5)) + jk * 64 * D);
+        vf[n % 3] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)(jv << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
     };
     auto scales = [&](int j, int g) {                     // of tokens 32 j + 8 g + 4 h ..
         sk[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 128 * j + 32 * g);
         sv[g & 1] = *reinterpret_cast<const float4*>(smem + sat + 128 * j + 32 * g + 4 * kTokens);
     };
-    auto begin = [&](int j) {                             // of tile j of this step
-        kat = (j + 1 < TJ ? now : next) + kplace;
-        vat = (j > 0 ? now : before) + vplace;
-        sat = now + splace;
+    auto begin = [&](int j, bool of_next) {               // of tile j of this step, or of the next one's first
+        kat = (j + 1 < TJ && !of_next ? now : next) + kplace;
+        vat = (j > 0 || of_next ? now : before) + vplace;
+        sat = (of_next ? next : now) + splace;
         pin(kat);
         pin(vat);
         pin(sat);
         fetch(j, 0);
+        fetch(j, 1);
         scales(j, 0);
     };
     auto output = [&](int j, int n) {
         const int u = n / DT, d = n % DT;
-        const uint4 v = 32 * d >= 64 ? make_uint4(vf[n & 1].z, vf[n & 1].w, vf[n & 1].x, vf[n & 1].y) : vf[n & 1];
         const uint32_t(&w)[8] = pk[(j + 1) & 1];
-        o[d] = mfma32(v, make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]), o[d]);
+        o[d] = mfma32(vf[n % 3], make_uint4(w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]), o[d]);
     };
     auto zero = [](f32x16_t& y) {
 #pragma unroll
@@ -325,9 +327,9 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
             constexpr int per = 16 / KS;                  // weights of a turn
-            if (k + 1 < KS)
-                fetch(j, k + 1);
-            y = mfma32(kf[k & 1], qv[k], y);
+            if (k + 2 < KS)
+                fetch(j, k + 2);
+            y = mfma32(kf[k % 3], qv[k], y);
             output(j, k);
             if (per * k % 4 == 0 && per * k / 4 + 1 < 4)
                 scales(j, per * k / 4 + 1);
@@ -339,6 +341,8 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
             __asm__ volatile("" : "+v"(sum));
             __builtin_amdgcn_sched_barrier(0);
         }
+        if (j > 0)
+            begin((j + 1) % TJ, j + 1 == TJ);
         if (!full) {
             // what a row does not see weighs nothing, whatever lies there
 #pragma unroll
@@ -378,6 +382,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
 #pragma unroll
         for (int k = 0; k < KS; ++k)
             x[0] = mfma32(*reinterpret_cast<const uint4*>(smem + (kat ^ (uint32_t)(k << 5))), qv[k], x[0]);
+        begin(0, false);
     }
     auto last_output = [&] {
         vat = before + vplace;
@@ -385,7 +390,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
 #pragma unroll
         for (int n = 0; n < KS; ++n) {
             const int u = n / DT, d = n % DT;
-            vf[n & 1] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)((TJ - 1) << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
+            vf[n % 3] = *reinterpret_cast<const uint4*>(smem + (vat ^ (uint32_t)((TJ - 1) << 6 ^ u << 5 ^ (d & 1) << 6)) + d * 64 * kTokens);
             output(0, n);
         }
     };
@@ -395,10 +400,9 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
         const uint4 aw = *reinterpret_cast<const uint4*>(s.away), aw2 = *reinterpret_cast<const uint4*>(s.away + 4);
         const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w | aw2.x | aw2.y | aw2.z | aw2.w) == 0 &&
                                                          t + kTokens - 1 <= wfirst && (!a.window || t > wlast - a.window));
-        begin(0);
         section(std::integral_constant<int, 0>{}, t, full);
         __syncthreads();
-        begin(1);
+        begin(1, false);
         if (i + 2 < i1) {
             put(*reinterpret_cast<St*>(smem + (i == i0 ? 2 * (uint32_t)sizeof(St) : before)));
             if (i + 3 < i1) {
@@ -409,9 +413,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
         }
         section(std::integral_constant<int, 1>{}, t, full);
         if constexpr (TJ > 2) {
-            begin(2);
             section(std::integral_constant<int, 2>{}, t, full);
-            begin(3);
             section(std::integral_constant<int, 3>{}, t, full);
         }
         const uint32_t free = i == i0 ? 2 * (uint32_t)sizeof(St) : before;

@@ -66,8 +66,10 @@ __device__ __forceinline__ uint32_t highs(uint32_t a, uint32_t b) { return __bui
 __device__ __forceinline__ uint32_t add2(uint32_t a, uint32_t b) {
     return __builtin_bit_cast(uint32_t, (half2_t)(__builtin_bit_cast(half2_t, a) + __builtin_bit_cast(half2_t, b)));
 }
+// The larger halves: of binary16 numbers that are not negative, the larger numbers.
 __device__ __forceinline__ uint32_t max2(uint32_t a, uint32_t b) {
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(half2_t, a), __builtin_bit_cast(half2_t, b)));
+    typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, a), __builtin_bit_cast(u16x2_t, b)));
 }
 __device__ __forceinline__ uint32_t comp(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
