@@ -584,10 +584,17 @@ size_t qmlp_kv_cache_bytes(int pages, int kv_heads, int head_dim, int page);
  * 0 <= B <= 2048, 1 <= W <= 2^20, W * page <= 2^30, 0 <= N, 0 <= tokens <= 2^24.  One launch
  * (none with B = 0: nothing is written).
  */
-qmlp_status qmlp_kv_plan(const int32_t *lens, const int32_t *new_tokens, int B, int page, int32_t *table, int W,
-                         int32_t *free_pages, int N, const int32_t *n_free, int tokens, int32_t *slots,
-                         int32_t *positions, int32_t *starts, int32_t *lens_out, int32_t *n_free_out,
-                         int32_t *short_out, qmlp_stream stream);
+typedef struct {
+    const int32_t *lens, *new_tokens;   /* [B] */
+    int32_t *table, *free_pages;        /* [B][W], [N] */
+    const int32_t *n_free;              /* [1] */
+    int32_t *slots, *positions;         /* [tokens] */
+    int32_t *starts;                    /* [B+1] */
+    int32_t *lens_out, *n_free_out, *short_out;     /* [B], [1], [1] */
+    int32_t B, page, W, N, tokens;
+} qmlp_plan;
+
+qmlp_status qmlp_kv_plan(const qmlp_plan *p, qmlp_stream stream);
 
 /* Which dims of a head turn together: (i, i + rot/2), or (2i, 2i + 1). */
 typedef enum { QMLP_PAIRS_HALF = 0, QMLP_PAIRS_NEXT = 1 } qmlp_pairs;
@@ -656,13 +663,21 @@ qmlp_status qmlp_kv_read(const qmlp_kv_cache *cache, const int32_t *slots, int T
  * a call that failed); each call leaves it ready for the next, of any shape it is large enough for.  One call at
  * a time per workspace.
  */
+typedef struct {
+    const void *q;                      /* [T][heads][head_dim], 16-byte aligned */
+    void *y;                            /* the same */
+    int64_t ldq, ldy;                   /* elements from row to row, multiples of 8 */
+    const int32_t *table, *lens, *starts;       /* [B][W], [B], [B+1] or NULL */
+    const float *sinks;                 /* [heads] or NULL */
+    void *ws;
+    size_t ws_bytes;
+    int32_t T, heads, B, W, max_new, window;
+    float scale;
+} qmlp_attention;
+
 size_t qmlp_kv_attention_workspace_bytes(const qmlp_kv_cache *cache, int heads, int max_new);
 
-qmlp_status qmlp_kv_attention(const qmlp_kv_cache *cache, const void *q, int64_t ldq, int T, int heads,
-                              qmlp_dtype dtype, const int32_t *table, int W, const int32_t *lens,
-                              const int32_t *starts, int B, int max_new, float scale, int window,
-                              const float *sinks, void *y, int64_t ldy, void *ws, size_t ws_bytes,
-                              qmlp_stream stream);
+qmlp_status qmlp_kv_attention(const qmlp_kv_cache *cache, const qmlp_attention *a, qmlp_dtype dtype, qmlp_stream stream);
 
 /* ---------------------------------------------- inspection (not timed) */
 

@@ -23,6 +23,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -78,6 +79,23 @@ class HeadsC(ctypes.Structure):
                [(n, ctypes.c_float) for n in ("eps", "mul")]
 
 
+class PlanC(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("lens", "new_tokens", "table", "free_pages", "n_free", "slots", "positions",
+                                               "starts", "lens_out", "n_free_out", "short_out")] + \
+               [(n, ctypes.c_int32) for n in ("B", "page", "W", "N", "tokens")]
+
+
+class AttentionC(ctypes.Structure):
+    _fields_ = [("q", ctypes.c_void_p), ("y", ctypes.c_void_p), ("ldq", ctypes.c_int64), ("ldy", ctypes.c_int64)] + \
+               [(n, ctypes.c_void_p) for n in ("table", "lens", "starts", "sinks", "ws")] + [("ws_bytes", ctypes.c_size_t)] + \
+               [(n, ctypes.c_int32) for n in ("T", "heads", "B", "W", "max_new", "window")] + [("scale", ctypes.c_float)]
+
+
+# The same structures as packed bytes: to fill one of ctypes' own costs about 1.5 us a call, to pass its members one by one
+# 4 us, this 0.3 us (their members are ordered so that nothing is padded between them).
+_HEADS, _PLAN, _ATTENTION = struct.Struct("@3P3q2P2q5P5i2f"), struct.Struct("@11P5i"), struct.Struct("@2P2q5PN6if")
+
+
 _LIB = None
 
 
@@ -93,7 +111,7 @@ def _lib():
         pm = ctypes.POINTER(MlpC)
         po = ctypes.POINTER(MoeC)
         pa, L = ctypes.POINTER(AdaptersC), ctypes.c_int64
-        pc, F = ctypes.POINTER(KVCacheC), ctypes.c_float
+        pc = ctypes.POINTER(KVCacheC)
         sig = {
             "qmlp_codes_bytes": (Z, [I, I, I]),
             "qmlp_meta_bytes": (Z, [I, I, I]),
@@ -132,11 +150,11 @@ def _lib():
             "qmlp_moe_layer": (I, [po, P, I, I, P, P, Z, P]),
             "qmlp_linear_lora": (I, [pq, pa, P, P, L, I, I, P, L, P, Z, P]),
             "qmlp_kv_cache_bytes": (Z, [I, I, I, I]),
-            "qmlp_kv_plan": (I, [P, P, I, I, P, I, P, I, P, I, P, P, P, P, P, P, P]),
-            "qmlp_qk_norm_rope": (I, [ctypes.POINTER(HeadsC), I, I, pc, P]),
-            "qmlp_kv_read": (I, [pc, P, I, I, P, P, P]),
+            "qmlp_kv_plan": (I, [ctypes.c_char_p, P]),
+            "qmlp_qk_norm_rope": (I, [ctypes.c_char_p, I, I, P, P]),
+            "qmlp_kv_read": (I, [P, P, I, I, P, P, P]),
             "qmlp_kv_attention_workspace_bytes": (Z, [pc, I, I]),
-            "qmlp_kv_attention": (I, [pc, P, L, I, I, I, P, I, P, P, I, I, F, I, P, P, L, P, Z, P]),
+            "qmlp_kv_attention": (I, [P, ctypes.c_char_p, I, P]),
         }
         for name, (res, args) in sig.items():
             fn = getattr(lib, name)
@@ -703,6 +721,7 @@ class KVCache:
         if not _lib().qmlp_kv_cache_bytes(self.pages, self.kv_heads, self.head_dim, self.page):
             raise QmlpError(4, "KVCache")
         self._c = KVCacheC(data.data_ptr(), self.pages, self.kv_heads, self.head_dim, self.page)
+        self._at = ctypes.addressof(self._c)
 
     def c(self) -> KVCacheC:
         return self._c
@@ -713,10 +732,31 @@ def kv_cache(pages: int, kv_heads: int, head_dim: int, page: int = 64, device="c
     return KVCache(torch.zeros((pages, kv_heads, 2, page * (head_dim // 2 + 4)), dtype=torch.uint8, device=device), page)
 
 
+def _here(*tensors):
+    """_one_device for the calls of a decoding step, with one question a tensor (the first is not None)."""
+    here = tensors[0].get_device()
+    for t in tensors:
+        if t is not None and t.get_device() != here:
+            here = -1
+    if here < 0 or here != torch.cuda.current_device():
+        raise ValueError("every tensor must be on the current CUDA device")
+    return here
+
+
+def _at(t):
+    return 0 if t is None else t.data_ptr()
+
+
 def _ints(n, what, *tensors):
     for t in tensors:
-        if t is not None and (t.dtype != torch.int32 or t.shape != (n,) or not t.is_contiguous()):
+        if t is not None and (t.dtype is not torch.int32 or t.shape != (n,) or not t.is_contiguous()):
             raise ValueError("%s must be int32 [%d], contiguous" % (what, n))
+
+
+def _is_table(table, B):
+    if table.dim() != 2 or table.shape[0] != B or table.dtype is not torch.int32 or not table.is_contiguous():
+        raise ValueError("table must be int32 [B][W], contiguous")
+    return table.shape[1]
 
 
 class KVPlan:
@@ -730,6 +770,11 @@ class KVPlan:
         self.lens, self.n_free = new(B) if lens is None else lens, new(1) if n_free is None else n_free
         _ints(B, "lens", self.lens)
         _ints(1, "n_free", self.n_free)
+        t = (self.slots, self.positions, self.starts, self.lens, self.n_free, self.short)
+        if len({v.device for v in t}) != 1:
+            raise ValueError("lens and n_free must be on the plan's device")
+        self.B, self.tokens = B, tokens
+        self._out = tuple(v.data_ptr() for v in t)
 
 
 def kv_plan(plan: KVPlan, lens: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free: torch.Tensor,
@@ -737,17 +782,15 @@ def kv_plan(plan: KVPlan, lens: torch.Tensor, new: torch.Tensor, table: torch.Te
     """The pages of a step (qmlp_kv_plan): requests with ``lens`` cached tokens add ``new`` (-1: ended, pages back on the
     stack ``free`` of ``n_free``); ``table`` [B][W] grows in place and ``plan`` takes starts, slots, positions and the new
     lens and n_free (which may be the same tensors as the old ones).  All int32."""
-    B = lens.shape[0]
-    _ints(B, "lens and new", lens, new, plan.lens)
-    _ints(B + 1, "plan.starts", plan.starts)
+    B = plan.B
+    _ints(B, "lens and new", lens, new)
     _ints(1, "n_free", n_free)
-    _ints(free.shape[0], "free", free)
-    if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or not table.is_contiguous():
-        raise ValueError("table must be int32 [B][W], contiguous")
-    here = _one_device(lens, new, table, free, n_free, plan.slots, plan.positions, plan.starts, plan.lens, plan.n_free, plan.short)
-    _check(_lib().qmlp_kv_plan(_addr(lens), _addr(new), B, page, _addr(table), table.shape[1], _addr(free), free.shape[0],
-                               _addr(n_free), plan.slots.shape[0], _addr(plan.slots), _addr(plan.positions),
-                               _addr(plan.starts), _addr(plan.lens), _addr(plan.n_free), _addr(plan.short),
+    N = free.numel()
+    _ints(N, "free", free)
+    W = _is_table(table, B)
+    here = _here(plan.slots, lens, new, table, free, n_free)
+    _check(_lib().qmlp_kv_plan(_PLAN.pack(lens.data_ptr(), new.data_ptr(), table.data_ptr(), free.data_ptr(), n_free.data_ptr(),
+                                          *plan._out, B, page, W, N, plan.tokens),
                                torch._C._cuda_getCurrentRawStream(here)), "kv_plan")
     return plan
 
@@ -756,13 +799,15 @@ PAIRS = {"half": 0, "next": 1}
 
 
 def _head_rows(t, what, T, D, dtype):
-    """The row stride of [T][heads][D] with the heads of a row side by side."""
-    if t.dim() != 3 or t.shape[0] != T or t.shape[2] != D or t.dtype != dtype:
+    """(heads, row stride) of [T][heads][D] with the heads of a row side by side."""
+    if t.dim() != 3 or t.dtype is not dtype:
         raise ValueError("%s must be [T][heads][head_dim] of q's type" % what)
-    H = t.shape[1]
-    if t.stride(2) != 1 or (H > 1 and t.stride(1) != D):
+    (t0, H, d), (ld, hs, ds) = t.shape, t.stride()
+    if t0 != T or d != D:
+        raise ValueError("%s must be [T][heads][head_dim] of q's type" % what)
+    if ds != 1 or (H > 1 and hs != D):
         raise ValueError("the heads of a row of %s must lie side by side" % what)
-    return t.stride(0) if T > 1 else H * D
+    return H, ld if T > 1 else H * D
 
 
 def qk_norm_rope(q: torch.Tensor | None, k: torch.Tensor | None, positions: torch.Tensor | None = None,
@@ -778,48 +823,48 @@ def qk_norm_rope(q: torch.Tensor | None, k: torch.Tensor | None, positions: torc
     if x is None or x.dim() != 3:
         raise ValueError("q or k must be given, [T][heads][head_dim]")
     T, _, D = x.shape
-    code = _dtype_code(x)
-    h = HeadsC()
+    code, dtype = _dtype_code(x), x.dtype
+    Hq = ldq = ldqo = Hk = ldk = ldko = ldv = rot = 0
     if q is not None:
+        Hq, ldq = _head_rows(q, "q", T, D, dtype)
         if q_out is None:
-            q_out = torch.empty((T, q.shape[1], D), dtype=q.dtype, device=q.device)
-        if q_out.shape != q.shape:
+            q_out = torch.empty((T, Hq, D), dtype=dtype, device=q.device)
+        H, ldqo = _head_rows(q_out, "q_out", T, D, dtype)
+        if H != Hq:
             raise ValueError("q_out must have q's shape")
-        h.ldq, h.ldq_out, h.heads = _head_rows(q, "q", T, D, x.dtype), _head_rows(q_out, "q_out", T, D, x.dtype), q.shape[1]
-        h.q, h.q_out = _addr(q), _addr(q_out)
     elif q_out is not None:
         raise ValueError("q_out without q")
     if k is not None:
+        Hk, ldk = _head_rows(k, "k", T, D, dtype)
         if k_out is None and cache is None:
-            k_out = torch.empty((T, k.shape[1], D), dtype=k.dtype, device=k.device)
-        h.ldk, h.kv_heads, h.k = _head_rows(k, "k", T, D, x.dtype), k.shape[1], _addr(k)
+            k_out = torch.empty((T, Hk, D), dtype=dtype, device=k.device)
         if k_out is not None:
-            if k_out.shape != k.shape:
+            H, ldko = _head_rows(k_out, "k_out", T, D, dtype)
+            if H != Hk:
                 raise ValueError("k_out must have k's shape")
-            h.ldk_out, h.k_out = _head_rows(k_out, "k_out", T, D, x.dtype), _addr(k_out)
     elif k_out is not None or cache is not None:
         raise ValueError("a cache and k_out need k")
     if (cache is None) != (v is None) or (cache is None) != (slots is None):
         raise ValueError("cache, v and slots go together")
     if cache is not None:
-        if v.shape != k.shape:
+        H, ldv = _head_rows(v, "v", T, D, dtype)
+        if H != Hk:
             raise ValueError("v must have k's shape")
         _ints(T, "slots", slots)
-        h.ldv, h.v, h.slots = _head_rows(v, "v", T, D, x.dtype), _addr(v), _addr(slots)
     if (inv_freq is None) != (positions is None):
         raise ValueError("positions and inv_freq go together")
     if inv_freq is not None:
         _ints(T, "positions", positions)
-        if inv_freq.dtype != torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
+        if inv_freq.dtype is not torch.float32 or inv_freq.dim() != 1 or not inv_freq.is_contiguous():
             raise ValueError("inv_freq must be float32 [rot/2], contiguous")
-        h.positions, h.inv_freq, h.rot = _addr(positions), _addr(inv_freq), 2 * inv_freq.shape[0]
+        rot = 2 * inv_freq.numel()
     for w in (q_weight, k_weight):
-        if w is not None and (w.dtype != x.dtype or w.shape != (D,) or not w.is_contiguous()):
+        if w is not None and (w.dtype is not dtype or w.shape != (D,) or not w.is_contiguous()):
             raise ValueError("weights must be [head_dim] of q's type, contiguous")
-    h.q_weight, h.k_weight = _addr(q_weight), _addr(k_weight)
-    h.head_dim, h.pairs, h.eps, h.mul = D, PAIRS[pairs], eps, mul
-    here = _one_device(q, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, slots, cache.data if cache else None)
-    _check(_lib().qmlp_qk_norm_rope(ctypes.byref(h), T, code, ctypes.byref(cache._c) if cache else None,
+    here = _here(x, k, v, positions, inv_freq, q_weight, k_weight, q_out, k_out, slots, cache.data if cache else None)
+    _check(_lib().qmlp_qk_norm_rope(_HEADS.pack(_at(q), _at(k), _at(v), ldq, ldk, ldv, _at(q_out), _at(k_out), ldqo, ldko,
+                                                _at(q_weight), _at(k_weight), _at(positions), _at(inv_freq), _at(slots), Hq, Hk, D,
+                                                rot, PAIRS[pairs], eps, mul), T, code, cache._at if cache else None,
                                     torch._C._cuda_getCurrentRawStream(here)), "qk_norm_rope")
     return q_out, k_out
 
@@ -828,16 +873,18 @@ def kv_read(cache: KVCache, slots: torch.Tensor, k: torch.Tensor | None = None, 
             dtype=torch.float16):
     """(k, v) [T][kv_heads][head_dim] as the cache holds them at slots int32 [T]; zeros for a slot outside it.  Both are
     made if neither is given; else the given ones are written."""
-    T, shape = slots.shape[0], (slots.shape[0], cache.kv_heads, cache.head_dim)
+    T = slots.numel()
+    shape = (T, cache.kv_heads, cache.head_dim)
     _ints(T, "slots", slots)
     if k is None and v is None:
         k, v = (torch.empty(shape, dtype=dtype, device=slots.device) for _ in range(2))
+    x = k if k is not None else v
     for t in (k, v):
-        if t is not None and (tuple(t.shape) != shape or not t.is_contiguous() or t.dtype != (k if k is not None else v).dtype):
+        if t is not None and (t.shape != shape or not t.is_contiguous() or t.dtype is not x.dtype):
             raise ValueError("k and v must be [T][kv_heads][head_dim], contiguous and of one type")
-    code = _dtype_code(k if k is not None else v)
-    here = _one_device(slots, k, v, cache.data)
-    _check(_lib().qmlp_kv_read(ctypes.byref(cache._c), _addr(slots), T, code, _addr(k), _addr(v),
+    code = _dtype_code(x)
+    here = _here(slots, k, v, cache.data)
+    _check(_lib().qmlp_kv_read(cache._at, slots.data_ptr(), T, code, _addr(k), _addr(v),
                                torch._C._cuda_getCurrentRawStream(here)), "kv_read")
     return k, v
 
@@ -857,36 +904,36 @@ def kv_attention(q: torch.Tensor, cache: KVCache, table: torch.Tensor, lens: tor
                  sinks: torch.Tensor | None = None, ws: torch.Tensor | None = None) -> torch.Tensor:
     """y [T][heads][D]: causal attention of a step's rows q over the cache.  Request b has lens[b] cached tokens, pages
     table[b], and the rows starts[b] .. starts[b+1] (None: one row each), which are its last tokens.  scale: head_dim^-0.5
-    unless given; window: tokens a row sees, itself among them (0: all); sinks float32 [heads] or None.  max_new: the most new tokens of a request
-    (a bound chooses kernels; unless given 1 without starts, T with them).  Rows before starts[0] and from starts[B] on are left as
-    they are (a y made here starts at zeros)."""
+    unless given; window: tokens a row sees, itself among them (0: all); sinks float32 [heads] or None.  max_new: the most
+    new tokens of a request (it chooses kernels; unless given, 1 without starts and T with them).  Rows before starts[0]
+    and from starts[B] on are left as they are (a y made here starts at zeros)."""
     if q.dim() != 3:
         raise ValueError("q must be [T][heads][head_dim]")
-    T, H, D = q.shape
-    code = _dtype_code(q)
+    code, dtype = _dtype_code(q), q.dtype
+    T, _, D = q.shape
+    H, ldq = _head_rows(q, "q", T, D, dtype)
     if D != cache.head_dim:
         raise ValueError("q and the cache differ in head_dim")
     if y is None:
-        y = torch.zeros((T, H, D), dtype=q.dtype, device=q.device)
-    elif y.shape != q.shape:
+        y = torch.zeros((T, H, D), dtype=dtype, device=q.device)
+    Hy, ldy = _head_rows(y, "y", T, D, dtype)
+    if Hy != H:
         raise ValueError("y must have q's shape")
-    ldq, ldy = _head_rows(q, "q", T, D, q.dtype), _head_rows(y, "y", T, D, q.dtype)
-    B = lens.shape[0]
+    B = lens.numel()
     _ints(B, "lens", lens)
     _ints(B + 1, "starts", starts)
-    if table.dim() != 2 or table.shape[0] != B or table.dtype != torch.int32 or not table.is_contiguous():
-        raise ValueError("table must be int32 [B][W], contiguous")
-    if sinks is not None and (sinks.dtype != torch.float32 or sinks.shape != (H,) or not sinks.is_contiguous()):
+    W = _is_table(table, B)
+    if sinks is not None and (sinks.dtype is not torch.float32 or sinks.shape != (H,) or not sinks.is_contiguous()):
         raise ValueError("sinks must be float32 [heads]")
     if max_new is None:
         max_new = T if starts is not None else 1
     if ws is None:
         ws = kv_attention_workspace(q, cache, table, max_new)
-    here = _one_device(q, y, table, lens, starts, sinks, ws, cache.data)
-    _check(_lib().qmlp_kv_attention(ctypes.byref(cache._c), _addr(q), ldq, T, H, code, _addr(table), table.shape[1], _addr(lens),
-                                    _addr(starts), B, max_new, D ** -0.5 if scale is None else scale, window, _addr(sinks),
-                                    _addr(y), ldy, _addr(ws), ws.numel(), torch._C._cuda_getCurrentRawStream(here)),
-           "kv_attention")
+    here = _here(q, y, table, lens, starts, sinks, ws, cache.data)
+    _check(_lib().qmlp_kv_attention(cache._at, _ATTENTION.pack(q.data_ptr(), y.data_ptr(), ldq, ldy, table.data_ptr(), lens.data_ptr(),
+                                                               _at(starts), _at(sinks), ws.data_ptr(), ws.numel(), T, H, B, W,
+                                                               max_new, window, D ** -0.5 if scale is None else scale),
+                                    code, torch._C._cuda_getCurrentRawStream(here)), "kv_attention")
     return y
 
 

@@ -83,28 +83,27 @@ size_t qmlp_kv_cache_bytes(int pages, int kv_heads, int head_dim, int page) {
     return (size_t)pages * kv_heads * 2 * page * (head_dim / 2 + 4);
 }
 
-qmlp_status qmlp_kv_plan(const int32_t* lens, const int32_t* new_tokens, int B, int page, int32_t* table, int W,
-                         int32_t* free_pages, int N, const int32_t* n_free, int tokens, int32_t* slots,
-                         int32_t* positions, int32_t* starts, int32_t* lens_out, int32_t* n_free_out,
-                         int32_t* short_out, qmlp_stream stream) {
-    if (!page_ok(page))
-        return QMLP_ERR_UNSUPPORTED;
-    if (B < 0 || W < 1 || N < 0 || tokens < 0)
-        return QMLP_ERR_SHAPE;
-    if (B > kKvRequests || W > (1 << 20) || (int64_t)W * page > (1ll << 30) || tokens > (1 << 24))
-        return QMLP_ERR_UNSUPPORTED;
-    if (B == 0)
-        return QMLP_OK;
-    if (!lens || !new_tokens || !table || !n_free || !starts || !lens_out || !n_free_out || !short_out ||
-        (N > 0 && !free_pages) || (tokens > 0 && (!slots || !positions)))
+qmlp_status qmlp_kv_plan(const qmlp_plan* p, qmlp_stream stream) {
+    if (!p)
         return QMLP_ERR_NULL;
-    for (const void* p : {(const void*)lens, (const void*)new_tokens, (const void*)table, (const void*)free_pages,
-                          (const void*)n_free, (const void*)slots, (const void*)positions, (const void*)starts,
-                          (const void*)lens_out, (const void*)n_free_out, (const void*)short_out})
-        if (!aligned4(p))
+    if (!page_ok(p->page))
+        return QMLP_ERR_UNSUPPORTED;
+    if (p->B < 0 || p->W < 1 || p->N < 0 || p->tokens < 0)
+        return QMLP_ERR_SHAPE;
+    if (p->B > kKvRequests || p->W > (1 << 20) || (int64_t)p->W * p->page > (1ll << 30) || p->tokens > (1 << 24))
+        return QMLP_ERR_UNSUPPORTED;
+    if (p->B == 0)
+        return QMLP_OK;
+    if (!p->lens || !p->new_tokens || !p->table || !p->n_free || !p->starts || !p->lens_out || !p->n_free_out ||
+        !p->short_out || (p->N > 0 && !p->free_pages) || (p->tokens > 0 && (!p->slots || !p->positions)))
+        return QMLP_ERR_NULL;
+    for (const int32_t* v : {p->lens, p->new_tokens, (const int32_t*)p->table, (const int32_t*)p->free_pages, p->n_free,
+                             (const int32_t*)p->slots, (const int32_t*)p->positions, (const int32_t*)p->starts,
+                             (const int32_t*)p->lens_out, (const int32_t*)p->n_free_out, (const int32_t*)p->short_out})
+        if (!aligned4(v))
             return QMLP_ERR_ALIGN;
-    const PlanArgs a{lens, new_tokens, n_free, table, free_pages, slots, positions, starts, lens_out, n_free_out,
-                     short_out, B, log2_of(page), W, N, tokens};
+    const PlanArgs a{p->lens, p->new_tokens, p->n_free, p->table, p->free_pages, p->slots, p->positions, p->starts,
+                     p->lens_out, p->n_free_out, p->short_out, p->B, log2_of(p->page), p->W, p->N, p->tokens};
     return from_hip(launch_kv_plan(a, static_cast<hipStream_t>(stream)));
 }
 
@@ -207,46 +206,45 @@ size_t qmlp_kv_attention_workspace_bytes(const qmlp_kv_cache* cache, int heads, 
     return kv_attention_bytes(cache->head_dim, heads / cache->kv_heads, max_new);
 }
 
-qmlp_status qmlp_kv_attention(const qmlp_kv_cache* cache, const void* q, int64_t ldq, int T, int heads,
-                              qmlp_dtype dtype, const int32_t* table, int W, const int32_t* lens,
-                              const int32_t* starts, int B, int max_new, float scale, int window,
-                              const float* sinks, void* y, int64_t ldy, void* ws, size_t ws_bytes,
-                              qmlp_stream stream) {
+qmlp_status qmlp_kv_attention(const qmlp_kv_cache* cache, const qmlp_attention* p, qmlp_dtype dtype, qmlp_stream stream) {
+    if (!p)
+        return QMLP_ERR_NULL;
     const int dt = number(dtype);
-    qmlp_status s = check_tokens(T, dt);
+    qmlp_status s = check_tokens(p->T, dt);
     if (s != QMLP_OK)
         return s;
-    if ((s = check_attention(cache, heads, max_new)) != QMLP_OK)
+    if ((s = check_attention(cache, p->heads, p->max_new)) != QMLP_OK)
         return s;
-    if (B < 0 || W < 1 || window < 0 || (!starts && T != B))
+    if (p->B < 0 || p->W < 1 || p->window < 0 || (!p->starts && p->T != p->B))
         return QMLP_ERR_SHAPE;
-    if (B > kKvRequests || (int64_t)W * cache->page > (1ll << 30) || !isfinite(scale))
+    if (p->B > kKvRequests || (int64_t)p->W * cache->page > (1ll << 30) || !isfinite(p->scale))
         return QMLP_ERR_UNSUPPORTED;
-    if (T == 0 || B == 0)
+    if (p->T == 0 || p->B == 0)
         return QMLP_OK;
-    if (!table || !lens)
+    if (!p->table || !p->lens)
         return QMLP_ERR_NULL;
-    if ((s = check_rows(q, ldq, heads, cache->head_dim, T)) != QMLP_OK)
+    if ((s = check_rows(p->q, p->ldq, p->heads, cache->head_dim, p->T)) != QMLP_OK)
         return s;
-    if ((s = check_rows(y, ldy, heads, cache->head_dim, T)) != QMLP_OK)
+    if ((s = check_rows(p->y, p->ldy, p->heads, cache->head_dim, p->T)) != QMLP_OK)
         return s;
-    if (!aligned4(table) || !aligned4(lens) || !aligned4(starts) || !aligned4(sinks))
+    if (!aligned4(p->table) || !aligned4(p->lens) || !aligned4(p->starts) || !aligned4(p->sinks))
         return QMLP_ERR_ALIGN;
-    const int G = heads / cache->kv_heads;
-    if (!ws || ws_bytes < kv_attention_bytes(cache->head_dim, G, max_new))
+    const int G = p->heads / cache->kv_heads;
+    if (!p->ws || p->ws_bytes < kv_attention_bytes(cache->head_dim, G, p->max_new))
         return QMLP_ERR_WORKSPACE;
-    if (!aligned16(ws))
+    if (!aligned16(p->ws))
         return QMLP_ERR_ALIGN;
     AttnArgs a{};
     a.cache = view(cache);
-    a.q = static_cast<const uint16_t*>(q);
-    a.y = static_cast<uint16_t*>(y);
-    a.table = table; a.lens = lens; a.starts = starts; a.sinks = sinks;
-    a.ldq = ldq; a.ldy = ldy;
-    a.done = static_cast<uint32_t*>(ws);
-    a.T = T; a.B = B; a.W = W; a.Hq = heads; a.G = G; a.D = cache->head_dim; a.bf = dt == QMLP_BF16; a.window = window;
-    a.scale = (float)((double)scale * 1.4426950408889634);
-    return from_hip(launch_kv_attention(a, max_new, static_cast<hipStream_t>(stream)));
+    a.q = static_cast<const uint16_t*>(p->q);
+    a.y = static_cast<uint16_t*>(p->y);
+    a.table = p->table; a.lens = p->lens; a.starts = p->starts; a.sinks = p->sinks;
+    a.ldq = p->ldq; a.ldy = p->ldy;
+    a.done = static_cast<uint32_t*>(p->ws);
+    a.T = p->T; a.B = p->B; a.W = p->W; a.Hq = p->heads; a.G = G; a.D = cache->head_dim; a.bf = dt == QMLP_BF16;
+    a.window = p->window;
+    a.scale = (float)((double)p->scale * 1.4426950408889634);
+    return from_hip(launch_kv_attention(a, p->max_new, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -121,21 +121,6 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
             for (int i = 0; i < D / 32; ++i)
                 qv[i] = col < rows ? reinterpret_cast<const uint4*>(src)[i] : make_uint4(0, 0, 0, 0);
         }
-        auto quarters = [](float v) {
-            v += __shfl_xor(v, 16, 64);
-            return v + __shfl_xor(v, 32, 64);
-        };
-        const float scale = a.scale * operand_rows(qv, a.bf, qsum, quarters, [](uint32_t v) {
-            v |= __shfl_xor(v, 16, 64);
-            return v | (uint32_t)__shfl_xor((int)v, 32, 64);
-        }, [](uint32_t top) { return top; });
-
-        // minus the row's sum, in the places of the first quarter
-        uint32_t part3[3];
-        three_bf16(-qsum, part3);
-        const uint4 qz = h == 0 ? make_uint4(part3[0] | part3[1] << 16, part3[2], 0, 0) : make_uint4(0, 0, 0, 0);
-        const float away = scale < 0.0f ? INFINITY : -INFINITY;      // a score that weighs nothing
-
         f32x4_t o[NT], oz = {0, 0, 0, 0};
 #pragma unroll
         for (int i = 0; i < NT; ++i)
@@ -162,6 +147,25 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                 load_tile<D>(d.tile[j], a, d.hidden[j] ? 0 : p, head, (t + 16 * j) & ((1 << lg) - 1));
             }
         };
+        // (the first steps are under way before q is seen to)
+        load(buf[0], 0);
+        if (n > 1)
+            load(buf[1], 1);
+        auto quarters = [](float v) {
+            v += __shfl_xor(v, 16, 64);
+            return v + __shfl_xor(v, 32, 64);
+        };
+        const float scale = a.scale * operand_rows(qv, a.bf, qsum, quarters, [](uint32_t v) {
+            v |= __shfl_xor(v, 16, 64);
+            return v | (uint32_t)__shfl_xor((int)v, 32, 64);
+        }, [](uint32_t top) { return top; });
+
+        // minus the row's sum, in the places of the first quarter
+        uint32_t part3[3];
+        three_bf16(-qsum, part3);
+        const uint4 qz = h == 0 ? make_uint4(part3[0] | part3[1] << 16, part3[2], 0, 0) : make_uint4(0, 0, 0, 0);
+        const float away = scale < 0.0f ? INFINITY : -INFINITY;      // a score that weighs nothing
+
         auto multiply = [&](const Step<D>& s, int i) {
             const Tile<D>* cur = s.tile;
             const bool hid0 = s.hidden[0], hid1 = s.hidden[1];
@@ -270,9 +274,6 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                 }
             }
         };
-        load(buf[0], 0);
-        if (n > 1)
-            load(buf[1], 1);
         for (int i = 0; i < n; i += 3) {
 #pragma unroll
             for (int j = 0; j < 3; ++j)

@@ -39,23 +39,32 @@ def test_cache_bytes(lib):
     assert lib.qmlp_kv_cache_bytes((1 << 27) - 1, 8, 128, 16) == ((1 << 27) - 1) * 8 * 2 * 16 * 68
 
 
-def _plan(lib, B=0, page=16, W=4, N=8, tokens=8, **ptr):
-    p = {n: P(ptr.get(n, FAKE)) for n in ("lens", "new", "table", "free", "n_free", "slots", "positions", "starts", "lens_out",
-                                          "n_free_out", "short")}
-    return lib.qmlp_kv_plan(p["lens"], p["new"], B, page, p["table"], W, p["free"], N, p["n_free"], tokens, p["slots"],
-                            p["positions"], p["starts"], p["lens_out"], p["n_free_out"], p["short"], None)
+PLAN = ("lens", "new_tokens", "table", "free_pages", "n_free", "slots", "positions", "starts", "lens_out", "n_free_out", "short_out")
 
 
-def test_plan_refusals(lib):
-    assert _plan(lib) == 0
-    assert _plan(lib, B=-1) == SHAPE and _plan(lib, W=0) == SHAPE and _plan(lib, N=-1) == SHAPE and _plan(lib, tokens=-1) == SHAPE
+def _bytes(c):
+    return bytes(c)
+
+
+def test_plan_refusals(q, lib):
+    def call(B=0, page=16, W=4, N=8, tokens=8, **ptr):
+        return lib.qmlp_kv_plan(_bytes(q.PlanC(*[ptr.get(n, FAKE) for n in PLAN], B, page, W, N, tokens)), None)
+    assert call() == 0 and lib.qmlp_kv_plan(None, None) == NULL
+    assert call(B=-1) == SHAPE and call(W=0) == SHAPE and call(N=-1) == SHAPE and call(tokens=-1) == SHAPE
     for page in (0, 8, 24, 512, -16):
-        assert _plan(lib, page=page) == UNSUP
-    assert _plan(lib, B=2049) == UNSUP and _plan(lib, W=(1 << 20) + 1) == UNSUP and _plan(lib, W=1 << 20, page=256) == 0
-    assert _plan(lib, tokens=(1 << 24) + 1) == UNSUP
-    for n in ("lens", "new", "table", "free", "n_free", "slots", "positions", "starts", "lens_out", "n_free_out", "short"):
-        assert _plan(lib, B=2, **{n: 0}) == NULL, n
-        assert _plan(lib, B=2, **{n: FAKE + 2}) == ALIGN, n
+        assert call(page=page) == UNSUP
+    assert call(B=2049) == UNSUP and call(W=(1 << 20) + 1) == UNSUP and call(W=1 << 20, page=256) == 0
+    assert call(tokens=(1 << 24) + 1) == UNSUP
+    for n in PLAN:
+        assert call(B=2, **{n: 0}) == NULL, n
+        assert call(B=2, **{n: FAKE + 2}) == ALIGN, n
+
+
+def test_the_packed_structures(q):
+    """The bytes the binding packs are those of the C structures."""
+    for s, c in ((q._HEADS, q.HeadsC), (q._PLAN, q.PlanC), (q._ATTENTION, q.AttentionC)):
+        v = [i + 1 for i in range(len(c._fields_))]
+        assert bytes(c(*v))[:s.size] == s.pack(*v) and 0 <= ctypes.sizeof(c) - s.size < 8
 
 
 def _heads(mod, **kw):
@@ -68,7 +77,7 @@ def _heads(mod, **kw):
 
 def test_qk_norm_rope_refusals(q, lib):
     def call(T=0, dt=0, cache=_cache(q), **kw):
-        return lib.qmlp_qk_norm_rope(ctypes.byref(_heads(q, **kw)), T, dt, None if cache is None else ctypes.byref(cache), None)
+        return lib.qmlp_qk_norm_rope(_bytes(_heads(q, **kw)), T, dt, None if cache is None else ctypes.byref(cache), None)
     assert call() == 0 and lib.qmlp_qk_norm_rope(None, 0, 0, None, None) == NULL
     assert call(T=-1) == SHAPE and call(T=(1 << 20) + 1) == UNSUP and call(dt=2) == UNSUP and call(dt=-1) == UNSUP
     assert call(head_dim=96) == UNSUP and call(heads=-1) == SHAPE and call(heads=0, kv_heads=0, cache=None) == SHAPE
@@ -109,8 +118,9 @@ def test_kv_read_refusals(q, lib):
 def test_kv_attention_refusals(q, lib):
     def call(T=0, B=2, heads=4, dt=0, c=_cache(q), W=4, new=1, scale=0.1, window=0, ldq=512, ldy=512, x=FAKE, table=FAKE, lens=FAKE,
              starts=FAKE, sinks=0, y=FAKE, ws=FAKE, wsb=1 << 40):
-        return lib.qmlp_kv_attention(None if c is None else ctypes.byref(c), P(x), ldq, T, heads, dt, P(table), W, P(lens), P(starts),
-                                     B, new, scale, window, P(sinks), P(y), ldy, P(ws), wsb, None)
+        return lib.qmlp_kv_attention(None if c is None else ctypes.byref(c), _bytes(q.AttentionC(
+            x, y, ldq, ldy, table, lens, starts, sinks, ws, wsb, T, heads, B, W, new, window, scale)), dt, None)
+    assert lib.qmlp_kv_attention(ctypes.byref(_cache(q)), None, 0, None) == NULL
     assert call() == 0 and call(B=0, T=5) == 0 and call(c=None) == NULL
     assert call(T=-1) == SHAPE and call(T=(1 << 20) + 1) == UNSUP and call(dt=2) == UNSUP
     assert call(heads=0) == SHAPE and call(heads=5) == SHAPE and call(heads=4098) == UNSUP
