@@ -17,9 +17,11 @@ namespace qmlp {
 namespace {
 
 // 16-bit activation <-> fp32
-__device__ __forceinline__ float up16(uint32_t bits, bool bf) { return bf ? __uint_as_float(bits << 16) : h2f(bits); }
-__device__ __forceinline__ uint32_t down16(float v, bool bf) {
-    return bf ? (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v) : f2h(v);
+template <bool BF>
+__device__ __forceinline__ float up16(uint32_t bits) { return BF ? __uint_as_float(bits << 16) : h2f(bits); }
+template <bool BF>
+__device__ __forceinline__ uint32_t down16(float v) {
+    return BF ? (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v) : f2h(v);
 }
 __device__ __forceinline__ uint32_t word_at(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
 
@@ -77,14 +79,13 @@ __device__ __forceinline__ void store_codes(const KvView& c, int slot, int head,
 }
 
 // One head: norm and rotation of a lane's 8 numbers in F.  `turn`: (cos, sin) of each pair, scaled.
-template <int D, typename F>
-__device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, const uint16_t* weight, const F* turn, int lane) {
+template <int D, bool BF, typename F, typename P>
+__device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, const uint16_t* weight, const P* turn, int lane) {
     constexpr int LPH = D / 8;
-    const bool bf = a.bf;
     F x[8], p[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        x[i] = (F)up16(i & 1 ? word_at(raw, i >> 1) >> 16 : word_at(raw, i >> 1) & 0xFFFFu, bf);
+        x[i] = (F)up16<BF>(i & 1 ? word_at(raw, i >> 1) >> 16 : word_at(raw, i >> 1) & 0xFFFFu);
     F inv = (F)1;
     if (weight) {
         F s = 0;
@@ -100,7 +101,7 @@ __device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, con
         const uint4 w = reinterpret_cast<const uint4*>(weight)[lane];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-            x[i] = x[i] * inv * (F)up16(i & 1 ? word_at(w, i >> 1) >> 16 : word_at(w, i >> 1) & 0xFFFFu, bf);
+            x[i] = x[i] * inv * (F)up16<BF>(i & 1 ? word_at(w, i >> 1) >> 16 : word_at(w, i >> 1) & 0xFFFFu);
     }
     if (a.inv) {
         const int half = a.rot / 2, hl = half / 8;        // lanes to the partner where halves turn
@@ -108,17 +109,19 @@ __device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, con
         if (a.next) {
 #pragma unroll
             for (int i = 0; i < 8; i += 2) {
-                const F c = on ? turn[2 * (4 * lane + i / 2)] : (F)1, s = on ? turn[2 * (4 * lane + i / 2) + 1] : (F)0;
+                const auto cs = turn[on ? i / 2 * (a.rot / 8) + lane : 0];
+                const F c = cs.x, s = cs.y;
                 p[i] = x[i] * c - x[i + 1] * s;
                 p[i + 1] = x[i + 1] * c + x[i] * s;
             }
         } else {
             const bool first = lane < hl;
             const int me = threadIdx.x & 63, from = on ? (first ? me + hl : me - hl) : me;
-            const int at = on ? 8 * (first ? lane : lane - hl) : 0;
+            const int at = on ? (first ? lane : lane - hl) : 0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const F o = __shfl(x[i], from, 64), c = turn[2 * (at + i)], s = turn[2 * (at + i) + 1];
+                const auto cs = turn[i * hl + at];
+                const F o = __shfl(x[i], from, 64), c = cs.x, s = cs.y;
                 p[i] = first ? x[i] * c - o * s : x[i] * c + o * s;
             }
         }
@@ -129,36 +132,36 @@ __device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, con
     uint32_t h[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        h[i] = down16((float)x[i], bf);
+        h[i] = down16<BF>((float)x[i]);
     return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
 }
 
-__device__ __forceinline__ void unpacked(const uint4& v, bool bf, float (&x)[8]) {
+template <bool BF>
+__device__ __forceinline__ void unpacked(const uint4& v, float (&x)[8]) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        x[i] = up16(i & 1 ? word_at(v, i >> 1) >> 16 : word_at(v, i >> 1) & 0xFFFFu, bf);
+        x[i] = up16<BF>(i & 1 ? word_at(v, i >> 1) >> 16 : word_at(v, i >> 1) & 0xFFFFu);
 }
 
 // A workgroup takes one token's heads g, g + step, ... (q, then k, then v), D/8 lanes each; the token's
 // angles are reduced once, a thread a pair: positions times frequencies as a product of fp64 (far positions
 // lose nothing that a 16-bit result or a code shows), in turns, then cos and sin of what is left of a turn.
-template <int D>
+template <int D, bool BF>
 __global__ void __launch_bounds__(256) qk_kernel(HeadsArgs a) {
     constexpr int LPH = D / 8, HPW = 256 / LPH;           // heads at a time
-    __shared__ double turn64[D];
-    __shared__ float turn32[D];
+    __shared__ double2 turn64[D / 2];
+    __shared__ float2 turn32[D / 2];
     const int t = blockIdx.x, tid = threadIdx.x, lane = tid % LPH;
-    const bool bf = a.bf;
     if (a.inv) {
         if (tid < a.rot / 2) {
+            // pairs as the lanes take them, neighbouring lanes side by side
+            const int n = a.next ? (tid & 3) * (a.rot / 8) + tid / 4 : (tid & 7) * (a.rot / 16) + tid / 8;
             double turns = (double)a.pos[t] * (double)a.inv[tid] * 0.15915494309189533577;    // 1 / (2 pi)
             turns -= __builtin_rint(turns);
             double s, c;
             sincospi(2.0 * turns, &s, &c);
-            turn64[2 * tid] = c * (double)a.mul;
-            turn64[2 * tid + 1] = s * (double)a.mul;
-            turn32[2 * tid] = (float)turn64[2 * tid];
-            turn32[2 * tid + 1] = (float)turn64[2 * tid + 1];
+            turn64[n] = {c * (double)a.mul, s * (double)a.mul};
+            turn32[n] = {(float)turn64[n].x, (float)turn64[n].y};
         }
         __syncthreads();
     }
@@ -178,18 +181,18 @@ __global__ void __launch_bounds__(256) qk_kernel(HeadsArgs a) {
         const uint16_t* src = side == 0 ? a.q + t * a.ldq : side == 1 ? a.k + t * a.ldk : a.v + t * a.ldv;
         uint4 v = reinterpret_cast<const uint4*>(src + (long)h * D)[lane];
         if (side == 0) {
-            v = turned<D, float>(a, v, a.qw, turn32, lane);
+            v = turned<D, BF, float>(a, v, a.qw, turn32, lane);
             reinterpret_cast<uint4*>(a.q_out + t * a.ldqo + (long)h * D)[lane] = v;
             continue;
         }
         if (side == 1) {
-            v = turned<D, double>(a, v, a.kw, turn64, lane);
+            v = turned<D, BF, double>(a, v, a.kw, turn64, lane);
             if (a.k_out)
                 reinterpret_cast<uint4*>(a.k_out + t * a.ldko + (long)h * D)[lane] = v;
         }
         if (slot >= 0) {
             float x[8];
-            unpacked(v, bf, x);
+            unpacked<BF>(v, x);
             uint32_t meta;
             const uint32_t w = quantize<LPH>(x, meta);
             store_codes<D>(a.cache, slot, h, side - 1, lane, w, meta);
@@ -198,8 +201,8 @@ __global__ void __launch_bounds__(256) qk_kernel(HeadsArgs a) {
 }
 
 // A lane a word of codes: 16 bytes out.
-template <int D>
-__global__ void __launch_bounds__(256) read_kernel(KvView c, const int32_t* slots, int T, int bf, uint16_t* k, uint16_t* v) {
+template <int D, bool BF>
+__global__ void __launch_bounds__(256) read_kernel(KvView c, const int32_t* slots, int T, uint16_t* k, uint16_t* v) {
     constexpr int WPH = D / 8;
     const long i = (long)blockIdx.x * 256 + threadIdx.x;
     const int w = (int)(i % WPH);
@@ -226,7 +229,7 @@ __global__ void __launch_bounds__(256) read_kernel(KvView c, const int32_t* slot
         uint32_t r[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-            r[j] = in ? down16(s * ((float)((word >> (4 * ((j >> 1) + 4 * (j & 1)))) & 15u) - z), bf) : 0u;
+            r[j] = in ? down16<BF>(s * ((float)((word >> (4 * ((j >> 1) + 4 * (j & 1)))) & 15u) - z)) : 0u;
         reinterpret_cast<uint4*>(out + th * D)[w] = make_uint4(r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16);
     }
 }
@@ -239,9 +242,9 @@ hipError_t launch_qk_norm_rope(const HeadsArgs& a, hipStream_t st) {
     const int sets = (all + hpw - 1) / hpw, split = a.T >= 512 ? 1 : sets;
     const dim3 grid(a.T, split);
     if (a.D == 128)
-        qk_kernel<128><<<grid, 256, 0, st>>>(a);
+        a.bf ? qk_kernel<128, true><<<grid, 256, 0, st>>>(a) : qk_kernel<128, false><<<grid, 256, 0, st>>>(a);
     else
-        qk_kernel<64><<<grid, 256, 0, st>>>(a);
+        a.bf ? qk_kernel<64, true><<<grid, 256, 0, st>>>(a) : qk_kernel<64, false><<<grid, 256, 0, st>>>(a);
     return hipGetLastError();
 }
 
@@ -249,9 +252,9 @@ hipError_t launch_kv_read(const KvView& c, int D, const int32_t* slots, int T, i
     const long lanes = (long)T * c.heads * (D / 8);
     const unsigned grid = (unsigned)((lanes + 255) / 256);
     if (D == 128)
-        read_kernel<128><<<grid, 256, 0, st>>>(c, slots, T, bf, k, v);
+        bf ? read_kernel<128, true><<<grid, 256, 0, st>>>(c, slots, T, k, v) : read_kernel<128, false><<<grid, 256, 0, st>>>(c, slots, T, k, v);
     else
-        read_kernel<64><<<grid, 256, 0, st>>>(c, slots, T, bf, k, v);
+        bf ? read_kernel<64, true><<<grid, 256, 0, st>>>(c, slots, T, k, v) : read_kernel<64, false><<<grid, 256, 0, st>>>(c, slots, T, k, v);
     return hipGetLastError();
 }
 
