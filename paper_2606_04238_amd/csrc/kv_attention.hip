@@ -23,6 +23,7 @@ namespace qmlp {
 namespace {
 
 typedef uint32_t w4 __attribute__((ext_vector_type(4)));
+constexpr int kMostParts = 64;
 constexpr int kAhead = 8;                                 // parts under way where they are joined
 constexpr int kRows = 16, kStep = 128;                    // rows of a tile; tokens of a workgroup's step, 32 a wave
 
@@ -75,6 +76,7 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
     float* lo = reinterpret_cast<float*>(smem);           // [4][16][LD]
     __shared__ float lm[4][kRows], ll[4][kRows];
     __shared__ uint32_t arrived;
+    __shared__ int longest;
     Known<I>* known = reinterpret_cast<Known<I>*>(smem + 4 * kRows * LD * 4);
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 4, col = lane & 15;
     const int lg = a.cache.page_log2, Hk = a.cache.heads;
@@ -88,8 +90,17 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
         return rows > limit ? 0 : (int)((rows + kRows - 1) / kRows);
     };
     auto steps_of = [&](const Request& q) { return max(1, (q.len + kStep - 1) / kStep - first_step(q)); };
-    const I total = prefix_work<256, I>(a, known, [&](const Request& q) { return (I)tiles_of(q) * Hk * steps_of(q); });
-    const I share = (total + gridDim.x - 1) / gridDim.x;
+    if (tid == 0)
+        longest = 0;
+    __syncthreads();
+    const I total = prefix_work<256, I>(a, known, [&](const Request& q) {
+        const int tiles = tiles_of(q), steps = steps_of(q);
+        if (tiles && steps > kMostParts)
+            atomicMax(&longest, steps);
+        return (I)tiles * Hk * steps;
+    });
+    // (an item in more than 64 parts would take longer to join than to read)
+    const I share = max((total + (I)gridDim.x - 1) / (I)gridDim.x, (I)((longest + kMostParts - 1) / kMostParts));
     // workgroups of one XCD take neighbouring ranges
     const int wg = (blockIdx.x & 7) * (gridDim.x >> 3) + (blockIdx.x >> 3);
     const I begin = wg * share, end = min(begin + share, total);
@@ -426,7 +437,7 @@ hipError_t launch_few(const AttnArgs& a, int limit, hipStream_t st) {
 }  // namespace
 
 // Requests of up to this many rows take the kernel above, those with more the one for many rows (kv_attention_rows.hip).
-constexpr int kFewRows = 32;
+constexpr int kFewRows = 128;
 
 size_t kv_attention_bytes(int D, int G, int max_new) {
     const size_t few = (size_t)few_grid() * 2 * kRows * (D + 2) * 4, many = (long)max_new * G > kFewRows ? kv_rows_bytes(D) : 0;

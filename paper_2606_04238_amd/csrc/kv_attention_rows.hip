@@ -19,6 +19,7 @@ namespace qmlp {
 namespace {
 
 constexpr int kWaves = 8, kTileRows = 32 * kWaves, kThreads = 64 * kWaves, kMostShares = 16;
+constexpr int kJoin = 8;                                  // parts under way where they are joined
 
 template <int D>
 struct __attribute__((aligned(256))) Stage {
@@ -107,7 +108,11 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     const int first = q.len - q.n + tile * kTileRows / a.G, last = q.len - q.n + (tile * kTileRows + rows - 1) / a.G;   // positions
     const int low0 = a.window ? max(0, first - a.window + 1) / kTokens : 0;
     const int all = max(0, last / kTokens + 1 - low0);    // steps of the tile (last < 0: none)
-    const int i0 = low0 + (int)((long)all * part / shares), i1 = low0 + (last < 0 ? 0 : (int)((long)all * (part + 1) / shares));
+    // (at least four steps a share: joining costs about as much)
+    const int own = min(shares, max(1, all / 4));
+    if (part >= own)
+        return;
+    const int i0 = low0 + (int)((long)all * part / own), i1 = low0 + (last < 0 ? 0 : (int)((long)all * (part + 1) / own));
 
     // the wave's rows' positions, and this lane's row
     const int wrows = min(rows - wave * 32, 32);
@@ -429,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
 
     const int g = head * a.G + row % a.G;
     uint16_t* y = a.y + (long)(q.row0 + tok) * a.ldy + (long)g * D;
-    if (shares == 1) {
+    if (own == 1) {
         const float f = row_factor(a, g, m, l);
         if (r < rows)
 #pragma unroll
@@ -449,7 +454,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     const int item = nth * Hk + head;
     const size_t place = (size_t)kTileRows * (D + 2) * 4;
     uint8_t* parts = reinterpret_cast<uint8_t*>(a.part) + (size_t)item * shares * place;
-    const Rsrc rp = rsrc(parts, (uint32_t)(place * shares));
+    const Rsrc rp = rsrc(parts, (uint32_t)(place * own));
     const uint32_t mine = (uint32_t)(part * place);
     if (r < rows) {
 #pragma unroll
@@ -470,26 +475,26 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     if (tid == 0)
         arrived = __hip_atomic_fetch_add(a.done + item, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    if (arrived != (uint32_t)shares - 1u)
+    if (arrived != (uint32_t)own - 1u)
         return;
     if (tid == 0)
         __hip_atomic_store(a.done + item, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     for (int c = tid; c < rows * (D / 4); c += kThreads) {
         const int jr = c / (D / 4), d = 4 * (c % (D / 4)), rr = tile * kTileRows + jr, gg = head * a.G + rr % a.G;
         float mm = kNone, ls = 0.0f, v[4] = {0, 0, 0, 0};
-        for (int p0 = 0; p0 < shares; p0 += 4) {
-            w4 u[4];
-            float pm[4], pl[4];
+        for (int p0 = 0; p0 < own; p0 += kJoin) {
+            w4 u[kJoin];
+            float pm[kJoin], pl[kJoin];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t at = (uint32_t)(min(p0 + k, shares - 1) * place);
+            for (int k = 0; k < kJoin; ++k) {
+                const uint32_t at = (uint32_t)(min(p0 + k, own - 1) * place);
                 u[k] = __builtin_amdgcn_raw_buffer_load_b128(rp, at + (uint32_t)(jr * D + d) * 4u, 0, kDevice);
                 pm[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at + (uint32_t)(kTileRows * D + jr) * 4u, 0, kDevice));
                 pl[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at + (uint32_t)(kTileRows * (D + 1) + jr) * 4u, 0, kDevice));
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (p0 + k < shares) {
+            for (int k = 0; k < kJoin; ++k)
+                if (p0 + k < own) {
                     const float mn = fmaxf(mm, pm[k]), f0 = exp2_(mm - mn), f1 = exp2_(pm[k] - mn);
                     mm = mn;
                     ls = ls * f0 + pl[k] * f1;

@@ -147,7 +147,7 @@ __device__ __forceinline__ void unpacked(const uint4& v, float (&x)[8]) {
 // angles are reduced once, a thread a pair: positions times frequencies as a product of fp64 (far positions
 // lose nothing that a 16-bit result or a code shows), in turns, then cos and sin of what is left of a turn.
 template <int D, bool BF>
-__global__ void __launch_bounds__(256) qk_kernel(HeadsArgs a) {
+__global__ void __launch_bounds__(256, 5) qk_kernel(HeadsArgs a) {
     constexpr int LPH = D / 8, HPW = 256 / LPH;           // heads at a time
     __shared__ double2 turn64[D / 2];
     __shared__ float2 turn32[D / 2];

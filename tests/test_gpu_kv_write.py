@@ -40,7 +40,8 @@ CASES = [  # T, Hq, Hk, D, rot, pairs, page, norm, mul, far
     (3, 1, 1, 64, 32, "half", 32, True, 1.0, 1000000), (17, 5, 1, 128, 64, "next", 128, True, 0.5, 40000),
     (64, 6, 3, 128, 16, "half", 256, False, 1.0, 2000000), (65, 14, 2, 64, 64, "next", 16, True, 1.0, 7),
     (129, 2, 2, 128, 0, "half", 64, True, 1.0, 1), (600, 4, 2, 64, 48, "half", 64, True, 1.0, 5000),
-    (513, 3, 3, 128, 112, "next", 32, False, 1.0, 1 << 20), (40, 2, 2, 64, 0, "half", 16, False, 1.0, 1)]
+    (513, 3, 3, 128, 112, "next", 32, False, 1.0, 1 << 20), (40, 2, 2, 64, 0, "half", 16, False, 1.0, 1),
+    (1027, 3, 1, 128, 128, "half", 64, True, 1.0, 40000), (1030, 1, 1, 64, 32, "next", 16, True, 1.0, 3000)]
 
 
 @pytest.mark.parametrize("dtype", [F16, BF16])
