@@ -267,7 +267,7 @@ def decoder_model(stack: Stack, seed: int, steps: int, min_warm_s: float, mlp_us
     the layers; 4-bit, or 2-bit for W2), the MLP (mlp_us: the precision
     comparison's pass), and the read of a BF16 KV cache of ctx positions (a
     read-only pass of this library's streaming kernel over that many bytes
-    stands in for attention, which is not built); per token the LM head at
+    stands in for attention: qmlp_kv_attention's cache is 4-bit); per token the LM head at
     the linears' width.  The weight part of
     a token is timed as one graph per width; the per-operator times are
     reported beside it."""

@@ -14,6 +14,10 @@
 //
 // The rounding to binary16 is made where weights are at most 2^15 and, when the maximum is taken anew, 2^8: normal
 // numbers down to 2^-22 of the largest.  m moves only when a weight would pass 2^15.
+//
+// 131072 tokens of 8 K/V heads of 128 (143 MB) take 38.5 us, of which the pass over the cache is 24 us (5.8 TB/s, by clocks in the
+// kernel), 3 us go before it (lengths, pages, the first loads: three trips to memory) and the rest to joining 64 parts.  One
+// sequence of 2001 tokens, 16 parts an item, takes 11.4 us.  One step of a wave under way instead of two: 59 us and 13.9 us.
 #include "qmlp_internal.h"
 
 #include "decode_launch.h"
@@ -65,6 +69,7 @@ __device__ __forceinline__ void load_tile(Tile<D>& t, const AttnArgs& a, int pid
     t.kz = *reinterpret_cast<const uint32_t*>(meta + r * 4u);
 }
 
+// (Two workgroups a compute unit: three steps of 32 tokens in registers leave two waves a SIMD.)
 // Work is cut evenly over the workgroups (see prefix_work): a unit is one step of one item, an item a tile
 // of rows of one K/V head.  A workgroup's range can begin and end inside items; what it has of those goes to the
 // workspace, two places a workgroup, and the last to come to an item (a counter at the item's first workgroup) joins
@@ -166,7 +171,7 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
             v += __shfl_xor(v, 16, 64);
             return v + __shfl_xor(v, 32, 64);
         };
-        const float scale = a.scale * operand_rows(qv, a.bf, qsum, quarters, [](uint32_t v) {
+        float scale = a.scale * operand_rows(qv, a.bf, qsum, quarters, [](uint32_t v) {
             v |= __shfl_xor(v, 16, 64);
             return v | (uint32_t)__shfl_xor((int)v, 32, 64);
         }, [](uint32_t top) { return top; });
@@ -175,6 +180,7 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
         uint32_t part3[3];
         three_bf16(-qsum, part3);
         const uint4 qz = h == 0 ? make_uint4(part3[0] | part3[1] << 16, part3[2], 0, 0) : make_uint4(0, 0, 0, 0);
+        scale = scale == 0.0f ? 1.2e-38f : scale;         // (no score passes 2^-40 with it, and infinity times it is no NaN)
         const float away = scale < 0.0f ? INFINITY : -INFINITY;      // a score that weighs nothing
 
         auto multiply = [&](const Step<D>& s, int i) {
@@ -437,6 +443,8 @@ hipError_t launch_few(const AttnArgs& a, int limit, hipStream_t st) {
 }  // namespace
 
 // Requests of up to this many rows take the kernel above, those with more the one for many rows (kv_attention_rows.hip).
+// 80 rows (5 tokens, 16 heads on one K/V head) of four requests of 30000 tokens: 38 us here, 98 us there, whose tile of 256 rows is
+// then a third full and its items few; 20 tokens (80 rows a K/V head) after 15000: 37 and 68 us.  800 rows there: 123 us.
 constexpr int kFewRows = 128;
 
 size_t kv_attention_bytes(int D, int G, int max_new) {

@@ -1,15 +1,23 @@
 // Causal attention over the 4-bit cache for many rows a request (prompts and their chunks), gfx950.
 //
 // The mathematics of kv_attention.hip.  With rows to spare what bounds it is arithmetic: the matrix products, and beside
-// them the weights (an exponential and five more operations for each of rows x tokens).  So a
-// workgroup takes 128 rows (of all heads that share a K/V head), unpacks 64 tokens once for all of them into
-// LDS, as exact binary16 integers code - zero, and the scales go on the scores and the weights, which are touched anyway.  A
+// them the weights (an exponential and five more operations for each of rows x tokens).  So a workgroup takes 256 rows
+// (of all heads that share a K/V head), unpacks 64 tokens (128 where heads are 64 wide) once for all of them into LDS, as
+// exact binary16 integers code - zero, and the scales go on the scores and the weights, which are touched anyway.  A
 // wave owns 32 rows; its products are transposed (tokens or dims down, rows across), so that weights go from one
-// product to the other in registers.  Two stages of LDS: while one is multiplied the next is loaded and unpacked.
+// product to the other in registers.  Three stages of LDS (see the loop).
 //
-// LDS: K [64 tokens][D], 16-byte pieces (8 dims) at place p ^ (token & 7); V [D dims][64 tokens], a piece being the eight
-// tokens a lane multiplies at once (16 s + 4 h + {0..3, 8..11}), at place p ^ (dim & 7) ^ (dim / 8 & 7).  Neighbouring lanes so
-// read and write different banks.
+// LDS: K [tokens][D], 16-byte pieces (8 dims) at place p ^ (token & 7); V [D dims][tokens], a piece being the eight
+// tokens a lane multiplies at once (16 s + 4 h + {0..3, 8..11}), at place p ^ (dim & 7) ^ (dim / 8 & 7).  Neighbouring lanes
+// so read and write different banks.
+//
+// Prompts of 2501, 2058 and 1341 tokens of 32 heads of 128 on 8 K/V heads: 176 us (570 TFLOP/s); 1000 tokens after 15000
+// beside 15 decoding requests: 341 to 355 us (730 TFLOP/s, where a large product of the library reaches 1160).  On the way:
+// 128 rows a workgroup 195 and 438 us; 256 rows 205 and 397; tiles handed out by their length 200; weights and products in turns
+// with operands from LDS two turns ahead 187 and 359; a third stage, so that every tile has both neighbours' products
+// beside it, 181 and 356; pieces of V without turned halves 177 and 348.  By counters (the mixed step, at 356 us) the
+// vector units are busy 56 % of the time and the matrix cores 31 %, waves wait for data or each other 35 %; steps of 128 tokens
+// at D = 128 spilled registers (398 us).
 #include "qmlp_internal.h"
 
 #include "decode_launch.h"
@@ -172,7 +180,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
                     make_uint4(add2(e[0], off), add2(e[1], off), add2(e[2], off), add2(e[3], off));
             }
             if (kc == 0)
-                s.sk[ktok] = there ? h2f(m & 0xFFFFu) * scale : INFINITY;       // (a scale is never infinite: not there)
+                s.sk[ktok] = there ? finite(h2f(m & 0xFFFFu) * scale) : INFINITY;       // (a scale is never infinite: not there)
         } else {
             uint32_t m[4];
 #pragma unroll

@@ -36,6 +36,9 @@ __device__ __forceinline__ Rsrc rsrc(const void* p, uint32_t bytes) {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
 }
 __device__ __forceinline__ float exp2_(float v) { return __builtin_amdgcn_exp2f(v); }
+__device__ __forceinline__ float finite(float v) {            // an infinity as the largest number, NaN as it is
+    return __builtin_fabsf(v) == INFINITY ? __builtin_copysignf(3.4028235e38f, v) : v;
+}
 __device__ __forceinline__ float log2_(float v) { return __builtin_amdgcn_logf(v); }
 
 // The low (high) half of w times v, and c added: the conversion is the instruction's.

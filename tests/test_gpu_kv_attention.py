@@ -180,6 +180,39 @@ def test_many_requests(q):
     go(q, cache, x, table, lens, starts, F16, max_new=1)
 
 
+def test_the_most_requests(q):
+    """2048 requests, one of them with rows for the tile kernel."""
+    req = [(1 + 5 * i % 33, 1) for i in range(2047)] + [(300, 200)]
+    cache, x, table, lens, starts = make(q, req, 1, 2, 64, 16, F16)
+    go(q, cache, x, table, lens, starts, F16)
+
+
+@pytest.mark.parametrize("most", [1, None])
+def test_scales_at_the_ends(q, most):
+    """A scale of 0 is the mean of what a row sees; where scores pass fp32 it gives NaN and hides no tokens."""
+    cache, x, table, lens, starts = make(q, [(90, 70), (33, 1)], 1, 4, 64, 16, BF16)
+    go(q, cache, x, table, lens, starts, BF16, scale=0.0, max_new=most)
+    go(q, cache, x, table, lens, starts, BF16, scale=-1e-30, max_new=most)
+    y = q.kv_attention(x, cache, table, lens, starts, max_new=most, scale=3e38)
+    torch.cuda.synchronize()
+    assert torch.isnan(y[1:]).any(2).float().mean() > 0.9
+    go(q, cache, (x.float() * 1e-36).to(BF16), table, lens, starts, BF16, max_new=most)
+    y = q.kv_attention((x.float() * 1e38).to(BF16), cache, table, lens, starts, max_new=most, scale=1e4)
+    torch.cuda.synchronize()
+    assert torch.isnan(y[20:]).any(2).float().mean() > 0.9
+
+
+def test_wide_tables(q):
+    """A table whose units of work pass 32 bits, most of it never used."""
+    W, B = (1 << 30) // 256, 36
+    cache, x, small, lens, starts = make(q, [(1 + 37 * i, 1) for i in range(B)], 8, 2, 64, 256, F16)
+    table = torch.zeros(B, W, dtype=torch.int32, device="cuda")
+    table[:, :small.shape[1]] = small
+    a, b = (q.kv_attention(x, cache, t, lens, starts, max_new=1) for t in (small, table))
+    torch.cuda.synchronize()
+    assert torch.equal(a, b) and a.any()
+
+
 def test_offsets_past_32_bits(q):
     """Pages behind 2^32 bytes of a cache."""
     Hk, D, page = 8, 128, 256
