@@ -495,7 +495,9 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
             float pm[kJoin], pl[kJoin];
 #pragma unroll
             for (int k = 0; k < kJoin; ++k) {
-                const uint32_t at = (uint32_t)(min(p0 + k, own - 1) * place);
+                if (p0 + k >= own)
+                    break;
+                const uint32_t at = (uint32_t)((p0 + k) * place);
                 u[k] = __builtin_amdgcn_raw_buffer_load_b128(rp, at + (uint32_t)(jr * D + d) * 4u, 0, kDevice);
                 pm[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at + (uint32_t)(kTileRows * D + jr) * 4u, 0, kDevice));
                 pl[k] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(rp, at + (uint32_t)(kTileRows * (D + 1) + jr) * 4u, 0, kDevice));

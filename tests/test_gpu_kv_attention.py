@@ -202,6 +202,16 @@ def test_scales_at_the_ends(q, most):
     assert torch.isnan(y[20:]).any(2).float().mean() > 0.9
 
 
+@pytest.mark.parametrize("most", [1, None])
+def test_queries_below_the_normal_numbers(q, most):
+    """Rows of q among binary16's subnormal numbers, alone and beside ordinary ones, at a scale that makes them count."""
+    cache, x, table, lens, starts = make(q, [(90, 70), (33, 1)], 1, 4, 128, 16, F16)
+    small = (x.float() * 1.5e-5).to(F16)
+    go(q, cache, small, table, lens, starts, F16, scale=5000.0, max_new=most)
+    small[:, :, ::3] = (x[:, :, ::3].float() * 2e-3).to(F16)
+    go(q, cache, small, table, lens, starts, F16, scale=40.0, max_new=most)
+
+
 def test_wide_tables(q):
     """A table whose units of work pass 32 bits, most of it never used."""
     W, B = (1 << 30) // 256, 36
