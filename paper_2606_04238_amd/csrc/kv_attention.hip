@@ -444,7 +444,7 @@ hipError_t launch_few(const AttnArgs& a, int limit, hipStream_t st) {
 
 // Requests of up to this many rows take the kernel above, those with more the one for many rows (kv_attention_rows.hip).
 // 80 rows (5 tokens, 16 heads on one K/V head) of four requests of 30000 tokens: 38 us here, 98 us there, whose tile of 256 rows is
-// then a third full and its items few; 20 tokens (80 rows a K/V head) after 15000: 37 and 68 us.  800 rows there: 123 us.
+// then a third full and its items few; 20 tokens (80 rows a K/V head) after 15000: 37 and 68 us.  800 rows there: 120 us.
 constexpr int kFewRows = 128;
 
 size_t kv_attention_bytes(int D, int G, int max_new) {

@@ -12,7 +12,7 @@
 // so read and write different banks.
 //
 // Prompts of 2501, 2058 and 1341 tokens of 32 heads of 128 on 8 K/V heads: 176 us (570 TFLOP/s); 1000 tokens after 15000
-// beside 15 decoding requests: 341 to 355 us (730 TFLOP/s, where a large product of the library reaches 1160).  On the way:
+// beside 15 decoding requests: 345 us (738 TFLOP/s, where a large product of the library reaches 1160).  On the way:
 // 128 rows a workgroup 195 and 438 us; 256 rows 205 and 397; tiles handed out by their length 200; weights and products in turns
 // with operands from LDS two turns ahead 187 and 359; a third stage, so that every tile has both neighbours' products
 // beside it, 181 and 356; pieces of V without turned halves 177 and 348.  By counters (the mixed step, at 356 us) the
