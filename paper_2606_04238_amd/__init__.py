@@ -776,6 +776,11 @@ class KVPlan:
         self.B, self.tokens = B, tokens
         self._out = tuple(v.data_ptr() for v in t)
 
+    def __setattr__(self, name, value):
+        if hasattr(self, "_out"):
+            raise AttributeError("a plan keeps its tensors (their contents change)")
+        super().__setattr__(name, value)
+
 
 def kv_plan(plan: KVPlan, lens: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free: torch.Tensor,
             n_free: torch.Tensor, page: int) -> KVPlan:

@@ -163,6 +163,10 @@ def test_python_refusals(q):
     c = q.KVCache(torch.zeros(3, 2, 2, 64 * 68, dtype=torch.uint8), 64)
     assert (c.pages, c.kv_heads, c.head_dim) == (3, 2, 128)
     p = q.KVPlan(2, 4, device="cpu")
+    with pytest.raises(AttributeError):
+        p.lens = i(2)
+    with pytest.raises(ValueError):
+        q.KVPlan(2, 4, device="cpu", lens=i(3))
     for args in ((i(3), i(2), torch.zeros(2, 4, dtype=torch.int32)), (i(2), i(2), torch.zeros(3, 4, dtype=torch.int32)),
                  (i(2).long(), i(2), torch.zeros(2, 4, dtype=torch.int32)), (i(2), i(2), torch.zeros(2, 4, dtype=torch.int32))):
         with pytest.raises(ValueError):                     # shapes, types, and at last the device
