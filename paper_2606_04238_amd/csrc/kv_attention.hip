@@ -22,6 +22,7 @@
 
 #include "decode_launch.h"
 #include "kv_device.h"
+#include "kv_window.h"
 
 namespace qmlp {
 namespace {
@@ -86,10 +87,7 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 4, col = lane & 15;
     const int lg = a.cache.page_log2, Hk = a.cache.heads;
 
-    auto first_step = [&](const Request& q) {             // the first token any row sees, in steps
-        const int p = q.len - q.n - a.window + 1;
-        return a.window && p > 0 ? p / kStep : 0;
-    };
+    auto first_step = [&](const Request& q) { return first_seen(q.len - q.n, a.window) / kStep; };      // of the first row, in steps
     auto tiles_of = [&](const Request& q) {
         const long rows = (long)q.n * a.G;
         return rows > limit ? 0 : (int)((rows + kRows - 1) / kRows);
@@ -123,10 +121,10 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
         const int rows = min((int)min((long)q.n * a.G, (long)INT32_MAX) - tile * kRows, kRows);
         const int row = tile * kRows + col, tok = row / a.G;
         const int pos = col < rows ? q.len - q.n + tok : -1;
-        const int low = a.window ? max(0, pos - a.window + 1) : 0;
+        const int low = first_seen(pos, a.window);
         // tokens that every row of the tile sees
         const int all_hi = q.len - q.n + tile * kRows / a.G;
-        const int all_lo = a.window ? q.len - q.n + (tile * kRows + rows - 1) / a.G - a.window + 1 : 0;
+        const int all_lo = first_seen(q.len - q.n + (tile * kRows + rows - 1) / a.G, a.window);
 
         // q as the second operand: lane's row, dims (D/4) h ..
         uint4 qv[D / 32];

@@ -22,6 +22,7 @@
 
 #include "decode_launch.h"
 #include "kv_device.h"
+#include "kv_window.h"
 
 namespace qmlp {
 namespace {
@@ -114,7 +115,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     tile = tiles_of(q) - 1 - tile;
     const int rows = min((int)((long)q.n * a.G - (long)tile * kTileRows), kTileRows);
     const int first = q.len - q.n + tile * kTileRows / a.G, last = q.len - q.n + (tile * kTileRows + rows - 1) / a.G;   // positions
-    const int low0 = a.window ? max(0, first - a.window + 1) / kTokens : 0;
+    const int low0 = first_seen(first, a.window) / kTokens;
     const int all = max(0, last / kTokens + 1 - low0);    // steps of the tile (last < 0: none)
     // (at least four steps a share: joining costs about as much)
     const int own = min(shares, max(1, all / 4));
@@ -128,7 +129,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     const int wlast = wrows > 0 ? q.len - q.n + (tile * kTileRows + wave * 32 + wrows - 1) / a.G : -1;
     const int r = wave * 32 + col, row = tile * kTileRows + r, tok = row / a.G;
     const int pos = r < rows ? q.len - q.n + tok : -1;
-    const int low = a.window ? max(0, pos - a.window + 1) : 0;
+    const int low = first_seen(pos, a.window);
     uint4 qv[KS];
     {
         const uint16_t* src = a.q + (long)(q.row0 + tok) * a.ldq + ((long)head * a.G + row % a.G) * D + h * 8;
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
         const St& s = *reinterpret_cast<const St*>(smem + now);
         const uint4 aw = *reinterpret_cast<const uint4*>(s.away), aw2 = *reinterpret_cast<const uint4*>(s.away + 4);
         const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w | aw2.x | aw2.y | aw2.z | aw2.w) == 0 &&
-                                                         t + kTokens - 1 <= wfirst && (!a.window || t > wlast - a.window));
+                                                         t + kTokens - 1 <= wfirst && t >= first_seen(wlast, a.window));
         section(std::integral_constant<int, 0>{}, t, full);
         __syncthreads();
         begin(1, false);

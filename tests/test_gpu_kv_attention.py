@@ -294,3 +294,26 @@ def test_steps_together(q, graph):
         # the newest tokens are in the cache where the plan put them
         rk, rv = q.kv_read(cache, p.slots[:n].contiguous(), dtype=BF16)
         assert (rv.float() - v[:n].float()).abs().max() <= 8.0 / 15 and rk.abs().max() > 0
+
+
+def tiles(q, cache, heads, new):
+    """Whether requests of this many new tokens go to the kernel for many rows (whose part of the workspace is larger)."""
+    size = lambda n: q.kv_attention_workspace_bytes(cache, heads, n)
+    return size(new) > size(0)
+
+
+@pytest.mark.parametrize("window", [2 ** 31 - 1, 2 ** 31 - 600, 1 << 30, 300, 5])
+@pytest.mark.parametrize("D,G", [(128, 4), (64, 8)])
+@pytest.mark.parametrize("many", [False, True])
+def test_windows_to_the_largest(q, many, D, G, window):
+    """Every window that an int holds, with more new tokens than cached ones (rows before the first position), as a plan
+    leaves a request that it refused."""
+    print("\n[case]", many, D, G, window, flush=True)
+    cache, x, table, lens, starts = make(q, [(60, 60), (50, 40), (200, 45), (500, 500)], 1, G, D, 16, BF16)
+    lens[0], lens[1], lens[3] = 0, 7, 90
+    most = 500 if many else 1
+    assert tiles(q, cache, G, 40) and not tiles(q, cache, G, 1)
+    y = go(q, cache, x, table, lens, starts, BF16, window=window, max_new=most)
+    assert not y[:60].any() and not y[60:93].any() and y[93:100].any()
+    if window >= 300:
+        assert torch.equal(y, go(q, cache, x, table, lens, starts, BF16, max_new=most))
