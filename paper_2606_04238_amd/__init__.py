@@ -707,6 +707,12 @@ def moe_layer(moe: MoE, x: torch.Tensor, y: torch.Tensor | None = None, ws: torc
     return y
 
 
+def _kept(obj, last, why):
+    """Refuses to change an object whose tensors' addresses have been taken (`last` is set last, when they have)."""
+    if hasattr(obj, last):
+        raise AttributeError(why)
+
+
 class KVCache:
     """A paged cache of keys and values in 4 bits: ``data`` uint8 [pages][kv_heads][2][page * (head_dim/2 + 4)] on the
     device (the storage format of qmlp_kv_cache; kv_cache makes an empty one)."""
@@ -722,6 +728,13 @@ class KVCache:
             raise QmlpError(4, "KVCache")
         self._c = KVCacheC(data.data_ptr(), self.pages, self.kv_heads, self.head_dim, self.page)
         self._at = ctypes.addressof(self._c)
+
+    def __setattr__(self, name, value):
+        _kept(self, "_at", "a cache keeps its tensor (its contents change)")
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError("a cache keeps its tensor (its contents change)")
 
     def c(self) -> KVCacheC:
         return self._c
@@ -777,9 +790,11 @@ class KVPlan:
         self._out = tuple(v.data_ptr() for v in t)
 
     def __setattr__(self, name, value):
-        if hasattr(self, "_out"):
-            raise AttributeError("a plan keeps its tensors (their contents change)")
+        _kept(self, "_out", "a plan keeps its tensors (their contents change)")
         super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        raise AttributeError("a plan keeps its tensors (their contents change)")
 
 
 def kv_plan(plan: KVPlan, lens: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free: torch.Tensor,

@@ -210,3 +210,18 @@ def test_the_plain_forms(q):
     assert r["slots"] == [7 * 16, 3 * 16 + 8, -1] and r["positions"] == [16, 40, 0] and r["starts"] == [0, 1, 1, 2] and r["lens"] == [17, 0, 41]
     r = plan([16, 16, 5], [1, 20, 1], [[4, 0, 0], [7, 0, 0], [1, 2, 3]], [9, 8], 2, 16, 30)
     assert r["short"] == [1] and r["lens"] == [17, 16, 6] and r["n_free"] == [1]
+
+
+def test_a_cache_keeps_its_tensor(q):
+    """The kernels hold the address: another tensor cannot take its place, and another size neither."""
+    data = torch.zeros(3, 2, 2, 64 * 68, dtype=torch.uint8)
+    c = q.KVCache(data, 64)
+    for name, v in (("data", torch.zeros_like(data)), ("page", 16), ("pages", 2), ("kv_heads", 1), ("head_dim", 64)):
+        with pytest.raises(AttributeError):
+            setattr(c, name, v)
+    with pytest.raises(AttributeError):
+        del c.data
+    assert c.data is data and c.c().data == data.data_ptr() and c.page == 64
+    data.fill_(1)                                           # the contents are the caller's
+    with pytest.raises(AttributeError):
+        del q.KVPlan(2, 4, device="cpu").slots
