@@ -224,33 +224,38 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
                     }
                 }
                 float w[8], sum, top;
-                auto weigh = [&] {
+                auto weigh = [&](auto raw) {                  // x as it is, or already times the scale
                     sum = 0.0f;
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const float e = exp2_(__builtin_fmaf(x[k], scale, -m));
+                        const float e = exp2_(decltype(raw)::value ? __builtin_fmaf(x[k], scale, -m) : x[k] - m);
                         w[k] = fma_lo(sv[k], e, 0.0f);
                         sum += e;
                     }
                     top = fmaxf(fmaxf(fmaxf(w[0], w[1]), fmaxf(w[2], w[3])), fmaxf(fmaxf(w[4], w[5]), fmaxf(w[6], w[7])));
                 };
-                weigh();
+                weigh(std::true_type{});
                 // (a scale of 0, as in an empty cache, hides a large weight from the first test)
                 if (__ballot(top > kTop || sum > 8.0f * kTop * kLeast)) {
-                    float best = kNone;
+                    float best = kNone, most = kNone;
 #pragma unroll
-                    for (int k = 0; k < 8; ++k)
-                        best = fmaxf(best, __builtin_fmaf(x[k], scale, log2_(fmaxf(h2f(sv[k] & 0xFFFFu), 1.0f / kLeast))));
+                    for (int k = 0; k < 8; ++k) {
+                        x[k] = rounded(x[k] * scale);
+                        most = fmaxf(most, x[k]);
+                        best = fmaxf(best, x[k] + log2_(fmaxf(h2f(sv[k] & 0xFFFFu), 1.0f / kLeast)));
+                    }
+                    most = fmaxf(most, __shfl_xor(most, 16, 64));
+                    most = fmaxf(most, __shfl_xor(most, 32, 64));
                     best = fmaxf(best, __shfl_xor(best, 16, 64));
                     best = fmaxf(best, __shfl_xor(best, 32, 64));
-                    const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
+                    const float mn = shifted(m, most, best), f = exp2_(m - mn);
                     m = mn;
                     l *= f;
                     oz *= f;
 #pragma unroll
                     for (int d = 0; d < NT; ++d)
                         o[d] *= f;
-                    weigh();
+                    weigh(std::false_type{});
                 }
                 l += sum;
                 const uint4 p = make_uint4(pack2(w[0], w[1]), pack2(w[2], w[3]), pack2(w[4], w[5]), pack2(w[6], w[7]));

@@ -363,22 +363,24 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
             for (int e = 0; e < 16; ++e) {
                 const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3), n = t + at;
                 const float k1 = s.sk[at];
-                xj[e] = n <= pos && n >= low && k1 != INFINITY ? xj[e] * k1 : -INFINITY;
+                xj[e] = n <= pos && n >= low && k1 != INFINITY ? rounded(xj[e] * k1) : -INFINITY;
             }
             weigh();
         }
         // (a weight that passes binary16 is infinite there)
         if (__ballot(h2f(top & 0xFFFFu) > kTop || h2f(top >> 16) > kTop || sum > 16.0f * kTop * kLeast)) {
-            float best = kNone;
+            float best = kNone, most = kNone;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3);
                 if (full)
-                    xj[e] *= s.sk[at];
+                    xj[e] = rounded(xj[e] * s.sk[at]);
+                most = fmaxf(most, xj[e]);
                 best = fmaxf(best, xj[e] + log2_(fmaxf(s.sv[at], 1.0f / kLeast)));
             }
+            most = fmaxf(most, __shfl_xor(most, 32, 64));
             best = fmaxf(best, __shfl_xor(best, 32, 64));
-            const float mn = fmaxf(m, best - kReset), f = exp2_(m - mn);
+            const float mn = shifted(m, most, best), f = exp2_(m - mn);
             m = mn;
             l *= f;
 #pragma unroll

@@ -17,9 +17,10 @@ typedef float f32x16_t __attribute__((ext_vector_type(16)));
 typedef float f32x2_t __attribute__((ext_vector_type(2)));
 typedef __amdgpu_buffer_rsrc_t Rsrc;
 
-constexpr float kNone = -1e30f;                           // a maximum before any score
+constexpr float kNone = -3.4028235e38f;                   // a maximum before any score: none is lower
 constexpr float kTop = 32768.0f, kReset = 8.0f;           // weights in binary16: at most 2^15, 2^8 where the maximum is taken anew
 constexpr float kLeast = 16777216.0f;                     // 1 / the least scale (a scale of 0, as in an empty cache, counts as that for the maximum)
+constexpr float kFar = 1048576.0f;                        // scores past 2^20: see shifted()
 constexpr int kDevice = 16;                               // device-coherent (sc1): read or written by other compute units
 
 __device__ __forceinline__ f32x4_t mfma16(const uint4& a, const uint4& b, f32x4_t c) {
@@ -83,6 +84,19 @@ __device__ __forceinline__ void three_bf16(float v, uint32_t (&p)[3]) {
         p[i] = (uint32_t)__builtin_bit_cast(uint16_t, (__bf16)v);
         v -= __uint_as_float(p[i] << 16);
     }
+}
+
+// The maximum taken anew from a row's scores (rounded to fp32): most, the largest, and best, the largest with its value's scale
+// added as a power of two.  It leaves 2^kReset to the best; past 2^20 an fp32 number cannot carry that difference (its
+// neighbours are up to 2^104 away), so there the largest score itself weighs 1, and no weight times a scale passes 65504.
+__device__ __forceinline__ float shifted(float m, float most, float best) {
+    return fmaxf(m, __builtin_fabsf(most) > kFar ? most : best - kReset);
+}
+
+// A product is rounded here: not joined with the sum it goes into.
+__device__ __forceinline__ float rounded(float v) {
+    __asm__ volatile("" : "+v"(v));
+    return v;
 }
 
 // One request of a call.

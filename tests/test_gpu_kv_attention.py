@@ -3,7 +3,7 @@ import numpy as np
 import pytest
 import torch
 
-from kv_testutil import attention, check, f64
+from kv_testutil import HALF, attention, check, decode, f64
 
 pytestmark = pytest.mark.gpu
 F16, BF16 = torch.float16, torch.bfloat16
@@ -317,3 +317,49 @@ def test_windows_to_the_largest(q, many, D, G, window):
     assert not y[:60].any() and not y[60:93].any() and y[93:100].any()
     if window >= 300:
         assert torch.equal(y, go(q, cache, x, table, lens, starts, BF16, max_new=most))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D,G", [(128, 8), (64, 20)])
+@pytest.mark.parametrize("new", [1, 20])
+def test_scores_that_fp32_cannot_shift(q, new, D, G, dtype):
+    """Scores up to about 2^33, where the neighbours of an fp32 number are 2^10 away: rows whose largest score leads by more
+    than scores are off give its token's value (one rounding; the weight times the value's scale 2^-11, sums and quotient 16 2^-24)."""
+    print("\n[case]", new, D, G, dtype, flush=True)
+    cache, x, table, lens, starts = make(q, [(300, new), (77, new)], 1, G, D, 16, dtype)
+    assert tiles(q, cache, G, new) == (new > 1)
+    data = cache.data.cpu().numpy()
+    ref = lambda scale: attention(f64(x), data, 16, table.cpu().numpy(), lens.tolist(), starts.tolist(), scale, 0, None, dtype)[0]
+    K, _, _, _ = decode(data, 16)
+    for e in range(8, 28):
+        scale = 2.0 ** e
+        y = q.kv_attention(x, cache, table, lens, starts, max_new=new, scale=scale)
+        torch.cuda.synchronize()
+        want, sure = ref(scale), np.zeros((x.shape[0], G), bool)
+        for b in range(2):
+            n = int(lens[b])
+            k = np.stack([K[int(table[b, j // 16]), 0, j % 16] for j in range(n)])
+            for i in range(new):
+                s = np.sort(scale * (f64(x)[int(starts[b]) + i] @ k[:n - new + i + 1].T), 1)[:, -2:]
+                # each score is off by less than 2^-18 of its terms, which are below 40 times it here
+                sure[int(starts[b]) + i] = s[:, 1] - s[:, 0] > 64 + 2.0 ** -12 * np.abs(s[:, 1])
+        assert sure.mean() > 0.5 or e < 10
+        tol = (HALF[dtype] + 2.0 ** -11 + 16 * 2.0 ** -24) * np.abs(want) + 2.0 ** -24
+        bad = ~(np.abs(f64(y) - want) <= tol)
+        assert np.isfinite(f64(y)).all() and not bad[sure].any(), (e, np.isfinite(f64(y)).all(), bad[sure].mean())
+
+
+@pytest.mark.parametrize("most", [1, 40])
+def test_scores_below_all_others(q, most):
+    """One token, or many alike, at -1e37 to -1e5: what a row sees has its weight, however far below 0."""
+    cache, x, table, lens, starts = make(q, [(40, 40), (1, 1)], 1, 4, 64, 16, BF16)
+    one = torch.full((41, 1, 64), 0.75, dtype=BF16).cuda()
+    slots = i32([int(table[0, j // 16]) * 16 + j % 16 for j in range(40)] + [int(table[1, 0]) * 16])
+    v = torch.full_like(one, 0.5)
+    q.qk_norm_rope(None, one, cache=cache, v=v, slots=slots)
+    _, held = q.kv_read(cache, slots[:1].contiguous(), dtype=BF16)
+    for size in (1e5, 1e20, 1e29, 1e31, 1e34, 1e36):
+        y = q.kv_attention(torch.full_like(x, -size), cache, table, lens, starts, max_new=most, scale=0.25)
+        torch.cuda.synchronize()
+        # equal values: their mean is the value, weights and sums of equal numbers to 2^-11 and 2^-18
+        assert ((y.float() - held.float()).abs() <= (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -18) * 0.5).all(), size
