@@ -654,6 +654,8 @@ qmlp_status qmlp_kv_read(const qmlp_kv_cache *cache, const int32_t *slots, int T
  * Codes enter the products as exact integers; scores, sums and outputs are fp32; weights times the
  * value's scale are rounded to binary16, with a power of two that keeps 2^-22 of the largest normal (where a row's largest score
  * passes 2^20 in size, it weighs 1).  Scores past fp32 make their rows NaN (zeros, where all of a row's are -infinity).
+ * bfloat16 queries enter them as binary16 times a power of two: a number of a row loses at most 2^-27 of the row's
+ * largest, whatever the other rows hold.
  * Keys or values that are NaN, and rows of q with an infinity or NaN, make the rows that
  * see them NaN and no others.
  * max_new: the most new tokens of any request, as far as the host knows.  It chooses kernels and sizes

@@ -172,7 +172,10 @@ __global__ void __launch_bounds__(256, 2) few_kernel(AttnArgs a, int limit) {
         float scale = a.scale * operand_rows(qv, a.bf, qsum, quarters, [](uint32_t v) {
             v |= __shfl_xor(v, 16, 64);
             return v | (uint32_t)__shfl_xor((int)v, 32, 64);
-        }, [](uint32_t top) { return top; });
+        }, [](uint32_t top) {                             // each row a power of its own
+            top = max(top, (uint32_t)__shfl_xor((int)top, 16, 64));
+            return max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+        });
 
         // minus the row's sum, in the places of the first quarter
         uint32_t part3[3];

@@ -28,6 +28,7 @@ namespace qmlp {
 namespace {
 
 constexpr int kWaves = 8, kTileRows = 32 * kWaves, kThreads = 64 * kWaves, kMostShares = 16;
+constexpr uint32_t kApart = 12;                           // powers of two
 constexpr int kJoin = 8;                                  // parts under way where they are joined
 
 template <int D>
@@ -44,7 +45,8 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
     constexpr int KS = D / 16, DT = D / 32, kTokens = Stage<D>::tokens, TJ = kTokens / 32;
     using St = Stage<D>;
     extern __shared__ __attribute__((aligned(16))) uint8_t smem[];
-    __shared__ uint32_t arrived, tops[kWaves];
+    __shared__ uint32_t arrived, tops[kWaves], leasts[kWaves];
+    __shared__ float backs[kTileRows];                    // of each row, where they differ: its power's inverse
     Stage<D>* stage = reinterpret_cast<Stage<D>*>(smem);
     Known<int32_t>* known = reinterpret_cast<Known<int32_t>*>(smem + 3 * sizeof(Stage<D>));
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), h = lane >> 5, col = lane & 31;
@@ -228,18 +230,31 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
             load_pages(i0 + 1);
     }
     float qsum;
-    scale = a.scale * operand_rows(qv, a.bf, qsum, [](float v) { return v + __shfl_xor(v, 32, 64); },
-                                   [](uint32_t v) { return v | (uint32_t)__shfl_xor((int)v, 32, 64); },
-                                   [&](uint32_t top) {
-                                       // one power of two for the workgroup
-                                       if (lane == 0)
-                                           tops[wave] = top;
-                                       __syncthreads();
-                                       #pragma unroll
-                                       for (int w = 0; w < kWaves; ++w)
-                                           top = max(top, tops[w]);
-                                       return top;
-                                   });
+    // One power of two for the workgroup's rows, which the scales of keys take along, unless a row's largest number is below 2^-kApart
+    // of the others'.  Then each row has its own, and every step goes the way of partly seen ones, which multiplies by it: what a
+    // row shares loses below 2^-(39 - kApart) of its largest number, less than an fp32 sum does.
+    bool apart = false;
+    const float back = operand_rows(qv, a.bf, qsum, [](float v) { return v + __shfl_xor(v, 32, 64); },
+                                    [](uint32_t v) { return v | (uint32_t)__shfl_xor((int)v, 32, 64); },
+                                    [&](uint32_t top) {
+                                        top = max(top, (uint32_t)__shfl_xor((int)top, 32, 64));
+                                        uint32_t most = wave_max(top), least = ~wave_max(top ? ~top : 0u);      // (no row of zeros)
+                                        if (lane == 0) {
+                                            tops[wave] = most;
+                                            leasts[wave] = least;
+                                        }
+                                        __syncthreads();
+#pragma unroll
+                                        for (int w = 0; w < kWaves; ++w) {
+                                            most = max(most, tops[w]);
+                                            least = min(least, leasts[w]);
+                                        }
+                                        apart = __builtin_amdgcn_readfirstlane(least < most && (most >> 7) - (least >> 7) > kApart);
+                                        return apart ? top : most;
+                                    });
+    if (apart && h == 0)
+        backs[r] = back;                                  // (read by this wave alone)
+    scale = apart ? a.scale : a.scale * back;
     const bool bad = qsum != qsum;                        // an infinity or NaN in the row
 
     // Three stages: at step i the matrix cores read stages i and i + 1 and, in the step's first turns, i - 1, whose
@@ -359,11 +374,12 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
             begin((j + 1) % TJ, j + 1 == TJ);
         if (!full) {
             // what a row does not see weighs nothing, whatever lies there
+            const float back = apart ? backs[r] : 1.0f;
 #pragma unroll
             for (int e = 0; e < 16; ++e) {
                 const int at = 32 * j + 8 * (e >> 2) + 4 * h + (e & 3), n = t + at;
                 const float k1 = s.sk[at];
-                xj[e] = n <= pos && n >= low && k1 != INFINITY ? rounded(xj[e] * k1) : -INFINITY;
+                xj[e] = n <= pos && n >= low && k1 != INFINITY ? rounded(xj[e] * k1 * back) : -INFINITY;
             }
             weigh();
         }
@@ -414,7 +430,7 @@ __global__ void __launch_bounds__(kThreads, 2) rows_kernel(AttnArgs a, int limit
         const int t = i * kTokens;
         const St& s = *reinterpret_cast<const St*>(smem + now);
         const uint4 aw = *reinterpret_cast<const uint4*>(s.away), aw2 = *reinterpret_cast<const uint4*>(s.away + 4);
-        const bool full = __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w | aw2.x | aw2.y | aw2.z | aw2.w) == 0 &&
+        const bool full = !apart && __builtin_amdgcn_readfirstlane((aw.x | aw.y | aw.z | aw.w | aw2.x | aw2.y | aw2.z | aw2.w) == 0 &&
                                                          t + kTokens - 1 <= wfirst && t >= first_seen(wlast, a.window));
         section(std::integral_constant<int, 0>{}, t, full);
         __syncthreads();

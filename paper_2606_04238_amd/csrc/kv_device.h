@@ -119,12 +119,12 @@ __device__ __forceinline__ Request request(const AttnArgs& a, int b) {
 }
 
 // A wave's rows of q as operands: `n` 16-byte pieces a lane, all of a lane's from one row, whose other pieces are
-// with the lanes that `over_row` and `or_row` join.  bfloat16 is rewritten as binary16 times a power of two common to the
-// waves that `widest` joins, which puts its largest finite number into [2^14, 2^15): 8 significant bits fit the 11, and what falls below
-// 2^-14 then is below 2^-28 of the wave's largest.  A row with an infinity or NaN becomes zeros, and its sum NaN.
+// with the lanes that `over_row` and `or_row` join.  bfloat16 is rewritten as binary16 times a power of two which puts the number
+// that `largest` makes of the lane's largest (of its row, or of several rows) into [2^14, 2^15): 8 significant bits fit the 11,
+// and what that cannot hold is below 2^-31 of that number.  A row with an infinity or NaN becomes zeros, and its sum NaN.
 // Returns the power's inverse; sum: of the row as it is now.
-template <int N, typename Over, typename OverOr, typename Wide>
-__device__ __forceinline__ float operand_rows(uint4 (&v)[N], bool bf, float& sum, Over over_row, OverOr or_row, Wide widest) {
+template <int N, typename Over, typename OverOr, typename Largest>
+__device__ __forceinline__ float operand_rows(uint4 (&v)[N], bool bf, float& sum, Over over_row, OverOr or_row, Largest largest) {
     const uint32_t ebits = bf ? 0x7F80u : 0x7C00u;
     uint32_t bad = 0, top = 0;
 #pragma unroll
@@ -144,7 +144,7 @@ __device__ __forceinline__ float operand_rows(uint4 (&v)[N], bool bf, float& sum
     }
     float back = 1.0f;
     if (bf) {
-        top = widest(wave_max(top));
+        top = largest(top);
         const int e = (int)(top >> 7);                    // biased by 127
         const int k = top == 0 ? 0 : min(14 + 127 - max(e, 1), 126);
         const float up = __uint_as_float((uint32_t)(k + 127) << 23);

@@ -363,3 +363,17 @@ def test_scores_below_all_others(q, most):
         torch.cuda.synchronize()
         # equal values: their mean is the value, weights and sums of equal numbers to 2^-11 and 2^-18
         assert ((y.float() - held.float()).abs() <= (2.0 ** -8 + 2.0 ** -11 + 2.0 ** -18) * 0.5).all(), size
+
+
+@pytest.mark.parametrize("most", [1, 40])
+@pytest.mark.parametrize("D,G", [(128, 4), (64, 5)])
+def test_rows_of_very_different_size(q, D, G, most):
+    """bfloat16 rows of q from 2^-100 to 2^20 of each other beside ordinary ones keep their bits."""
+    print("\n[case]", D, G, most, flush=True)
+    g = torch.Generator().manual_seed(23)
+    cache, x, table, lens, starts = make(q, [(300, 40), (100, 1), (90, 33)], 1, G, D, 16, BF16)
+    assert tiles(q, cache, G, 40)
+    for low, high, scale in ((0, 20, 2.0 ** -20), (-100, 0, 1.0), (-60, 20, 2.0 ** 10), (-14, 0, 2.0 ** 6)):
+        far = 2.0 ** torch.randint(low, high + 1, (x.shape[0], G, 1), generator=g).double().cuda()
+        z = (x.double() * far).to(BF16)
+        go(q, cache, z, table, lens, starts, BF16, scale=scale, max_new=most)
