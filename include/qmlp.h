@@ -610,8 +610,9 @@ typedef enum { QMLP_PAIRS_HALF = 0, QMLP_PAIRS_NEXT = 1 } qmlp_pairs;
  * are quantized from the activation type and written there.  q, k and v are
  * rows ldq, ldk, ldv elements apart with their heads side by side (views of one
  * q/k/v row, for instance).  q_out may be q and k_out may be k, at the same
- * address and stride; otherwise outputs overlap nothing.  q arithmetic is fp32 and k's fp64 (a code
- * hangs on the last bits of numbers next to a border), angles are reduced in fp64.
+ * address and stride; otherwise outputs overlap nothing.  q arithmetic is fp32 (fp64 for heads whose
+ * mean square leaves 2^-100 .. 2^120) and k's fp64 (a code hangs on the last bits of numbers next to a border), angles are
+ * reduced in fp64.
  */
 typedef struct {
     const void *q, *k, *v;              /* [T][heads or kv_heads][head_dim], 16-byte aligned; v only with a cache */

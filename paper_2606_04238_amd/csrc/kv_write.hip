@@ -81,9 +81,10 @@ __device__ __forceinline__ void store_codes(const KvView& c, int slot, int head,
         reinterpret_cast<uint32_t*>(base + ((size_t)(D / 2) << lg))[o] = meta;
 }
 
-// One head: norm and rotation of a lane's 8 numbers in F.  `turn`: (cos, sin) of each pair, scaled.
+// One head: norm and rotation of a lane's 8 numbers in F.  `turn`: (cos, sin) of each pair, scaled.  `far` (fp32): the squares
+// pass fp32 on either side (bfloat16 numbers of 2^60, or with eps 0 of 2^-50), and the result does not count.
 template <int D, bool BF, typename F, typename P>
-__device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, const uint16_t* weight, const P* turn, int lane) {
+__device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, const uint16_t* weight, const P* turn, int lane, bool& far) {
     constexpr int LPH = D / 8;
     F x[8], p[8];
 #pragma unroll
@@ -97,10 +98,12 @@ __device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, con
             s += x[i] * x[i];
         s = over_head<LPH>(s, [](F u, F v) { return u + v; });
         const F m = s / (F)D + (F)a.eps;
-        if constexpr (std::is_same<F, double>::value)
+        if constexpr (std::is_same<F, double>::value) {
             inv = 1.0 / __builtin_sqrt(m);
-        else
+        } else {
             inv = 1.0f / __builtin_sqrtf(m);
+            far = !(m >= 0x1p-100f && m <= 0x1p120f);
+        }
         const uint4 w = reinterpret_cast<const uint4*>(weight)[lane];
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -183,16 +186,19 @@ __global__ void __launch_bounds__(256, 5) qk_kernel(HeadsArgs a) {
         const int side = g < a.Hq ? 0 : g < a.Hq + kv ? 1 : 2, h = g - (side == 0 ? 0 : side == 1 ? a.Hq : a.Hq + kv);
         const uint16_t* src = side == 0 ? a.q + t * a.ldq : side == 1 ? a.k + t * a.ldk : a.v + t * a.ldv;
         uint4 v = reinterpret_cast<const uint4*>(src + (long)h * D)[lane];
+        bool far = false;
+        uint4 u = v;
+        if (side == 0)
+            u = turned<D, BF, float>(a, v, a.qw, turn32, lane, far);
+        if (side == 1 || far)
+            u = turned<D, BF, double>(a, v, side == 0 ? a.qw : a.kw, turn64, lane, far);
         if (side == 0) {
-            v = turned<D, BF, float>(a, v, a.qw, turn32, lane);
-            reinterpret_cast<uint4*>(a.q_out + t * a.ldqo + (long)h * D)[lane] = v;
+            reinterpret_cast<uint4*>(a.q_out + t * a.ldqo + (long)h * D)[lane] = u;
             continue;
         }
-        if (side == 1) {
-            v = turned<D, BF, double>(a, v, a.kw, turn64, lane);
-            if (a.k_out)
-                reinterpret_cast<uint4*>(a.k_out + t * a.ldko + (long)h * D)[lane] = v;
-        }
+        v = u;
+        if (side == 1 && a.k_out)
+            reinterpret_cast<uint4*>(a.k_out + t * a.ldko + (long)h * D)[lane] = v;
         if (slot >= 0) {
             float x[8];
             unpacked<BF>(v, x);

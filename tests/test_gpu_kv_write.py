@@ -147,3 +147,18 @@ def test_a_row_of_nan_keeps_to_itself(q):
     assert torch.isnan(y2[3, 1]).all()
     y2[3, 1] = y[3, 1]
     assert torch.equal(y, y2)
+
+
+@pytest.mark.parametrize("D,rot,pairs", [(128, 128, "half"), (64, 32, "next")])
+def test_norms_of_far_sizes(q, D, rot, pairs):
+    """bfloat16 heads whose squares leave fp32 on either side, beside ordinary heads of the same tokens; one large number in a head."""
+    x, k, v, (qw, kw), pos, inv = make(40, 6, 2, D, BF16, True, rot, 5000)
+    for eps, sizes in ((1e-6, (1.0, 1e12, 3e18, 1e25, 1e37, 1e-4)), (0.0, (1.0, 1e-15, 1e-20, 1e-25, 1e-36, 1e25))):
+        z = (x.float() * torch.tensor(sizes).cuda()[:, None]).to(BF16)
+        z[7, 1, 3], z[8, 2, 5] = 3e38, -2e19
+        kz = (k.float() * torch.tensor([1e25, 1e-25]).cuda()[:, None]).to(BF16)
+        y, ko = q.qk_norm_rope(z, kz, pos, inv, qw, kw, eps=eps, pairs=pairs)
+        torch.cuda.synchronize()
+        p, i = pos.cpu().numpy(), inv.cpu().numpy()
+        near(y, turned(f64(z), f64(qw), p, i, eps, pairs, 1.0), BF16, D)
+        near(ko, turned(f64(kz), f64(kw), p, i, eps, pairs, 1.0), BF16, D)
