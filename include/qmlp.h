@@ -573,7 +573,7 @@ size_t qmlp_kv_cache_bytes(int pages, int kv_heads, int head_dim, int page);
  * starts [B+1]: the first token of each request among the step's, the sums of
  * the new tokens (refused ones too, ended ones none; at most 2^31 - 1).  positions and
  * slots [tokens]: place in its request and slot of every token; slot -1 for
- * the tokens of refused requests; past the last token position 0, slot -1.
+ * the tokens of refused requests and of pages whose slots are not in [0, 2^31); past the last token position 0, slot -1.
  * lens_out [B]: lens + new, lens for a refused request, 0 for an ended one.
  * n_free_out[0]; short_out[0]: requests refused.  lens_out may be lens and
  * n_free_out may be n_free (a chain of steps); otherwise no two arrays overlap.

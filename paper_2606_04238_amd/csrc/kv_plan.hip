@@ -146,8 +146,11 @@ __global__ void __launch_bounds__(NT) kv_plan_kernel(PlanArgs a) {
             const int b = find(begin, a.B, i);
             const int64_t at64 = (int64_t)len[b] + i - begin[b];
             pos = (int)min(at64, (int64_t)INT32_MAX);
-            if (served[b])
-                slot = (a.table[(long)b * a.W + (pos >> lg)] << lg) | (pos & (page - 1));
+            if (served[b]) {
+                const int p = a.table[(long)b * a.W + (pos >> lg)];
+                if (p >= 0 && p <= INT32_MAX >> lg)       // (another one's slots are not numbers of 31 bits)
+                    slot = (p << lg) | (pos & (page - 1));
+            }
         }
         a.slots[i] = slot;
         a.positions[i] = pos;

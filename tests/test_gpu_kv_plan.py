@@ -103,3 +103,12 @@ def test_a_chain_in_place_and_a_graph(q):
             R = plan_ref(R["lens"], add, R["table"], R["free"], R["n_free"][0], page, 40)
             assert lens.tolist() == R["lens"] and nf.tolist() == R["n_free"] and p.slots.tolist() == R["slots"], i
             assert table.tolist() == R["table"] and free.tolist() == R["free"] and p.short.tolist() == R["short"], i
+
+
+def test_pages_past_the_last_slot(q):
+    """A page number whose slots would pass 2^31 (or below 0) has none: slot -1, as for a refused request."""
+    for page, last in ((16, 2 ** 27 - 1), (64, 2 ** 25 - 1), (256, 2 ** 23 - 1)):
+        table = [[last, 0], [last + 1, 0], [2 * last + 2, 0], [-3, 0], [2 ** 31 - 1, 0], [7, 0]]
+        got = run(q, [5] * 6, [2] * 6, table, [0], 0, page, 12)
+        assert got["slots"] == [last * page + 5, last * page + 6, -1, -1, -1, -1, -1, -1, -1, -1, 7 * page + 5, 7 * page + 6], page
+        assert got["lens"] == [7] * 6 and got["short"] == [0]
