@@ -377,3 +377,127 @@ def test_rows_of_very_different_size(q, D, G, most):
         far = 2.0 ** torch.randint(low, high + 1, (x.shape[0], G, 1), generator=g).double().cuda()
         z = (x.double() * far).to(BF16)
         go(q, cache, z, table, lens, starts, BF16, scale=scale, max_new=most)
+
+
+def parts(q, cache, heads, total, new, most):
+    """Workgroups that share each tile of 256 rows of a lone request without a window, in the kernel for many rows."""
+    assert tiles(q, cache, heads, new) and tiles(q, cache, heads, most)
+    items = -(-new * heads // cache.kv_heads // 256) * cache.kv_heads
+    shares = min(max(torch.cuda.get_device_properties(0).multi_processor_count // items, 1), 16)
+    step = 8192 // cache.head_dim
+    return [min(shares, max(1, ((total - new + min(256 * (i + 1) // (heads // cache.kv_heads), new) - 1) // step + 1) // 4))
+            for i in range(items // cache.kv_heads)]
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D,total,new,G,Hk,want", [
+    (128, 700, 40, 4, 1, 2), (128, 1500, 17, 8, 2, 6), (128, 2400, 33, 4, 1, 9), (128, 4300, 40, 4, 1, 16), (128, 5000, 70, 8, 1, 16),
+    (64, 1200, 40, 4, 1, 2), (64, 4800, 35, 8, 1, 9), (64, 8400, 33, 4, 1, 16)])
+def test_many_rows_in_parts(q, D, total, new, G, Hk, want, dtype):
+    """Tiles of many rows shared by 2 to 16 workgroups (one and two rounds of the join), and the same again on a workspace
+    that calls of other shapes use in between."""
+    print("\n[case]", D, total, new, G, Hk, dtype, flush=True)
+    cache, x, table, lens, starts = make(q, [(total, new)], Hk, G, D, 64, dtype)
+    assert max(parts(q, cache, Hk * G, total, new, new)) == want
+    ws = q.kv_attention_workspace(x, cache, table, new)
+    y = go(q, cache, x, table, lens, starts, dtype, max_new=new, ws=ws)
+    for _ in range(3):
+        for one in (i32([total - 31]), i32([5 * total // 8])):
+            q.kv_attention(x[:1].contiguous(), cache, table, one, max_new=1, ws=ws)
+        q.kv_attention(x[:20].contiguous(), cache, table, i32([total // 2]), i32([0, 20]), max_new=new, ws=ws)
+        z = q.kv_attention(x, cache, table, lens, starts, max_new=new, ws=ws)
+        torch.cuda.synchronize()
+        assert torch.equal(y, z)
+
+
+@pytest.mark.parametrize("D,total", [(128, 2700), (64, 5200)])
+def test_many_rows_in_parts_windows_and_sinks(q, D, total):
+    """Parts that begin at a window's start, holes and sinks."""
+    new, G = 45, 4
+    cache, x, table, lens, starts = make(q, [(total, new)], 1, G, D, 64, BF16)
+    assert max(parts(q, cache, G, total, new, new)) >= 10
+    sinks = torch.tensor([0.5, -2.0, 9.0, float("-inf")]).cuda()
+    for window in (0, total // 2 + 3, total - 50, total - 40):
+        go(q, cache, x, table, lens, starts, BF16, window=window, sinks=sinks if window else None)
+    table[0, 5], table[0, total // 64 - 1] = -1, cache.pages
+    go(q, cache, x, table, lens, starts, BF16, sinks=sinks)
+
+
+@pytest.mark.parametrize("window", [1, 31, 64, 128, 1000])
+@pytest.mark.parametrize("D", [64, 128])
+def test_many_rows_windows_and_sinks_bf16(q, D, window):
+    print("\n[case]", D, window, flush=True)
+    cache, x, table, lens, starts = make(q, [(400, 150), (333, 40), (90, 90), (9, 1)], 2, 8, D, 16, BF16)
+    assert tiles(q, cache, 16, 40)
+    sinks = torch.cat([torch.linspace(-4, 4, 15), torch.tensor([float("-inf")])]).cuda()
+    for s in (None, sinks):
+        go(q, cache, x, table, lens, starts, BF16, window=window, sinks=s)
+
+
+@pytest.mark.parametrize("D,total,new", [(64, 60, 20), (128, 60, 20), (128, 900, 20), (64, 2100, 20)])
+def test_many_rows_bad_values_keep_to_their_rows(q, D, total, new):
+    """As test_bad_values_keep_to_their_rows, in the kernel for many rows; tiles in one part and in several."""
+    G, page = 8, 16
+    cache, x, table, lens, starts = make(q, [(total, new), (90, 1), (70, 18)], 1, G, D, page, F16)
+    assert tiles(q, cache, G, 18)
+    clean = go(q, cache, x, table, lens, starts, F16)
+    k = torch.ones(2, 1, D, dtype=F16).cuda()
+    k[0, 0, 3] = float("nan")
+    bad = total - 10
+    at = i32([int(table[0, bad // page]) * page + bad % page, int(table[2, 3]) * page + 7])
+    q.qk_norm_rope(None, k[:1].contiguous(), cache=cache, v=torch.ones_like(k[:1]), slots=at[:1].contiguous())        # a key
+    q.qk_norm_rope(None, k[1:].contiguous(), cache=cache, v=k[:1].contiguous(), slots=at[1:].contiguous())            # a value
+    n2 = int(starts[2])
+    x[3, 2, 5], x[n2, 0, 0], x[0, 7, D - 1] = float("inf"), float("nan"), float("-inf")
+    y = q.kv_attention(x, cache, table, lens, starts)
+    torch.cuda.synchronize()
+    nan = torch.isnan(y).all(2)
+    want = torch.zeros_like(nan)
+    want[new - 10:new] = True                               # positions from the key on
+    want[n2 + max(0, 55 - (70 - 18)):n2 + 18] = True
+    want[3, 2], want[n2, 0], want[0, 7] = True, True, True
+    assert torch.equal(nan, want) and not torch.isnan(y[~nan]).any()
+    keep = ~nan
+    keep[n2:n2 + 18] = False                                # (one token has another value there)
+    assert torch.equal(y[keep], clean[keep])
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("D,total", [(128, 300), (64, 300), (128, 1300)])
+def test_many_rows_ranges(q, D, total, dtype):
+    """As test_ranges, in the kernel for many rows; in one part and in several."""
+    g = torch.Generator().manual_seed(29)
+    new, G, page = 36, 4, 32
+    for spread, vmul, qmul in ((2.0, 1.0, 8.0), (0.1, 1e-4, 0.01), (0.5, 3000.0, 1.0)):
+        cache, x, table, lens, starts = make(q, [(total, new), (257, 1)], 1, G, D, page, dtype, spread=spread)
+        assert tiles(q, cache, G, new)
+        v = (torch.randn(total, 1, D, generator=g) * vmul * torch.exp(2 * torch.randn(total, 1, 1, generator=g))).clamp(-65000, 65000).to(dtype).cuda()
+        slots = i32([int(table[0, j // page]) * page + j % page for j in range(total)])
+        k, _ = q.kv_read(cache, slots, dtype=dtype)
+        q.qk_norm_rope(None, k, cache=cache, v=v, slots=slots)
+        x = (x.float() * qmul * 2.0 ** torch.randint(-6, 3, (x.shape[0], G, 1), generator=g).cuda()).to(dtype)
+        go(q, cache, x, table, lens, starts, dtype)
+
+
+def test_many_rows_on_another_stream_and_in_a_graph(q):
+    """A prompt's chunk in parts beside decoding requests, replayed: each replay is the eager result of the inputs it finds."""
+    cache, x, table, lens, starts = make(q, [(2500, 60), (700, 1), (90, 3)], 1, 4, 128, 64, BF16)
+    assert tiles(q, cache, 4, 60)
+    ws, y, s = q.kv_attention_workspace(x, cache, table, 60), torch.zeros_like(x), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(s):
+        q.kv_attention(x, cache, table, lens, starts, y, max_new=60, ws=ws)
+    torch.cuda.synchronize()
+    gr = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(gr, stream=s):
+        q.kv_attention(x, cache, table, lens, starts, y, max_new=60, ws=ws)
+    g = torch.Generator().manual_seed(5)
+    for i in range(4):
+        x.copy_(torch.randn(x.shape, generator=g).to(BF16))
+        lens.copy_(i32([2500 - 700 * i, 700 - 11 * i, 90]))
+        y.fill_(3.0)
+        torch.cuda.synchronize()
+        gr.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, q.kv_attention(x, cache, table, lens, starts, max_new=60))
+    go(q, cache, x, table, lens, starts, BF16)

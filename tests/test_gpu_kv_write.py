@@ -162,3 +162,14 @@ def test_norms_of_far_sizes(q, D, rot, pairs):
         p, i = pos.cpu().numpy(), inv.cpu().numpy()
         near(y, turned(f64(z), f64(qw), p, i, eps, pairs, 1.0), BF16, D)
         near(ko, turned(f64(kz), f64(kw), p, i, eps, pairs, 1.0), BF16, D)
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("case", [
+    (515, 20, 3, 128, 128, "half", 64, True, 1.0, 40000), (520, 35, 5, 64, 64, "half", 16, True, 1.0, 9000),
+    (513, 17, 9, 128, 64, "next", 32, True, 1.0, 100000), (530, 33, 1, 64, 48, "next", 64, False, float(np.float32(1.3466)), 131072),
+    (512, 32, 8, 128, 128, "half", 128, True, 1.0, 40000)], ids=lambda c: "x".join(map(str, c)))
+def test_several_turns_of_heads(q, case, dtype):
+    """Long steps, whose workgroups take a token's heads in several turns: the borders of q, k and v inside a turn and a wave, and
+    the last turn not full.  (The factor as the call takes it, binary32: the codes are those of that number.)"""
+    test_against_64_bits(q, case, dtype)
