@@ -605,7 +605,7 @@ typedef enum { QMLP_PAIRS_HALF = 0, QMLP_PAIRS_NEXT = 1 } qmlp_pairs;
  *   (u_i, u_j) -> mul (u_i cos a - u_j sin a, u_j cos a + u_i sin a) with
  *   a = positions[t] inv_freq[p] for the p-th pair of the first `rot` dims
  *   (inv_freq NULL: no rotation),
- * rounded once to the activation type; q goes to q_out, k to k_out (or NULL)
+ * rounded to the activation type (q once, k to fp32 first); q goes to q_out, k to k_out (or NULL)
  * and, with a cache, k and v of the tokens with a slot in [0, slots of the cache)
  * are quantized from the activation type and written there.  q, k and v are
  * rows ldq, ldk, ldv elements apart with their heads side by side (views of one
@@ -650,7 +650,7 @@ qmlp_status qmlp_kv_read(const qmlp_kv_cache *cache, const int32_t *slots, int T
  * j over max(0, p - window + 1) .. p (window 0: from 0), sinks NULL: no such term.
  * A row that sees nothing is zeros.  A page number outside the cache hides its tokens.
  * table [B][W]; lens past W pages count as W pages.  q and y [T][heads][head_dim] in
- * rows ldq and ldy elements apart.  Rows of y before starts[0] and from starts[B] on
+ * rows ldq and ldy elements apart, y overlapping nothing.  Rows of y before starts[0] and from starts[B] on
  * are left as they are (starts has to be rising, 0 <= starts <= T; rows past T are not touched).
  * Codes enter the products as exact integers; scores, sums and outputs are fp32; weights times the
  * value's scale are rounded to binary16, with a power of two that keeps 2^-22 of the largest normal (where a row's largest score

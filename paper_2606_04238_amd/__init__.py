@@ -837,7 +837,7 @@ def qk_norm_rope(q: torch.Tensor | None, k: torch.Tensor | None, positions: torc
                  v: torch.Tensor | None = None, slots: torch.Tensor | None = None):
     """RMS norm of each head (with a weight) and rotation by position (with inv_freq float32 [rot/2]; positions int32 [T])
     of q [T][heads][D] and k [T][kv_heads][D]; with a cache, k and v are quantized into it at slots int32 [T] (negative: not
-    written).  Returns (q_out, k_out); without a cache k_out is made if it is not given, with one it is None unless given.
+    written).  eps and mul are binary32.  Returns (q_out, k_out); without a cache k_out is made if it is not given, with one it is None unless given.
     q_out may be q and k_out may be k."""
     x = q if q is not None else k
     if x is None or x.dim() != 3:

@@ -12,7 +12,7 @@ against it with clang's ASan runtime preloaded:
     QMLP_LIB_PATH=paper_2606_04238_amd/_build_san/libqmlp_san.so \
     LD_PRELOAD=$(ls /opt/rocm/llvm/lib/clang/*/lib/linux/libclang_rt.asan-x86_64.so) \
     ASAN_OPTIONS=detect_leaks=0 UBSAN_OPTIONS=halt_on_error=1 \
-    python -m pytest -s tests/test_abi.py tests/test_abi_tokens.py tests/test_bench_cli.py
+    python -m pytest -s tests/test_abi.py tests/test_abi_tokens.py tests/test_abi_kv.py tests/test_bench_cli.py
 """
 import concurrent.futures
 import glob

@@ -15,9 +15,9 @@
 // The rounding to binary16 is made where weights are at most 2^15 and, when the maximum is taken anew, 2^8: normal
 // numbers down to 2^-22 of the largest.  m moves only when a weight would pass 2^15.
 //
-// 131072 tokens of 8 K/V heads of 128 (143 MB) take 38.5 us, of which the pass over the cache is 24 us (5.8 TB/s, by clocks in the
+// 131072 tokens of 8 K/V heads of 128 (143 MB) take 38.9 us, of which the pass over the cache is 24 us (5.8 TB/s, by clocks in the
 // kernel), 3 us go before it (lengths, pages, the first loads: three trips to memory) and the rest to joining 64 parts.  One
-// sequence of 2001 tokens, 16 parts an item, takes 11.4 us.  One step of a wave under way instead of two: 59 us and 13.9 us.
+// sequence of 2001 tokens, 16 parts an item, takes 11.6 us.  One step of a wave under way instead of two: 59 us and 13.9 us.
 #include "qmlp_internal.h"
 
 #include "decode_launch.h"
@@ -451,6 +451,7 @@ hipError_t launch_few(const AttnArgs& a, int limit, hipStream_t st) {
 // Requests of up to this many rows take the kernel above, those with more the one for many rows (kv_attention_rows.hip).
 // 80 rows (5 tokens, 16 heads on one K/V head) of four requests of 30000 tokens: 38 us here, 98 us there, whose tile of 256 rows is
 // then a third full and its items few; 20 tokens (80 rows a K/V head) after 15000: 37 and 68 us.  800 rows there: 120 us.
+// (Every 16 rows read and unpack the cache again here: both are far from reading it once.)
 constexpr int kFewRows = 128;
 
 size_t kv_attention_bytes(int D, int G, int max_new) {

@@ -8,15 +8,16 @@
 // product to the other in registers.  Three stages of LDS (see the loop).
 //
 // LDS: K [tokens][D], 16-byte pieces (8 dims) at place p ^ (token & 7); V [D dims][tokens], a piece being the eight
-// tokens a lane multiplies at once (16 s + 4 h + {0..3, 8..11}), at place p ^ (dim & 7) ^ (dim / 8 & 7).  Neighbouring lanes
-// so read and write different banks.
+// tokens a lane multiplies at once (16 s + 4 h + {0..3, 8..11}), at place p ^ (dim & 7) ^ (dim / 8 & 7), so that
+// eight neighbouring lanes read different banks.  (Not all: at D = 128 a row of K has 16 pieces and a read stays in half of them.
+// By counters 21 % of the cycles of LDS are conflicts.)
 //
-// Prompts of 2501, 2058 and 1341 tokens of 32 heads of 128 on 8 K/V heads: 176 us (570 TFLOP/s); 1000 tokens after 15000
-// beside 15 decoding requests: 345 us (738 TFLOP/s, where a large product of the library reaches 1160).  On the way:
+// Prompts of 2501, 2058 and 1341 tokens of 32 heads of 128 on 8 K/V heads: 179 us (563 TFLOP/s); 1000 tokens after 15000
+// beside 15 decoding requests: 337 us (754 TFLOP/s, where a large product of the library reaches 1160).  On the way:
 // 128 rows a workgroup 195 and 438 us; 256 rows 205 and 397; tiles handed out by their length 200; weights and products in turns
 // with operands from LDS two turns ahead 187 and 359; a third stage, so that every tile has both neighbours' products
-// beside it, 181 and 356; pieces of V without turned halves 177 and 348.  By counters (the mixed step, at 356 us) the
-// vector units are busy 56 % of the time and the matrix cores 31 %, waves wait for data or each other 35 %; steps of 128 tokens
+// beside it, 181 and 356; pieces of V without turned halves 177 and 348.  By counters (the mixed step) the
+// vector units are busy 54 % of the time and the matrix cores 33 %, waves wait for data or each other 35 %; steps of 128 tokens
 // at D = 128 spilled registers (398 us).
 #include "qmlp_internal.h"
 

@@ -5,9 +5,9 @@
 // quarter of k and v), so every element is loaded once, 16 bytes a lane: a head is
 // D/8 lanes of a wave and the 8 numbers of a lane are one word of codes.  Sums,
 // ranges and the partner of a rotated dim come from other lanes of the head.  One token of 32 + 8 + 8 heads of 128 takes
-// 4.6 us; 4096 tokens 40 us (2.4 TB/s, half of what a large copy reaches: the chain of a head, load, sums
-// over its lanes, fp64 for keys, is what its waves wait for.  Four tokens a workgroup 62 us, a workgroup for every
-// 16 heads 50 us, the next head's load ahead 50 to 64 us: each costs more in registers or repeated angles than it hides).
+// 4.5 us; 4096 tokens 37 us (2.4 TB/s, half of what a large copy reaches).  By counters the vector units are then busy 59 % of the
+// time, and waves, three a SIMD, wait 54 % of theirs: the fp64 of keys and angles is work, and the chain of a head (load, sums over its
+// lanes) is not hidden.  Four tokens a workgroup 62 us, a workgroup for every 16 heads 50 us, the next head's load ahead 50 to 64 us.
 #include <type_traits>
 
 #include "kv_cache.h"
@@ -81,7 +81,8 @@ __device__ __forceinline__ void store_codes(const KvView& c, int slot, int head,
         reinterpret_cast<uint32_t*>(base + ((size_t)(D / 2) << lg))[o] = meta;
 }
 
-// One head: norm and rotation of a lane's 8 numbers in F.  `turn`: (cos, sin) of each pair, scaled.  `far` (fp32): the squares
+// One head: norm and rotation of a lane's 8 numbers in F, rounded to fp32 and then to the activation type (in fp32, once).
+// `turn`: (cos, sin) of each pair, scaled.  `far` (fp32): the squares
 // pass fp32 on either side (bfloat16 numbers of 2^60, or with eps 0 of 2^-50), and the result does not count.
 template <int D, bool BF, typename F, typename P>
 __device__ __forceinline__ uint4 turned(const HeadsArgs& a, const uint4 raw, const uint16_t* weight, const P* turn, int lane, bool& far) {
@@ -247,7 +248,8 @@ __global__ void __launch_bounds__(256) read_kernel(KvView c, const int32_t* slot
 
 hipError_t launch_qk_norm_rope(const HeadsArgs& a, hipStream_t st) {
     const int all = a.Hq + (a.k ? a.Hk : 0) * (a.cache.data ? 2 : 1), hpw = 256 / (a.D / 8);
-    // few tokens: every set of heads a workgroup of its own
+    // few tokens: every set of heads a workgroup of its own; many: one workgroup, which forms the angles once (us, 32 + 8 + 8 heads of
+    // 128, sets and one: 32 tokens 4.4 and 6.1, 384 6.7 and 7.6, 512 7.8 and 7.8, 1024 11.5 and 10.1, 4096 35 and 29)
     const int sets = (all + hpw - 1) / hpw, split = a.T >= 512 ? 1 : sets;
     const dim3 grid(a.T, split);
     if (a.D == 128)
