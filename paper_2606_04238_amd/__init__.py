@@ -707,15 +707,26 @@ def moe_layer(moe: MoE, x: torch.Tensor, y: torch.Tensor | None = None, ws: torc
     return y
 
 
-def _kept(obj, last, why):
-    """Refuses to change an object whose tensors' addresses have been taken (`last` is set last, when they have)."""
-    if hasattr(obj, last):
-        raise AttributeError(why)
+class _Keeps:
+    """An object whose tensors' addresses the kernels are given: what _KEPT names is set once."""
+    _KEPT, _WHY = (), ""
+
+    def __setattr__(self, name, value):
+        if name in self._KEPT and self.__dict__.get(name, value) is not value:     # (the same again: lens += 1)
+            raise AttributeError(self._WHY)
+        super().__setattr__(name, value)
+
+    def __delattr__(self, name):
+        if name in self._KEPT:
+            raise AttributeError(self._WHY)
+        super().__delattr__(name)
 
 
-class KVCache:
+class KVCache(_Keeps):
     """A paged cache of keys and values in 4 bits: ``data`` uint8 [pages][kv_heads][2][page * (head_dim/2 + 4)] on the
     device (the storage format of qmlp_kv_cache; kv_cache makes an empty one)."""
+    _KEPT = ("data", "page", "pages", "kv_heads", "head_dim", "_c", "_at")
+    _WHY = "a cache keeps its tensor (its contents change)"
 
     def __init__(self, data: torch.Tensor, page: int):
         if data.dim() != 4 or data.dtype != torch.uint8 or data.shape[2] != 2 or not data.is_contiguous() or \
@@ -728,13 +739,6 @@ class KVCache:
             raise QmlpError(4, "KVCache")
         self._c = KVCacheC(data.data_ptr(), self.pages, self.kv_heads, self.head_dim, self.page)
         self._at = ctypes.addressof(self._c)
-
-    def __setattr__(self, name, value):
-        _kept(self, "_at", "a cache keeps its tensor (its contents change)")
-        super().__setattr__(name, value)
-
-    def __delattr__(self, name):
-        raise AttributeError("a cache keeps its tensor (its contents change)")
 
     def c(self) -> KVCacheC:
         return self._c
@@ -772,9 +776,11 @@ def _is_table(table, B):
     return table.shape[1]
 
 
-class KVPlan:
+class KVPlan(_Keeps):
     """What kv_plan writes for up to ``B`` requests and ``tokens`` new tokens of a step: int32 ``slots`` and ``positions``
     [tokens], ``starts`` [B + 1], ``lens`` [B], ``n_free`` [1], ``short`` [1] (requests refused)."""
+    _KEPT = ("slots", "positions", "starts", "short", "lens", "n_free", "B", "tokens", "_out")
+    _WHY = "a plan keeps its tensors (their contents change)"
 
     def __init__(self, B: int, tokens: int, device="cuda", lens: torch.Tensor | None = None,
                  n_free: torch.Tensor | None = None):
@@ -788,13 +794,6 @@ class KVPlan:
             raise ValueError("lens and n_free must be on the plan's device")
         self.B, self.tokens = B, tokens
         self._out = tuple(v.data_ptr() for v in t)
-
-    def __setattr__(self, name, value):
-        _kept(self, "_out", "a plan keeps its tensors (their contents change)")
-        super().__setattr__(name, value)
-
-    def __delattr__(self, name):
-        raise AttributeError("a plan keeps its tensors (their contents change)")
 
 
 def kv_plan(plan: KVPlan, lens: torch.Tensor, new: torch.Tensor, table: torch.Tensor, free: torch.Tensor,

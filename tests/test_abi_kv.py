@@ -225,3 +225,20 @@ def test_a_cache_keeps_its_tensor(q):
     data.fill_(1)                                           # the contents are the caller's
     with pytest.raises(AttributeError):
         del q.KVPlan(2, 4, device="cpu").slots
+
+
+def test_caches_and_plans_take_a_callers_own_attributes(q):
+    for o in (q.KVCache(torch.zeros(3, 2, 2, 64 * 68, dtype=torch.uint8), 64), q.KVPlan(2, 4, device="cpu")):
+        o.layer = 3
+        o.layer += 1
+        assert o.layer == 4
+        del o.layer
+        for name in o._KEPT:
+            with pytest.raises(AttributeError):
+                setattr(o, name, object())
+            with pytest.raises(AttributeError):
+                delattr(o, name)
+        assert set(o._KEPT) == set(vars(o))
+    o.n_free.zero_()
+    o.n_free += 5                                           # in place
+    assert o.n_free.tolist() == [5]
